@@ -63,7 +63,8 @@ typedef enum {
   MORELLO_ERR_CUDA = 6,               /* a CUDA call failed; see morello_last_cuda_error() */
   MORELLO_ERR_DEVICE_TIMEOUT = 7,     /* a bounded device-side wait gave up; only reported by
                                          morello_read_device_status() */
-  MORELLO_ERR_UNSUPPORTED_PATH = 8    /* a forced path cannot run this shape / alignment */
+  MORELLO_ERR_UNSUPPORTED_PATH = 8,   /* a forced path cannot run this shape / alignment */
+  MORELLO_ERR_INVALID_ARGUMENT = 9    /* an enumerated argument or a flag has no such value */
 } morello_status_t;
 
 /* Kernel families behind the shape selector (Section 2 of the paper tiles one
@@ -241,6 +242,148 @@ int morello_matmul_accum_noalloc(int split_k, int64_t b, int64_t m, int64_t k, i
 
 /* MORELLO_NOALLOC_SCRATCH_BYTES as the loaded library was built with. */
 size_t morello_noalloc_scratch_limit(void);
+
+/* --- feed-forward operators ------------------------------------------------- */
+
+/* Activations (z in f32): max(z, 0); z Phi(z) with the normal distribution function; the same by
+ * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; z / (1 + e^-z). */
+enum {
+  MORELLO_ACT_NONE = 0,
+  MORELLO_ACT_RELU = 1,
+  MORELLO_ACT_GELU = 2,
+  MORELLO_ACT_GELU_TANH = 3,
+  MORELLO_ACT_SILU = 4
+};
+/* Types of outputs that may be either. */
+enum { MORELLO_BF16 = 0, MORELLO_F32 = 1 };
+/* Storage of a weight matrix of k inputs and w outputs: [k][w] or [w][k]. */
+enum { MORELLO_W_ROWMAJOR = 0, MORELLO_W_COLMAJOR = 1 };
+/* Scores of the router. */
+enum { MORELLO_SCORE_SOFTMAX = 0, MORELLO_SCORE_SIGMOID = 1 };
+
+/*
+ * A linear layer with its epilogue (the product of MatmulAccum, then everything that follows it in
+ * a feed-forward block, before the sums leave the chip):
+ *
+ *     z[i,j] = sum_{p<k} X[i,p] * W[p,j] + bias[j]
+ *     gated == 0:  Y[i,j] = act(z[i,j]) + R[i,j]
+ *     gated == 1:  Y[i,j] = act(z[i,j]) * z[i,n+j] + R[i,j]          (W and bias have 2 n columns)
+ *
+ *     X[m][k] bf16;  W bf16, [k][w] or, with w_layout = MORELLO_W_COLMAJOR, [w][k], w = n or 2 n;
+ *     bias[w] bf16 or NULL;  R[m][n] bf16 or NULL;  Y[m][n] bf16 or f32 (y_type);
+ *     Z[m][w] bf16 or NULL: z, for the backward pass.
+ *
+ * Sums, bias, activation and residual are f32; Y and Z are rounded once.  k == 0 is an empty sum
+ * (Y = act(bias) + R); m == 0 or n == 0 does nothing.  R may be Y itself when both are bf16; no other
+ * overlap is allowed.  Extents up to 2^31 - 1024.  Any extent and alignment runs; where rows of X or W
+ * are not multiples of 16 bytes (k % 8 != 0; row-major W: n % 8 != 0) or start off a 16-byte boundary, the
+ * operand goes through a zero-padded copy in the workspace.
+ *
+ * `workspace`: morello_linear_workspace_bytes() bytes, 16-byte aligned (16-byte-aligned tensors; an X or
+ * W that is not needs its own bytes, rows rounded up to 16 bytes and the whole to 256, besides, and
+ * MORELLO_ERR_WORKSPACE is returned when that does not fit), or NULL and 0 for the library's own scratch
+ * (rules as in morello_matmul_accum).  Deterministic, asynchronous on `stream`.
+ */
+int morello_linear(int act, int gated, int y_type, int w_layout, int64_t m, int64_t k, int64_t n,
+                   const void* X, const void* W, const void* bias, const void* R, void* Y, void* Z,
+                   void* workspace, size_t workspace_bytes, void* stream);
+size_t morello_linear_workspace_bytes(int gated, int w_layout, int64_t m, int64_t k, int64_t n);
+
+/*
+ * Gradients of morello_linear from dY[m][n] (bf16) and the kept Z:
+ *
+ *     dz[i,j] = dY[i,j] * act'(z[i,j]);   gated: dY * act'(z_gate) * z_up and dY * act(z_gate)
+ *     dX[m][k] = dz W^T  (bf16);   dW = X^T dz, W's layout (grad_type);   dbias[w] = column sums of dz (f32)
+ *
+ * dX, dW and dbias may each be NULL (not wanted).  accumulate == 1 (f32 gradients only) adds to dW and
+ * dbias instead of setting them.  Z may be NULL for MORELLO_ACT_NONE without gating.  The gradient of R is
+ * dY itself.  dz is rounded to bf16 for the two products (they run on the bf16 tensor cores) and kept in
+ * f32 for dbias.  m == 0 and k == 0 or n == 0 sums are empty: zero, or nothing added.  Workspace as in morello_linear.
+ */
+int morello_linear_backward(int act, int gated, int grad_type, int accumulate, int w_layout,
+                            int64_t m, int64_t k, int64_t n,
+                            const void* X, const void* W, const void* Z, const void* dY,
+                            void* dX, void* dW, float* dbias,
+                            void* workspace, size_t workspace_bytes, void* stream);
+size_t morello_linear_backward_workspace_bytes(int act, int gated, int w_layout, int64_t m, int64_t k, int64_t n);
+
+/*
+ * Routing of tokens to experts.  With x = logits[t][e] (f32 or bf16, logits_type) and s_e = 1 / (1 + e^-x_e):
+ *
+ *     key_e = x_e + bias_e (softmax)  or  s_e + bias_e (sigmoid);       bias[experts] f32 or NULL
+ *     groups > 1: experts are groups of experts / groups neighbours; the topk_groups best groups stay, a
+ *       group's rank being its largest key (softmax) or the sum of its two largest (sigmoid)
+ *     idx[t][0 .. topk): the experts of the topk largest keys, largest first
+ *     weights[t][j] = scale * p, p = softmax(x)_e or s_e of the chosen; renorm == 1: divided by their sum
+ *
+ * The bias steers the choice alone.  Ties go to the lowest index, among groups too; -0 equals +0 and a NaN key
+ * is below every number.  A logit of -inf has weight 0 (it is chosen only when nothing else is left); a row of
+ * nothing else, and a sum of 0, give weights of 0.  Otherwise infinities and NaN follow the formulas.
+ * experts <= 1024, topk <= 32, groups <= 32 and dividing experts, topk <= topk_groups * experts / groups.
+ */
+int morello_route(int score, int renorm, float scale, int logits_type, int64_t tokens, int64_t experts,
+                  int64_t topk, int64_t groups, int64_t topk_groups, const void* logits, const float* bias,
+                  int32_t* idx, float* weights, void* stream);
+/* Gradient of the logits (their type; every element is written) from that of the weights; the choice is
+ * constant.  idx entries outside 0 .. experts - 1 are skipped. */
+int morello_route_backward(int score, int renorm, float scale, int logits_type, int64_t tokens,
+                           int64_t experts, int64_t topk, const void* logits, const int32_t* idx,
+                           const float* dweights, void* dlogits, void* stream);
+
+/*
+ * The row layout of the experts' products: the pairs (token, place) of idx[tokens][topk], sorted by expert and
+ * then by token * topk + place; every expert's rows begin at a multiple of 128.  With R =
+ * morello_expert_plan_rows() = 128 * floor((P + 127 min(experts, P)) / 128), P = tokens * topk, the plan is one
+ * int32 buffer of morello_expert_plan_words() words:
+ *
+ *     row_src[R]             token * topk + place of the row, -1 where the row holds none
+ *     block_expert[R / 128]  expert of the 128 rows, -1 past the live ones
+ *     offsets[experts + 1]   first row of every expert; the last entry: the live rows
+ *     counts[experts]        rows of every expert that hold a pair
+ *     slot[tokens][topk]     row of the pair, -1 where idx is outside 0 .. experts - 1 (not routed)
+ *     scratch                (ceil(P / 2048) * experts words)
+ *
+ * A tensor "in the layout" is [R][columns]; rows past offsets[experts] are neither read nor written.  Rows before
+ * it that hold no pair are written as zeros by every entry point below, and have to be zeros (or at least finite)
+ * in the tensors they read.  Both functions return -1 for sizes that no entry point takes.
+ */
+int64_t morello_expert_plan_rows(int64_t tokens, int64_t topk, int64_t experts);
+int64_t morello_expert_plan_words(int64_t tokens, int64_t topk, int64_t experts);
+int morello_expert_plan(int64_t tokens, int64_t topk, int64_t experts, const int32_t* idx, int32_t* plan, void* stream);
+
+/*
+ * morello_linear with the weights of every row's expert: W[experts] matrices, bias[experts][w], Y and Z in the
+ * layout; X in the layout, or, with gather == 1, X[tokens][k], row r reading token row_src[r] / topk.
+ */
+int morello_expert_linear(int act, int gated, int y_type, int w_layout, int gather, int64_t tokens,
+                          int64_t topk, int64_t experts, int64_t k, int64_t n, const int32_t* plan,
+                          const void* X, const void* W, const void* bias, void* Y, void* Z,
+                          void* workspace, size_t workspace_bytes, void* stream);
+size_t morello_expert_linear_workspace_bytes(int gated, int w_layout, int gather, int64_t tokens, int64_t topk,
+                                             int64_t experts, int64_t k, int64_t n);
+/* Its gradients: Z and dY in the layout, dW[experts], dbias[experts][w] (experts without rows: zero, or nothing
+ * added); dX in the layout or, with gather == 1, dX[tokens][k], the f32 sum over a token's rows in order. */
+int morello_expert_linear_backward(int act, int gated, int grad_type, int accumulate, int w_layout, int gather,
+                                   int64_t tokens, int64_t topk, int64_t experts, int64_t k, int64_t n,
+                                   const int32_t* plan, const void* X, const void* W, const void* Z,
+                                   const void* dY, void* dX, void* dW, float* dbias,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+size_t morello_expert_linear_backward_workspace_bytes(int act, int gated, int w_layout, int gather,
+                                                      int64_t tokens, int64_t topk, int64_t experts, int64_t k,
+                                                      int64_t n);
+
+/*
+ * out[t] = R[t] + sum_j weights[t][j] * Y[slot[t][j]], places in order, f32, rounded once: Y in the layout
+ * (y_type), weights[tokens][topk] f32 or NULL (ones), R[tokens][n] bf16 or NULL (may be out itself), out bf16.
+ */
+int morello_expert_combine(int y_type, int64_t tokens, int64_t topk, int64_t experts, int64_t n,
+                           const int32_t* plan, const float* weights, const void* Y, const void* R, void* out,
+                           void* stream);
+/* dY[slot[t][j]] = weights[t][j] * dout[t] (bf16, in the layout) and dweights[t][j] = <dout[t], Y[slot[t][j]]>
+ * (0 where a pair is not routed); either may be NULL, and Y without dweights. */
+int morello_expert_combine_backward(int y_type, int64_t tokens, int64_t topk, int64_t experts, int64_t n,
+                                    const int32_t* plan, const float* weights, const void* Y, const void* dout,
+                                    void* dY, float* dweights, void* stream);
 
 /* --- introspection and experiments (tests and benchmarks) ------------------ */
 

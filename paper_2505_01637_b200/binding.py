@@ -24,10 +24,16 @@ MORELLO_ERR_WORKSPACE = 5
 MORELLO_ERR_CUDA = 6
 MORELLO_ERR_DEVICE_TIMEOUT = 7
 MORELLO_ERR_UNSUPPORTED_PATH = 8
+MORELLO_ERR_INVALID_ARGUMENT = 9
 
 MORELLO_PATH_AUTO = -1
 MORELLO_PATH_SKINNY = 0
 MORELLO_PATH_TCGEN05 = 1
+
+MORELLO_ACT_NONE, MORELLO_ACT_RELU, MORELLO_ACT_GELU, MORELLO_ACT_GELU_TANH, MORELLO_ACT_SILU = range(5)
+MORELLO_BF16, MORELLO_F32 = 0, 1
+MORELLO_W_ROWMAJOR, MORELLO_W_COLMAJOR = 0, 1
+MORELLO_SCORE_SOFTMAX, MORELLO_SCORE_SIGMOID = 0, 1
 
 _i64, _vp, _int, _sz = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
 
@@ -55,6 +61,21 @@ SIGNATURES = {
     "morello_matmul_accum_forced": (_int, [_int, _int, _i64, _i64, _i64, _i64, _vp, _vp, _vp,
                                            _vp, _sz, _vp]),
     "morello_workspace_bytes_forced": (_sz, [_int, _int, _i64, _i64, _i64, _i64]),
+    "morello_linear": (_int, [_int] * 4 + [_i64] * 3 + [_vp] * 7 + [_sz, _vp]),
+    "morello_linear_workspace_bytes": (_sz, [_int] * 2 + [_i64] * 3),
+    "morello_linear_backward": (_int, [_int] * 5 + [_i64] * 3 + [_vp] * 8 + [_sz, _vp]),
+    "morello_linear_backward_workspace_bytes": (_sz, [_int] * 3 + [_i64] * 3),
+    "morello_route": (_int, [_int, _int, ctypes.c_float, _int] + [_i64] * 5 + [_vp] * 5),
+    "morello_route_backward": (_int, [_int, _int, ctypes.c_float, _int] + [_i64] * 3 + [_vp] * 5),
+    "morello_expert_plan_rows": (_i64, [_i64] * 3),
+    "morello_expert_plan_words": (_i64, [_i64] * 3),
+    "morello_expert_plan": (_int, [_i64] * 3 + [_vp] * 3),
+    "morello_expert_linear": (_int, [_int] * 5 + [_i64] * 5 + [_vp] * 7 + [_sz, _vp]),
+    "morello_expert_linear_workspace_bytes": (_sz, [_int] * 3 + [_i64] * 5),
+    "morello_expert_linear_backward": (_int, [_int] * 6 + [_i64] * 5 + [_vp] * 9 + [_sz, _vp]),
+    "morello_expert_linear_backward_workspace_bytes": (_sz, [_int] * 4 + [_i64] * 5),
+    "morello_expert_combine": (_int, [_int] + [_i64] * 4 + [_vp] * 6),
+    "morello_expert_combine_backward": (_int, [_int] + [_i64] * 4 + [_vp] * 7),
     "morello_read_device_status": (_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "morello_device_limits": (_int, [ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]),
     "morello_launch_count": (ctypes.c_uint64, []),
@@ -228,6 +249,104 @@ def morello_matmul_accum_forced(path, split_k, b, m, k, n, A, B, C, workspace=No
 
 def morello_workspace_bytes_forced(path, split_k, b, m, k, n) -> int:
     return int(lib().morello_workspace_bytes_forced(path, split_k, b, m, k, n))
+
+
+def morello_linear(act, gated, y_type, w_layout, m, k, n, X, W, bias, R, Y, Z=None, workspace=None,
+                   workspace_bytes=0, stream=None) -> None:
+    """Y = act(X W + bias) + R, or gated act(X Wg + bg) * (X Wu + bu) + R; bias, R and Z may be None."""
+    _check(lib().morello_linear(act, gated, y_type, w_layout, m, k, n, _addr(X), _addr(W), _addr(bias), _addr(R),
+                                _addr(Y), _addr(Z), _addr(workspace), workspace_bytes, _stream(stream)),
+           "morello_linear")
+
+
+def morello_linear_workspace_bytes(gated, w_layout, m, k, n) -> int:
+    return int(lib().morello_linear_workspace_bytes(gated, w_layout, m, k, n))
+
+
+def morello_linear_backward(act, gated, grad_type, accumulate, w_layout, m, k, n, X, W, Z, dY, dX, dW, dbias,
+                            workspace=None, workspace_bytes=0, stream=None) -> None:
+    """Gradients of morello_linear; dX, dW and dbias may be None."""
+    _check(lib().morello_linear_backward(act, gated, grad_type, accumulate, w_layout, m, k, n, _addr(X), _addr(W),
+                                         _addr(Z), _addr(dY), _addr(dX), _addr(dW), _addr(dbias), _addr(workspace),
+                                         workspace_bytes, _stream(stream)),
+           "morello_linear_backward")
+
+
+def morello_linear_backward_workspace_bytes(act, gated, w_layout, m, k, n) -> int:
+    return int(lib().morello_linear_backward_workspace_bytes(act, gated, w_layout, m, k, n))
+
+
+def morello_route(score, renorm, scale, logits_type, tokens, experts, topk, groups, topk_groups, logits, bias, idx,
+                  weights, stream=None) -> None:
+    """Chooses every token's experts and their weights; bias may be None."""
+    _check(lib().morello_route(score, renorm, scale, logits_type, tokens, experts, topk, groups, topk_groups,
+                               _addr(logits), _addr(bias), _addr(idx), _addr(weights), _stream(stream)),
+           "morello_route")
+
+
+def morello_route_backward(score, renorm, scale, logits_type, tokens, experts, topk, logits, idx, dweights, dlogits,
+                           stream=None) -> None:
+    _check(lib().morello_route_backward(score, renorm, scale, logits_type, tokens, experts, topk, _addr(logits),
+                                        _addr(idx), _addr(dweights), _addr(dlogits), _stream(stream)),
+           "morello_route_backward")
+
+
+def morello_expert_plan_rows(tokens, topk, experts) -> int:
+    return int(lib().morello_expert_plan_rows(tokens, topk, experts))
+
+
+def morello_expert_plan_words(tokens, topk, experts) -> int:
+    return int(lib().morello_expert_plan_words(tokens, topk, experts))
+
+
+def morello_expert_plan(tokens, topk, experts, idx, plan, stream=None) -> None:
+    """Sorts the routed pairs by expert; plan is an int32 buffer of morello_expert_plan_words() words."""
+    _check(lib().morello_expert_plan(tokens, topk, experts, _addr(idx), _addr(plan), _stream(stream)),
+           "morello_expert_plan")
+
+
+def morello_expert_linear(act, gated, y_type, w_layout, gather, tokens, topk, experts, k, n, plan, X, W, bias, Y,
+                          Z=None, workspace=None, workspace_bytes=0, stream=None) -> None:
+    """morello_linear with the weights of every row's expert, rows in the plan's layout."""
+    _check(lib().morello_expert_linear(act, gated, y_type, w_layout, gather, tokens, topk, experts, k, n, _addr(plan),
+                                       _addr(X), _addr(W), _addr(bias), _addr(Y), _addr(Z), _addr(workspace),
+                                       workspace_bytes, _stream(stream)),
+           "morello_expert_linear")
+
+
+def morello_expert_linear_workspace_bytes(gated, w_layout, gather, tokens, topk, experts, k, n) -> int:
+    return int(lib().morello_expert_linear_workspace_bytes(gated, w_layout, gather, tokens, topk, experts, k, n))
+
+
+def morello_expert_linear_backward(act, gated, grad_type, accumulate, w_layout, gather, tokens, topk, experts, k, n,
+                                   plan, X, W, Z, dY, dX, dW, dbias, workspace=None, workspace_bytes=0,
+                                   stream=None) -> None:
+    """Gradients of morello_expert_linear; dX, dW and dbias may be None."""
+    _check(lib().morello_expert_linear_backward(act, gated, grad_type, accumulate, w_layout, gather, tokens, topk,
+                                                experts, k, n, _addr(plan), _addr(X), _addr(W), _addr(Z), _addr(dY),
+                                                _addr(dX), _addr(dW), _addr(dbias), _addr(workspace),
+                                                workspace_bytes, _stream(stream)),
+           "morello_expert_linear_backward")
+
+
+def morello_expert_linear_backward_workspace_bytes(act, gated, w_layout, gather, tokens, topk, experts, k, n) -> int:
+    return int(lib().morello_expert_linear_backward_workspace_bytes(act, gated, w_layout, gather, tokens, topk,
+                                                                    experts, k, n))
+
+
+def morello_expert_combine(y_type, tokens, topk, experts, n, plan, weights, Y, R, out, stream=None) -> None:
+    """out[t] = R[t] + sum_j weights[t][j] * Y[slot[t][j]]; weights and R may be None."""
+    _check(lib().morello_expert_combine(y_type, tokens, topk, experts, n, _addr(plan), _addr(weights), _addr(Y),
+                                        _addr(R), _addr(out), _stream(stream)),
+           "morello_expert_combine")
+
+
+def morello_expert_combine_backward(y_type, tokens, topk, experts, n, plan, weights, Y, dout, dY, dweights,
+                                    stream=None) -> None:
+    """Gradients of morello_expert_combine; dY and dweights may be None."""
+    _check(lib().morello_expert_combine_backward(y_type, tokens, topk, experts, n, _addr(plan), _addr(weights),
+                                                 _addr(Y), _addr(dout), _addr(dY), _addr(dweights), _stream(stream)),
+           "morello_expert_combine_backward")
 
 
 def morello_selftest_wait_timeout(limit_ms, stream=None) -> None:

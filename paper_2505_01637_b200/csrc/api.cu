@@ -9,6 +9,7 @@
 
 #include "../../include/morello.h"
 #include "internal.h"
+#include "linear.h"
 
 namespace morello {
 namespace {
@@ -77,6 +78,25 @@ int device_state(DeviceState** out) {
   }
   *out = &st;
   return st.status_code;
+}
+
+// Makes the library-owned scratch at least `need` bytes, under g_mutex.
+int grow_scratch(DeviceState* st, size_t need, cudaStream_t stream) {
+  if (st->scratch_bytes >= need) return MORELLO_OK;
+  if (capturing(stream)) return MORELLO_ERR_WORKSPACE;
+  // Work already enqueued may still be using the old buffer.
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) return cuda_fail(e);
+  if (st->scratch) cudaFree(st->scratch);
+  st->scratch = nullptr;
+  st->scratch_bytes = 0;
+  const size_t grow = std::max(need, (size_t)(8u << 20));
+  if ((e = cudaMalloc(&st->scratch, grow)) != cudaSuccess) {
+    cuda_fail(e);
+    return MORELLO_ERR_WORKSPACE;
+  }
+  st->scratch_bytes = grow;
+  return MORELLO_OK;
 }
 
 // Bounded text output for morello_describe_route.
@@ -315,21 +335,7 @@ int run(int path, int split_k, int64_t b, int64_t m, int64_t k, int64_t n, const
   if (need > 0) {
     if (own_scratch) {
       std::lock_guard<std::mutex> lock(g_mutex);
-      if (st->scratch_bytes < need) {
-        if (capturing(static_cast<cudaStream_t>(stream))) return MORELLO_ERR_WORKSPACE;
-        // Work already enqueued may still be using the old buffer.
-        cudaError_t e = cudaDeviceSynchronize();
-        if (e != cudaSuccess) return cuda_fail(e);
-        if (st->scratch) cudaFree(st->scratch);
-        st->scratch = nullptr;
-        st->scratch_bytes = 0;
-        const size_t grow = std::max(need, (size_t)(8u << 20));
-        if ((e = cudaMalloc(&st->scratch, grow)) != cudaSuccess) {
-          cuda_fail(e);
-          return MORELLO_ERR_WORKSPACE;
-        }
-        st->scratch_bytes = grow;
-      }
+      if ((rc = grow_scratch(st, need, static_cast<cudaStream_t>(stream))) != MORELLO_OK) return rc;
       ws = static_cast<float*>(st->scratch);
     } else if (!ws || workspace_bytes < need) {
       return MORELLO_ERR_WORKSPACE;
@@ -387,6 +393,25 @@ int run(int path, int split_k, int64_t b, int64_t m, int64_t k, int64_t n, const
 
 void count_launches(uint64_t launches) { g_launches.fetch_add(launches, std::memory_order_relaxed); }
 int record_cuda_error(cudaError_t e) { return cuda_fail(e); }
+
+int operator_workspace(size_t need, void* given, size_t given_bytes, cudaStream_t stream, void** out,
+                       DeviceInfo* dev) {
+  *out = nullptr;
+  std::lock_guard<std::mutex> lock(g_mutex);
+  DeviceState* st = nullptr;
+  int rc = device_state(&st);
+  if (rc != MORELLO_OK) return rc;
+  *dev = st->info;
+  if (need == 0) return MORELLO_OK;
+  if (given || given_bytes) {
+    if (!given || given_bytes < need) return MORELLO_ERR_WORKSPACE;
+    *out = given;
+    return MORELLO_OK;
+  }
+  if ((rc = grow_scratch(st, need, stream)) != MORELLO_OK) return rc;
+  *out = st->scratch;
+  return MORELLO_OK;
+}
 
 }  // namespace morello
 
@@ -792,6 +817,7 @@ const char* morello_status_string(int status) {
     case MORELLO_ERR_WORKSPACE: return "workspace too small or its allocation failed";
     case MORELLO_ERR_CUDA: return "a CUDA call failed (see morello_last_cuda_error)";
     case MORELLO_ERR_DEVICE_TIMEOUT: return "a bounded device-side wait gave up";
+    case MORELLO_ERR_INVALID_ARGUMENT: return "an enumerated argument or flag has no such value";
     case MORELLO_ERR_UNSUPPORTED_PATH: return "the forced path cannot run this shape or alignment";
     default: return "unknown status";
   }

@@ -1,0 +1,377 @@
+// The memory-bound companions of the linear layers' products: zero-padded and gathered copies of
+// operands, the activation's slope with the bias gradient, and the weighted sum of a token's rows.
+// Each is one pass over its data in 16-byte accesses where alignment allows.
+#include <algorithm>
+
+#include "activation.cuh"
+#include "linear.h"
+#include "sm100.cuh"
+
+namespace morello {
+namespace {
+
+using namespace sm100;
+
+constexpr int kThreads = 256;
+constexpr int kSlopeRows = 32;      // rows per partial sum of the bias gradient
+constexpr int kSlopeLanes = 8;      // rows a block takes at a time
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+__device__ __forceinline__ uint4 load8_raw(const uint16_t* src, bool vec, int64_t cols) {
+  if (vec) return *reinterpret_cast<const uint4*>(src);
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t v = e < cols ? (uint32_t)src[e] : 0u;
+    w[e >> 1] |= v << ((e & 1) * 16);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void unpack8(const uint4& w, float (&v)[8]) {
+  v[0] = bf16_low(w.x); v[1] = bf16_high(w.x); v[2] = bf16_low(w.y); v[3] = bf16_high(w.y);
+  v[4] = bf16_low(w.z); v[5] = bf16_high(w.z); v[6] = bf16_low(w.w); v[7] = bf16_high(w.w);
+}
+__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
+  return make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7]));
+}
+
+struct CopyParams {
+  const uint16_t* src;
+  uint4* dst;
+  int64_t rows_in, cols_in, rows_out, octets;   // octets: 8-column groups of a row of dst
+  int64_t threads;
+  bool vec;
+  int topk;
+  const int32_t* row_src;     // gather
+  const int32_t* live;        // number of live rows, or null
+};
+
+__global__ void __launch_bounds__(kThreads) copy_kernel(const CopyParams p) {
+  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  pdl_wait();
+  pdl_release();
+  if (idx >= p.threads) return;
+  const int64_t o = idx % p.octets;
+  const int64_t r = (idx / p.octets) % p.rows_out;
+  const int64_t g = idx / (p.octets * p.rows_out);
+  if (p.live && r >= *p.live) return;
+  int64_t from = r;
+  if (p.row_src) {
+    const int32_t s = p.row_src[r];
+    from = s < 0 ? -1 : s / p.topk;
+  }
+  uint4 w = make_uint4(0u, 0u, 0u, 0u);
+  const int64_t left = p.cols_in - o * 8;
+  if (from >= 0 && from < p.rows_in && left > 0)
+    w = load8_raw(p.src + (g * p.rows_in + from) * p.cols_in + o * 8, p.vec && left >= 8, left);
+  p.dst[idx] = w;
+}
+
+struct SlopeParams {
+  const uint16_t* dY;
+  const uint16_t* Z;
+  uint16_t* dZ;
+  float* partial;
+  int64_t rows, n, pitch;      // pitch: columns of a row of dZ, the width rounded up to 8
+  int act;
+  bool vec;
+  const int32_t* row_src;
+  const int32_t* live;
+};
+
+__device__ __forceinline__ float slope_by(int act, float z) {
+  if (act == kActNone) return 1.f;
+  if (act == kActRelu) return act_slope<kActRelu>(z);
+  if (act == kActGelu) return act_slope<kActGelu>(z);
+  if (act == kActGeluTanh) return act_slope<kActGeluTanh>(z);
+  return act_slope<kActSilu>(z);
+}
+__device__ __forceinline__ float value_by(int act, float z) {
+  if (act == kActNone) return z;
+  if (act == kActRelu) return act_value<kActRelu>(z);
+  if (act == kActGelu) return act_value<kActGelu>(z);
+  if (act == kActGeluTanh) return act_value<kActGeluTanh>(z);
+  return act_value<kActSilu>(z);
+}
+
+// A block: 256 columns (32 groups of 8) x kSlopeRows rows, eight rows at a time.
+template <bool kGated>
+__global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeParams p) {
+  __shared__ float sums[kSlopeLanes][kGated ? 2 : 1][256 + 8];
+  const int group = threadIdx.x & 31, lane = threadIdx.x >> 5;
+  const int64_t col = (int64_t)blockIdx.y * 256 + group * 8;
+  const int64_t row_begin = (int64_t)blockIdx.x * kSlopeRows;
+  pdl_wait();
+  pdl_release();
+  if (p.live && row_begin >= *p.live) return;
+  const int64_t row_end = min(p.rows, row_begin + kSlopeRows);
+  const int64_t left = p.n - col;
+  const bool vec = p.vec && left >= 8;
+  const bool vec_out = (p.n & 7) == 0;
+  float s0[8], s1[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s0[e] = s1[e] = 0.f;
+  if (left > 0) {
+#pragma unroll 2
+    for (int64_t row = row_begin + lane; row < row_end; row += kSlopeLanes) {
+      float d0[8], d1[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d0[e] = d1[e] = 0.f;
+      const bool holds = !p.row_src || p.row_src[row] >= 0;
+      if (holds) {
+        float dy[8], z0[8], z1[8];
+        const int64_t width = kGated ? 2 * p.n : p.n;
+        const uint4 wd = load8_raw(p.dY + row * p.n + col, vec, left);
+        uint4 w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
+        if (p.Z) {
+          w0 = load8_raw(p.Z + row * width + col, vec, left);
+          if constexpr (kGated) w1 = load8_raw(p.Z + row * width + p.n + col, vec, left);
+        }
+        unpack8(wd, dy);
+        unpack8(w0, z0);
+        unpack8(w1, z1);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float slope = slope_by(p.act, z0[e]);
+          if constexpr (kGated) {
+            d0[e] = dy[e] * z1[e] * slope;
+            d1[e] = dy[e] * value_by(p.act, z0[e]);
+          } else {
+            d0[e] = dy[e] * slope;
+          }
+        }
+      }
+      if (p.dZ) {
+        uint16_t* dst = p.dZ + row * p.pitch + col;
+        if (vec_out) {
+          *reinterpret_cast<uint4*>(dst) = pack8(d0);
+          if constexpr (kGated) *reinterpret_cast<uint4*>(dst + p.n) = pack8(d1);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (e >= left) continue;
+            dst[e] = bf16_round(d0[e]);
+            if constexpr (kGated) dst[p.n + e] = bf16_round(d1[e]);
+          }
+          if (left <= 8)       // the columns that round the row up to eight
+            for (int64_t c = kGated ? 2 * p.n : p.n; c < p.pitch; ++c) p.dZ[row * p.pitch + c] = 0;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { s0[e] += d0[e]; s1[e] += d1[e]; }
+    }
+  }
+  if (!p.partial) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    sums[lane][0][group * 8 + e] = s0[e];
+    if constexpr (kGated) sums[lane][1][group * 8 + e] = s1[e];
+  }
+  __syncthreads();
+  const int64_t c = (int64_t)blockIdx.y * 256 + threadIdx.x;
+  if (c < p.n) {
+    const int64_t width = kGated ? 2 * p.n : p.n;
+#pragma unroll
+    for (int h = 0; h < (kGated ? 2 : 1); ++h) {
+      float s = 0.f;
+#pragma unroll
+      for (int l = 0; l < kSlopeLanes; ++l) s += sums[l][h][threadIdx.x];
+      p.partial[(int64_t)blockIdx.x * width + h * p.n + c] = s;
+    }
+  }
+}
+
+// db[g][c] = the partial sums of group g's rows, in order: eight strided runs, then the eight.
+__global__ void __launch_bounds__(kThreads)
+slope_sum_kernel(const float* partial, float* db, int64_t width, int64_t parts, const int32_t* offsets, bool accumulate) {
+  __shared__ float sums[8][33];
+  const int x = threadIdx.x & 31, lane = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + x;
+  pdl_wait();
+  pdl_release();
+  const int64_t g = blockIdx.y;
+  int64_t first = 0, last = parts;
+  if (offsets) {
+    first = offsets[g] / kSlopeRows;
+    last = offsets[g + 1] / kSlopeRows;
+  }
+  float s = 0.f;
+  if (c < width)
+    for (int64_t i = first + lane; i < last; i += 8) s += partial[i * width + c];
+  sums[lane][x] = s;
+  __syncthreads();
+  if (lane == 0 && c < width) {
+    float total = 0.f;
+#pragma unroll
+    for (int l = 0; l < 8; ++l) total += sums[l][x];
+    float* dst = db + g * width + c;
+    *dst = accumulate ? *dst + total : total;
+  }
+}
+
+struct CombineParams {
+  const int32_t* slot;
+  const float* weights;
+  const void* Y;
+  const uint16_t* residual;
+  uint16_t* out;
+  int64_t n, y_pitch;
+  int topk;
+  int64_t octets, threads;
+  bool vec_y, vec;
+};
+
+template <bool kF32>
+__global__ void __launch_bounds__(kThreads) combine_kernel(const CombineParams p) {
+  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  pdl_wait();
+  pdl_release();
+  if (idx >= p.threads) return;
+  const int64_t o = idx % p.octets, t = idx / p.octets;
+  const int64_t col = o * 8, left = p.n - col;
+  const bool vec_y = p.vec_y && left >= 8, vec = p.vec && left >= 8;
+  float sum[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < p.topk; ++k) {
+    const int32_t row = p.slot[t * p.topk + k];
+    if (row < 0) continue;
+    const float w = p.weights ? p.weights[t * p.topk + k] : 1.f;
+    float v[8];
+    if constexpr (kF32) {
+      const float* y = static_cast<const float*>(p.Y) + (int64_t)row * p.y_pitch + col;
+      if (vec_y) {
+        const float4 a = reinterpret_cast<const float4*>(y)[0], b = reinterpret_cast<const float4*>(y)[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = e < left ? y[e] : 0.f;
+      }
+    } else {
+      unpack8(load8_raw(static_cast<const uint16_t*>(p.Y) + (int64_t)row * p.y_pitch + col, vec_y, left), v);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = fmaf(w, v[e], sum[e]);
+  }
+  if (p.residual) {
+    float r[8];
+    unpack8(load8_raw(p.residual + t * p.n + col, vec, left), r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += r[e];
+  }
+  uint16_t* dst = p.out + t * p.n + col;
+  if (vec) {
+    *reinterpret_cast<uint4*>(dst) = pack8(sum);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) dst[e] = bf16_round(sum[e]);
+  }
+}
+
+cudaError_t grid_for(int64_t threads, unsigned* blocks) {
+  const int64_t n = (threads + kThreads - 1) / kThreads;
+  if (n >= (1ll << 31)) return cudaErrorInvalidValue;
+  *blocks = (unsigned)n;
+  return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t copy_launch(const CopyJob& j, cudaStream_t stream, uint64_t* launches) {
+  CopyParams p{};
+  p.src = j.src;
+  p.dst = reinterpret_cast<uint4*>(j.dst);
+  p.rows_in = j.rows_in;
+  p.cols_in = j.cols_in;
+  p.rows_out = j.rows_out;
+  p.octets = j.cols_out / 8;
+  p.threads = j.groups * j.rows_out * p.octets;
+  p.vec = j.cols_in % 8 == 0 && aligned16(j.src);
+  if (j.experts) {
+    p.live = j.experts->offsets + j.experts->experts;
+    if (j.gather) {
+      p.row_src = j.experts->row_src;
+      p.topk = (int)j.experts->topk;
+    }
+  }
+  if (p.threads <= 0) return cudaSuccess;
+  unsigned blocks = 0;
+  cudaError_t e = grid_for(p.threads, &blocks);
+  if (e == cudaSuccess) e = launch_pdl(copy_kernel, dim3(blocks), dim3(kThreads), 0, stream, 1, p);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+size_t slope_partial_bytes(int64_t rows, int64_t n, bool gated) {
+  return (size_t)((rows + kSlopeRows - 1) / kSlopeRows) * n * (gated ? 2 : 1) * 4;
+}
+
+cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& c, cudaStream_t stream, uint64_t* launches) {
+  (void)dev;
+  if (c.n <= 0) return cudaSuccess;
+  const int64_t parts = (c.rows + kSlopeRows - 1) / kSlopeRows;
+  const int64_t width = c.gated ? 2 * c.n : c.n;
+  cudaError_t e = cudaSuccess;
+  if (parts > 0) {
+    SlopeParams p{};
+    p.dY = c.dY;
+    p.Z = c.Z;
+    p.dZ = c.dZ;
+    p.partial = c.db ? c.partial : nullptr;
+    p.rows = c.rows;
+    p.n = c.n;
+    p.pitch = (width + 7) / 8 * 8;
+    p.act = c.act;
+    p.vec = c.n % 8 == 0 && aligned16(c.dY) && aligned16(c.Z);
+    if (c.experts) {
+      p.row_src = c.experts->row_src;
+      p.live = c.experts->offsets + c.experts->experts;
+    }
+    const int64_t strips = (c.n + 255) / 256;
+    if (parts >= (1ll << 31) || strips > 65535) return cudaErrorInvalidValue;
+    const dim3 grid((unsigned)parts, (unsigned)strips);
+    e = c.gated ? launch_pdl(slope_kernel<true>, grid, dim3(kThreads), 0, stream, 1, p)
+                : launch_pdl(slope_kernel<false>, grid, dim3(kThreads), 0, stream, 1, p);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
+  if (c.db) {
+    const int64_t groups = c.experts ? c.experts->experts : 1;
+    e = launch_pdl(slope_sum_kernel, dim3((unsigned)((width + 31) / 32), (unsigned)groups), dim3(kThreads), 0, stream, 1,
+                   (const float*)c.partial, c.db, width, parts,
+                   c.experts ? c.experts->offsets : (const int32_t*)nullptr, c.accumulate);
+    if (e == cudaSuccess) ++*launches;
+  }
+  return e;
+}
+
+cudaError_t combine_launch(const ExpertRows& x, bool y_f32, int64_t n, int64_t y_pitch, const float* weights,
+                           const void* Y, const uint16_t* residual, uint16_t* out, cudaStream_t stream,
+                           uint64_t* launches) {
+  CombineParams p{};
+  p.slot = x.slot;
+  p.weights = weights;
+  p.Y = Y;
+  p.residual = residual;
+  p.out = out;
+  p.n = n;
+  p.y_pitch = y_pitch;
+  p.topk = (int)x.topk;
+  p.octets = (n + 7) / 8;
+  p.threads = x.tokens * p.octets;
+  p.vec = n % 8 == 0 && aligned16(out) && aligned16(residual);
+  p.vec_y = y_pitch % 8 == 0 && aligned16(Y);
+  if (p.threads <= 0) return cudaSuccess;
+  unsigned blocks = 0;
+  cudaError_t e = grid_for(p.threads, &blocks);
+  if (e != cudaSuccess) return e;
+  e = y_f32 ? launch_pdl(combine_kernel<true>, dim3(blocks), dim3(kThreads), 0, stream, 1, p)
+            : launch_pdl(combine_kernel<false>, dim3(blocks), dim3(kThreads), 0, stream, 1, p);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+}  // namespace morello

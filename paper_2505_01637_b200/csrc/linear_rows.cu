@@ -1,0 +1,356 @@
+// Linear layers on few rows (at most 64, or at most 64 per expert): a decoding step.  The call
+// streams the weights once and is bound by memory.
+//
+// The operands trade places: a block owns 128 columns of W (gated: 64 of either half), which become
+// the M side of the MMA, and the rows of X, rounded up to 16, are its N side.  The MMA's cost
+// follows the rows instead of a fixed 128, and a column of Y is one thread's.  Few strips and a long
+// contraction: it is cut into 2, 4 or 8 slices, one block of a cluster each; every block parks its
+// sums in its shared memory and finishes its share of the rows, adding the slices in slice order
+// through distributed shared memory, then the epilogue: one launch, no scratch, a fixed order.
+// Experts: grid.y is the block of the row layout; a block past the live ones leaves at once.
+#include <algorithm>
+
+#include "activation.cuh"
+#include "linear.h"
+#include "sm100.cuh"
+#include "tensormap.h"
+
+namespace morello {
+namespace {
+
+using namespace sm100;
+
+constexpr int kStrip = 128;
+constexpr int kTileK = 64;
+constexpr int kBoxBytes = 64 * kTileK * 2;
+constexpr int kThreads = 192;
+constexpr int kMaxStages = 8;
+constexpr int kPrefetchBlocks = 6;     // contraction blocks asked into L2 before the wait
+
+template <int kRows>
+struct Shape {
+  static constexpr int kStageBytes = 2 * kBoxBytes + kRows * kTileK * 2;
+  // Up to 16 rows two blocks fit an SM: the next strip (or the next launch) streams beside this one.
+  static constexpr int kRing = (kRows <= 16 ? 108 : 200) * 1024;
+  static constexpr int kFit = kRing / kStageBytes;
+  static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
+  static constexpr int kTmemCols = kRows <= 32 ? 32 : 64;
+  static constexpr size_t kSmemBytes = (size_t)kStages * kStageBytes + 1024 + 256;
+  static_assert(kRows * kStrip * 4 <= kStages * kStageBytes, "the parked sums reuse the stages");
+};
+
+struct RowsParams {
+  int m, n;              // rows (dense) and output columns
+  int k_blocks, split, per_slice;
+  int b_up;
+  uint8_t b_mn, gated, grouped, zero_padding;
+  const int32_t* block_expert;
+  const int32_t* offsets;
+  const int32_t* counts;
+  uint8_t act, out_f32, accumulate;
+  int z_pitch;
+  const uint16_t* bias;
+  const uint16_t* residual;
+  void* Y;
+  uint16_t* Z;
+  uint32_t* status;
+};
+
+struct Barriers {
+  uint64_t full[kMaxStages];
+  uint64_t empty[kMaxStages];
+  uint64_t acc_full;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+__device__ __forceinline__ float act_by(int act, float v) {
+  if (act == kActNone) return v;
+  if (act == kActRelu) return act_value<kActRelu>(v);
+  if (act == kActGelu) return act_value<kActGelu>(v);
+  if (act == kActGeluTanh) return act_value<kActGeluTanh>(v);
+  return act_value<kActSilu>(v);
+}
+
+template <int kRows>
+__global__ void __launch_bounds__(kThreads)
+linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                   const RowsParams p) {
+  using S = Shape<kRows>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* stages = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Barriers* bars = reinterpret_cast<Barriers*>(stages + (size_t)S::kStages * S::kStageBytes);
+  volatile int* abort_flag = &bars->abort_flag;
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const int slice = (int)blockIdx.x % p.split;
+  const int strip = (int)blockIdx.x / p.split;
+  const int out_cols = p.gated ? kStrip / 2 : kStrip;       // output columns of a strip
+  const int col0 = strip * out_cols;
+  const int col1 = p.gated ? p.b_up + col0 : col0 + 64;     // stored column of the second box
+  const int kb0 = slice * p.per_slice, kb1 = min(p.k_blocks, kb0 + p.per_slice);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      mbar_init(&bars->full[s], 1);
+      mbar_init(&bars->empty[s], 1);
+    }
+    mbar_init(&bars->acc_full, 1);
+    bars->abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_descriptor(&map_a);
+    tma_prefetch_descriptor(&map_b);
+    if (!p.grouped) {
+      // The weights' first blocks into L2 while the predecessor drains.
+      for (int kb = kb0; kb < min(kb1, kb0 + kPrefetchBlocks); ++kb) {
+        if (p.b_mn) {
+          tma_prefetch_l2_3d(&map_b, col0, kb * kTileK, 0);
+          tma_prefetch_l2_3d(&map_b, col1, kb * kTileK, 0);
+        } else {
+          tma_prefetch_l2_3d(&map_b, kb * kTileK, col0, 0);
+          tma_prefetch_l2_3d(&map_b, kb * kTileK, col1, 0);
+        }
+      }
+    }
+  }
+  pdl_wait();
+
+  // Which rows, and whose weights.
+  int row0 = 0, rows = p.m, group = 0;
+  if (p.grouped) {
+    row0 = (int)blockIdx.y * kExpertBlock;
+    group = p.block_expert[blockIdx.y];
+    if (group < 0) {            // past the live blocks: the whole cluster leaves
+      pdl_release();
+      return;
+    }
+    rows = min(kExpertBlock, p.offsets[group] + p.counts[group] - row0);
+  }
+  const int chunks = (rows + kRows - 1) / kRows;     // of rows; more than one only when an expert has many
+
+  if (warp == 1) {
+    tmem_alloc(&bars->tmem_base, S::kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = bars->tmem_base;
+
+  int stage = 0;
+  uint32_t phase = 0, acc_phase = 0;
+  bool ok = true;
+  for (int chunk = 0; chunk < chunks; ++chunk) {
+    const int first = row0 + chunk * kRows;
+    const int rows_here = min(kRows, rows - chunk * kRows);
+    if (warp == 0) {
+      // ---------------------------------------------------------------- producer
+      if (elect_one()) {
+        for (int kb = kb0; kb < kb1 && ok; ++kb) {
+          if (!(ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 41))) break;
+          uint8_t* sb = stages + (size_t)stage * S::kStageBytes;
+          mbar_arrive_expect_tx(&bars->full[stage], S::kStageBytes);
+          const int kc = kb * kTileK;
+          if (p.b_mn) {
+            tma_load_3d(sb, &map_b, &bars->full[stage], col0, kc, group);
+            tma_load_3d(sb + kBoxBytes, &map_b, &bars->full[stage], col1, kc, group);
+          } else {
+            tma_load_3d(sb, &map_b, &bars->full[stage], kc, col0, group);
+            tma_load_3d(sb + kBoxBytes, &map_b, &bars->full[stage], kc, col1, group);
+          }
+          tma_load_3d(sb + 2 * kBoxBytes, &map_a, &bars->full[stage], kc, first, 0);
+          if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+        }
+        if (chunk + 1 == chunks) pdl_release();
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // -------------------------------------------------------------- MMA issuer
+      if (elect_one()) {
+        const uint32_t idesc = instr_desc_bf16(kStrip, kRows, p.b_mn != 0, false);
+        const uint32_t step = p.b_mn ? 2048u : 32u, lbo = p.b_mn ? (uint32_t)kBoxBytes : 16u;
+        for (int kb = kb0; kb < kb1 && ok; ++kb) {
+          if (!(ok = mbar_wait(&bars->full[stage], phase, abort_flag, p.status, 42))) break;
+          tc_fence_after_sync();
+          const uint32_t sb = smem_u32(stages + (size_t)stage * S::kStageBytes);
+          const uint32_t sa = sb + 2 * kBoxBytes;
+#pragma unroll
+          for (int j = 0; j < kTileK / 16; ++j)
+            mma_bf16_ss(tmem_base, smem_desc_sw128(sb + j * step, lbo, 1024), smem_desc_sw128(sa + j * 32, 16, 1024),
+                        idesc, ((kb - kb0) | j) != 0 ? 1u : 0u);
+          mma_commit(&bars->empty[stage]);
+          if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+        }
+        if (ok) mma_commit(&bars->acc_full);
+      }
+      __syncwarp();
+    } else {
+      // ---------------------------------------------------------------- epilogue
+      const int quarter = warp & 3;
+      ok = mbar_wait(&bars->acc_full, acc_phase, abort_flag, p.status, 43);
+      ok = __all_sync(0xffffffffu, ok);
+      acc_phase ^= 1;
+      if (ok) {
+        tc_fence_after_sync();
+        // Every MMA has completed, so the stages are free: the sums are parked there as
+        // part[row][column of the strip].
+        float* part = reinterpret_cast<float*>(stages);
+        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll
+        for (int g = 0; g < kRows / 16; ++g) {
+          uint32_t r[16];
+          if (kb1 > kb0) {
+            tmem_ld_32x16(taddr + g * 16, r);
+            tmem_ld_wait();
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) r[i] = 0u;     // an empty sum
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            part[(g * 16 + i) * kStrip + quarter * 32 + lane] = __uint_as_float(r[i]);
+        }
+        tc_fence_before_sync();
+      }
+      __syncwarp();
+    }
+    cluster_sync();
+    if (warp >= 2 && !*abort_flag) {
+      const float* part = reinterpret_cast<const float*>(stages);
+      const int t = (int)threadIdx.x - 64;                  // 0 .. 127
+      const int j = p.gated ? t & 63 : t;                   // column inside the strip
+      const int col = col0 + j;
+      const uint16_t* bias = p.bias ? p.bias + (int64_t)group * p.z_pitch : nullptr;
+      if (col < p.n) {
+        const float b0 = bias ? bf16_value(bias[col]) : 0.f;
+        const float b1 = bias && p.gated ? bf16_value(bias[p.n + col]) : 0.f;
+        // Gated: two rows at a time, one per half of the threads.
+        const int skip = p.gated ? 2 : 1, lead = p.gated ? t >> 6 : 0;
+        for (int i = slice * skip + lead; i < rows_here; i += p.split * skip) {
+          const float* at = part + i * kStrip + j;
+          float v = *peer_shared(at, 0u), u = 0.f;
+          for (int s = 1; s < p.split; ++s) v += *peer_shared(at, (uint32_t)s);
+          if (p.gated) {
+            u = *peer_shared(at + 64, 0u);
+            for (int s = 1; s < p.split; ++s) u += *peer_shared(at + 64, (uint32_t)s);
+            u += b1;
+          }
+          v += b0;
+          const int64_t row = first + i;
+          if (p.Z) {
+            p.Z[row * p.z_pitch + col] = bf16_round(v);
+            if (p.gated) p.Z[row * p.z_pitch + p.n + col] = bf16_round(u);
+          }
+          v = act_by(p.act, v);
+          if (p.gated) v *= u;
+          const int64_t out = row * p.n + col;
+          if (p.residual) v += bf16_value(p.residual[out]);
+          if (p.out_f32) {
+            float* y = static_cast<float*>(p.Y) + out;
+            *y = p.accumulate ? *y + v : v;
+          } else {
+            static_cast<uint16_t*>(p.Y)[out] = bf16_round(v);
+          }
+        }
+        // The block's rows that hold no token are zeros.
+        if (p.zero_padding && chunk + 1 == chunks) {
+          for (int i = rows + slice * skip + lead; i < kExpertBlock; i += p.split * skip) {
+            const int64_t row = row0 + i, out = row * p.n + col;
+            if (p.Z) {
+              p.Z[row * p.z_pitch + col] = 0;
+              if (p.gated) p.Z[row * p.z_pitch + p.n + col] = 0;
+            }
+            if (p.out_f32) static_cast<float*>(p.Y)[out] = 0.f;
+            else static_cast<uint16_t*>(p.Y)[out] = 0;
+          }
+        }
+      }
+    }
+    __syncwarp();
+    cluster_sync();      // the parked sums have been read by every block of the cluster
+    fence_proxy_async_smem();   // ... before the next chunk's copies land on them
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc(tmem_base, S::kTmemCols);
+  }
+}
+
+template <int kRows>
+cudaError_t launch(const DeviceInfo& dev, const TileCall& c, RowsParams p, cudaStream_t stream) {
+  using S = Shape<kRows>;
+  static PerDeviceOnce once;
+  cudaError_t e = once.run_current([] {
+    return cudaFuncSetAttribute(linear_rows_kernel<kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)S::kSmemBytes);
+  });
+  if (e != cudaSuccess) return e;
+  const int64_t out_cols = c.epi.gated ? kStrip / 2 : kStrip;
+  const int64_t strips = (c.n + out_cols - 1) / out_cols;
+  const int64_t blocks = p.grouped ? c.experts.rows / kExpertBlock : 1;
+  // Slices: as many as keep every block slot of the device busy with at least four contraction blocks.
+  const int64_t live = p.grouped ? std::min(c.experts.experts, c.experts.tokens * c.experts.topk) : 1;
+  const int64_t slots = (int64_t)dev.sms * (kRows <= 16 ? 2 : 1);
+  int split = 1;
+  while (split < 8 && strips * live * split * 2 <= slots && p.k_blocks >= split * 2 * 4) split *= 2;
+  while (split > 1 && (p.k_blocks + split - 1) / split * (split - 1) >= p.k_blocks) split /= 2;   // no empty slice
+  p.split = split;
+  p.per_slice = (p.k_blocks + split - 1) / split;
+  if (blocks > 65535 || strips * split >= (1ll << 31)) return cudaErrorInvalidValue;
+  CUtensorMap ma{}, mb{};
+  if (c.k > 0) {
+    e = make_tensor_map_3d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.a.p, (uint64_t)c.a.cols, (uint64_t)c.a.rows, 1,
+                           kTileK, kRows, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (e == cudaSuccess)
+      e = make_tensor_map_3d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.b.p, (uint64_t)c.b.cols, (uint64_t)c.b.rows,
+                             (uint64_t)c.b.groups, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(linear_rows_kernel<kRows>, dim3((unsigned)(strips * split), (unsigned)blocks), dim3(kThreads),
+                    S::kSmemBytes, stream, split, ma, mb, p);
+}
+
+}  // namespace
+
+cudaError_t rows_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t stream, uint64_t* launches) {
+  if (c.m <= 0 || c.n <= 0) return cudaSuccess;
+  const LinearEpilogue& ep = c.epi;
+  RowsParams p{};
+  p.grouped = c.mode == TileMode::kRows;
+  const int64_t rows = p.grouped ? c.experts.tokens : c.m;
+  if (rows > kLinearFewRows || c.a_mn || c.mode == TileMode::kContract) return cudaErrorInvalidValue;
+  p.m = (int)c.m;
+  p.n = (int)c.n;
+  p.k_blocks = (int)((c.k + kTileK - 1) / kTileK);
+  p.b_up = (int)c.b_up;
+  p.b_mn = c.b_mn;
+  p.gated = ep.gated;
+  p.zero_padding = p.grouped && c.zero_padding;
+  p.block_expert = c.experts.block_expert;
+  p.offsets = c.experts.offsets;
+  p.counts = c.experts.counts;
+  p.act = (uint8_t)ep.act;
+  p.out_f32 = ep.out_f32;
+  p.accumulate = ep.accumulate;
+  p.z_pitch = (int)(c.n * (ep.gated ? 2 : 1));
+  p.bias = ep.bias;
+  p.residual = ep.residual;
+  p.Y = ep.Y;
+  p.Z = ep.Z;
+  p.status = dev.status;
+  cudaError_t e;
+  if (rows <= 16) e = launch<16>(dev, c, p, stream);
+  else if (rows <= 32) e = launch<32>(dev, c, p, stream);
+  else if (rows <= 48) e = launch<48>(dev, c, p, stream);
+  else e = launch<64>(dev, c, p, stream);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+}  // namespace morello

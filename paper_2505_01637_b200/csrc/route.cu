@@ -1,0 +1,648 @@
+// Routing to experts: scores, the choice of the best, their weights, the gradient of the logits, and
+// the plan that sorts the routed rows by expert.
+//
+// One warp per token.  Lane l holds experts l, l + 32, ...; a key is mapped to an unsigned integer of
+// the same order, so that the warp's maximum and the lowest index that has it are two integer
+// reductions (redux) per chosen expert.  All sums are in f32 in a fixed order.
+#include <algorithm>
+
+#include "activation.cuh"
+#include "route.h"
+#include "sm100.cuh"
+
+namespace morello {
+namespace {
+
+using namespace sm100;
+
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr uint32_t kFull = 0xffffffffu;
+constexpr uint32_t kNone = 0xffffffffu;
+
+// 0: out of the choice; 1: NaN, below every number; then the numbers in order (-0 equals +0).
+__device__ __forceinline__ uint32_t order_of(float key) {
+  if (key != key) return 1u;
+  const uint32_t u = __float_as_uint(key + 0.f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(kFull, v, d);
+  return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, d));
+  return v;
+}
+
+template <bool kF32>
+__device__ __forceinline__ float load_logit(const void* p, int64_t i) {
+  if constexpr (kF32) return static_cast<const float*>(p)[i];
+  else return bf16_value(static_cast<const uint16_t*>(p)[i]);
+}
+
+struct RouteParams {
+  const void* logits;
+  const float* bias;
+  int32_t* idx;
+  float* weights;
+  int64_t tokens;
+  int experts, topk, groups, topk_groups;
+  bool sigmoid, renorm;
+  float scale;
+};
+
+// kPer: experts per lane.
+template <int kPer, bool kF32>
+__global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
+  extern __shared__ uint32_t group_keys[];       // [kWarps][experts] when experts are grouped
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t t = (int64_t)blockIdx.x * kWarps + warp;
+  pdl_wait();
+  pdl_release();
+  if (t >= p.tokens) return;
+  float x[kPer];
+  uint32_t key[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int e = i * 32 + lane;
+    x[i] = e < p.experts ? load_logit<kF32>(p.logits, t * p.experts + e) : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int e = i * 32 + lane;
+    float s = p.sigmoid ? 1.f / (1.f + expf(-x[i])) : x[i];
+    if (p.bias && e < p.experts) s += p.bias[e];
+    key[i] = e < p.experts ? order_of(s) : 0u;
+  }
+  if (p.groups > 1) {
+    // Lane g scores group g: the sum of its two largest keys (sigmoid) or its largest (softmax).
+    uint32_t* mine = group_keys + (size_t)warp * p.experts;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i * 32 + lane < p.experts) mine[i * 32 + lane] = key[i];
+    __syncwarp();
+    const int per = p.experts / p.groups;
+    uint32_t score = 0u;
+    if (lane < p.groups) {
+      uint32_t first = 0u, second = 0u;
+      for (int e = 0; e < per; ++e) {
+        const uint32_t v = mine[lane * per + e];
+        second = max(second, min(first, v));
+        first = max(first, v);
+      }
+      score = first;
+      if (p.sigmoid) {
+        auto value = [](uint32_t o) {
+          return o <= 1u ? __uint_as_float(0x7fc00000u) : __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
+        };
+        score = per > 1 ? order_of(value(first) + value(second)) : first;
+      }
+    }
+    int rank = 0;
+    for (int g = 0; g < p.groups; ++g) {
+      const uint32_t other = __shfl_sync(kFull, score, g);
+      rank += (other > score || (other == score && g < lane)) ? 1 : 0;
+    }
+    const uint32_t keep = __ballot_sync(kFull, lane < p.groups && rank < p.topk_groups);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = i * 32 + lane;
+      if (e < p.experts && !((keep >> (e / per)) & 1u)) key[i] = 0u;
+    }
+  }
+
+  // Lane j ends up with the j-th choice.
+  int my_idx = -1;
+  float my_x = 0.f;
+  for (int j = 0; j < p.topk; ++j) {
+    uint32_t best = 0u;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) best = max(best, key[i]);
+    best = __reduce_max_sync(kFull, best);
+    uint32_t at = kNone;
+#pragma unroll
+    for (int i = kPer - 1; i >= 0; --i)
+      if (key[i] == best) at = (uint32_t)(i * 32 + lane);
+    at = __reduce_min_sync(kFull, at);
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (at == (uint32_t)(i * 32 + lane)) {
+        key[i] = 0u;
+        v = x[i];
+      }
+    v = __shfl_sync(kFull, v, (int)(at & 31u));
+    if (lane == j) {
+      my_idx = (int)at;
+      my_x = v;
+    }
+  }
+
+  float w = 0.f;
+  if (p.sigmoid) {
+    w = lane < p.topk ? 1.f / (1.f + expf(-my_x)) : 0.f;
+  } else {
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i * 32 + lane < p.experts) m = fmaxf(m, x[i]);
+    m = warp_max(m);
+    if (m == -INFINITY) m = 0.f;           // nothing but masked logits: every weight is 0
+    w = lane < p.topk ? expf(my_x - m) : 0.f;
+    if (!p.renorm) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (i * 32 + lane < p.experts) sum += expf(x[i] - m);
+      sum = warp_sum(sum);
+      w = sum == 0.f ? 0.f : w / sum;
+    }
+  }
+  if (p.renorm) {
+    const float sum = warp_sum(w);
+    w = sum == 0.f ? 0.f : w / sum;
+  }
+  if (lane < p.topk) {
+    p.idx[t * p.topk + lane] = my_idx;
+    p.weights[t * p.topk + lane] = w * p.scale;
+  }
+}
+
+struct RouteBackParams {
+  const void* logits;
+  const int32_t* idx;
+  const float* dweights;
+  void* dlogits;
+  int64_t tokens;
+  int experts, topk;
+  bool sigmoid, renorm;
+  float scale;
+};
+
+// With g = scale * dweights and w the weights before scaling:
+//   softmax, all experts:   dx_e = w_e [chosen] g_e - p_e sum(g w)
+//   softmax, renormalised:  dx_e = w_e (g_e - sum(g w)), chosen experts only
+//   sigmoid:                dx_e = g_e s_e (1 - s_e)
+//   sigmoid, renormalised:  dx_e = w_e (g_e - sum(g w)) (1 - s_e)
+template <int kPer, bool kF32>
+__global__ void __launch_bounds__(kThreads) route_backward_kernel(const RouteBackParams p) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t t = (int64_t)blockIdx.x * kWarps + warp;
+  pdl_wait();
+  pdl_release();
+  if (t >= p.tokens) return;
+  const bool softmax_all = !p.sigmoid && !p.renorm;
+  // Lane j: the j-th choice.
+  int e_j = -1;
+  float g = 0.f, x_j = 0.f;
+  if (lane < p.topk) {
+    e_j = p.idx[t * p.topk + lane];
+    if (e_j < 0 || e_j >= p.experts) e_j = -1;
+    if (e_j >= 0) {
+      g = p.scale * p.dweights[t * p.topk + lane];
+      x_j = load_logit<kF32>(p.logits, t * p.experts + e_j);
+    }
+  }
+  float x[kPer];
+  float m = -INFINITY, inv = 0.f;
+  if (softmax_all) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = i * 32 + lane;
+      x[i] = e < p.experts ? load_logit<kF32>(p.logits, t * p.experts + e) : -INFINITY;
+      m = fmaxf(m, x[i]);
+    }
+    m = warp_max(m);
+    if (m == -INFINITY) m = 0.f;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      x[i] = i * 32 + lane < p.experts ? expf(x[i] - m) : 0.f;
+      sum += x[i];
+    }
+    sum = warp_sum(sum);
+    inv = sum == 0.f ? 0.f : 1.f / sum;
+  }
+  float w = 0.f, d = 0.f;
+  if (p.sigmoid) {
+    const float s = e_j >= 0 ? 1.f / (1.f + expf(-x_j)) : 0.f;
+    if (p.renorm) {
+      const float sum = warp_sum(s);
+      w = sum == 0.f ? 0.f : s / sum;
+      const float dot = warp_sum(g * w);
+      d = w * (g - dot) * (1.f - s);
+    } else {
+      d = g * s * (1.f - s);
+    }
+  } else if (p.renorm) {
+    float mm = warp_max(e_j >= 0 ? x_j : -INFINITY);
+    if (mm == -INFINITY) mm = 0.f;
+    w = e_j >= 0 ? expf(x_j - mm) : 0.f;
+    const float sum = warp_sum(w);
+    w = sum == 0.f ? 0.f : w / sum;
+    const float dot = warp_sum(g * w);
+    d = w * (g - dot);
+  } else {
+    w = e_j >= 0 ? expf(x_j - m) * inv : 0.f;
+    const float dot = warp_sum(g * w);
+    d = g * w;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] *= -dot * inv;
+  }
+  if (!softmax_all) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = 0.f;
+  }
+  for (int j = 0; j < p.topk; ++j) {
+    const int e = __shfl_sync(kFull, e_j, j);
+    const float v = __shfl_sync(kFull, d, j);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (e == i * 32 + lane) x[i] += v;
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int e = i * 32 + lane;
+    if (e >= p.experts) continue;
+    if constexpr (kF32) static_cast<float*>(p.dlogits)[t * p.experts + e] = x[i];
+    else static_cast<uint16_t*>(p.dlogits)[t * p.experts + e] = bf16_round(x[i]);
+  }
+}
+
+template <bool kF32>
+cudaError_t launch_route(const RouteParams& p, unsigned blocks, cudaStream_t stream) {
+  const size_t smem = p.groups > 1 ? (size_t)kWarps * p.experts * 4 : 0;
+  const dim3 g(blocks), b(kThreads);
+  if (p.experts <= 32) return launch_pdl(route_kernel<1, kF32>, g, b, smem, stream, 1, p);
+  if (p.experts <= 64) return launch_pdl(route_kernel<2, kF32>, g, b, smem, stream, 1, p);
+  if (p.experts <= 128) return launch_pdl(route_kernel<4, kF32>, g, b, smem, stream, 1, p);
+  if (p.experts <= 256) return launch_pdl(route_kernel<8, kF32>, g, b, smem, stream, 1, p);
+  if (p.experts <= 512) return launch_pdl(route_kernel<16, kF32>, g, b, smem, stream, 1, p);
+  return launch_pdl(route_kernel<32, kF32>, g, b, smem, stream, 1, p);
+}
+template <bool kF32>
+cudaError_t launch_route_backward(const RouteBackParams& p, unsigned blocks, cudaStream_t stream) {
+  const dim3 g(blocks), b(kThreads);
+  if (p.experts <= 32) return launch_pdl(route_backward_kernel<1, kF32>, g, b, 0, stream, 1, p);
+  if (p.experts <= 64) return launch_pdl(route_backward_kernel<2, kF32>, g, b, 0, stream, 1, p);
+  if (p.experts <= 128) return launch_pdl(route_backward_kernel<4, kF32>, g, b, 0, stream, 1, p);
+  if (p.experts <= 256) return launch_pdl(route_backward_kernel<8, kF32>, g, b, 0, stream, 1, p);
+  if (p.experts <= 512) return launch_pdl(route_backward_kernel<16, kF32>, g, b, 0, stream, 1, p);
+  return launch_pdl(route_backward_kernel<32, kF32>, g, b, 0, stream, 1, p);
+}
+
+// ---- the plan: a stable counting sort of the routed pairs by expert ---------------------------------
+// Pairs (token, place) are numbered token * topk + place.  A chunk of kPlanChunk pairs is one block's;
+// each of its eight warps takes 256 consecutive pairs.  (1) every chunk counts its pairs per expert;
+// (2) one block turns the counts into row offsets and every chunk's first row per expert; (3) every chunk
+// places its pairs: a warp's pairs of one expert find their order with a match over the lanes.
+// A single chunk does all three in one launch.
+
+struct PlanParams {
+  const int32_t* idx;
+  int32_t* row_src;
+  int32_t* block_expert;
+  int32_t* offsets;
+  int32_t* counts;
+  int32_t* slot;
+  int32_t* scratch;      // [chunks][experts]: counts, then first rows
+  int64_t pairs, rows;
+  int experts, chunks;
+};
+constexpr int kPerWarp = kPlanChunk / kWarps;
+
+__device__ __forceinline__ int pair_expert(const PlanParams& p, int64_t i) {
+  if (i >= p.pairs) return -1;
+  const int e = p.idx[i];
+  return e >= 0 && e < p.experts ? e : -1;
+}
+
+// hist[warp][expert] = pairs of the warp's span per expert.
+__device__ void warp_histograms(const PlanParams& p, int32_t* hist, int64_t chunk) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < kWarps * p.experts; i += kThreads) hist[i] = 0;
+  __syncthreads();
+  const int64_t base = chunk * kPlanChunk + warp * kPerWarp;
+  for (int r = 0; r < kPerWarp; r += 32) {
+    const int e = pair_expert(p, base + r + lane);
+    if (e >= 0) atomicAdd(&hist[warp * p.experts + e], 1);     // a count: the order does not matter
+  }
+  __syncthreads();
+}
+
+// first[expert] becomes the row of every warp's first pair of the expert, in hist.
+__device__ void warp_starts(const PlanParams& p, int32_t* hist, const int32_t* first) {
+  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
+    int32_t at = first[e];
+    for (int w = 0; w < kWarps; ++w) {
+      const int32_t n = hist[w * p.experts + e];
+      hist[w * p.experts + e] = at;
+      at += n;
+    }
+  }
+  __syncthreads();
+}
+
+__device__ void place_pairs(const PlanParams& p, int32_t* hist, int64_t chunk) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int32_t* mine = hist + warp * p.experts;
+  const int64_t base = chunk * kPlanChunk + warp * kPerWarp;
+  for (int r = 0; r < kPerWarp; r += 32) {
+    const int64_t i = base + r + lane;
+    const int e = pair_expert(p, i);
+    const uint32_t same = __match_any_sync(kFull, e);
+    int row = -1;
+    if (e >= 0) row = mine[e] + __popc(same & ((1u << lane) - 1u));
+    __syncwarp();
+    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+    __syncwarp();
+    if (i < p.pairs) {
+      p.slot[i] = row;
+      if (row >= 0) p.row_src[row] = (int32_t)i;
+    }
+  }
+}
+
+// offsets, counts, block_expert and, in first[], the first row of every expert; total[] holds the counts.
+__device__ void scan_experts(const PlanParams& p, const int32_t* total, int32_t* first, int32_t* warp_sums) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int32_t carry = 0;
+  for (int base = 0; base < p.experts; base += kThreads) {
+    const int e = base + threadIdx.x;
+    const int32_t blocks = e < p.experts ? (total[e] + kExpertBlock - 1) / kExpertBlock : 0;
+    int32_t v = blocks;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int32_t o = __shfl_up_sync(kFull, v, d);
+      if (lane >= d) v += o;
+    }
+    if (lane == 31) warp_sums[warp] = v;
+    __syncthreads();
+    int32_t before = carry, all = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) before += warp_sums[w];
+      all += warp_sums[w];
+    }
+    const int32_t at = before + v - blocks;
+    if (e < p.experts) {
+      first[e] = at * kExpertBlock;
+      p.offsets[e] = at * kExpertBlock;
+      p.counts[e] = total[e];
+      for (int32_t b = 0; b < blocks; ++b) p.block_expert[at + b] = e;
+    }
+    carry += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) p.offsets[p.experts] = carry * kExpertBlock;
+  for (int64_t b = carry + threadIdx.x; b < p.rows / kExpertBlock; b += kThreads) p.block_expert[b] = -1;
+  __syncthreads();
+}
+
+__global__ void __launch_bounds__(kThreads) plan_one_kernel(const PlanParams p) {
+  extern __shared__ int32_t hist[];       // [kWarps][experts], then total[experts], first[experts], sums
+  int32_t* total = hist + kWarps * p.experts;
+  int32_t* first = total + p.experts;
+  int32_t* sums = first + p.experts;
+  pdl_wait();
+  pdl_release();
+  for (int64_t i = threadIdx.x; i < p.rows; i += kThreads) p.row_src[i] = -1;
+  warp_histograms(p, hist, 0);
+  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
+    int32_t n = 0;
+    for (int w = 0; w < kWarps; ++w) n += hist[w * p.experts + e];
+    total[e] = n;
+  }
+  __syncthreads();
+  scan_experts(p, total, first, sums);
+  warp_starts(p, hist, first);
+  place_pairs(p, hist, 0);
+}
+
+__global__ void __launch_bounds__(kThreads) plan_count_kernel(const PlanParams p) {
+  extern __shared__ int32_t hist[];
+  pdl_wait();
+  pdl_release();
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.rows; i += (int64_t)gridDim.x * kThreads)
+    p.row_src[i] = -1;
+  warp_histograms(p, hist, blockIdx.x);
+  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
+    int32_t n = 0;
+    for (int w = 0; w < kWarps; ++w) n += hist[w * p.experts + e];
+    p.scratch[(int64_t)blockIdx.x * p.experts + e] = n;
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) plan_scan_kernel(const PlanParams p) {
+  extern __shared__ int32_t total[];      // [experts], then first[experts], sums
+  int32_t* first = total + p.experts;
+  int32_t* sums = first + p.experts;
+  pdl_wait();
+  pdl_release();
+  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
+    int32_t n = 0;
+    for (int c = 0; c < p.chunks; ++c) n += p.scratch[(int64_t)c * p.experts + e];
+    total[e] = n;
+  }
+  __syncthreads();
+  scan_experts(p, total, first, sums);
+  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
+    int32_t at = first[e];
+    for (int c = 0; c < p.chunks; ++c) {
+      int32_t* s = p.scratch + (int64_t)c * p.experts + e;
+      const int32_t n = *s;
+      *s = at;
+      at += n;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) plan_place_kernel(const PlanParams p) {
+  extern __shared__ int32_t hist[];
+  pdl_wait();
+  pdl_release();
+  warp_histograms(p, hist, blockIdx.x);
+  warp_starts(p, hist, p.scratch + (int64_t)blockIdx.x * p.experts);
+  place_pairs(p, hist, blockIdx.x);
+}
+
+// ---- gradient of the weighted sum -----------------------------------------------------------------
+struct CombineBackParams {
+  const int32_t* row_src;
+  const int32_t* live;
+  const int32_t* slot;
+  const float* weights;
+  const void* Y;
+  const uint16_t* dout;
+  uint16_t* dY;
+  float* dweights;
+  int64_t n, pairs, row_blocks;
+  int topk;
+  bool vec;
+};
+
+// One warp per row of the layout; the blocks past row_blocks clear the weights' gradient of pairs that are
+// not routed.
+template <bool kF32>
+__global__ void __launch_bounds__(kThreads) combine_backward_kernel(const CombineBackParams p) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();
+  pdl_release();
+  if ((int64_t)blockIdx.x >= p.row_blocks) {
+    const int64_t i = ((int64_t)blockIdx.x - p.row_blocks) * kThreads + threadIdx.x;
+    if (p.dweights && i < p.pairs && p.slot[i] < 0) p.dweights[i] = 0.f;
+    return;
+  }
+  const int64_t row = (int64_t)blockIdx.x * kWarps + warp;
+  if (row >= *p.live) return;
+  const int32_t src = p.row_src[row];
+  const int64_t t = src < 0 ? 0 : src / p.topk;
+  const float w = src < 0 ? 0.f : (p.weights ? p.weights[src] : 1.f);
+  float dot = 0.f;
+  for (int64_t c = lane * 8; c < p.n; c += 256) {
+    const int64_t left = p.n - c;
+    const bool vec = p.vec && left >= 8;
+    float d[8], out[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d[e] = 0.f;
+    if (src >= 0) {
+      const uint16_t* g = p.dout + t * p.n + c;
+      if (vec) {
+        const uint4 q = *reinterpret_cast<const uint4*>(g);
+        d[0] = bf16_low(q.x); d[1] = bf16_high(q.x); d[2] = bf16_low(q.y); d[3] = bf16_high(q.y);
+        d[4] = bf16_low(q.z); d[5] = bf16_high(q.z); d[6] = bf16_low(q.w); d[7] = bf16_high(q.w);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < left) d[e] = bf16_value(g[e]);
+      }
+      if (p.dweights) {
+        if constexpr (kF32) {
+          const float* y = static_cast<const float*>(p.Y) + row * p.n + c;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < left) dot = fmaf(d[e], y[e], dot);
+        } else {
+          const uint16_t* y = static_cast<const uint16_t*>(p.Y) + row * p.n + c;
+          if (vec) {
+            const uint4 q = *reinterpret_cast<const uint4*>(y);
+            dot = fmaf(d[0], bf16_low(q.x), dot); dot = fmaf(d[1], bf16_high(q.x), dot);
+            dot = fmaf(d[2], bf16_low(q.y), dot); dot = fmaf(d[3], bf16_high(q.y), dot);
+            dot = fmaf(d[4], bf16_low(q.z), dot); dot = fmaf(d[5], bf16_high(q.z), dot);
+            dot = fmaf(d[6], bf16_low(q.w), dot); dot = fmaf(d[7], bf16_high(q.w), dot);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e < left) dot = fmaf(d[e], bf16_value(y[e]), dot);
+          }
+        }
+      }
+    }
+    if (!p.dY) continue;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = src < 0 ? 0.f : w * d[e];
+    uint16_t* dst = p.dY + row * p.n + c;
+    if (vec) {
+      *reinterpret_cast<uint4*>(dst) = make_uint4(bf16_pack(out[0], out[1]), bf16_pack(out[2], out[3]),
+                                                  bf16_pack(out[4], out[5]), bf16_pack(out[6], out[7]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < left) dst[e] = bf16_round(out[e]);
+    }
+  }
+  if (p.dweights && src >= 0) {
+    dot = warp_sum(dot);
+    if (lane == 0) p.dweights[src] = dot;
+  }
+}
+
+}  // namespace
+
+cudaError_t route_launch(const RouteCall& c, cudaStream_t stream, uint64_t* launches) {
+  if (c.tokens <= 0) return cudaSuccess;
+  const int64_t blocks = (c.tokens + kWarps - 1) / kWarps;
+  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
+  RouteParams p{c.logits, c.bias, c.idx, c.weights, c.tokens, (int)c.experts, (int)c.topk, (int)c.groups,
+                (int)c.topk_groups, c.sigmoid, c.renorm, c.scale};
+  const cudaError_t e = c.logits_f32 ? launch_route<true>(p, (unsigned)blocks, stream)
+                                     : launch_route<false>(p, (unsigned)blocks, stream);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+cudaError_t route_backward_launch(const RouteCall& c, const int32_t* idx, const float* dweights, void* dlogits,
+                                  cudaStream_t stream, uint64_t* launches) {
+  if (c.tokens <= 0) return cudaSuccess;
+  const int64_t blocks = (c.tokens + kWarps - 1) / kWarps;
+  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
+  RouteBackParams p{c.logits, idx, dweights, dlogits, c.tokens, (int)c.experts, (int)c.topk, c.sigmoid, c.renorm,
+                    c.scale};
+  const cudaError_t e = c.logits_f32 ? launch_route_backward<true>(p, (unsigned)blocks, stream)
+                                     : launch_route_backward<false>(p, (unsigned)blocks, stream);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+cudaError_t plan_launch(const ExpertRows& x, const int32_t* idx, cudaStream_t stream, uint64_t* launches) {
+  PlanParams p{};
+  p.idx = idx;
+  p.row_src = const_cast<int32_t*>(x.row_src);
+  p.block_expert = const_cast<int32_t*>(x.block_expert);
+  p.offsets = const_cast<int32_t*>(x.offsets);
+  p.counts = const_cast<int32_t*>(x.counts);
+  p.slot = const_cast<int32_t*>(x.slot);
+  p.scratch = x.scratch;
+  p.pairs = x.tokens * x.topk;
+  p.rows = x.rows;
+  p.experts = (int)x.experts;
+  p.chunks = (int)((p.pairs + kPlanChunk - 1) / kPlanChunk);
+  const size_t hist = (size_t)kWarps * p.experts * 4, lists = (size_t)p.experts * 8 + kWarps * 4;
+  const dim3 block(kThreads);
+  cudaError_t e;
+  if (p.chunks <= 1) {
+    e = launch_pdl(plan_one_kernel, dim3(1), block, hist + lists, stream, 1, p);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+  }
+  e = launch_pdl(plan_count_kernel, dim3((unsigned)p.chunks), block, hist, stream, 1, p);
+  if (e == cudaSuccess) ++*launches;
+  if (e == cudaSuccess) e = launch_pdl(plan_scan_kernel, dim3(1), block, lists, stream, 1, p);
+  if (e == cudaSuccess) ++*launches;
+  if (e == cudaSuccess) e = launch_pdl(plan_place_kernel, dim3((unsigned)p.chunks), block, hist, stream, 1, p);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+cudaError_t combine_backward_launch(const ExpertRows& x, bool y_f32, int64_t n, const float* weights, const void* Y,
+                                    const uint16_t* dout, uint16_t* dY, float* dweights, cudaStream_t stream,
+                                    uint64_t* launches) {
+  CombineBackParams p{};
+  p.row_src = x.row_src;
+  p.live = x.offsets + x.experts;
+  p.slot = x.slot;
+  p.weights = weights;
+  p.Y = Y;
+  p.dout = dout;
+  p.dY = dY;
+  p.dweights = dweights;
+  p.n = n;
+  p.pairs = x.tokens * x.topk;
+  p.topk = (int)x.topk;
+  p.row_blocks = (x.rows + kWarps - 1) / kWarps;
+  auto aligned = [](const void* q) { return reinterpret_cast<uintptr_t>(q) % 16 == 0; };
+  p.vec = n % 8 == 0 && aligned(dout) && aligned(dY) && (y_f32 || aligned(Y));
+  const int64_t blocks = p.row_blocks + (dweights ? (p.pairs + kThreads - 1) / kThreads : 0);
+  if (blocks <= 0) return cudaSuccess;
+  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
+  const dim3 grid((unsigned)blocks), block(kThreads);
+  const cudaError_t e = y_f32 ? launch_pdl(combine_backward_kernel<true>, grid, block, 0, stream, 1, p)
+                              : launch_pdl(combine_backward_kernel<false>, grid, block, 0, stream, 1, p);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+}  // namespace morello
