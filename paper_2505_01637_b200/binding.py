@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmorello.so")
@@ -127,11 +128,17 @@ def _addr(x):
 
 def _stream(stream):
     if stream is None:
-        import sys
         torch = sys.modules.get("torch")
-        if torch is not None and torch.cuda.is_available():
-            return torch.cuda.current_stream().cuda_stream or None
-        return None
+        if torch is None:
+            return None
+        if not torch.cuda.is_initialized() and not torch.cuda.is_available():
+            return None
+        # The raw handle of the current device's current stream, where torch has a call for it: building a
+        # Stream object costs microseconds, as much as a small call's launch.
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(torch.cuda.current_device()) or None
+        return torch.cuda.current_stream().cuda_stream or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None

@@ -64,12 +64,19 @@ struct Barriers {
   int abort_flag;
 };
 
-__device__ __forceinline__ float act_by(int act, float v) {
-  if (act == kActNone) return v;
-  if (act == kActRelu) return act_value<kActRelu>(v);
-  if (act == kActGelu) return act_value<kActGelu>(v);
-  if (act == kActGeluTanh) return act_value<kActGeluTanh>(v);
-  return act_value<kActSilu>(v);
+constexpr int kBatch = 16;     // rows a thread finishes at a time
+
+template <int kAct>
+__device__ __forceinline__ void act_batch(float (&v)[kBatch]) {
+#pragma unroll
+  for (int q = 0; q < kBatch; ++q) v[q] = act_value<kAct>(v[q]);
+}
+__device__ __forceinline__ void act_batch_by(int act, float (&v)[kBatch]) {
+  if (act == kActNone) return;
+  if (act == kActRelu) act_batch<kActRelu>(v);
+  else if (act == kActGelu) act_batch<kActGelu>(v);
+  else if (act == kActGeluTanh) act_batch<kActGeluTanh>(v);
+  else act_batch<kActSilu>(v);
 }
 
 template <int kRows>
@@ -139,6 +146,22 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_after_sync();
   const uint32_t tmem_base = bars->tmem_base;
 
+  // The finishing of rows: this thread's column, and its rows lead + j * stride of a chunk (the cluster's
+  // blocks share the rows out; gated: so do the two halves of the threads).
+  const int t = (int)threadIdx.x - 64;                  // 0 .. 127 in the epilogue warps
+  const int j_col = p.gated ? t & 63 : t;
+  const int col = col0 + j_col;
+  const int stride = p.split * (p.gated ? 2 : 1);
+  const int lead = p.gated ? slice * 2 + (t >> 6) : slice;
+  uint16_t held[kBatch];                                // residual of the next batch of rows
+  auto load_residual = [&](int first, int rows_here, int j0, uint16_t (&x)[kBatch]) {
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int i = lead + (j0 + q) * stride;
+      x[q] = p.residual && i < rows_here && col < p.n ? p.residual[(int64_t)(first + i) * p.n + col] : (uint16_t)0;
+    }
+  };
+
   int stage = 0;
   uint32_t phase = 0, acc_phase = 0;
   bool ok = true;
@@ -189,6 +212,7 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     } else {
       // ---------------------------------------------------------------- epilogue
       const int quarter = warp & 3;
+      load_residual(first, rows_here, 0, held);
       ok = mbar_wait(&bars->acc_full, acc_phase, abort_flag, p.status, 43);
       ok = __all_sync(0xffffffffu, ok);
       acc_phase ^= 1;
@@ -217,54 +241,74 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       __syncwarp();
     }
     cluster_sync();
-    if (warp >= 2 && !*abort_flag) {
-      const float* part = reinterpret_cast<const float*>(stages);
-      const int t = (int)threadIdx.x - 64;                  // 0 .. 127
-      const int j = p.gated ? t & 63 : t;                   // column inside the strip
-      const int col = col0 + j;
+    if (warp >= 2 && !*abort_flag && col < p.n) {
+      const float* part = reinterpret_cast<const float*>(stages) + j_col;
       const uint16_t* bias = p.bias ? p.bias + (int64_t)group * p.z_pitch : nullptr;
-      if (col < p.n) {
-        const float b0 = bias ? bf16_value(bias[col]) : 0.f;
-        const float b1 = bias && p.gated ? bf16_value(bias[p.n + col]) : 0.f;
-        // Gated: two rows at a time, one per half of the threads.
-        const int skip = p.gated ? 2 : 1, lead = p.gated ? t >> 6 : 0;
-        for (int i = slice * skip + lead; i < rows_here; i += p.split * skip) {
-          const float* at = part + i * kStrip + j;
-          float v = *peer_shared(at, 0u), u = 0.f;
-          for (int s = 1; s < p.split; ++s) v += *peer_shared(at, (uint32_t)s);
-          if (p.gated) {
-            u = *peer_shared(at + 64, 0u);
-            for (int s = 1; s < p.split; ++s) u += *peer_shared(at + 64, (uint32_t)s);
-            u += b1;
+      const float b0 = bias ? bf16_value(bias[col]) : 0.f;
+      const float b1 = bias && p.gated ? bf16_value(bias[p.n + col]) : 0.f;
+      for (int j0 = 0; lead + j0 * stride < rows_here; j0 += kBatch) {
+        if (j0 > 0) load_residual(first, rows_here, j0, held);
+        float v[kBatch], u[kBatch];
+        auto sum = [&](int offset, float (&x)[kBatch]) {
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q) x[q] = 0.f;
+          for (int s = 0; s < p.split; ++s) {
+            const float* peer = peer_shared(part + offset, (uint32_t)s);
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q) {
+              const int i = lead + (j0 + q) * stride;
+              if (i < rows_here) x[q] += peer[i * kStrip];
+            }
           }
-          v += b0;
-          const int64_t row = first + i;
-          if (p.Z) {
-            p.Z[row * p.z_pitch + col] = bf16_round(v);
-            if (p.gated) p.Z[row * p.z_pitch + p.n + col] = bf16_round(u);
-          }
-          v = act_by(p.act, v);
-          if (p.gated) v *= u;
-          const int64_t out = row * p.n + col;
-          if (p.residual) v += bf16_value(p.residual[out]);
-          if (p.out_f32) {
-            float* y = static_cast<float*>(p.Y) + out;
-            *y = p.accumulate ? *y + v : v;
-          } else {
-            static_cast<uint16_t*>(p.Y)[out] = bf16_round(v);
+        };
+        sum(0, v);
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) v[q] += b0;
+        if (p.gated) {
+          sum(64, u);
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q) u[q] += b1;
+        }
+        if (p.Z) {
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q) {
+            const int i = lead + (j0 + q) * stride;
+            if (i >= rows_here) continue;
+            uint16_t* z = p.Z + (int64_t)(first + i) * p.z_pitch + col;
+            z[0] = bf16_round(v[q]);
+            if (p.gated) z[p.n] = bf16_round(u[q]);
           }
         }
-        // The block's rows that hold no token are zeros.
-        if (p.zero_padding && chunk + 1 == chunks) {
-          for (int i = rows + slice * skip + lead; i < kExpertBlock; i += p.split * skip) {
-            const int64_t row = row0 + i, out = row * p.n + col;
-            if (p.Z) {
-              p.Z[row * p.z_pitch + col] = 0;
-              if (p.gated) p.Z[row * p.z_pitch + p.n + col] = 0;
-            }
-            if (p.out_f32) static_cast<float*>(p.Y)[out] = 0.f;
-            else static_cast<uint16_t*>(p.Y)[out] = 0;
+        act_batch_by(p.act, v);
+        if (p.gated) {
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q) v[q] *= u[q];
+        }
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+          const int i = lead + (j0 + q) * stride;
+          if (i >= rows_here) continue;
+          const int64_t out = (int64_t)(first + i) * p.n + col;
+          const float y = v[q] + bf16_value(held[q]);
+          if (p.out_f32) {
+            float* dst = static_cast<float*>(p.Y) + out;
+            *dst = p.accumulate ? *dst + y : y;
+          } else {
+            static_cast<uint16_t*>(p.Y)[out] = bf16_round(y);
           }
+        }
+      }
+      // The rows that hold no token are zeros up to the next multiple of 16 (what the weight gradient's
+      // contraction reads); a decoding step does not write 127 rows for one.
+      if (p.zero_padding && chunk + 1 == chunks) {
+        for (int i = rows + lead; i < (rows + 15) / 16 * 16; i += stride) {
+          const int64_t row = row0 + i, out = row * p.n + col;
+          if (p.Z) {
+            p.Z[row * p.z_pitch + col] = 0;
+            if (p.gated) p.Z[row * p.z_pitch + p.n + col] = 0;
+          }
+          if (p.out_f32) static_cast<float*>(p.Y)[out] = 0.f;
+          else static_cast<uint16_t*>(p.Y)[out] = 0;
         }
       }
     }

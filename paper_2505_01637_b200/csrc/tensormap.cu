@@ -25,11 +25,18 @@ cudaError_t make_tensor_map_3d(CUtensorMap* out, CUtensorMapDataType dtype, int 
                                const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
                                uint32_t box0, uint32_t box1, CUtensorMapSwizzle swizzle,
                                CUtensorMapL2promotion promotion) {
+  return make_tensor_map_3d_box(out, dtype, elem_bytes, base, d0, d1, d2, box0, box1, 1, swizzle, promotion);
+}
+
+cudaError_t make_tensor_map_3d_box(CUtensorMap* out, CUtensorMapDataType dtype, int elem_bytes,
+                                   const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
+                                   uint32_t box0, uint32_t box1, uint32_t box2, CUtensorMapSwizzle swizzle,
+                                   CUtensorMapL2promotion promotion) {
   std::call_once(g_once, resolve);
   if (!g_encode) return cudaErrorNotSupported;
   cuuint64_t dims[3] = {d0, d1, d2};
   cuuint64_t strides[2] = {d0 * (uint64_t)elem_bytes, d0 * d1 * (uint64_t)elem_bytes};
-  cuuint32_t box[3] = {box0, box1, 1};
+  cuuint32_t box[3] = {box0, box1, box2};
   cuuint32_t estr[3] = {1, 1, 1};
   CUresult r = g_encode(out, dtype, 3, const_cast<void*>(base), dims, strides, box, estr,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion,

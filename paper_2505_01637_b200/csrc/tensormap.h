@@ -17,4 +17,10 @@ cudaError_t make_tensor_map_3d(CUtensorMap* out, CUtensorMapDataType dtype, int 
                                uint32_t box0, uint32_t box1, CUtensorMapSwizzle swizzle,
                                CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 
+// The same with a box {box0, box1, box2}.
+cudaError_t make_tensor_map_3d_box(CUtensorMap* out, CUtensorMapDataType dtype, int elem_bytes,
+                                   const void* base, uint64_t d0, uint64_t d1, uint64_t d2,
+                                   uint32_t box0, uint32_t box1, uint32_t box2, CUtensorMapSwizzle swizzle,
+                                   CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+
 }  // namespace morello
