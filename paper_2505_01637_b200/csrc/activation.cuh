@@ -25,62 +25,83 @@ __device__ __forceinline__ float fast_reciprocal(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// p(t) = 1 / (1 + e^-t); e^-t may overflow to infinity, the quotient is then 0.
-__device__ __forceinline__ float logistic(float t) { return fast_reciprocal(1.f + __expf(-t)); }
+__device__ __forceinline__ float fast_exp2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -3.402823466e38f;
+// p(t) = 1 / (1 + e^-t), given t log2(e); the power may overflow to infinity, the quotient is then 0.
+__device__ __forceinline__ float logistic2(float t_log2e) { return fast_reciprocal(1.f + fast_exp2(-t_log2e)); }
 
-constexpr float kSqrtHalf = 0.70710678118654752f;
-// Phi(z), and e^(-z^2 / 2) for the slope.
-__device__ __forceinline__ float normal_cdf(float z, float* bell) {
-  const float x = fabsf(z) * kSqrtHalf;
-  const float t = fast_reciprocal(fmaf(0.3275911f, x, 1.f));
-  float s = fmaf(t, 1.061405429f, -1.453152027f);
-  s = fmaf(t, s, 1.421413741f);
-  s = fmaf(t, s, -0.284496736f);
-  s = fmaf(t, s, 0.254829592f);
-  *bell = __expf(-x * x);
-  const float tail = 0.5f * s * t * *bell;
-  return z < 0.f ? tail : 1.f - tail;
+// The tail 1 - Phi(a) of the normal distribution, a >= 0 and moderate, and its bell e^(-a^2 / 2).
+__device__ __forceinline__ float normal_tail(float a, float* bell) {
+  const float t = fast_reciprocal(fmaf(0.23164189f, a, 1.f));        // 0.3275911 / sqrt 2
+  float s = fmaf(t, 0.5307027145f, -0.7265760135f);                  // the coefficients halved
+  s = fmaf(t, s, 0.7107068705f);
+  s = fmaf(t, s, -0.142248368f);
+  s = fmaf(t, s, 0.127414796f);
+  *bell = fast_exp2(a * (-0.5f * kLog2e) * a);
+  return s * t * *bell;
 }
 
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kTwoSqrt2OverPi = 1.5957691216057308f;   // 2 sqrt(2 / pi)
-
-// Beyond kTail every one of them has reached its limits in f32 (z or 0, slope 1 or 0): the limits are
-// returned there, so that an infinite z gives them too instead of inf * 0.  NaN stays NaN.
+// Where |z| is past kTail every activation has reached its limits in f32.
 constexpr float kTail = 100.f;
 
+// Every result is free of branches and of inf * 0: at z = -inf the other factor is 0, so z is kept finite
+// there (max with the lowest number; a NaN z, which max would swallow, is still in the other factor).
 template <int kAct>
 __device__ __forceinline__ float act_value(float z) {
   if constexpr (kAct == kActNone) return z;
-  if constexpr (kAct == kActRelu) return z < 0.f ? 0.f : z;
-  float p;
+  const float relu = z < 0.f ? 0.f : z;
+  if constexpr (kAct == kActRelu) return relu;
   if constexpr (kAct == kActGelu) {
+    // z Phi(z) = max(z, 0) - |z| (1 - Phi(|z|))
     float bell;
-    p = normal_cdf(z, &bell);
-  } else if constexpr (kAct == kActGeluTanh) {
-    p = logistic(kTwoSqrt2OverPi * fmaf(0.044715f * z * z, z, z));
-  } else {
-    p = logistic(z);
+    const float a = fminf(fabsf(z), kTail);
+    return fmaf(-a, normal_tail(a, &bell), relu);
   }
-  return z < -kTail ? 0.f : z > kTail ? z : z * p;
+  if constexpr (kAct == kActGeluTanh)
+    return fmaxf(z, kLowest) * logistic2(z * fmaf(0.044715f * kTwoSqrt2OverPi * kLog2e * z, z, kTwoSqrt2OverPi * kLog2e));
+  return fmaxf(z, kLowest) * logistic2(z * kLog2e);
 }
+// act'(z), and act(z) beside it: both come from the same exponential.
 template <int kAct>
-__device__ __forceinline__ float act_slope(float z) {
-  if constexpr (kAct == kActNone) return 1.f;
-  if constexpr (kAct == kActRelu) return z > 0.f ? 1.f : (z != z ? z : 0.f);
+__device__ __forceinline__ float act_slope(float z, float* value) {
+  if constexpr (kAct == kActNone) {
+    *value = z;
+    return 1.f;
+  }
+  const float relu = z < 0.f ? 0.f : z;
+  if constexpr (kAct == kActRelu) {
+    *value = relu;
+    return z > 0.f ? 1.f : (z != z ? z : 0.f);
+  }
   float d;
   if constexpr (kAct == kActGelu) {
     float bell;
-    const float phi = normal_cdf(z, &bell);
-    d = phi + z * kInvSqrt2Pi * bell;
-  } else if constexpr (kAct == kActGeluTanh) {
-    const float p = logistic(kTwoSqrt2OverPi * fmaf(0.044715f * z * z, z, z));
-    d = p + z * p * (1.f - p) * kTwoSqrt2OverPi * (1.f + 3.f * 0.044715f * z * z);
-  } else {
-    const float p = logistic(z);
-    d = p * (1.f + z * (1.f - p));
+    const float a = fminf(fabsf(z), kTail);
+    const float tail = normal_tail(a, &bell);
+    *value = fmaf(-a, tail, relu);
+    d = (z < 0.f ? tail : 1.f - tail) + copysignf(a, z) * kInvSqrt2Pi * bell;
+    return z != z ? z : d;
   }
-  return z < -kTail ? 0.f : z > kTail ? 1.f : d;
+  // Past the tail p (1 - p) is 0; c is z held where its products stay finite.
+  const float c = fminf(fmaxf(z, -kTail), kTail);
+  if constexpr (kAct == kActGeluTanh) {
+    const float p = logistic2(c * fmaf(0.044715f * kTwoSqrt2OverPi * kLog2e * c, c, kTwoSqrt2OverPi * kLog2e));
+    *value = fmaxf(z, kLowest) * p;
+    d = p + c * p * (1.f - p) * kTwoSqrt2OverPi * fmaf(3.f * 0.044715f * c, c, 1.f);
+  } else {
+    const float p = logistic2(c * kLog2e);
+    *value = fmaxf(z, kLowest) * p;
+    d = p * fmaf(c, 1.f - p, 1.f);
+  }
+  if (z != z) *value = z;
+  return z != z ? z : d;
 }
 
 // f32 <-> bf16, the rounding of every 16-bit output: to nearest, ties to even.

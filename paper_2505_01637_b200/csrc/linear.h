@@ -64,6 +64,7 @@ struct TileCall {
   int64_t m = 0, n = 0, k = 0;   // extents of one output (gated: n columns, B has 2 n); k unused by kContract
   int64_t b_up = 0;        // gated: where the second half of B's columns begins in its stored order
   bool zero_padding = false;     // kRows: rows that hold no token are written as zeros
+  bool gather_a = false;         // few-rows kernel: A is [tokens][cols], its rows fetched through the plan
   ExpertRows experts;
   LinearEpilogue epi;
 };
@@ -73,14 +74,13 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& call, cudaStream_
 constexpr int kLinearFewRows = 64;
 cudaError_t rows_launch(const DeviceInfo& dev, const TileCall& call, cudaStream_t stream, uint64_t* launches);
 
-// Copies with zero padding (and an optional gather): dst[g][r][c] = src[g][row(r)][c] inside the
-// source, else 0; dst's cols_out is a multiple of 8, its base 16-byte aligned.
+// Copies with zero padding: dst[g][r][c] = src[g][row(r)][c] inside the source, else 0; dst's cols_out is a multiple of 8, its base 16-byte aligned.
 struct CopyJob {
   const uint16_t* src = nullptr;
   uint16_t* dst = nullptr;
   int64_t groups = 1, rows_in = 0, cols_in = 0, rows_out = 0, cols_out = 0;
-  bool gather = false;                  // with experts: row r of dst is token row_src[r] / topk of src
   const ExpertRows* experts = nullptr;  // rows past the live ones are left alone
+  bool gather = false;                  // with experts: row r of dst is token row_src[r] / topk of src
 };
 cudaError_t copy_launch(const CopyJob& job, cudaStream_t stream, uint64_t* launches);
 

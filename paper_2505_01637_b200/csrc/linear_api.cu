@@ -69,6 +69,9 @@ struct Layer {
   int64_t x_rows() const { return gather ? x.tokens : m; }
 };
 
+// Few rows per weight matrix: the weights' stream is what counts.
+bool few_rows(const Layer& l) { return (l.grouped ? l.x.tokens : l.m) <= kLinearFewRows; }
+
 int check_extents(int64_t m, int64_t k, int64_t n, int64_t wide, int64_t groups) {
   if (m < 0 || k < 0 || n < 0) return MORELLO_ERR_INVALID_SHAPE;
   if (m > kMaxExtent || k > kMaxExtent || n > kMaxExtent || wide > kMaxExtent) return MORELLO_ERR_INVALID_SHAPE;
@@ -95,27 +98,29 @@ struct Operands {
   int64_t w_up = 0;   // forward form, gated: where the second half begins
 };
 
-// X: [rows][k]; gathered through the plan, or padded when the TMA engine cannot address it.
-int stage_x(const Layer& l, const void* X, Carver& ws, bool dry, cudaStream_t s, uint64_t* launches, MatrixView* out) {
+// X: [rows][k], padded when the TMA engine cannot address it; with `gather` its rows are copied in the
+// experts' layout (the tile kernel's gathered loads, 32 of four rows per stage, were measured at twice the
+// time of the whole product; the few-rows kernel gathers for itself).
+int stage_x(const Layer& l, const void* X, bool gather, Carver& ws, bool dry, cudaStream_t s, uint64_t* launches, MatrixView* out) {
   const uint16_t* src = static_cast<const uint16_t*>(X);
-  const bool copy = l.gather || l.k % 8 != 0 || (!dry && !aligned(X, 16));
-  out->rows = l.m;
+  const bool copy = gather || l.k % 8 != 0 || (!dry && !aligned(X, 16));
+  out->rows = gather ? l.m : l.x_rows();
   out->groups = 1;
   out->cols = copy ? round8(l.k) : l.k;
   out->p = src;
   if (!copy) return MORELLO_OK;
-  uint16_t* dst = ws.take<uint16_t>((size_t)l.m * out->cols * 2);
+  uint16_t* dst = ws.take<uint16_t>((size_t)out->rows * out->cols * 2);
   out->p = dst;
   if (!ws.base) return MORELLO_OK;
   CopyJob j;
   j.src = src;
   j.dst = dst;
   j.rows_in = l.x_rows();
+  j.rows_out = out->rows;
   j.cols_in = l.k;
-  j.rows_out = l.m;
   j.cols_out = out->cols;
-  j.gather = l.gather;
-  if (l.grouped) j.experts = &l.x;
+  j.gather = gather;
+  if (gather || (l.grouped && !l.gather)) j.experts = &l.x;
   const cudaError_t e = copy_launch(j, s, launches);
   return e == cudaSuccess ? MORELLO_OK : record_cuda_error(e);
 }
@@ -157,9 +162,6 @@ struct ForwardArgs {
   bool y_f32;
 };
 
-// Few rows per weight matrix: the weights' stream is what counts.
-bool few_rows(const Layer& l) { return (l.grouped ? l.x.tokens : l.m) <= kLinearFewRows; }
-
 int product(const DeviceInfo& dev, const Layer& l, const TileCall& c, cudaStream_t s, uint64_t* launches) {
   const cudaError_t e = c.mode != TileMode::kContract && !c.a_mn && few_rows(l) ? rows_launch(dev, c, s, launches)
                                                                                 : tile_launch(dev, c, s, launches);
@@ -173,7 +175,7 @@ int forward(const DeviceInfo& dev, const Layer& l, const ForwardArgs& a, Carver&
   int64_t up = 0;
   int rc;
   if (l.k > 0) {
-    if ((rc = stage_x(l, a.X, ws, dry, s, launches, &x)) != MORELLO_OK) return rc;
+    if ((rc = stage_x(l, a.X, l.gather && !few_rows(l), ws, dry, s, launches, &x)) != MORELLO_OK) return rc;
     if ((rc = stage_w(l, a.W, true, ws, dry, s, launches, &w, &up)) != MORELLO_OK) return rc;
   }
   if (!ws.base) return MORELLO_OK;
@@ -186,6 +188,7 @@ int forward(const DeviceInfo& dev, const Layer& l, const ForwardArgs& a, Carver&
   c.n = l.n;
   c.k = l.k;
   c.b_up = up;
+  c.gather_a = l.gather && few_rows(l);
   c.zero_padding = l.grouped;
   c.experts = l.x;
   c.epi.act = l.act;
@@ -263,7 +266,7 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
   }
   if (want_dw) {
     MatrixView x;
-    if ((rc = stage_x(l, a.X, ws, dry, s, launches, &x)) != MORELLO_OK) return rc;
+    if ((rc = stage_x(l, a.X, l.gather, ws, dry, s, launches, &x)) != MORELLO_OK) return rc;
     if (ws.base) {
       TileCall c;
       c.mode = l.grouped ? TileMode::kContract : TileMode::kDense;

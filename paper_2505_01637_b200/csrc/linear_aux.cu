@@ -1,4 +1,4 @@
-// The memory-bound companions of the linear layers' products: zero-padded and gathered copies of
+// The memory-bound companions of the linear layers' products: zero-padded copies of
 // operands, the activation's slope with the bias gradient, and the weighted sum of a token's rows.
 // Each is one pass over its data in 16-byte accesses where alignment allows.
 #include <algorithm>
@@ -14,6 +14,7 @@ using namespace sm100;
 
 constexpr int kThreads = 256;
 constexpr int kSlopeRows = 32;      // rows per partial sum of the bias gradient
+constexpr int kSlopeUnroll = kSlopeRows / 8;   // rows a thread has in flight
 constexpr int kSlopeLanes = 8;      // rows a block takes at a time
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -36,36 +37,45 @@ __device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
   return make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7]));
 }
 
+// A thread moves kCopyRows rows' worth of one 8-column group, their loads in flight together.
+constexpr int kCopyRows = 4;
 struct CopyParams {
   const uint16_t* src;
   uint4* dst;
-  int64_t rows_in, cols_in, rows_out, octets;   // octets: 8-column groups of a row of dst
-  int64_t threads;
+  int64_t rows_in, cols_in, rows_out;
+  int octets;                 // 8-column groups of a row of dst
   bool vec;
   int topk;
   const int32_t* row_src;     // gather
   const int32_t* live;        // number of live rows, or null
 };
 
+// Grid: x = row groups (all groups of dst one after another), y = spans of kThreads octets.
 __global__ void __launch_bounds__(kThreads) copy_kernel(const CopyParams p) {
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int o = blockIdx.y * kThreads + threadIdx.x;
+  const int64_t spans = (p.rows_out + kCopyRows - 1) / kCopyRows;
+  const int64_t g = blockIdx.x / spans;
+  const int64_t r0 = (blockIdx.x - g * spans) * kCopyRows;
   pdl_wait();
   pdl_release();
-  if (idx >= p.threads) return;
-  const int64_t o = idx % p.octets;
-  const int64_t r = (idx / p.octets) % p.rows_out;
-  const int64_t g = idx / (p.octets * p.rows_out);
-  if (p.live && r >= *p.live) return;
-  int64_t from = r;
-  if (p.row_src) {
-    const int32_t s = p.row_src[r];
-    from = s < 0 ? -1 : s / p.topk;
+  if (o >= p.octets || (p.live && r0 >= *p.live)) return;
+  const int64_t left = p.cols_in - (int64_t)o * 8;
+  uint4 w[kCopyRows];
+#pragma unroll
+  for (int i = 0; i < kCopyRows; ++i) {
+    const int64_t r = r0 + i;
+    int64_t from = r;
+    if (p.row_src && r < p.rows_out) {
+      const int32_t s = p.row_src[r];
+      from = s < 0 ? -1 : s / p.topk;
+    }
+    w[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (r < p.rows_out && from >= 0 && from < p.rows_in && left > 0)
+      w[i] = load8_raw(p.src + (g * p.rows_in + from) * p.cols_in + (int64_t)o * 8, p.vec && left >= 8, left);
   }
-  uint4 w = make_uint4(0u, 0u, 0u, 0u);
-  const int64_t left = p.cols_in - o * 8;
-  if (from >= 0 && from < p.rows_in && left > 0)
-    w = load8_raw(p.src + (g * p.rows_in + from) * p.cols_in + o * 8, p.vec && left >= 8, left);
-  p.dst[idx] = w;
+#pragma unroll
+  for (int i = 0; i < kCopyRows; ++i)
+    if (r0 + i < p.rows_out) p.dst[(g * p.rows_out + r0 + i) * p.octets + o] = w[i];
 }
 
 struct SlopeParams {
@@ -74,29 +84,13 @@ struct SlopeParams {
   uint16_t* dZ;
   float* partial;
   int64_t rows, n, pitch;      // pitch: columns of a row of dZ, the width rounded up to 8
-  int act;
   bool vec;
   const int32_t* row_src;
   const int32_t* live;
 };
 
-__device__ __forceinline__ float slope_by(int act, float z) {
-  if (act == kActNone) return 1.f;
-  if (act == kActRelu) return act_slope<kActRelu>(z);
-  if (act == kActGelu) return act_slope<kActGelu>(z);
-  if (act == kActGeluTanh) return act_slope<kActGeluTanh>(z);
-  return act_slope<kActSilu>(z);
-}
-__device__ __forceinline__ float value_by(int act, float z) {
-  if (act == kActNone) return z;
-  if (act == kActRelu) return act_value<kActRelu>(z);
-  if (act == kActGelu) return act_value<kActGelu>(z);
-  if (act == kActGeluTanh) return act_value<kActGeluTanh>(z);
-  return act_value<kActSilu>(z);
-}
-
 // A block: 256 columns (32 groups of 8) x kSlopeRows rows, eight rows at a time.
-template <bool kGated>
+template <int kAct, bool kGated>
 __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeParams p) {
   __shared__ float sums[kSlopeLanes][kGated ? 2 : 1][256 + 8];
   const int group = threadIdx.x & 31, lane = threadIdx.x >> 5;
@@ -113,33 +107,38 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeParams p) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) s0[e] = s1[e] = 0.f;
   if (left > 0) {
-#pragma unroll 2
-    for (int64_t row = row_begin + lane; row < row_end; row += kSlopeLanes) {
-      float d0[8], d1[8];
+    // All loads of the thread's rows first.
+    uint4 wd[kSlopeUnroll], w0[kSlopeUnroll], w1[kGated ? kSlopeUnroll : 1];
+    const int64_t width = kGated ? 2 * p.n : p.n;
+    const bool wants_z = kAct != kActNone || kGated;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d0[e] = d1[e] = 0.f;
-      const bool holds = !p.row_src || p.row_src[row] >= 0;
-      if (holds) {
-        float dy[8], z0[8], z1[8];
-        const int64_t width = kGated ? 2 * p.n : p.n;
-        const uint4 wd = load8_raw(p.dY + row * p.n + col, vec, left);
-        uint4 w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
-        if (p.Z) {
-          w0 = load8_raw(p.Z + row * width + col, vec, left);
-          if constexpr (kGated) w1 = load8_raw(p.Z + row * width + p.n + col, vec, left);
-        }
-        unpack8(wd, dy);
-        unpack8(w0, z0);
-        unpack8(w1, z1);
+    for (int i = 0; i < kSlopeUnroll; ++i) {
+      const int64_t row = row_begin + lane + i * kSlopeLanes;
+      wd[i] = w0[i] = make_uint4(0u, 0u, 0u, 0u);
+      if constexpr (kGated) w1[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (row >= row_end || (p.row_src && p.row_src[row] < 0)) continue;      // zeros give zeros
+      wd[i] = load8_raw(p.dY + row * p.n + col, vec, left);
+      if (wants_z) w0[i] = load8_raw(p.Z + row * width + col, vec, left);
+      if constexpr (kGated) w1[i] = load8_raw(p.Z + row * width + p.n + col, vec, left);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float slope = slope_by(p.act, z0[e]);
-          if constexpr (kGated) {
-            d0[e] = dy[e] * z1[e] * slope;
-            d1[e] = dy[e] * value_by(p.act, z0[e]);
-          } else {
-            d0[e] = dy[e] * slope;
-          }
+    for (int i = 0; i < kSlopeUnroll; ++i) {
+      const int64_t row = row_begin + lane + i * kSlopeLanes;
+      if (row >= row_end) break;
+      float dy[8], z0[8], z1[8], d0[8], d1[8];
+      unpack8(wd[i], dy);
+      unpack8(w0[i], z0);
+      if constexpr (kGated) unpack8(w1[i], z1);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float value;
+        const float slope = act_slope<kAct>(z0[e], &value);
+        if constexpr (kGated) {
+          d0[e] = dy[e] * z1[e] * slope;
+          d1[e] = dy[e] * value;
+        } else {
+          d0[e] = dy[e] * slope;
+          d1[e] = 0.f;
         }
       }
       if (p.dZ) {
@@ -155,7 +154,7 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeParams p) {
             if constexpr (kGated) dst[p.n + e] = bf16_round(d1[e]);
           }
           if (left <= 8)       // the columns that round the row up to eight
-            for (int64_t c = kGated ? 2 * p.n : p.n; c < p.pitch; ++c) p.dZ[row * p.pitch + c] = 0;
+            for (int64_t c = width; c < p.pitch; ++c) p.dZ[row * p.pitch + c] = 0;
         }
       }
 #pragma unroll
@@ -287,8 +286,7 @@ cudaError_t copy_launch(const CopyJob& j, cudaStream_t stream, uint64_t* launche
   p.rows_in = j.rows_in;
   p.cols_in = j.cols_in;
   p.rows_out = j.rows_out;
-  p.octets = j.cols_out / 8;
-  p.threads = j.groups * j.rows_out * p.octets;
+  p.octets = (int)(j.cols_out / 8);
   p.vec = j.cols_in % 8 == 0 && aligned16(j.src);
   if (j.experts) {
     p.live = j.experts->offsets + j.experts->experts;
@@ -297,10 +295,11 @@ cudaError_t copy_launch(const CopyJob& j, cudaStream_t stream, uint64_t* launche
       p.topk = (int)j.experts->topk;
     }
   }
-  if (p.threads <= 0) return cudaSuccess;
-  unsigned blocks = 0;
-  cudaError_t e = grid_for(p.threads, &blocks);
-  if (e == cudaSuccess) e = launch_pdl(copy_kernel, dim3(blocks), dim3(kThreads), 0, stream, 1, p);
+  const int64_t blocks = j.groups * ((j.rows_out + kCopyRows - 1) / kCopyRows);
+  const int64_t spans = (p.octets + kThreads - 1) / kThreads;
+  if (blocks <= 0 || spans <= 0) return cudaSuccess;
+  if (blocks >= (1ll << 31) || spans > 65535) return cudaErrorInvalidValue;
+  const cudaError_t e = launch_pdl(copy_kernel, dim3((unsigned)blocks, (unsigned)spans), dim3(kThreads), 0, stream, 1, p);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
@@ -324,7 +323,6 @@ cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& c, cudaStream_t
     p.rows = c.rows;
     p.n = c.n;
     p.pitch = (width + 7) / 8 * 8;
-    p.act = c.act;
     p.vec = c.n % 8 == 0 && aligned16(c.dY) && aligned16(c.Z);
     if (c.experts) {
       p.row_src = c.experts->row_src;
@@ -333,8 +331,19 @@ cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& c, cudaStream_t
     const int64_t strips = (c.n + 255) / 256;
     if (parts >= (1ll << 31) || strips > 65535) return cudaErrorInvalidValue;
     const dim3 grid((unsigned)parts, (unsigned)strips);
-    e = c.gated ? launch_pdl(slope_kernel<true>, grid, dim3(kThreads), 0, stream, 1, p)
-                : launch_pdl(slope_kernel<false>, grid, dim3(kThreads), 0, stream, 1, p);
+    auto go = [&](auto kern) { return launch_pdl(kern, grid, dim3(kThreads), 0, stream, 1, p); };
+    switch (c.act * 2 + (c.gated ? 1 : 0)) {
+      case 0: e = go(slope_kernel<kActNone, false>); break;
+      case 1: e = go(slope_kernel<kActNone, true>); break;
+      case 2: e = go(slope_kernel<kActRelu, false>); break;
+      case 3: e = go(slope_kernel<kActRelu, true>); break;
+      case 4: e = go(slope_kernel<kActGelu, false>); break;
+      case 5: e = go(slope_kernel<kActGelu, true>); break;
+      case 6: e = go(slope_kernel<kActGeluTanh, false>); break;
+      case 7: e = go(slope_kernel<kActGeluTanh, true>); break;
+      case 8: e = go(slope_kernel<kActSilu, false>); break;
+      default: e = go(slope_kernel<kActSilu, true>); break;
+    }
     if (e != cudaSuccess) return e;
     ++*launches;
   }

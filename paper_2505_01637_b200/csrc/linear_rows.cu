@@ -43,7 +43,9 @@ struct RowsParams {
   int m, n;              // rows (dense) and output columns
   int k_blocks, split, per_slice;
   int b_up;
-  uint8_t b_mn, gated, grouped, zero_padding;
+  uint8_t b_mn, gated, grouped, zero_padding, gather;
+  int topk, tokens;
+  const int32_t* row_src;
   const int32_t* block_expert;
   const int32_t* offsets;
   const int32_t* counts;
@@ -170,20 +172,39 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const int rows_here = min(kRows, rows - chunk * kRows);
     if (warp == 0) {
       // ---------------------------------------------------------------- producer
-      if (elect_one()) {
-        for (int kb = kb0; kb < kb1 && ok; ++kb) {
-          if (!(ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 41))) break;
-          uint8_t* sb = stages + (size_t)stage * S::kStageBytes;
-          mbar_arrive_expect_tx(&bars->full[stage], S::kStageBytes);
-          const int kc = kb * kTileK;
-          if (p.b_mn) {
-            tma_load_3d(sb, &map_b, &bars->full[stage], col0, kc, group);
-            tma_load_3d(sb + kBoxBytes, &map_b, &bars->full[stage], col1, kc, group);
-          } else {
-            tma_load_3d(sb, &map_b, &bars->full[stage], kc, col0, group);
-            tma_load_3d(sb + kBoxBytes, &map_b, &bars->full[stage], kc, col1, group);
+      // One lane, or, when the rows are gathered through the plan, the whole warp: a lane fetches four rows.
+      if (p.gather || elect_one()) {
+        const bool lead = !p.gather || lane == 0;
+        int from[4] = {0, 0, 0, 0};
+        if (p.gather && lane < kRows / 4) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int32_t src = p.row_src[first + lane * 4 + i];
+            from[i] = src < 0 ? p.tokens : src / p.topk;      // past the last token: zeros
           }
-          tma_load_3d(sb + 2 * kBoxBytes, &map_a, &bars->full[stage], kc, first, 0);
+        }
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (ok) ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 41);
+          if (p.gather) ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          uint8_t* sb = stages + (size_t)stage * S::kStageBytes;
+          const int kc = kb * kTileK;
+          if (lead) {
+            mbar_arrive_expect_tx(&bars->full[stage], S::kStageBytes);
+            if (p.b_mn) {
+              tma_load_3d(sb, &map_b, &bars->full[stage], col0, kc, group);
+              tma_load_3d(sb + kBoxBytes, &map_b, &bars->full[stage], col1, kc, group);
+            } else {
+              tma_load_3d(sb, &map_b, &bars->full[stage], kc, col0, group);
+              tma_load_3d(sb + kBoxBytes, &map_b, &bars->full[stage], kc, col1, group);
+            }
+            if (!p.gather) tma_load_3d(sb + 2 * kBoxBytes, &map_a, &bars->full[stage], kc, first, 0);
+          }
+          if (p.gather) {
+            __syncwarp();
+            if (lane < kRows / 4)
+              tma_gather4(sb + 2 * kBoxBytes + lane * 512, &map_a, &bars->full[stage], kc, from[0], from[1], from[2], from[3]);
+          }
           if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         }
         if (chunk + 1 == chunks) pdl_release();
@@ -349,8 +370,9 @@ cudaError_t launch(const DeviceInfo& dev, const TileCall& c, RowsParams p, cudaS
   if (blocks > 65535 || strips * split >= (1ll << 31)) return cudaErrorInvalidValue;
   CUtensorMap ma{}, mb{};
   if (c.k > 0) {
-    e = make_tensor_map_3d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.a.p, (uint64_t)c.a.cols, (uint64_t)c.a.rows, 1,
-                           kTileK, kRows, CU_TENSOR_MAP_SWIZZLE_128B);
+    e = c.gather_a ? make_gather_map(&ma, c.a.p, (uint64_t)c.a.cols, (uint64_t)c.a.rows)
+                   : make_tensor_map_3d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.a.p, (uint64_t)c.a.cols,
+                                        (uint64_t)c.a.rows, 1, kTileK, kRows, CU_TENSOR_MAP_SWIZZLE_128B);
     if (e == cudaSuccess)
       e = make_tensor_map_3d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.b.p, (uint64_t)c.b.cols, (uint64_t)c.b.rows,
                              (uint64_t)c.b.groups, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
@@ -376,6 +398,10 @@ cudaError_t rows_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   p.b_mn = c.b_mn;
   p.gated = ep.gated;
   p.zero_padding = p.grouped && c.zero_padding;
+  p.gather = c.gather_a;
+  p.topk = (int)std::max<int64_t>(1, c.experts.topk);
+  p.tokens = (int)c.experts.tokens;
+  p.row_src = c.experts.row_src;
   p.block_expert = c.experts.block_expert;
   p.offsets = c.experts.offsets;
   p.counts = c.experts.counts;

@@ -16,12 +16,16 @@
 // Experts: their rows begin at multiples of 128, so a 128-row tile belongs to one expert and the weight
 // gradient's contraction runs over its rows alone (rounded up to 16, where padding rows are zero).
 //
-// Epilogue, two warps per quarter of the rows, each with half of the tile's columns.  Where the TMA
-// engine can address Y, Z and the residual: a thread holds one row of 32 columns, the residual's block
-// arrives in shared memory by TMA while the accumulator is awaited, y replaces it there and leaves by TMA, Z
-// beside it (blocks of 32 rows in the 64- or 128-byte swizzle).  Anything else (n % 8 != 0, odd
-// addresses): a warp parks 32 rows x 64 accumulator columns (f32) in shared memory and reads them back
-// with eight (gated: four) lanes to a row, so that any n and alignment is a matter of predicates.
+// Epilogue: eight warps, two per quarter of the rows, which take its 32-column steps in turn; a thread
+// holds one row of 32 columns.  Where the TMA engine can address Y and Z they leave through shared memory
+// in blocks of 32 rows x 32 columns (64- or 128-byte swizzle), two of which a warp uses in turn; the residual is
+// read straight into registers while the accumulator is awaited.  Anything else (n % 8 != 0, odd addresses): a
+// warp parks 32 rows x 32 accumulator columns (f32) and reads them back with four (gated: two) lanes to a row, so
+// that any n and alignment is a matter of predicates.
+// A step is a chain of tensor-memory load, conversion, shared store, proxy fence and TMA store, about 1,100
+// cycles; eight warps keep it under a main loop of 8 contraction blocks or more.  Twelve and sixteen warps were
+// measured slower (their share of the registers spills: 4096 x 4096 x 4096 with GELU, bias, residual and Z
+// 116, 123 and 127 us).
 #include <algorithm>
 
 #include "activation.cuh"
@@ -40,13 +44,15 @@ constexpr int kBytesA = kRowsPerCta * kTileK * 2;   // 16 KiB
 constexpr int kBoxBytes = 64 * kTileK * 2;          // a 64 x 64 box: 8 KiB
 constexpr int kAccStride = 256;
 constexpr int kTmemColumns = 2 * kAccStride;
-constexpr int kEpiWarps = 8;
+constexpr int kEpiWarps = 8;                        // two per quarter of the rows
+constexpr int kParts = kEpiWarps / 4;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
 constexpr int kMaxStages = 8;
-constexpr int kEpiBlockBytes = 8 * 1024;            // per warp: four blocks of 32 x 32 bf16, or 32 x 64 f32
+constexpr int kEpiBlockBytes = 4 * 1024;            // per warp: two blocks of 32 x 32 bf16, or one of f32
 constexpr int kEpiBytes = kEpiWarps * kEpiBlockBytes;
 constexpr int kBlock16 = 32 * 32 * 2;               // 32 rows x 32 columns of bf16
 constexpr int kSmemBudget = 227 * 1024;
+constexpr int kPairTable = 257;                     // experts whose pairs of blocks a CTA pair can look up, + 1
 
 template <bool kPair, int kTileN>
 struct Shape {
@@ -55,9 +61,9 @@ struct Shape {
   static constexpr int kColsB = kTileN / kCtas;
   static constexpr int kBoxesB = kColsB / 64;
   static constexpr int kStageBytes = kBytesA + kBoxesB * kBoxBytes;
-  static constexpr int kFit = (kSmemBudget - kEpiBytes - 1024 - 512) / kStageBytes;
+  static constexpr int kFit = (kSmemBudget - kEpiBytes - 1024 - 1536) / kStageBytes;
   static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
-  static constexpr size_t kSmemBytes = (size_t)kStages * kStageBytes + kEpiBytes + 1024 + 512;
+  static constexpr size_t kSmemBytes = (size_t)kStages * kStageBytes + kEpiBytes + 1024 + 1536;
   static_assert(kColsB % 64 == 0 && kTileN <= kAccStride, "tile shape");
 };
 
@@ -65,10 +71,10 @@ struct TileParams {
   int64_t m;             // rows of one output
   int n;                 // columns of one output
   int k_blocks;          // contraction blocks (kContract: of the expert, from counts)
-  int m_tiles, n_tiles, raster;
+  int m_tiles, n_tiles;
   int64_t tiles;         // kRows: decided on the device
   int b_up;
-  uint8_t mode, a_mn, b_mn, zero_padding;
+  uint8_t mode, a_mn, b_mn, zero_padding, halves;
   // experts
   const int32_t* block_expert;
   const int32_t* offsets;
@@ -89,56 +95,111 @@ struct Barriers {
   uint64_t empty[kMaxStages];
   uint64_t acc_full[2];
   uint64_t acc_empty[2];
-  uint64_t resid[kEpiWarps][2];
   uint32_t tmem_base;
   int abort_flag;
+  int pairs_before[kPairTable];   // kRows, pairs: pairs of blocks of the experts before each
 };
 
 struct Item {
-  int mt, nt;
+  int row0, nt;     // first row of the tile
+  int row_end;      // its rows end here (kRows: the expert's blocks do), for what is written
+  int n_off, cols;  // first accumulator column inside the tile's, and how many: the tile or half of it
   int group;        // expert (bias, weights, output of kContract)
   int k_blocks;
   int k_row0;       // kContract: first row of the contraction
   int k_steps;      // 16-deep steps of the last contraction block
-  int live_end;     // rows of the output from here on hold no token (kRows), else m
+  int live_end;     // rows of the output from here on hold no token (kRows)
 };
 
-// Tiles are walked in groups of `raster` rows of tiles, row-fastest inside a group, so that the tiles
-// in flight share a few rows of A and a few columns of B in L2.
-__device__ __forceinline__ void raster_decode(int raster, int m_tiles, int n_tiles, int within, int* mt, int* nt) {
-  const int per_group = raster * n_tiles;
-  const int grp = within / per_group, r = within - grp * per_group;
-  const int rows = min(raster, m_tiles - grp * raster);
-  *nt = r / rows;
-  *mt = grp * raster + (r - *nt * rows);
-}
+// Tiles are walked in groups of kRaster rows of tiles, row-fastest inside a group, so that the tiles in
+// flight share a few rows of A and a few columns of B in L2.
+constexpr int kRasterLog = 3, kRaster = 1 << kRasterLog;
 
-template <bool kPair>
-__device__ __forceinline__ Item decode_item(const TileParams& p, int m_tiles, int64_t t) {
-  Item it;
-  it.k_row0 = 0;
-  it.k_blocks = p.k_blocks;
-  it.k_steps = kTileK / 16;
-  it.group = 0;
-  it.live_end = (int)p.m;
-  int within = (int)t;
-  if (p.mode == (int)TileMode::kContract) {
-    const int per = m_tiles * p.n_tiles;
-    it.group = (int)(t / per);
-    within = (int)(t - (int64_t)it.group * per);
-    it.k_row0 = p.offsets[it.group];
-    const int count = p.counts[it.group];
-    it.k_blocks = (count + kTileK - 1) / kTileK;
-    // Rows past the next multiple of 16 are never multiplied: they may hold anything.
-    it.k_steps = (count - (it.k_blocks - 1) * kTileK + 15) / 16;
+// What the tile loop walks: whole tiles, then the column halves of the last wave's.
+struct Walk {
+  int m_tiles, n_tiles;
+  int whole, items;
+};
+
+// A role's place in the walk.  It moves by additions: an item is decoded by every role of a block, and with
+// divisions that took 1,000 cycles, as long as two contraction blocks.
+template <bool kPair, int kTileN>
+class Cursor {
+ public:
+  __device__ __forceinline__ Cursor(const TileParams& p, const Walk& w, const int* pairs_before, int unit, int units)
+      : p_(p), w_(w), pairs_before_(pairs_before), units_(units), t_(unit) {
+    at_ = unit;
+    settle();
   }
-  raster_decode(p.raster, m_tiles, p.n_tiles, within, &it.mt, &it.nt);
-  if (p.mode == (int)TileMode::kRows) {
-    it.group = p.block_expert[it.mt];
-    it.live_end = p.offsets[it.group] + p.counts[it.group];
+  __device__ __forceinline__ bool valid() const { return t_ < w_.items; }
+  __device__ __forceinline__ bool is_half() const { return t_ >= w_.whole; }
+  __device__ __forceinline__ void next() {
+    t_ += units_;
+    if (t_ < w_.whole) {
+      at_ += units_;
+      settle();
+    } else if (t_ < w_.items) {      // once or twice a launch
+      at_ = w_.whole + ((t_ - w_.whole) >> 1);
+      expert_ = grp_ = 0;
+      settle();
+    }
   }
-  return it;
-}
+  __device__ __forceinline__ Item item() const {
+    constexpr int kTileM = kPair ? 2 * kRowsPerCta : kRowsPerCta;
+    Item it;
+    it.k_row0 = 0;
+    it.k_blocks = p_.k_blocks;
+    it.k_steps = kTileK / 16;
+    it.group = 0;
+    it.live_end = it.row_end = (int)p_.m;
+    it.n_off = is_half() ? ((t_ - w_.whole) & 1) * (kTileN / 2) : 0;
+    it.cols = is_half() ? kTileN / 2 : kTileN;
+    const int rows = min(kRaster, w_.m_tiles - (grp_ << kRasterLog));
+    it.nt = rows == kRaster ? at_ >> kRasterLog : at_ / rows;
+    const int mt = (grp_ << kRasterLog) + at_ - it.nt * rows;
+    it.row0 = mt * kTileM;
+    if (p_.mode == (int)TileMode::kContract) {
+      it.group = expert_;
+      it.k_row0 = p_.offsets[expert_];
+      const int count = p_.counts[expert_];
+      it.k_blocks = (count + kTileK - 1) / kTileK;
+      // Rows past the next multiple of 16 are never multiplied: they may hold anything.
+      it.k_steps = (count - (it.k_blocks - 1) * kTileK + 15) / 16;
+    } else if (p_.mode == (int)TileMode::kRows) {
+      if constexpr (kPair) {
+        int lo = 0, hi = p_.experts;      // the expert whose pairs hold number mt
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (pairs_before_[mid] <= mt) lo = mid; else hi = mid;
+        }
+        it.group = lo;
+        it.row0 = p_.offsets[lo] + (mt - pairs_before_[lo]) * kTileM;
+      } else {
+        it.group = p_.block_expert[mt];
+      }
+      it.row_end = p_.offsets[it.group + 1];
+      it.live_end = p_.offsets[it.group] + p_.counts[it.group];
+    }
+    return it;
+  }
+
+ private:
+  // Carries at_ into the expert (kContract) and the group of rows of tiles it lies in.
+  __device__ __forceinline__ void settle() {
+    if (p_.mode == (int)TileMode::kContract) {
+      const int per = w_.m_tiles * w_.n_tiles;
+      at_ += grp_ * (kRaster * w_.n_tiles);
+      grp_ = 0;
+      while (at_ >= per) { at_ -= per; ++expert_; }
+    }
+    while (at_ >= kRaster * w_.n_tiles) { at_ -= kRaster * w_.n_tiles; ++grp_; }
+  }
+  const TileParams& p_;
+  const Walk& w_;
+  const int* pairs_before_;
+  const int units_;
+  int t_, at_ = 0, grp_ = 0, expert_ = 0;
+};
 
 // Eight columns of one row, on their way out.
 template <int kAct>
@@ -189,22 +250,12 @@ __device__ __forceinline__ void store8_f32(float* dst, bool vec, int cols, bool 
       if (e < cols) dst[e] = accumulate ? dst[e] + v[e] : v[e];
   }
 }
-// v += the eight staged columns at 16-byte chunks c0, c0 + 1 of the row; lanes of the upper half of a
-// row read the second chunk first, which keeps the eight lanes of an access on different banks.
-__device__ __forceinline__ void staged8(uint32_t row_addr, uint32_t c0, uint32_t sw, bool second_first, float (&v)[8]) {
-  const uint32_t a0 = row_addr + (((c0 + (second_first ? 1u : 0u)) ^ sw) << 4);
-  const uint32_t a1 = row_addr + (((c0 + (second_first ? 0u : 1u)) ^ sw) << 4);
-  float x[8];
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(a0));
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "r"(a1));
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += second_first ? x[(e + 4) & 7] : x[e];
-}
-
 constexpr uint32_t kFullMask = 0xffffffffu;
 
 struct EpilogueItem {
-  int row0, col0;        // first row of the warp's quarter, first output column of the tile
+  int row0, col0;        // first row of the warp's quarter, first output column of the item
+  int row_end;           // rows from here on are not the item's
+  int width;             // output columns of the item
   uint32_t taddr;
   const uint16_t* bias;
   int live_end;
@@ -224,8 +275,8 @@ __device__ __forceinline__ void act32_by(int act, float (&v)[32]) {
   else if (act == kActGeluTanh) act32<kActGeluTanh>(v);
   else act32<kActSilu>(v);
 }
-// A thread's 32 columns to or from its row of a 32 x 32 bf16 block in the 64-byte swizzle: the row's
-// 16-byte chunk j sits at chunk j ^ ((row / 2) % 4).
+// A thread's 32 columns to its row of a 32 x 32 block: bf16 in the 64-byte swizzle (the row's 16-byte chunk
+// j sits at chunk j ^ ((row / 2) % 4)), f32 in the 128-byte one (chunk j at j ^ (row % 8)).
 __device__ __forceinline__ void put_row16(uint32_t block, int lane, const float (&v)[32]) {
   const uint32_t at = block + (uint32_t)lane * 64u, sw = (uint32_t)(lane >> 1) & 3u;
 #pragma unroll
@@ -233,93 +284,84 @@ __device__ __forceinline__ void put_row16(uint32_t block, int lane, const float 
     st_shared_v4(at + (((uint32_t)j ^ sw) << 4), bf16_pack(v[8 * j], v[8 * j + 1]), bf16_pack(v[8 * j + 2], v[8 * j + 3]),
                  bf16_pack(v[8 * j + 4], v[8 * j + 5]), bf16_pack(v[8 * j + 6], v[8 * j + 7]));
 }
-__device__ __forceinline__ void add_row16(uint32_t block, int lane, float (&v)[32]) {
-  const uint32_t at = block + (uint32_t)lane * 64u, sw = (uint32_t)(lane >> 1) & 3u;
+__device__ __forceinline__ void put_row32(uint32_t block, int lane, const float (&v)[32]) {
+  const uint32_t at = block + (uint32_t)lane * 128u, sw = (uint32_t)(lane & 7);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint32_t w[4];
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at + (((uint32_t)j ^ sw) << 4)) : "memory");
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      v[8 * j + 2 * q] += bf16_low(w[q]);
-      v[8 * j + 2 * q + 1] += bf16_high(w[q]);
-    }
-  }
+  for (int j = 0; j < 8; ++j)
+    st_shared_v4(at + (((uint32_t)j ^ sw) << 4), __float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]),
+                 __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
 }
-__device__ __forceinline__ void sums32(uint32_t taddr, bool empty, float (&v)[32]) {
-  uint32_t r[32];
+// Starts the load of 32 columns of sums; tmem_ld_wait() completes it.
+__device__ __forceinline__ void start_sums32(uint32_t taddr, bool empty, uint32_t (&r)[32]) {
   if (!empty) {
     tmem_ld_32x32(taddr, r);
-    tmem_ld_wait();
   } else {
 #pragma unroll
     for (int e = 0; e < 32; ++e) r[e] = 0u;
   }
-#pragma unroll
-  for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[e]);
+}
+__device__ __forceinline__ void add_octet(const uint4& w, float* v) {
+  v[0] += bf16_low(w.x); v[1] += bf16_high(w.x); v[2] += bf16_low(w.y); v[3] += bf16_high(w.y);
+  v[4] += bf16_low(w.z); v[5] += bf16_high(w.z); v[6] += bf16_low(w.w); v[7] += bf16_high(w.w);
 }
 __device__ __forceinline__ void add_bias32(const uint16_t* bias, int cols, float (&v)[32]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (8 * j >= cols) break;          // cols is a multiple of 8 here
-    float b[8];
-    load8(bias + 8 * j, true, 8, b);
-#pragma unroll
-    for (int q = 0; q < 8; ++q) v[8 * j + q] += b[q];
-  }
+  for (int j = 0; j < 4; ++j)
+    if (8 * j < cols) add_octet(reinterpret_cast<const uint4*>(bias)[j], v + 8 * j);   // cols % 8 == 0 here
 }
 
-// Columns [0, kCols) of the tile's output belong to each half's warps, 32 at a time.
-template <int kTileN, bool kGated>
-struct EpilogueShape {
-  static constexpr int kOutCols = kGated ? kTileN / 2 : kTileN;
-  static constexpr int kCols = kOutCols / 2 < 32 ? 32 : kOutCols / 2;
-  static constexpr int kSteps = kCols / 32;
-};
-
-template <int kTileN, bool kGated, typename Wait, typename Release>
+// Y and Z by TMA: steps part, part + kParts, ... of 32 columns.
+template <bool kGated, typename Wait, typename Release>
 __device__ __forceinline__ bool epilogue_tma(const TileParams& p, const EpilogueItem& e, const CUtensorMap& map_y,
-                                             const CUtensorMap& map_z, const CUtensorMap& map_r, uint8_t* mine,
-                                             uint64_t* r_bar, int half, int lane, uint32_t& step_no, uint32_t& r_phase,
-                                             volatile int* abort_flag, Wait&& wait_sums, Release&& release_sums) {
-  using E = EpilogueShape<kTileN, kGated>;
-  const int first = half * E::kCols;                   // of this warp's output columns
-  const bool rows_live = e.row0 < p.m;
-  auto live_at = [&](int s) { return rows_live && s < E::kSteps && e.col0 + first + 32 * s < p.n; };
-  // Y's block of a step (bf16: 2 KiB, alternating; f32: 4 KiB, alternating unless Z or the residual needs the rest).
-  const bool one_y = p.out_f32 && (p.Z || p.residual);
-  auto y_block = [&](uint32_t n) {
-    return mine + (p.out_f32 ? (one_y ? 0u : (n & 1u) * 2u * kBlock16) : (n & 1u) * kBlock16);
-  };
-  auto load_residual = [&](int s, uint32_t n) {        // lane 0
-    const uint32_t b = n & 1u;
-    mbar_arrive_expect_tx(&r_bar[b], kBlock16);
-    tma_load_3d(mine + (p.out_f32 ? 2u * kBlock16 + b * kBlock16 : b * kBlock16), &map_r, &r_bar[b],
-                e.col0 + first + 32 * s, e.row0, 0);
-  };
-  // The residual's blocks are Y's own (bf16), or the two behind Y's single block (f32).
-  if (p.residual && lane == 0 && live_at(0)) {
-    bulk_wait_group_read<0>();
-    load_residual(0, step_no);
-    if (live_at(1)) load_residual(1, step_no + 1);
-  }
-  if (!wait_sums()) return false;
+                                             const CUtensorMap& map_z, uint8_t* mine, int part, int lane,
+                                             Wait&& wait_sums, Release&& release_sums) {
   const int row = e.row0 + lane;
+  const int steps = e.row0 < e.row_end ? min(e.width, (p.n - e.col0 + 31) & ~31) / 32 : 0;
+  uint4 res[4];
+  auto load_residual = [&](int s) {
+    const int col = e.col0 + 32 * s;
+    const uint4* src = reinterpret_cast<const uint4*>(p.residual + (int64_t)row * p.n + col);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      res[j] = row < e.row_end && col + 8 * j < p.n ? src[j] : make_uint4(0u, 0u, 0u, 0u);
+  };
+  if (p.residual && part < steps) load_residual(part);
+  if (!wait_sums()) return false;
   const bool padding = p.zero_padding && row >= e.live_end;
+  // The two blocks take turns; a block may be rewritten once the store from it has been read.
+  uint32_t slot = 0;
+  auto next_block = [&](bool known_free) {
+    if (!known_free && lane == 0) bulk_wait_group_read<1>();
+    __syncwarp();
+    uint8_t* b = mine + slot * kBlock16;
+    slot ^= 1u;
+    return b;
+  };
+  if (part >= steps) release_sums();
 #pragma unroll 1
-  for (int s = 0; s < E::kSteps; ++s) {
-    const int c = first + 32 * s;
-    const bool live = live_at(s);
+  for (int s = part; s < steps; s += kParts) {
+    const int c = 32 * s, col = e.col0 + c;
     float v[32];
     [[maybe_unused]] float u[kGated ? 32 : 1];
-    if (live) {
-      sums32(e.taddr + (uint32_t)c, e.empty_sum, v);
-      if constexpr (kGated) sums32(e.taddr + (uint32_t)(kTileN / 2 + c), e.empty_sum, u);
+    {
+      uint32_t r[32];
+      [[maybe_unused]] uint32_t q[32];
+      start_sums32(e.taddr + (uint32_t)c, e.empty_sum, r);
+      if constexpr (kGated) start_sums32(e.taddr + (uint32_t)(e.width + c), e.empty_sum, q);
+      // Meanwhile: the block this step writes first must have been read.
+      if (lane == 0) {
+        if (p.out_f32) bulk_wait_group_read<0>(); else bulk_wait_group_read<1>();
+      }
+      tmem_ld_wait();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+      if constexpr (kGated) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) u[i] = __uint_as_float(q[i]);
+      }
     }
-    if (s + 1 == E::kSteps) release_sums();
-    if (!live) continue;
-    const int col = e.col0 + c;
+    bool free_block = true;      // the wait above covers the first block of the step
+    if (s + kParts >= steps) release_sums();
     if (e.bias) {
       add_bias32(e.bias + col, p.n - col, v);
       if constexpr (kGated) add_bias32(e.bias + p.n + col, p.n - col, u);
@@ -332,130 +374,129 @@ __device__ __forceinline__ bool epilogue_tma(const TileParams& p, const Epilogue
         for (int i = 0; i < 32; ++i) u[i] = 0.f;
       }
     }
-    const uint32_t n = step_no;
-    // The blocks written below must have left: those of the step before last, or of the last step where
-    // every step uses the same.
-    if (lane == 0) {
-      if (one_y || (kGated && p.Z)) bulk_wait_group_read<0>();
-      else bulk_wait_group_read<1>();
-    }
-    __syncwarp();
-    uint8_t* z0 = mine + 2 * kBlock16 + (kGated ? 0u : (n & 1u) * kBlock16);
-    uint8_t* z1 = mine + 3 * kBlock16;
     if (p.Z) {
-      put_row16(smem_u32(z0), lane, v);
-      if constexpr (kGated) put_row16(smem_u32(z1), lane, u);
+      auto send = [&](const float (&x)[32], int half) {
+        uint8_t* b = next_block(free_block);
+        free_block = false;
+        put_row16(smem_u32(b), lane, x);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_3d(&map_z, b, col, half, e.row0);
+          bulk_commit_group();
+        }
+      };
+      send(v, 0);
+      if constexpr (kGated) send(u, 1);
     }
     act32_by(p.act, v);
     if constexpr (kGated) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] *= u[i];
     }
-    uint8_t* yb = y_block(n);
     if (p.residual) {
-      const uint32_t b = n & 1u;
-      bool there = mbar_wait(&r_bar[b], (r_phase >> b) & 1u, abort_flag, p.status, 37);
-      there = __all_sync(kFullMask, there);
-      r_phase ^= 1u << b;
-      if (!there) return false;
-      add_row16(smem_u32(p.out_f32 ? mine + 2 * kBlock16 + b * kBlock16 : yb), lane, v);
-    }
-    if (p.out_f32) {
-      // 128-byte rows: chunk j at j ^ (row % 8).
-      const uint32_t at = smem_u32(yb) + (uint32_t)lane * 128u, sw = (uint32_t)(lane & 7);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        st_shared_v4(at + (((uint32_t)j ^ sw) << 4), __float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]),
-                     __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
+      for (int j = 0; j < 4; ++j) add_octet(res[j], v + 8 * j);
+      if (s + kParts < steps) load_residual(s + kParts);
+    }
+    uint8_t* b = mine;
+    if (p.out_f32) {
+      if (!free_block && lane == 0) bulk_wait_group_read<0>();      // both blocks are one
+      __syncwarp();
+      put_row32(smem_u32(b), lane, v);
+      slot = 0;
     } else {
-      put_row16(smem_u32(yb), lane, v);
+      b = next_block(free_block);
+      put_row16(smem_u32(b), lane, v);
     }
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) {
-      if (p.accumulate) tma_reduce_add_3d(&map_y, yb, col, e.row0, e.group);
-      else tma_store_3d(&map_y, yb, col, e.row0, e.group);
-      if (p.Z) {
-        tma_store_3d(&map_z, z0, col, 0, e.row0);
-        if constexpr (kGated) tma_store_3d(&map_z, z1, col, 1, e.row0);
-      }
+      if (p.accumulate) tma_reduce_add_3d(&map_y, b, col, e.row0, e.group);
+      else tma_store_3d(&map_y, b, col, e.row0, e.group);
       bulk_commit_group();
-      // The residual two steps ahead goes where this step's was read (f32) or where the step before
-      // left its y (bf16): that store has been read once this step's alone is pending.
-      if (p.residual) {
-        if (p.out_f32) {
-          if (live_at(s + 2)) load_residual(s + 2, n + 2);
-        } else if (s >= 1 && live_at(s + 1)) {
-          bulk_wait_group_read<1>();
-          load_residual(s + 1, n + 1);
-        }
-      }
+      // With f32 the next block written may be the upper half of this one.
+      if (p.out_f32 && p.Z) bulk_wait_group_read<0>();
     }
-    ++step_no;
   }
+  // The next item begins with the first block again: nothing but the last store may be pending from the second.
+  if (slot == 1u && lane == 0) bulk_wait_group_read<0>();
   return true;
 }
 
-template <int kTileN, bool kGated, typename Wait, typename Release>
-__device__ __forceinline__ bool epilogue_plain(const TileParams& p, const EpilogueItem& e, uint32_t block, int half, int lane,
+// v += the eight staged columns at 16-byte chunks c0, c0 + 1 of the row.
+__device__ __forceinline__ void staged8(uint32_t row_addr, uint32_t c0, uint32_t sw, float (&v)[8]) {
+  float x[8];
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
+               : "r"(row_addr + ((c0 ^ sw) << 4)));
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+               : "r"(row_addr + (((c0 + 1u) ^ sw) << 4)));
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] += x[e];
+}
+
+// Plain loads and stores, any n and alignment.
+template <bool kGated, typename Wait, typename Release>
+__device__ __forceinline__ bool epilogue_plain(const TileParams& p, const EpilogueItem& e, uint32_t block, int part, int lane,
                                                Wait&& wait_sums, Release&& release_sums) {
-  constexpr int kOutCols = kGated ? kTileN / 2 : kTileN;
-  // Reading back: kLanes lanes to a row, kRowsAt rows at a time.
-  constexpr int kLanes = kGated ? 4 : 8, kRowsAt = 32 / kLanes;
-  constexpr int kStep = kGated ? 32 : 64;          // output columns per block
-  constexpr int kCols = kOutCols / 2 < kStep ? kStep : kOutCols / 2;
+  constexpr int kStep = kGated ? 16 : 32;            // output columns per block (gated: of either half)
+  constexpr int kLanes = kStep / 8, kRowsAt = 32 / kLanes;
+  const int steps = e.row0 < e.row_end ? (min(e.width, p.n - e.col0) + kStep - 1) / kStep : 0;
   const int sub = lane % kLanes, row_in = lane / kLanes;
-  const bool swap = !kGated && sub >= 4;
   if (!wait_sums()) return false;
   const int64_t out_row0 = (int64_t)e.group * p.m;
-  const int row_end = (int)min(p.m, (int64_t)e.row0 + 32);
+  if (part >= steps) release_sums();
 #pragma unroll 1
-  for (int c = half * kCols; c < half * kCols + kCols; c += kStep) {
-    const bool live = c < kOutCols && e.row0 < p.m && e.col0 + c < p.n;
-    if (live) {
-      // 64 accumulator columns: the step's own, or its gate's and its partner's 32 each.
+  for (int s = part; s < steps; s += kParts) {
+    const int c = s * kStep;
+    {
+      // 32 accumulator columns: the step's own, or its gate's and its partner's 16 each.
+      uint32_t r[2][16];
+      if (!e.empty_sum) {
+        tmem_ld_32x16(e.taddr + (uint32_t)c, r[0]);
+        tmem_ld_32x16(e.taddr + (kGated ? (uint32_t)(e.width + c) : (uint32_t)(c + 16)), r[1]);
+        tmem_ld_wait();
+      } else {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float v[32];
-        sums32(e.taddr + (kGated ? (uint32_t)(c + h * (kTileN / 2)) : (uint32_t)(c + 32 * h)), e.empty_sum, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          st_shared_v4(block + (uint32_t)lane * 256u + ((((uint32_t)(h * 8 + j)) ^ (uint32_t)(lane & 7)) << 4),
-                       __float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]),
-                       __float_as_uint(v[4 * j + 3]));
+        for (int i = 0; i < 16; ++i) r[0][i] = r[1][i] = 0u;
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        st_shared_v4(block + (uint32_t)lane * 128u + (((uint32_t)j ^ (uint32_t)(lane & 7)) << 4), r[j >> 2][4 * (j & 3)],
+                     r[j >> 2][4 * (j & 3) + 1], r[j >> 2][4 * (j & 3) + 2], r[j >> 2][4 * (j & 3) + 3]);
     }
-    if (c + kStep >= half * kCols + kCols) release_sums();
-    if (!live) continue;
+    if (s + kParts >= steps) release_sums();
     __syncwarp();
     const int col = e.col0 + c + sub * 8;
     const int cols = p.n - col;                  // columns left from here (may be <= 0 or >= 8)
     const bool vec = p.vec && cols >= 8;
-    float b0[8], b1[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) b0[i] = b1[i] = 0.f;
-    if (e.bias && cols > 0) {
-      load8(e.bias + col, vec, cols, b0);
-      if constexpr (kGated) load8(e.bias + p.n + col, vec, cols, b1);
-    }
     if (cols > 0) {
-#pragma unroll 4
+      float b0[8], b1[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b0[i] = b1[i] = 0.f;
+      if (e.bias) {
+        load8(e.bias + col, vec, cols, b0);
+        if constexpr (kGated) load8(e.bias + p.n + col, vec, cols, b1);
+      }
+#pragma unroll 2
       for (int i = 0; i < 32 / kRowsAt; ++i) {
         const int r_in = i * kRowsAt + row_in;
         const int row = e.row0 + r_in;
-        if (row >= row_end) continue;
-        const uint32_t row_addr = block + (uint32_t)r_in * 256u, sw = (uint32_t)(r_in & 7);
+        if (row >= e.row_end) continue;
+        const uint32_t row_addr = block + (uint32_t)r_in * 128u, sw = (uint32_t)(r_in & 7);
+        const int64_t out_row = out_row0 + row;
+        float x[8];
+        if (p.residual) load8(p.residual + out_row * p.n + col, vec, cols, x);
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] = b0[q];
-        staged8(row_addr, 2u * sub, sw, swap, v);
-        const int64_t out_row = out_row0 + row;
+        staged8(row_addr, 2u * sub, sw, v);
         const bool padding = p.zero_padding && row >= e.live_end;
         if constexpr (kGated) {
           float u[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) u[q] = b1[q];
-          staged8(row_addr, 8u + 2u * sub, sw, false, u);
+          staged8(row_addr, 4u + 2u * sub, sw, u);
           if (padding) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] = u[q] = 0.f;
@@ -476,8 +517,6 @@ __device__ __forceinline__ bool epilogue_plain(const TileParams& p, const Epilog
           act8_by(p.act, v);
         }
         if (p.residual) {
-          float x[8];
-          load8(p.residual + out_row * p.n + col, vec, cols, x);
 #pragma unroll
           for (int q = 0; q < 8; ++q) v[q] += x[q];
         }
@@ -494,9 +533,8 @@ template <bool kPair, int kTileN, bool kGated>
 __global__ void __launch_bounds__(kThreads, 1)
 linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z,
-                   const __grid_constant__ CUtensorMap map_r, const TileParams p) {
+                   const TileParams p) {
   using S = Shape<kPair, kTileN>;
-  constexpr int kOutCols = kGated ? kTileN / 2 : kTileN;   // output columns of a tile
   extern __shared__ uint8_t smem_raw[];
   uint8_t* stages = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -507,8 +545,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
   const uint32_t rank = kPair ? cluster_ctarank() : 0u;
-  const int64_t unit = kPair ? (blockIdx.x >> 1) : blockIdx.x;
-  const int64_t units = kPair ? (gridDim.x >> 1) : gridDim.x;
+  const int unit = (int)(kPair ? (blockIdx.x >> 1) : blockIdx.x);
+  const int units = (int)(kPair ? (gridDim.x >> 1) : gridDim.x);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) {
@@ -519,11 +557,11 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       mbar_init(&bars->acc_full[i], 1);
       mbar_init(&bars->acc_empty[i], kEpiWarps * S::kCtas);
     }
-    for (int i = 0; i < 2 * kEpiWarps; ++i) mbar_init(&bars->resid[i >> 1][i & 1], 1);
     bars->abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_descriptor(&map_a);
     tma_prefetch_descriptor(&map_b);
+    if (p.tma) tma_prefetch_descriptor(&map_y);
   }
   if (warp == 1) {
     if constexpr (kPair) {
@@ -534,21 +572,45 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       tmem_relinquish();
     }
   }
+
+  pdl_wait();
+  pdl_release();
+
+  // The experts' rows that are live are known on the device only.
+  if (kPair && p.mode == (int)TileMode::kRows && warp == 2) {
+    int before = 0;
+    for (int e0 = 0; e0 < p.experts; e0 += 32) {
+      const int e = e0 + lane;
+      const int blocks = e < p.experts ? (p.offsets[e + 1] - p.offsets[e]) / kExpertBlock : 0;
+      const int mine = (blocks + 1) / 2;
+      int sum = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int o = __shfl_up_sync(kFullMask, sum, d);
+        if (lane >= d) sum += o;
+      }
+      if (e < p.experts) bars->pairs_before[e] = before + sum - mine;
+      before += __shfl_sync(kFullMask, sum, 31);
+    }
+    if (lane == 0) bars->pairs_before[p.experts] = before;
+  }
   tc_fence_before_sync();
   if constexpr (kPair) cluster_sync(); else __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = bars->tmem_base;
 
-  pdl_wait();
-  pdl_release();
-
-  // The experts' rows that are live: known on the device only.
-  int m_tiles = p.m_tiles;
-  int64_t tiles = p.tiles;
+  Walk w;
+  w.m_tiles = p.m_tiles;
+  w.n_tiles = p.n_tiles;
+  int tiles = (int)p.tiles;
   if (p.mode == (int)TileMode::kRows) {
-    m_tiles = p.offsets[p.experts] / kExpertBlock;
-    tiles = (int64_t)m_tiles * p.n_tiles;
+    w.m_tiles = kPair ? bars->pairs_before[p.experts] : p.offsets[p.experts] / kExpertBlock;
+    tiles = w.m_tiles * p.n_tiles;
   }
+  // The tiles of a last wave that would occupy at most half the units are cut into column halves.
+  const int tail = tiles % units;
+  w.whole = p.halves && tiles > units && tail > 0 && 2 * tail <= units ? tiles - tail : tiles;
+  w.items = w.whole + 2 * (tiles - w.whole);
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
@@ -558,46 +620,47 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       bool ok = true;
       const uint32_t leader_full = kPair ? map_to_cta(smem_u32(&bars->full[0]), 0) : 0u;
       (void)leader_full;
-      for (int64_t t = unit; t < tiles && ok; t += units) {
-        const Item it = decode_item<kPair>(p, m_tiles, t);
-        const int row0 = it.mt * S::kTileM + (int)rank * kRowsPerCta;
+      // The k loop is kept short: one thread issues it, and everything in it delays the next load.
+      const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
+      for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units); at.valid() && ok; at.next()) {
+        const Item it = at.item();
+        const int row0 = it.row0 + (int)rank * kRowsPerCta;
         const int z_b = p.mode == (int)TileMode::kRows ? it.group : 0;
+        const int cols_b = it.cols / S::kCtas, boxes_b = cols_b / 64;
+        const uint32_t tx = (uint32_t)(kBytesA + boxes_b * kBoxBytes);
+        const int col0 = kGated ? (it.nt * kTileN + it.n_off) / 2 : it.nt * kTileN + it.n_off;
         int cols[S::kBoxesB];      // stored column of every 64-column box of B
 #pragma unroll
         for (int j = 0; j < S::kBoxesB; ++j) {
-          const int at = (int)rank * S::kColsB + j * 64;      // accumulator column
-          if constexpr (kGated)
-            cols[j] = at < kTileN / 2 ? it.nt * kOutCols + at : p.b_up + it.nt * kOutCols + at - kTileN / 2;
-          else
-            cols[j] = it.nt * kOutCols + at;
+          const int at = (int)rank * cols_b + j * 64;      // accumulator column
+          if constexpr (kGated) cols[j] = at < it.cols / 2 ? col0 + at : p.b_up + col0 + at - it.cols / 2;
+          else cols[j] = col0 + at;
         }
-        for (int kb = 0; kb < it.k_blocks; ++kb) {
+        int kc = it.k_row0;
+        for (int kb = 0; kb < it.k_blocks; ++kb, kc += kTileK) {
           if (!(ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 33))) break;
           uint8_t* sa = stages + (size_t)stage * S::kStageBytes;
           uint8_t* sb = sa + kBytesA;
-          const int kc = it.k_row0 + kb * kTileK;
           const uint32_t full = leader_full + (uint32_t)stage * 8u;
           (void)full;
           if constexpr (kPair) {
-            if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * S::kStageBytes);
+            if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * tx);
           } else {
-            mbar_arrive_expect_tx(&bars->full[stage], S::kStageBytes);
+            mbar_arrive_expect_tx(&bars->full[stage], tx);
           }
           auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1, int c2) {
             if constexpr (kPair) tma_load_3d_pair(dst, map, full, c0, c1, c2);
             else tma_load_3d(dst, map, &bars->full[stage], c0, c1, c2);
           };
-          if (p.a_mn) {
+          if (a_mn) {
             load(sa, &map_a, row0, kc, 0);
             load(sa + kBoxBytes, &map_a, row0 + 64, kc, 0);
           } else {
             load(sa, &map_a, kc, row0, 0);
           }
 #pragma unroll
-          for (int j = 0; j < S::kBoxesB; ++j) {
-            if (p.b_mn) load(sb + j * kBoxBytes, &map_b, cols[j], kc, z_b);
-            else load(sb + j * kBoxBytes, &map_b, kc, cols[j], z_b);
-          }
+          for (int j = 0; j < S::kBoxesB; ++j)
+            if (j < boxes_b) load(sb + j * kBoxBytes, &map_b, b_mn ? cols[j] : kc, b_mn ? kc : cols[j], z_b);
           if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         }
       }
@@ -605,7 +668,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (rank == 0 && elect_one()) {
-      const uint32_t idesc = instr_desc_bf16(S::kTileM, kTileN, p.a_mn != 0, p.b_mn != 0);
+      const uint32_t idesc_tile = instr_desc_bf16(S::kTileM, kTileN, p.a_mn != 0, p.b_mn != 0);
+      const uint32_t idesc_half = instr_desc_bf16(S::kTileM, kTileN / 2, p.a_mn != 0, p.b_mn != 0);
       // Across the contraction: 64-column groups one box apart, 16 contraction rows = 2048 bytes.
       // Along it: 8-row groups 1024 bytes apart, 16 elements = 32 bytes along the row.
       const uint32_t step_a = p.a_mn ? 2048u : 32u, step_b = p.b_mn ? 2048u : 32u;
@@ -615,17 +679,24 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       int buf = 0;
       uint32_t acc_phase = 0;
       bool ok = true;
-      for (int64_t t = unit; t < tiles && ok; t += units) {
-        const Item it = decode_item<kPair>(p, m_tiles, t);
+      for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units); at.valid() && ok; at.next()) {
+        // The place of the tile does not matter here; its width and, by expert, its depth do.
+        int k_blocks = p.k_blocks, k_steps = kTileK / 16;
+        if (p.mode == (int)TileMode::kContract) {
+          const Item it = at.item();
+          k_blocks = it.k_blocks;
+          k_steps = it.k_steps;
+        }
+        const uint32_t idesc = at.is_half() ? idesc_half : idesc_tile;
         if (!(ok = mbar_wait(&bars->acc_empty[buf], acc_phase ^ 1, abort_flag, p.status, 34))) break;
         tc_fence_after_sync();
         const uint32_t d_tmem = tmem_base + (uint32_t)buf * kAccStride;
-        for (int kb = 0; kb < it.k_blocks; ++kb) {
+        for (int kb = 0; kb < k_blocks; ++kb) {
           if (!(ok = mbar_wait(&bars->full[stage], phase, abort_flag, p.status, 35))) break;
           tc_fence_after_sync();
           const uint32_t sa = smem_u32(stages + (size_t)stage * S::kStageBytes);
           const uint32_t sb = sa + kBytesA;
-          const int steps = kb + 1 == it.k_blocks ? it.k_steps : kTileK / 16;
+          const int steps = kb + 1 == k_blocks ? k_steps : kTileK / 16;
 #pragma unroll
           for (int j = 0; j < kTileK / 16; ++j) {
             if (j >= steps) break;
@@ -647,18 +718,18 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   } else {
     // ------------------------------------------------------------------ epilogue
     const int ew = warp - 2;
-    const int quarter = warp & 3, half = ew >> 2;      // TMEM lanes 32 quarter ..; half of the columns
+    const int quarter = warp & 3, part = ew >> 2;      // TMEM lanes 32 quarter ..; share of the columns
     uint8_t* mine = epi + (size_t)ew * kEpiBlockBytes;
     int buf = 0;
     uint32_t acc_phase = 0;
-    uint32_t step_no = 0;                              // steps taken: the block of a step is step_no % 2
-    uint32_t r_phase = 0;                              // bit b: phase of the residual barrier of block b
     bool ok = true;
-    for (int64_t t = unit; t < tiles && ok; t += units) {
-      const Item it = decode_item<kPair>(p, m_tiles, t);
+    for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units); at.valid() && ok; at.next()) {
+      const Item it = at.item();
       EpilogueItem e;
-      e.row0 = it.mt * S::kTileM + (int)rank * kRowsPerCta + quarter * 32;
-      e.col0 = it.nt * kOutCols;
+      e.row0 = it.row0 + (int)rank * kRowsPerCta + quarter * 32;
+      e.row_end = it.row_end;
+      e.col0 = kGated ? (it.nt * kTileN + it.n_off) / 2 : it.nt * kTileN + it.n_off;
+      e.width = kGated ? it.cols / 2 : it.cols;
       e.taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)buf * kAccStride;
       e.bias = p.bias ? p.bias + (int64_t)it.group * p.z_pitch : nullptr;
       e.live_end = it.live_end;
@@ -674,15 +745,12 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) {
-          if constexpr (kPair) mbar_arrive_cluster(map_to_cta(smem_u32(&bars->acc_empty[buf]), 0));
+          if constexpr (kPair) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&bars->acc_empty[buf]), 0));
           else mbar_arrive(&bars->acc_empty[buf]);
         }
       };
-      if (p.tma)
-        ok = epilogue_tma<kTileN, kGated>(p, e, map_y, map_z, map_r, mine, bars->resid[ew], half, lane, step_no,
-                                          r_phase, abort_flag, wait_sums, release_sums);
-      else
-        ok = epilogue_plain<kTileN, kGated>(p, e, smem_u32(mine), half, lane, wait_sums, release_sums);
+      if (p.tma) ok = epilogue_tma<kGated>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums);
+      else ok = epilogue_plain<kGated>(p, e, smem_u32(mine), part, lane, wait_sums, release_sums);
       if (++buf == 2) { buf = 0; acc_phase ^= 1; }
     }
     // Shared memory must outlive the engine's reads, and the stores must have been performed before the
@@ -702,7 +770,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 }
 
 struct Maps {
-  CUtensorMap a{}, b{}, y{}, z{}, r{};
+  CUtensorMap a{}, b{}, y{}, z{};
 };
 
 template <bool kPair, int kTileN, bool kGated>
@@ -717,8 +785,11 @@ cudaError_t launch_tile(const DeviceInfo& dev, const Maps& maps, const TileParam
   if (e != cudaSuccess) return e;
   const int64_t units = std::min<int64_t>(max_items, kPair ? gemm_pair_units(dev.sms) : dev.sms);
   return launch_pdl(linear_tile_kernel<kPair, kTileN, kGated>, dim3((unsigned)(units * S::kCtas)), dim3(kThreads),
-                    S::kSmemBytes, stream, S::kCtas, maps.a, maps.b, maps.y, maps.z, maps.r, p);
+                    S::kSmemBytes, stream, S::kCtas, maps.a, maps.b, maps.y, maps.z, p);
 }
+
+// A tile's column halves are whole 64-column boxes in every CTA (gated: of both halves of W).
+bool can_halve(int pair, int tile_n, bool gated) { return tile_n / (pair || gated ? 2 : 1) / 2 >= 64; }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -745,7 +816,7 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   p.out_f32 = ep.out_f32;
   p.accumulate = ep.accumulate;
   p.vec = c.n % 8 == 0 && aligned16(ep.Y) && aligned16(ep.Z) && aligned16(ep.bias) && aligned16(ep.residual);
-  p.tma = p.vec && !(ep.out_f32 && ep.residual && ep.Z);    // that one has no room for its blocks
+  p.tma = p.vec;
   p.z_pitch = (int)(c.n * width);
   p.bias = ep.bias;
   p.residual = ep.residual;
@@ -754,32 +825,37 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   p.status = dev.status;
 
   // The tile: the least waves x columns, weighted by what the narrower and the one-CTA tiles cost per
-  // column.  Experts: a 128-row block belongs to one expert, a pair of them may not.
+  // column.  A last wave that is cut into column halves costs about 0.6 of a whole one.
   const int64_t groups = c.mode == TileMode::kContract ? c.experts.experts : 1;
+  const int64_t pairs = c.experts.tokens * c.experts.topk;
   double best = 0;
   int best_pair = -1, best_n = 0;
   for (int pair = 0; pair < 2; ++pair) {
-    if (pair && (c.mode == TileMode::kRows || c.m <= kRowsPerCta)) continue;
+    if (pair && c.m <= kRowsPerCta) continue;
+    if (pair && c.mode == TileMode::kRows && c.experts.experts >= kPairTable) continue;
     const int64_t units = std::max(1, pair ? gemm_pair_units(dev.sms) : dev.sms);
     for (int tn = 256; tn >= 64; tn >>= 1) {
       if (tn == 64 && (pair || ep.gated)) continue;
       const int64_t out_cols = ep.gated ? tn / 2 : tn;
       const int64_t tile_m = kRowsPerCta << pair;
-      // Experts' blocks: the count is the device's; half of the padding's bound is the guess.
+      // Experts' rows: their number per expert is the device's; half a tile of padding each is the guess.
       const int64_t m_tiles = c.mode == TileMode::kRows
-                                  ? std::max<int64_t>(1, (c.experts.tokens * c.experts.topk / kExpertBlock + c.m / kExpertBlock) / 2)
+                                  ? std::max<int64_t>(1, (pairs + std::min(pairs, c.experts.experts) * tile_m / 2) / tile_m)
                                   : (c.m + tile_m - 1) / tile_m;
       const int64_t items = groups * m_tiles * ((c.n + out_cols - 1) / out_cols);
-      const double waves = (double)((items + units - 1) / units);
+      const int64_t tail = items % units;
+      const bool cut = can_halve(pair, tn, ep.gated) && items > units && tail > 0 && 2 * tail <= units;
+      const double waves = (double)(items / units) + (tail == 0 ? 0.0 : cut ? 0.625 : 1.0);
       const double cost = waves * tn * (pair ? 1.0 : 1.15) * (tn == 256 ? 1.0 : tn == 128 ? 1.25 : 1.6);
       if (best_n == 0 || cost < best) { best = cost; best_pair = pair; best_n = tn; }
     }
   }
+  p.halves = can_halve(best_pair, best_n, ep.gated);
   const int64_t tile_m = kRowsPerCta << best_pair, out_cols = ep.gated ? best_n / 2 : best_n;
   p.m_tiles = (int)((c.m + tile_m - 1) / tile_m);
   p.n_tiles = (int)((c.n + out_cols - 1) / out_cols);
-  p.raster = 8;
   p.tiles = groups * p.m_tiles * (int64_t)p.n_tiles;
+  if (p.tiles >= (1ll << 30) || p.n_tiles >= (1 << 27)) return cudaErrorInvalidValue;   // items are ints
 
   Maps maps;
   cudaError_t e = cudaSuccess;
@@ -800,9 +876,6 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
     if (e == cudaSuccess && ep.Z)
       e = make_tensor_map_3d_box(&maps.z, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ep.Z, (uint64_t)c.n, (uint64_t)width,
                                  (uint64_t)c.m, 32, 1, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-    if (e == cudaSuccess && ep.residual)
-      e = make_tensor_map_3d(&maps.r, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ep.residual, (uint64_t)c.n, (uint64_t)c.m, 1, 32,
-                             32, CU_TENSOR_MAP_SWIZZLE_64B);
     if (e != cudaSuccess) return e;
   }
   const int code = best_pair * 10000 + best_n * 10 + (ep.gated ? 1 : 0);

@@ -23,4 +23,8 @@ cudaError_t make_tensor_map_3d_box(CUtensorMap* out, CUtensorMapDataType dtype, 
                                    uint32_t box0, uint32_t box1, uint32_t box2, CUtensorMapSwizzle swizzle,
                                    CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 
+// A rank-2 map over a dense bf16 matrix [rows][cols] for loads that gather four rows at a time (tile::gather4):
+// a box of 64 columns and one row, 128-byte swizzle.
+cudaError_t make_gather_map(CUtensorMap* out, const void* base, uint64_t cols, uint64_t rows);
+
 }  // namespace morello
