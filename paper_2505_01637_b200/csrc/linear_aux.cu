@@ -111,12 +111,14 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeParams p) {
     uint4 wd[kSlopeUnroll], w0[kSlopeUnroll], w1[kGated ? kSlopeUnroll : 1];
     const int64_t width = kGated ? 2 * p.n : p.n;
     const bool wants_z = kAct != kActNone || kGated;
+    bool holds[kSlopeUnroll];     // looked at after the loads: rows without a token may hold anything
 #pragma unroll
     for (int i = 0; i < kSlopeUnroll; ++i) {
       const int64_t row = row_begin + lane + i * kSlopeLanes;
+      holds[i] = row < row_end && (!p.row_src || p.row_src[row] >= 0);
       wd[i] = w0[i] = make_uint4(0u, 0u, 0u, 0u);
       if constexpr (kGated) w1[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (row >= row_end || (p.row_src && p.row_src[row] < 0)) continue;      // zeros give zeros
+      if (row >= row_end) continue;
       wd[i] = load8_raw(p.dY + row * p.n + col, vec, left);
       if (wants_z) w0[i] = load8_raw(p.Z + row * width + col, vec, left);
       if constexpr (kGated) w1[i] = load8_raw(p.Z + row * width + p.n + col, vec, left);
@@ -140,6 +142,7 @@ __global__ void __launch_bounds__(kThreads) slope_kernel(const SlopeParams p) {
           d0[e] = dy[e] * slope;
           d1[e] = 0.f;
         }
+        if (!holds[i]) d0[e] = d1[e] = 0.f;
       }
       if (p.dZ) {
         uint16_t* dst = p.dZ + row * p.pitch + col;

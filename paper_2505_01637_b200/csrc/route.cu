@@ -2,8 +2,11 @@
 // the plan that sorts the routed rows by expert.
 //
 // One warp per token.  Lane l holds experts l, l + 32, ...; a key is mapped to an unsigned integer of
-// the same order, so that the warp's maximum and the lowest index that has it are two integer
-// reductions (redux) per chosen expert.  All sums are in f32 in a fixed order.
+// the same order.  With many experts per lane the choice is made among few: the topk-th largest of the lanes'
+// maxima is a lower bound of the topk-th largest key, so only keys from there on, a dozen or so, are candidates;
+// one to a lane, each counts the candidates before it, which is its place.  Few experts per lane, or more than 32
+// candidates (rows of equal logits): the warp's maximum and the lowest index that has it, two integer reductions
+// (redux) and a pass over the lane's keys per chosen expert.  All sums are in f32 in a fixed order.
 #include <algorithm>
 
 #include "activation.cuh"
@@ -59,6 +62,8 @@ struct RouteParams {
 template <int kPer, bool kF32>
 __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
   extern __shared__ uint32_t group_keys[];       // [kWarps][experts] when experts are grouped
+  __shared__ uint2 candidates[kWarps][32];       // key and expert
+  __shared__ float candidate_x[kWarps][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t t = (int64_t)blockIdx.x * kWarps + warp;
   pdl_wait();
@@ -118,7 +123,56 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
   // Lane j ends up with the j-th choice.
   int my_idx = -1;
   float my_x = 0.f;
-  for (int j = 0; j < p.topk; ++j) {
+  bool chosen = false;
+  if constexpr (kPer >= 4) {
+    uint32_t most = 0u;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) most = max(most, key[i]);
+    uint32_t bound = 0u, left = most;
+    for (int j = 0; j < p.topk; ++j) {
+      bound = __reduce_max_sync(kFull, left);
+      const uint32_t who = __ballot_sync(kFull, left == bound);
+      if (lane == __ffs(who) - 1) left = 0u;
+    }
+    // At least topk keys are >= bound (0 when lanes ran out: everything still in the choice is a candidate).
+    bound = max(bound, 1u);
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const uint32_t who = __ballot_sync(kFull, key[i] >= bound);
+      if (key[i] >= bound) {
+        const int at = count + __popc(who & ((1u << lane) - 1u));
+        if (at < 32) {
+          candidates[warp][at] = make_uint2(key[i], (uint32_t)(i * 32 + lane));
+          candidate_x[warp][at] = x[i];
+        }
+      }
+      count += __popc(who);
+    }
+    __syncwarp();
+    if (count <= 32) {
+      // In order of expert by construction, so among equal keys the earlier candidate comes first.
+      const uint2 mine = lane < count ? candidates[warp][lane] : make_uint2(0u, kNone);
+      int place = 0;
+      for (int j = 0; j < count; ++j) {
+        const uint32_t other = __shfl_sync(kFull, mine.x, j);
+        place += (other > mine.x || (other == mine.x && j < lane)) ? 1 : 0;
+      }
+      const float x_mine = lane < count ? candidate_x[warp][lane] : 0.f;
+      __syncwarp();
+      if (lane < count && place < p.topk) {
+        candidates[warp][place] = mine;
+        candidate_x[warp][place] = x_mine;
+      }
+      __syncwarp();
+      if (lane < p.topk) {
+        my_idx = (int)candidates[warp][lane].y;
+        my_x = candidate_x[warp][lane];
+      }
+      chosen = true;
+    }
+  }
+  for (int j = 0; j < p.topk && !chosen; ++j) {
     uint32_t best = 0u;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) best = max(best, key[i]);
@@ -181,6 +235,7 @@ struct RouteBackParams {
   int experts, topk;
   bool sigmoid, renorm;
   float scale;
+  bool vec;          // rows of dlogits in four-element accesses
 };
 
 // With g = scale * dweights and w the weights before scaling:
@@ -254,8 +309,28 @@ __global__ void __launch_bounds__(kThreads) route_backward_kernel(const RouteBac
     for (int i = 0; i < kPer; ++i) x[i] *= -dot * inv;
   }
   if (!softmax_all) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) x[i] = 0.f;
+    // Everything but the chosen is zero: the row is cleared, then the chosen are set.
+    const int64_t row = t * p.experts;
+    if constexpr (kF32) {
+      float* dst = static_cast<float*>(p.dlogits) + row;
+      if (p.vec) {
+        for (int e = lane * 4; e < p.experts; e += 128) *reinterpret_cast<float4*>(dst + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+      } else {
+        for (int e = lane; e < p.experts; e += 32) dst[e] = 0.f;
+      }
+      __syncwarp();
+      if (e_j >= 0) dst[e_j] = d;
+    } else {
+      uint16_t* dst = static_cast<uint16_t*>(p.dlogits) + row;
+      if (p.vec) {
+        for (int e = lane * 4; e < p.experts; e += 128) *reinterpret_cast<uint2*>(dst + e) = make_uint2(0u, 0u);
+      } else {
+        for (int e = lane; e < p.experts; e += 32) dst[e] = 0;
+      }
+      __syncwarp();
+      if (e_j >= 0) dst[e_j] = bf16_round(d);
+    }
+    return;
   }
   for (int j = 0; j < p.topk; ++j) {
     const int e = __shfl_sync(kFull, e_j, j);
@@ -296,11 +371,11 @@ cudaError_t launch_route_backward(const RouteBackParams& p, unsigned blocks, cud
 }
 
 // ---- the plan: a stable counting sort of the routed pairs by expert ---------------------------------
-// Pairs (token, place) are numbered token * topk + place.  A chunk of kPlanChunk pairs is one block's;
-// each of its eight warps takes 256 consecutive pairs.  (1) every chunk counts its pairs per expert;
-// (2) one block turns the counts into row offsets and every chunk's first row per expert; (3) every chunk
-// places its pairs: a warp's pairs of one expert find their order with a match over the lanes.
-// A single chunk does all three in one launch.
+// Pairs (token, place) are numbered token * topk + place.  A chunk of kPlanChunk pairs is one block's; its
+// warps take equal spans of it.  (1) every chunk counts its pairs per expert; (2) every block adds up the counts
+// of the chunks before its own and of all, which gives the experts' first rows and its own pairs' among them; (3) it
+// places its pairs: a warp's pairs of one expert find their order among the lanes.  A single
+// chunk does all three in one launch; more than kPlanDirect chunks have (2) done by one block in between.
 
 struct PlanParams {
   const int32_t* idx;
@@ -309,11 +384,11 @@ struct PlanParams {
   int32_t* offsets;
   int32_t* counts;
   int32_t* slot;
-  int32_t* scratch;      // [chunks][experts]: counts, then first rows
+  int32_t* scratch;      // [chunks][experts]: counts, or (after the scan kernel) first rows
   int64_t pairs, rows;
   int experts, chunks;
 };
-constexpr int kPerWarp = kPlanChunk / kWarps;
+constexpr int kPlanDirect = 128;
 
 __device__ __forceinline__ int pair_expert(const PlanParams& p, int64_t i) {
   if (i >= p.pairs) return -1;
@@ -321,44 +396,84 @@ __device__ __forceinline__ int pair_expert(const PlanParams& p, int64_t i) {
   return e >= 0 && e < p.experts ? e : -1;
 }
 
-// hist[warp][expert] = pairs of the warp's span per expert.
-__device__ void warp_histograms(const PlanParams& p, int32_t* hist, int64_t chunk) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = threadIdx.x; i < kWarps * p.experts; i += kThreads) hist[i] = 0;
+// A warp's span of the chunk, held in registers: round r of it is lane's pair at base + 32 r.
+constexpr int kMaxRounds = kPlanChunk / 8 / 32;
+struct Span {
+  int64_t base;
+  int rounds;
+  int expert[kMaxRounds];
+};
+__device__ __forceinline__ Span load_span(const PlanParams& p, int64_t chunk) {
+  Span s;
+  const int span = kPlanChunk / (blockDim.x >> 5);
+  s.base = chunk * kPlanChunk + (threadIdx.x >> 5) * span + (threadIdx.x & 31);
+  s.rounds = span / 32;
+#pragma unroll
+  for (int r = 0; r < kMaxRounds; ++r) s.expert[r] = r < s.rounds ? pair_expert(p, s.base + 32 * r) : -1;
+  return s;
+}
+
+// hist[expert * stride + warp] = pairs of the warp's span per expert; stride is odd, so that lanes that walk
+// either way meet different banks.
+__device__ __forceinline__ int hist_stride() { return (blockDim.x >> 5) + 1; }
+__device__ void clear_histograms(const PlanParams& p, int32_t* hist) {
+  for (int i = threadIdx.x; i < hist_stride() * p.experts; i += blockDim.x) hist[i] = 0;
   __syncthreads();
-  const int64_t base = chunk * kPlanChunk + warp * kPerWarp;
-  for (int r = 0; r < kPerWarp; r += 32) {
-    const int e = pair_expert(p, base + r + lane);
-    if (e >= 0) atomicAdd(&hist[warp * p.experts + e], 1);     // a count: the order does not matter
-  }
+}
+__device__ void fill_histograms(const Span& s, int32_t* hist) {
+#pragma unroll
+  for (int r = 0; r < kMaxRounds; ++r)
+    if (s.expert[r] >= 0) atomicAdd(&hist[s.expert[r] * hist_stride() + (threadIdx.x >> 5)], 1);   // counts: any order
   __syncthreads();
 }
 
-// first[expert] becomes the row of every warp's first pair of the expert, in hist.
+// hist becomes the row of every warp's first pair of the expert.  One thread per expert, its counts in
+// flight eight at a time.
 __device__ void warp_starts(const PlanParams& p, int32_t* hist, const int32_t* first) {
-  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
+  const int warps = blockDim.x >> 5;
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
     int32_t at = first[e];
-    for (int w = 0; w < kWarps; ++w) {
-      const int32_t n = hist[w * p.experts + e];
-      hist[w * p.experts + e] = at;
-      at += n;
+    int32_t* row = hist + e * hist_stride();
+    for (int w0 = 0; w0 < warps; w0 += 8) {
+      int32_t n[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) n[i] = row[w0 + i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        row[w0 + i] = at;
+        at += n[i];
+      }
     }
   }
   __syncthreads();
 }
 
-__device__ void place_pairs(const PlanParams& p, int32_t* hist, int64_t chunk) {
+// The lanes whose expert is this lane's, from one ballot per bit of the numbers (match.any goes through the distinct
+// values one by one, 2,000 cycles for a warp of them).  Lanes without a pair (-1) match each other.
+__device__ __forceinline__ uint32_t same_expert(int e, int bits) {
+  uint32_t same = __ballot_sync(kFull, e >= 0);
+  if (e < 0) same = ~same;
+  for (int b = 0; b < bits; ++b) {
+    const uint32_t ones = __ballot_sync(kFull, (e >> b) & 1);
+    same &= ((e >> b) & 1) ? ones : ~ones;
+  }
+  return same;
+}
+
+__device__ void place_pairs(const PlanParams& p, const Span& s, int32_t* hist) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int32_t* mine = hist + warp * p.experts;
-  const int64_t base = chunk * kPlanChunk + warp * kPerWarp;
-  for (int r = 0; r < kPerWarp; r += 32) {
-    const int64_t i = base + r + lane;
-    const int e = pair_expert(p, i);
-    const uint32_t same = __match_any_sync(kFull, e);
+  const int bits = 32 - __clz(p.experts);
+#pragma unroll
+  for (int r = 0; r < kMaxRounds; ++r) {
+    if (r >= s.rounds) break;
+    const int64_t i = s.base + 32 * r;
+    const int e = s.expert[r];
+    const uint32_t same = same_expert(e, bits);
+    int32_t* next = hist + max(e, 0) * hist_stride() + warp;
     int row = -1;
-    if (e >= 0) row = mine[e] + __popc(same & ((1u << lane) - 1u));
+    if (e >= 0) row = *next + __popc(same & ((1u << lane) - 1u));
     __syncwarp();
-    if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+    if (e >= 0 && lane == __ffs(same) - 1) *next += __popc(same);
     __syncwarp();
     if (i < p.pairs) {
       p.slot[i] = row;
@@ -367,89 +482,126 @@ __device__ void place_pairs(const PlanParams& p, int32_t* hist, int64_t chunk) {
   }
 }
 
-// offsets, counts, block_expert and, in first[], the first row of every expert; total[] holds the counts.
-__device__ void scan_experts(const PlanParams& p, const int32_t* total, int32_t* first, int32_t* warp_sums) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+// first[] = the first row of every expert, from total[] (its pairs; may be first[] itself); with `write` also offsets, counts and
+// block_expert.  sums: one word per warp.
+__device__ void scan_experts(const PlanParams& p, const int32_t* total, int32_t* first, int32_t* sums, bool write) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   int32_t carry = 0;
-  for (int base = 0; base < p.experts; base += kThreads) {
+  for (int base = 0; base < p.experts; base += blockDim.x) {
     const int e = base + threadIdx.x;
-    const int32_t blocks = e < p.experts ? (total[e] + kExpertBlock - 1) / kExpertBlock : 0;
+    const int32_t pairs = e < p.experts ? total[e] : 0, blocks = (pairs + kExpertBlock - 1) / kExpertBlock;
     int32_t v = blocks;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int32_t o = __shfl_up_sync(kFull, v, d);
       if (lane >= d) v += o;
     }
-    if (lane == 31) warp_sums[warp] = v;
+    if (lane == 31) sums[warp] = v;
     __syncthreads();
-    int32_t before = carry, all = 0;
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) before += warp_sums[w];
-      all += warp_sums[w];
+    int32_t over = lane < warps ? sums[lane] : 0;      // the warps' sums, scanned by every warp for itself
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int32_t o = __shfl_up_sync(kFull, over, d);
+      if (lane >= d) over += o;
     }
-    const int32_t at = before + v - blocks;
+    const int32_t all = __shfl_sync(kFull, over, 31);
+    const int32_t earlier = __shfl_sync(kFull, over, max(warp - 1, 0));
+    const int32_t at = carry + (warp > 0 ? earlier : 0) + v - blocks;
     if (e < p.experts) {
       first[e] = at * kExpertBlock;
-      p.offsets[e] = at * kExpertBlock;
-      p.counts[e] = total[e];
-      for (int32_t b = 0; b < blocks; ++b) p.block_expert[at + b] = e;
+      if (write) {
+        p.offsets[e] = at * kExpertBlock;
+        p.counts[e] = pairs;
+        for (int32_t b = 0; b < blocks; ++b) p.block_expert[at + b] = e;
+      }
     }
     carry += all;
     __syncthreads();
   }
+  if (!write) return;
   if (threadIdx.x == 0) p.offsets[p.experts] = carry * kExpertBlock;
-  for (int64_t b = carry + threadIdx.x; b < p.rows / kExpertBlock; b += kThreads) p.block_expert[b] = -1;
+  for (int64_t b = carry + threadIdx.x; b < p.rows / kExpertBlock; b += blockDim.x) p.block_expert[b] = -1;
+}
+
+// total[e] = pairs of expert e in all chunks, mine[e] = those in the chunks before `chunk`.
+__device__ void add_chunks(const PlanParams& p, int chunk, int32_t* total, int32_t* mine) {
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) total[e] = mine[e] = 0;
+  __syncthreads();
+  // Several threads per expert, a few chunks each; sums of integers, in any order.
+  const int groups = max(1, (int)blockDim.x / p.experts);
+  const int g = threadIdx.x / p.experts;
+  for (int e = threadIdx.x - g * p.experts; e < p.experts && g < groups; e += blockDim.x) {
+    int32_t all = 0, before = 0;
+    for (int c0 = g; c0 < p.chunks; c0 += 16 * groups) {
+      int32_t n[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int c = c0 + i * groups;
+        n[i] = c < p.chunks ? p.scratch[(int64_t)c * p.experts + e] : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        all += n[i];
+        if (c0 + i * groups < chunk) before += n[i];
+      }
+    }
+    atomicAdd(&total[e], all);
+    atomicAdd(&mine[e], before);
+  }
   __syncthreads();
 }
 
-__global__ void __launch_bounds__(kThreads) plan_one_kernel(const PlanParams p) {
-  extern __shared__ int32_t hist[];       // [kWarps][experts], then total[experts], first[experts], sums
-  int32_t* total = hist + kWarps * p.experts;
+__global__ void __launch_bounds__(1024) plan_one_kernel(const PlanParams p) {
+  extern __shared__ int32_t hist[];       // [experts][warps + 1], then total[experts], first[experts], sums
+  const int warps = blockDim.x >> 5;
+  int32_t* total = hist + hist_stride() * p.experts;
   int32_t* first = total + p.experts;
   int32_t* sums = first + p.experts;
   pdl_wait();
   pdl_release();
-  for (int64_t i = threadIdx.x; i < p.rows; i += kThreads) p.row_src[i] = -1;
-  warp_histograms(p, hist, 0);
-  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
+  const Span span = load_span(p, 0);
+  for (int64_t i = threadIdx.x; i < p.rows; i += blockDim.x) p.row_src[i] = -1;
+  clear_histograms(p, hist);
+  fill_histograms(span, hist);
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
     int32_t n = 0;
-    for (int w = 0; w < kWarps; ++w) n += hist[w * p.experts + e];
+#pragma unroll 8
+    for (int w = 0; w < warps; ++w) n += hist[e * hist_stride() + w];
     total[e] = n;
   }
   __syncthreads();
-  scan_experts(p, total, first, sums);
+  scan_experts(p, total, first, sums, true);
   warp_starts(p, hist, first);
-  place_pairs(p, hist, 0);
+  place_pairs(p, span, hist);
 }
 
-__global__ void __launch_bounds__(kThreads) plan_count_kernel(const PlanParams p) {
-  extern __shared__ int32_t hist[];
+__global__ void __launch_bounds__(1024) plan_count_kernel(const PlanParams p) {
+  extern __shared__ int32_t total[];
   pdl_wait();
   pdl_release();
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < p.rows; i += (int64_t)gridDim.x * kThreads)
-    p.row_src[i] = -1;
-  warp_histograms(p, hist, blockIdx.x);
-  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
-    int32_t n = 0;
-    for (int w = 0; w < kWarps; ++w) n += hist[w * p.experts + e];
-    p.scratch[(int64_t)blockIdx.x * p.experts + e] = n;
-  }
-}
-
-__global__ void __launch_bounds__(kThreads) plan_scan_kernel(const PlanParams p) {
-  extern __shared__ int32_t total[];      // [experts], then first[experts], sums
-  int32_t* first = total + p.experts;
-  int32_t* sums = first + p.experts;
-  pdl_wait();
-  pdl_release();
-  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
-    int32_t n = 0;
-    for (int c = 0; c < p.chunks; ++c) n += p.scratch[(int64_t)c * p.experts + e];
-    total[e] = n;
-  }
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) total[e] = 0;
   __syncthreads();
-  scan_experts(p, total, first, sums);
-  for (int e = threadIdx.x; e < p.experts; e += kThreads) {
+  const int64_t base = (int64_t)blockIdx.x * kPlanChunk;
+  for (int r = threadIdx.x; r < kPlanChunk; r += blockDim.x) {
+    const int e = pair_expert(p, base + r);
+    if (e >= 0) atomicAdd(&total[e], 1);
+  }
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < p.rows; i += (int64_t)gridDim.x * blockDim.x)
+    p.row_src[i] = -1;
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.scratch[(int64_t)blockIdx.x * p.experts + e] = total[e];
+}
+
+__global__ void __launch_bounds__(1024) plan_scan_kernel(const PlanParams p) {
+  extern __shared__ int32_t first[];      // [experts], then mine[experts], sums
+  int32_t* mine = first + p.experts;
+  int32_t* sums = mine + p.experts;
+  pdl_wait();
+  pdl_release();
+  add_chunks(p, 0, first, mine);
+  scan_experts(p, first, first, sums, true);
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
     int32_t at = first[e];
     for (int c = 0; c < p.chunks; ++c) {
       int32_t* s = p.scratch + (int64_t)c * p.experts + e;
@@ -460,13 +612,27 @@ __global__ void __launch_bounds__(kThreads) plan_scan_kernel(const PlanParams p)
   }
 }
 
-__global__ void __launch_bounds__(kThreads) plan_place_kernel(const PlanParams p) {
-  extern __shared__ int32_t hist[];
+__global__ void __launch_bounds__(1024) plan_place_kernel(const PlanParams p) {
+  extern __shared__ int32_t hist[];       // [experts][warps + 1], then first and mine [experts], sums
+  int32_t* first = hist + hist_stride() * p.experts;
+  int32_t* mine = first + p.experts;
+  int32_t* sums = mine + p.experts;
   pdl_wait();
   pdl_release();
-  warp_histograms(p, hist, blockIdx.x);
-  warp_starts(p, hist, p.scratch + (int64_t)blockIdx.x * p.experts);
-  place_pairs(p, hist, blockIdx.x);
+  const Span span = load_span(p, blockIdx.x);
+  clear_histograms(p, hist);
+  if (p.chunks > kPlanDirect) {
+    fill_histograms(span, hist);
+    warp_starts(p, hist, p.scratch + (int64_t)blockIdx.x * p.experts);
+  } else {
+    add_chunks(p, blockIdx.x, first, mine);
+    fill_histograms(span, hist);
+    scan_experts(p, first, first, sums, blockIdx.x == 0);
+    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) first[e] += mine[e];
+    __syncthreads();
+    warp_starts(p, hist, first);
+  }
+  place_pairs(p, span, hist);
 }
 
 // ---- gradient of the weighted sum -----------------------------------------------------------------
@@ -580,7 +746,7 @@ cudaError_t route_backward_launch(const RouteCall& c, const int32_t* idx, const 
   const int64_t blocks = (c.tokens + kWarps - 1) / kWarps;
   if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
   RouteBackParams p{c.logits, idx, dweights, dlogits, c.tokens, (int)c.experts, (int)c.topk, c.sigmoid, c.renorm,
-                    c.scale};
+                    c.scale, c.experts % 4 == 0 && reinterpret_cast<uintptr_t>(dlogits) % 16 == 0};
   const cudaError_t e = c.logits_f32 ? launch_route_backward<true>(p, (unsigned)blocks, stream)
                                      : launch_route_backward<false>(p, (unsigned)blocks, stream);
   if (e == cudaSuccess) ++*launches;
@@ -600,19 +766,23 @@ cudaError_t plan_launch(const ExpertRows& x, const int32_t* idx, cudaStream_t st
   p.rows = x.rows;
   p.experts = (int)x.experts;
   p.chunks = (int)((p.pairs + kPlanChunk - 1) / kPlanChunk);
-  const size_t hist = (size_t)kWarps * p.experts * 4, lists = (size_t)p.experts * 8 + kWarps * 4;
-  const dim3 block(kThreads);
+  // A histogram per warp: 32 warps while that fits the 48 KiB every kernel may use, else eight.
+  const int warps = p.experts <= 256 ? 32 : 8;
+  const size_t hist = (size_t)(warps + 1) * p.experts * 4, lists = (size_t)p.experts * 8 + 32 * 4;
+  const dim3 block(32 * warps);
   cudaError_t e;
   if (p.chunks <= 1) {
     e = launch_pdl(plan_one_kernel, dim3(1), block, hist + lists, stream, 1, p);
     if (e == cudaSuccess) ++*launches;
     return e;
   }
-  e = launch_pdl(plan_count_kernel, dim3((unsigned)p.chunks), block, hist, stream, 1, p);
+  e = launch_pdl(plan_count_kernel, dim3((unsigned)p.chunks), dim3(1024), (size_t)p.experts * 4, stream, 1, p);
   if (e == cudaSuccess) ++*launches;
-  if (e == cudaSuccess) e = launch_pdl(plan_scan_kernel, dim3(1), block, lists, stream, 1, p);
-  if (e == cudaSuccess) ++*launches;
-  if (e == cudaSuccess) e = launch_pdl(plan_place_kernel, dim3((unsigned)p.chunks), block, hist, stream, 1, p);
+  if (e == cudaSuccess && p.chunks > kPlanDirect) {
+    e = launch_pdl(plan_scan_kernel, dim3(1), dim3(1024), lists, stream, 1, p);
+    if (e == cudaSuccess) ++*launches;
+  }
+  if (e == cudaSuccess) e = launch_pdl(plan_place_kernel, dim3((unsigned)p.chunks), block, hist + lists, stream, 1, p);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
