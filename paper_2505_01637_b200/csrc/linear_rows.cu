@@ -30,8 +30,9 @@ constexpr int kPrefetchBlocks = 6;     // contraction blocks asked into L2 befor
 template <int kRows>
 struct Shape {
   static constexpr int kStageBytes = 2 * kBoxBytes + kRows * kTileK * 2;
-  // Up to 16 rows two blocks fit an SM: the next strip (or the next launch) streams beside this one.
-  static constexpr int kRing = (kRows <= 16 ? 108 : 200) * 1024;
+  // Two blocks fit an SM: another strip, or the next launch's, streams beside this one, and clusters of half-SM
+  // blocks pack well (200 KiB rings: 8192 x 2048 on 32 rows in clusters of eight took two waves, 26 us).
+  static constexpr int kRing = 108 * 1024;
   static constexpr int kFit = kRing / kStageBytes;
   static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
   static constexpr int kTmemCols = kRows <= 32 ? 32 : 64;
@@ -66,7 +67,10 @@ struct Barriers {
   int abort_flag;
 };
 
-constexpr int kBatch = 16;     // rows a thread finishes at a time
+// Rows a thread finishes at a time.  The loops over them are rolled and their addresses advance by additions: a
+// block runs this code once, from cold instruction caches and one warp to a scheduler, so every instruction
+// counts (sixteen rows unrolled, with products for addresses and a switch per batch: 2.5 us of a 16 us launch).
+constexpr int kBatch = 4;
 
 template <int kAct>
 __device__ __forceinline__ void act_batch(float (&v)[kBatch]) {
@@ -81,8 +85,116 @@ __device__ __forceinline__ void act_batch_by(int act, float (&v)[kBatch]) {
   else act_batch<kActSilu>(v);
 }
 
+// A thread's column of the outputs and its rows: row i of them is row0 + lead + i * stride of the tensors.
+struct Column {
+  char* y;
+  uint16_t* z;
+  const uint16_t* r;
+  int64_t y_step, z_step, r_step;     // bytes, elements, elements from one of its rows to the next
+  int z_up;                           // from the gate's z to its partner's
+  float b0, b1;
+  bool f32, accumulate;
+  uint16_t held[kBatch];              // residual of the next batch
+
+  __device__ __forceinline__ void hold(int left) {
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) held[q] = r && q < left ? r[q * r_step] : (uint16_t)0;
+  }
+  // The next `left` (at most kBatch are taken) rows from their sums.
+  template <bool kGated>
+  __device__ __forceinline__ void finish(int act, int left, float (&v)[kBatch], float (&u)[kBatch]) {
+    uint16_t res[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) res[q] = held[q];
+    if (r) {
+      r += kBatch * r_step;
+      hold(left - kBatch);
+    }
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      v[q] += b0;
+      if constexpr (kGated) u[q] += b1;
+    }
+    if (z) {
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) {
+        if (q < left) {
+          z[q * z_step] = bf16_round(v[q]);
+          if constexpr (kGated) z[q * z_step + z_up] = bf16_round(u[q]);
+        }
+      }
+      z += kBatch * z_step;
+    }
+    act_batch_by(act, v);
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      if constexpr (kGated) v[q] *= u[q];
+      v[q] += bf16_value(res[q]);
+    }
+    if (f32) {
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) {
+        float* dst = reinterpret_cast<float*>(y + q * y_step);
+        if (q < left) *dst = accumulate ? *dst + v[q] : v[q];
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q)
+        if (q < left) *reinterpret_cast<uint16_t*>(y + q * y_step) = bf16_round(v[q]);
+    }
+    y += kBatch * y_step;
+  }
+};
+
+// One slice and no gate: the sums come straight from tensor memory.
+__device__ __forceinline__ void finish_direct(Column& c, int act, uint32_t taddr, int rows, bool live) {
+#pragma unroll 1
+  for (int g = 0; g < rows; g += kBatch) {
+    uint32_t r[kBatch];
+    tmem_ld_32x4(taddr + g, r);
+    tmem_ld_wait();
+    float v[kBatch], u[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) v[i] = __uint_as_float(r[i]);
+    if (live) c.finish<false>(act, rows - g, v, u);
+  }
+}
+
+// `rows` rows, `step` bytes of the parked sums apart, from those that the `split` blocks of the cluster have parked
+// at shared address `part`.
+template <bool kGated>
+__device__ __forceinline__ void finish_parked(Column& c, int act, uint32_t part, uint32_t step, int rows, int split) {
+#pragma unroll 1
+  for (int j = 0; j < rows; j += kBatch) {
+    float v[kBatch], u[kBatch];
+    auto sum = [&](uint32_t at, float (&x)[kBatch]) {
+      float t[8][kBatch];        // every slice's in flight, then added in slice order
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        if (s < split) {
+          const uint32_t peer = map_to_cta(at, (uint32_t)s);
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q) t[s][q] = j + q < rows ? ld_cluster_f32(peer + q * step) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) x[q] = t[0][q];
+#pragma unroll
+      for (int s = 1; s < 8; ++s)
+        if (s < split) {
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q) x[q] += t[s][q];
+        }
+    };
+    sum(part, v);
+    if constexpr (kGated) sum(part + 64 * 4, u);
+    c.finish<kGated>(act, rows - j, v, u);
+    part += kBatch * step;
+  }
+}
+
 template <int kRows>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)       // two blocks to an SM, registers included
 linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const RowsParams p) {
   using S = Shape<kRows>;
@@ -124,11 +236,11 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       }
     }
   }
-  pdl_wait();
-
-  // Which rows, and whose weights.
+  // Which rows, and whose weights.  An expert's are known once the predecessor is done; a dense layer has set
+  // everything up by then.
   int row0 = 0, rows = p.m, group = 0;
   if (p.grouped) {
+    pdl_wait();
     row0 = (int)blockIdx.y * kExpertBlock;
     group = p.block_expert[blockIdx.y];
     if (group < 0) {            // past the live blocks: the whole cluster leaves
@@ -147,22 +259,17 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem_base = bars->tmem_base;
+  if (!p.grouped) pdl_wait();
 
   // The finishing of rows: this thread's column, and its rows lead + j * stride of a chunk (the cluster's
   // blocks share the rows out; gated: so do the two halves of the threads).
-  const int t = (int)threadIdx.x - 64;                  // 0 .. 127 in the epilogue warps
+  const int t = (warp & 3) * 32 + lane;                 // the epilogue thread's accumulator lane
   const int j_col = p.gated ? t & 63 : t;
   const int col = col0 + j_col;
   const int stride = p.split * (p.gated ? 2 : 1);
   const int lead = p.gated ? slice * 2 + (t >> 6) : slice;
-  uint16_t held[kBatch];                                // residual of the next batch of rows
-  auto load_residual = [&](int first, int rows_here, int j0, uint16_t (&x)[kBatch]) {
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q) {
-      const int i = lead + (j0 + q) * stride;
-      x[q] = p.residual && i < rows_here && col < p.n ? p.residual[(int64_t)(first + i) * p.n + col] : (uint16_t)0;
-    }
-  };
+  const bool direct = p.split == 1 && !p.gated;
+  const bool live = warp >= 2 && col < p.n;
 
   int stage = 0;
   uint32_t phase = 0, acc_phase = 0;
@@ -233,109 +340,93 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     } else {
       // ---------------------------------------------------------------- epilogue
       const int quarter = warp & 3;
-      load_residual(first, rows_here, 0, held);
+      const int mine = lead < rows_here ? (rows_here - lead + stride - 1) / stride : 0;    // rows of this thread
+      Column c;
+      c.r = nullptr;
+      c.z = nullptr;
+      if (live) {
+        const int64_t row = first + lead;
+        const int size = p.out_f32 ? 4 : 2;
+        c.f32 = p.out_f32;
+        c.accumulate = p.accumulate;
+        c.y = static_cast<char*>(p.Y) + (row * p.n + col) * size;
+        c.y_step = (int64_t)stride * p.n * size;
+        c.z_step = (int64_t)stride * p.z_pitch;
+        c.z_up = p.n;
+        c.r_step = (int64_t)stride * p.n;
+        if (p.Z) c.z = p.Z + row * p.z_pitch + col;
+        if (p.residual) c.r = p.residual + row * p.n + col;
+        const uint16_t* bias = p.bias ? p.bias + (int64_t)group * p.z_pitch + col : nullptr;
+        c.b0 = bias ? bf16_value(bias[0]) : 0.f;
+        c.b1 = bias && p.gated ? bf16_value(bias[p.n]) : 0.f;
+        c.hold(mine);
+      }
       ok = mbar_wait(&bars->acc_full, acc_phase, abort_flag, p.status, 43);
       ok = __all_sync(0xffffffffu, ok);
       acc_phase ^= 1;
       if (ok) {
         tc_fence_after_sync();
-        // Every MMA has completed, so the stages are free: the sums are parked there as
-        // part[row][column of the strip].
+        // One slice and no gate: the sums are finished as they come.  Otherwise they are parked in the stages (every
+        // MMA has completed, so those are free) as part[row][column of the strip].
         float* part = reinterpret_cast<float*>(stages);
         const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+        if (direct && kb1 > kb0) {
+          finish_direct(c, p.act, taddr, rows_here, live);
+        } else {
+#pragma unroll 1
+          for (int g = 0; g < rows_here; g += 16) {
+            uint32_t r[16];
+            if (kb1 > kb0) {
+              tmem_ld_32x16(taddr + g, r);
+              tmem_ld_wait();
+            } else {
 #pragma unroll
-        for (int g = 0; g < kRows / 16; ++g) {
-          uint32_t r[16];
-          if (kb1 > kb0) {
-            tmem_ld_32x16(taddr + g * 16, r);
-            tmem_ld_wait();
-          } else {
+              for (int i = 0; i < 16; ++i) r[i] = 0u;     // an empty sum
+            }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) r[i] = 0u;     // an empty sum
+            for (int i = 0; i < 16; ++i) part[(g + i) * kStrip + quarter * 32 + lane] = __uint_as_float(r[i]);
           }
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            part[(g * 16 + i) * kStrip + quarter * 32 + lane] = __uint_as_float(r[i]);
         }
         tc_fence_before_sync();
       }
       __syncwarp();
-    }
-    cluster_sync();
-    if (warp >= 2 && !*abort_flag && col < p.n) {
-      const float* part = reinterpret_cast<const float*>(stages) + j_col;
-      const uint16_t* bias = p.bias ? p.bias + (int64_t)group * p.z_pitch : nullptr;
-      const float b0 = bias ? bf16_value(bias[col]) : 0.f;
-      const float b1 = bias && p.gated ? bf16_value(bias[p.n + col]) : 0.f;
-      for (int j0 = 0; lead + j0 * stride < rows_here; j0 += kBatch) {
-        if (j0 > 0) load_residual(first, rows_here, j0, held);
-        float v[kBatch], u[kBatch];
-        auto sum = [&](int offset, float (&x)[kBatch]) {
-#pragma unroll
-          for (int q = 0; q < kBatch; ++q) x[q] = 0.f;
-          for (int s = 0; s < p.split; ++s) {
-            const float* peer = peer_shared(part + offset, (uint32_t)s);
-#pragma unroll
-            for (int q = 0; q < kBatch; ++q) {
-              const int i = lead + (j0 + q) * stride;
-              if (i < rows_here) x[q] += peer[i * kStrip];
-            }
-          }
-        };
-        sum(0, v);
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q) v[q] += b0;
-        if (p.gated) {
-          sum(64, u);
-#pragma unroll
-          for (int q = 0; q < kBatch; ++q) u[q] += b1;
+      if (!(direct && kb1 > kb0)) {
+        if (p.split > 1) cluster_sync();
+        else asm volatile("bar.sync 1, 128;" ::: "memory");     // the epilogue warps alone
+        if (live && !*abort_flag) {
+          const uint32_t part = smem_u32(stages) + (uint32_t)(lead * kStrip + j_col) * 4u;
+          const uint32_t step = (uint32_t)(stride * kStrip) * 4u;
+          if (p.gated) finish_parked<true>(c, p.act, part, step, mine, p.split);
+          else finish_parked<false>(c, p.act, part, step, mine, p.split);
         }
-        if (p.Z) {
-#pragma unroll
-          for (int q = 0; q < kBatch; ++q) {
-            const int i = lead + (j0 + q) * stride;
-            if (i >= rows_here) continue;
-            uint16_t* z = p.Z + (int64_t)(first + i) * p.z_pitch + col;
-            z[0] = bf16_round(v[q]);
-            if (p.gated) z[p.n] = bf16_round(u[q]);
-          }
-        }
-        act_batch_by(p.act, v);
-        if (p.gated) {
-#pragma unroll
-          for (int q = 0; q < kBatch; ++q) v[q] *= u[q];
-        }
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q) {
-          const int i = lead + (j0 + q) * stride;
-          if (i >= rows_here) continue;
-          const int64_t out = (int64_t)(first + i) * p.n + col;
-          const float y = v[q] + bf16_value(held[q]);
-          if (p.out_f32) {
-            float* dst = static_cast<float*>(p.Y) + out;
-            *dst = p.accumulate ? *dst + y : y;
-          } else {
-            static_cast<uint16_t*>(p.Y)[out] = bf16_round(y);
-          }
-        }
-      }
-      // The rows that hold no token are zeros up to the next multiple of 16 (what the weight gradient's
-      // contraction reads); a decoding step does not write 127 rows for one.
-      if (p.zero_padding && chunk + 1 == chunks) {
-        for (int i = rows + lead; i < (rows + 15) / 16 * 16; i += stride) {
-          const int64_t row = row0 + i, out = row * p.n + col;
-          if (p.Z) {
-            p.Z[row * p.z_pitch + col] = 0;
-            if (p.gated) p.Z[row * p.z_pitch + p.n + col] = 0;
-          }
-          if (p.out_f32) static_cast<float*>(p.Y)[out] = 0.f;
-          else static_cast<uint16_t*>(p.Y)[out] = 0;
-        }
+        __syncwarp();
       }
     }
-    __syncwarp();
-    cluster_sync();      // the parked sums have been read by every block of the cluster
-    fence_proxy_async_smem();   // ... before the next chunk's copies land on them
+    if (warp < 2 && p.split > 1) cluster_sync();     // the epilogue warps' barrier above
+    // The parked sums have been read by every block of the cluster, the accumulator by every warp.
+    if (p.split > 1) {
+      __syncwarp();
+      cluster_sync();
+    } else if (chunk + 1 < chunks) {
+      __syncthreads();
+    }
+    if (chunk + 1 < chunks) {
+      tc_fence_after_sync();
+      fence_proxy_async_smem();   // ... before the next chunk's copies land on them
+    }
+  }
+  // The rows that hold no token are zeros up to the next multiple of 16 (what the weight gradient's
+  // contraction reads); a decoding step does not write 127 rows for one.
+  if (live && p.zero_padding) {
+    for (int i = rows + lead; i < (rows + 15) / 16 * 16; i += stride) {
+      const int64_t row = row0 + i, out = row * p.n + col;
+      if (p.Z) {
+        p.Z[row * p.z_pitch + col] = 0;
+        if (p.gated) p.Z[row * p.z_pitch + p.n + col] = 0;
+      }
+      if (p.out_f32) static_cast<float*>(p.Y)[out] = 0.f;
+      else static_cast<uint16_t*>(p.Y)[out] = 0;
+    }
   }
 
   tc_fence_before_sync();
@@ -361,7 +452,7 @@ cudaError_t launch(const DeviceInfo& dev, const TileCall& c, RowsParams p, cudaS
   const int64_t blocks = p.grouped ? c.experts.rows / kExpertBlock : 1;
   // Slices: as many as keep every block slot of the device busy with at least four contraction blocks.
   const int64_t live = p.grouped ? std::min(c.experts.experts, c.experts.tokens * c.experts.topk) : 1;
-  const int64_t slots = (int64_t)dev.sms * (kRows <= 16 ? 2 : 1);
+  const int64_t slots = (int64_t)dev.sms * 2;
   int split = 1;
   while (split < 8 && strips * live * split * 2 <= slots && p.k_blocks >= split * 2 * 4) split *= 2;
   while (split > 1 && (p.k_blocks + split - 1) / split * (split - 1) >= p.k_blocks) split /= 2;   // no empty slice

@@ -81,7 +81,7 @@ struct TileParams {
   const int32_t* counts;
   int experts;
   // epilogue
-  uint8_t act, out_f32, accumulate, vec, tma;
+  uint8_t act, out_f32, accumulate, vec, tma, copy;   // copy: bf16 Y is the sums, nothing else
   int z_pitch;           // columns of a row of Z and of the bias: n or 2 n
   const uint16_t* bias;
   const uint16_t* residual;
@@ -308,6 +308,47 @@ __device__ __forceinline__ void add_bias32(const uint16_t* bias, int cols, float
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     if (8 * j < cols) add_octet(reinterpret_cast<const uint4*>(bias)[j], v + 8 * j);   // cols % 8 == 0 here
+}
+
+// bf16 Y by TMA with nothing to be done to the sums (the gradients): steps of 64 columns, one block of 32 rows x 128
+// bytes a warp.  Half the fences and stores of the steps below; where the contraction is short (the weights of an
+// expert with few rows) the epilogue is what the kernel waits for.
+template <typename Wait, typename Release>
+__device__ __forceinline__ bool epilogue_copy(const TileParams& p, const EpilogueItem& e, const CUtensorMap& map_y,
+                                              uint8_t* mine, int part, int lane, Wait&& wait_sums,
+                                              Release&& release_sums) {
+  const int steps = e.row0 < e.row_end ? (min(e.width, p.n - e.col0) + 63) / 64 : 0;
+  if (!wait_sums()) return false;
+  const bool padding = p.zero_padding && e.row0 + lane >= e.live_end;
+  if (part >= steps) release_sums();
+#pragma unroll 1
+  for (int s = part; s < steps; s += kParts) {
+    uint32_t r[64];
+    start_sums32(e.taddr + 64u * s, e.empty_sum, *reinterpret_cast<uint32_t(*)[32]>(r));
+    start_sums32(e.taddr + 64u * s + 32u, e.empty_sum, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+    if (lane == 0) bulk_wait_group_read<0>();        // meanwhile: the block's last store has been read
+    tmem_ld_wait();
+    if (s + kParts >= steps) release_sums();
+    __syncwarp();
+    const uint32_t at = smem_u32(mine) + (uint32_t)lane * 128u, sw = (uint32_t)(lane & 7);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        w[q] = bf16_pack(__uint_as_float(r[8 * j + 2 * q]), __uint_as_float(r[8 * j + 2 * q + 1]));
+        if (padding) w[q] = 0u;
+      }
+      st_shared_v4(at + (((uint32_t)j ^ sw) << 4), w[0], w[1], w[2], w[3]);
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_3d(&map_y, mine, e.col0 + 64 * s, e.row0, e.group);
+      bulk_commit_group();
+    }
+  }
+  return true;
 }
 
 // Y and Z by TMA: steps part, part + kParts, ... of 32 columns.
@@ -723,8 +764,16 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     int buf = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
-    for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units); at.valid() && ok; at.next()) {
-      const Item it = at.item();
+    Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units);
+    Item ahead{};
+    if (at.valid()) ahead = at.item();
+    bool more = at.valid();
+    while (more && ok) {
+      // The next item is decoded before this one's steps: its loads (an expert's rows) return under them.
+      const Item it = ahead;
+      at.next();
+      if (at.valid()) ahead = at.item();
+      more = at.valid();
       EpilogueItem e;
       e.row0 = it.row0 + (int)rank * kRowsPerCta + quarter * 32;
       e.row_end = it.row_end;
@@ -749,7 +798,8 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           else mbar_arrive(&bars->acc_empty[buf]);
         }
       };
-      if (p.tma) ok = epilogue_tma<kGated>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums);
+      if (p.copy) ok = epilogue_copy(p, e, map_y, mine, part, lane, wait_sums, release_sums);
+      else if (p.tma) ok = epilogue_tma<kGated>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums);
       else ok = epilogue_plain<kGated>(p, e, smem_u32(mine), part, lane, wait_sums, release_sums);
       if (++buf == 2) { buf = 0; acc_phase ^= 1; }
     }
@@ -817,6 +867,7 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   p.accumulate = ep.accumulate;
   p.vec = c.n % 8 == 0 && aligned16(ep.Y) && aligned16(ep.Z) && aligned16(ep.bias) && aligned16(ep.residual);
   p.tma = p.vec;
+  p.copy = p.vec && !ep.gated && ep.act == kActNone && !ep.bias && !ep.residual && !ep.Z && !ep.out_f32;
   p.z_pitch = (int)(c.n * width);
   p.bias = ep.bias;
   p.residual = ep.residual;
@@ -870,8 +921,8 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   if (p.tma) {
     const uint64_t out_groups = (uint64_t)groups;
     e = make_tensor_map_3d(&maps.y, ep.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                           ep.out_f32 ? 4 : 2, ep.Y, (uint64_t)c.n, (uint64_t)c.m, out_groups, 32, 32,
-                           ep.out_f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+                           ep.out_f32 ? 4 : 2, ep.Y, (uint64_t)c.n, (uint64_t)c.m, out_groups, p.copy ? 64 : 32, 32,
+                           ep.out_f32 || p.copy ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
     // Z's halves are a dimension of their own: a block at the right edge of the first must not reach the second.
     if (e == cudaSuccess && ep.Z)
       e = make_tensor_map_3d_box(&maps.z, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ep.Z, (uint64_t)c.n, (uint64_t)width,
