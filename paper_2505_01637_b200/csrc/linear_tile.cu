@@ -737,14 +737,17 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           tc_fence_after_sync();
           const uint32_t sa = smem_u32(stages + (size_t)stage * S::kStageBytes);
           const uint32_t sb = sa + kBytesA;
-          const int steps = kb + 1 == k_blocks ? k_steps : kTileK / 16;
-#pragma unroll
-          for (int j = 0; j < kTileK / 16; ++j) {
-            if (j >= steps) break;
+          auto mma = [&](int j) {
             const uint64_t da = smem_desc_sw128(sa + j * step_a, lbo_a, 1024);
             const uint64_t db = smem_desc_sw128(sb + j * step_b, lbo_b, 1024);
             if constexpr (kPair) mma_bf16_ss_pair(d_tmem, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
             else mma_bf16_ss(d_tmem, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
+          };
+          if (kb + 1 < k_blocks || k_steps == kTileK / 16) {
+#pragma unroll
+            for (int j = 0; j < kTileK / 16; ++j) mma(j);
+          } else {
+            for (int j = 0; j < k_steps; ++j) mma(j);
           }
           if constexpr (kPair) mma_commit_pair(&bars->empty[stage], 3);
           else mma_commit(&bars->empty[stage]);
@@ -906,6 +909,8 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   p.m_tiles = (int)((c.m + tile_m - 1) / tile_m);
   p.n_tiles = (int)((c.n + out_cols - 1) / out_cols);
   p.tiles = groups * p.m_tiles * (int64_t)p.n_tiles;
+  // Experts' pairs of blocks: up to one per block.
+  const int64_t most = c.mode == TileMode::kRows ? (c.m / kExpertBlock) * (int64_t)p.n_tiles : p.tiles;
   if (p.tiles >= (1ll << 30) || p.n_tiles >= (1 << 27)) return cudaErrorInvalidValue;   // items are ints
 
   Maps maps;
@@ -931,15 +936,15 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   }
   const int code = best_pair * 10000 + best_n * 10 + (ep.gated ? 1 : 0);
   switch (code) {
-    case 640: e = launch_tile<false, 64, false>(dev, maps, p, p.tiles, stream); break;
-    case 1280: e = launch_tile<false, 128, false>(dev, maps, p, p.tiles, stream); break;
-    case 2560: e = launch_tile<false, 256, false>(dev, maps, p, p.tiles, stream); break;
-    case 1281: e = launch_tile<false, 128, true>(dev, maps, p, p.tiles, stream); break;
-    case 2561: e = launch_tile<false, 256, true>(dev, maps, p, p.tiles, stream); break;
-    case 11280: e = launch_tile<true, 128, false>(dev, maps, p, p.tiles, stream); break;
-    case 12560: e = launch_tile<true, 256, false>(dev, maps, p, p.tiles, stream); break;
-    case 11281: e = launch_tile<true, 128, true>(dev, maps, p, p.tiles, stream); break;
-    case 12561: e = launch_tile<true, 256, true>(dev, maps, p, p.tiles, stream); break;
+    case 640: e = launch_tile<false, 64, false>(dev, maps, p, most, stream); break;
+    case 1280: e = launch_tile<false, 128, false>(dev, maps, p, most, stream); break;
+    case 2560: e = launch_tile<false, 256, false>(dev, maps, p, most, stream); break;
+    case 1281: e = launch_tile<false, 128, true>(dev, maps, p, most, stream); break;
+    case 2561: e = launch_tile<false, 256, true>(dev, maps, p, most, stream); break;
+    case 11280: e = launch_tile<true, 128, false>(dev, maps, p, most, stream); break;
+    case 12560: e = launch_tile<true, 256, false>(dev, maps, p, most, stream); break;
+    case 11281: e = launch_tile<true, 128, true>(dev, maps, p, most, stream); break;
+    case 12561: e = launch_tile<true, 256, true>(dev, maps, p, most, stream); break;
     default: return cudaErrorInvalidValue;
   }
   if (e == cudaSuccess) ++*launches;
