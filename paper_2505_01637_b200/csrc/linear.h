@@ -68,7 +68,9 @@ struct TileCall {
   ExpertRows experts;
   LinearEpilogue epi;
 };
-cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& call, cudaStream_t stream, uint64_t* launches);
+// One product, or two (of which only the first may be kRows), in one launch.
+cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count, cudaStream_t stream,
+                        uint64_t* launches);
 
 // The few-rows kernel: at most kLinearFewRows rows (per expert), B streamed once.
 constexpr int kLinearFewRows = 64;
@@ -82,7 +84,8 @@ struct CopyJob {
   const ExpertRows* experts = nullptr;  // rows past the live ones are left alone
   bool gather = false;                  // with experts: row r of dst is token row_src[r] / topk of src
 };
-cudaError_t copy_launch(const CopyJob& job, cudaStream_t stream, uint64_t* launches);
+constexpr int kMaxCopies = 2;
+cudaError_t copy_launch(const CopyJob* jobs, int count, cudaStream_t stream, uint64_t* launches);   // one launch
 
 // dZ = dY . act'(Z) into dZ [rows][width rounded up to 8] (bf16, the added columns zero; width = n or
 // 2 n), and, when db is given, the column sums of dZ (per expert with experts) in f32, in a fixed order through

@@ -91,28 +91,31 @@ int check_experts(int64_t tokens, int64_t topk, int64_t experts) {
   return MORELLO_OK;
 }
 
-// The operands as the tensor kernels can address them: the tensors themselves, or copies.
-struct Operands {
-  MatrixView x;       // [rows][k or k8]
-  MatrixView w;       // forward form (gated: halves apart) or plain form
-  int64_t w_up = 0;   // forward form, gated: where the second half begins
+// Copies that a pass needs before its products, made by one launch.
+struct Copies {
+  CopyJob job[kMaxCopies];
+  int count = 0;
+  int launch(cudaStream_t s, uint64_t* launches) {
+    const cudaError_t e = copy_launch(job, count, s, launches);
+    return e == cudaSuccess ? MORELLO_OK : record_cuda_error(e);
+  }
 };
 
 // X: [rows][k], padded when the TMA engine cannot address it; with `gather` its rows are copied in the
 // experts' layout (the tile kernel's gathered loads, 32 of four rows per stage, were measured at twice the
 // time of the whole product; the few-rows kernel gathers for itself).
-int stage_x(const Layer& l, const void* X, bool gather, Carver& ws, bool dry, cudaStream_t s, uint64_t* launches, MatrixView* out) {
+void stage_x(const Layer& l, const void* X, bool gather, Carver& ws, bool dry, Copies* copies, MatrixView* out) {
   const uint16_t* src = static_cast<const uint16_t*>(X);
   const bool copy = gather || l.k % 8 != 0 || (!dry && !aligned(X, 16));
   out->rows = gather ? l.m : l.x_rows();
   out->groups = 1;
   out->cols = copy ? round8(l.k) : l.k;
   out->p = src;
-  if (!copy) return MORELLO_OK;
+  if (!copy) return;
   uint16_t* dst = ws.take<uint16_t>((size_t)out->rows * out->cols * 2);
   out->p = dst;
-  if (!ws.base) return MORELLO_OK;
-  CopyJob j;
+  if (!ws.base) return;
+  CopyJob& j = copies->job[copies->count++];
   j.src = src;
   j.dst = dst;
   j.rows_in = l.x_rows();
@@ -121,14 +124,12 @@ int stage_x(const Layer& l, const void* X, bool gather, Carver& ws, bool dry, cu
   j.cols_out = out->cols;
   j.gather = gather;
   if (gather || (l.grouped && !l.gather)) j.experts = &l.x;
-  const cudaError_t e = copy_launch(j, s, launches);
-  return e == cudaSuccess ? MORELLO_OK : record_cuda_error(e);
 }
 
 // W for a product.  halves_apart: the forward pass of a gated layer reads its halves as two column
 // ranges, each of which has to begin on a 16-byte boundary.
-int stage_w(const Layer& l, const void* W, bool halves_apart, Carver& ws, bool dry, cudaStream_t s, uint64_t* launches,
-            MatrixView* out, int64_t* up) {
+void stage_w(const Layer& l, const void* W, bool halves_apart, Carver& ws, bool dry, Copies* copies, MatrixView* out,
+             int64_t* up) {
   const uint16_t* src = static_cast<const uint16_t*>(W);
   const int64_t parts = halves_apart && l.gated ? 2 : 1;       // column ranges of a row
   const int64_t cols_in = l.w_cols ? l.k : l.wide() / parts;
@@ -140,11 +141,11 @@ int stage_w(const Layer& l, const void* W, bool halves_apart, Carver& ws, bool d
   out->cols = l.w_cols ? cols : cols * parts;
   out->p = src;
   if (up) *up = l.w_cols ? l.n : cols;
-  if (!copy) return MORELLO_OK;
+  if (!copy) return;
   uint16_t* dst = ws.take<uint16_t>((size_t)l.groups * rows * cols * 2);
   out->p = dst;
-  if (!ws.base) return MORELLO_OK;
-  CopyJob j;
+  if (!ws.base) return;
+  CopyJob& j = copies->job[copies->count++];
   j.src = src;
   j.dst = dst;
   j.groups = l.groups;
@@ -152,8 +153,6 @@ int stage_w(const Layer& l, const void* W, bool halves_apart, Carver& ws, bool d
   j.rows_out = rows;
   j.cols_in = cols_in;
   j.cols_out = cols;
-  const cudaError_t e = copy_launch(j, s, launches);
-  return e == cudaSuccess ? MORELLO_OK : record_cuda_error(e);
 }
 
 struct ForwardArgs {
@@ -163,8 +162,7 @@ struct ForwardArgs {
 };
 
 int product(const DeviceInfo& dev, const Layer& l, const TileCall& c, cudaStream_t s, uint64_t* launches) {
-  const cudaError_t e = c.mode != TileMode::kContract && !c.a_mn && few_rows(l) ? rows_launch(dev, c, s, launches)
-                                                                                : tile_launch(dev, c, s, launches);
+  const cudaError_t e = few_rows(l) ? rows_launch(dev, c, s, launches) : tile_launch(dev, &c, 1, s, launches);
   return e == cudaSuccess ? MORELLO_OK : record_cuda_error(e);
 }
 
@@ -173,12 +171,13 @@ int forward(const DeviceInfo& dev, const Layer& l, const ForwardArgs& a, Carver&
             uint64_t* launches) {
   MatrixView x, w;
   int64_t up = 0;
-  int rc;
+  Copies copies;
   if (l.k > 0) {
-    if ((rc = stage_x(l, a.X, l.gather && !few_rows(l), ws, dry, s, launches, &x)) != MORELLO_OK) return rc;
-    if ((rc = stage_w(l, a.W, true, ws, dry, s, launches, &w, &up)) != MORELLO_OK) return rc;
+    stage_x(l, a.X, l.gather && !few_rows(l), ws, dry, &copies, &x);
+    stage_w(l, a.W, true, ws, dry, &copies, &w, &up);
   }
   if (!ws.base) return MORELLO_OK;
+  if (const int rc = copies.launch(s, launches)) return rc;
   TileCall c;
   c.mode = l.grouped ? TileMode::kRows : TileMode::kDense;
   c.a = x;
@@ -240,48 +239,55 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
     if ((e = slope_launch(dev, c, s, launches)) != cudaSuccess) return record_cuda_error(e);
   }
   const MatrixView z{dz, direct ? l.n : wide8, l.m, 1};
+  MatrixView x, w;
+  Copies copies;
+  float* rows = nullptr;       // gather: dX of the layout's rows, summed by token at the end
   if (want_dx) {
-    MatrixView w;
-    if ((rc = stage_w(l, a.W, false, ws, dry, s, launches, &w, nullptr)) != MORELLO_OK) return rc;
-    float* rows = l.gather ? ws.take<float>((size_t)l.m * l.k * 4) : nullptr;
-    if (ws.base) {
-      TileCall c;
-      c.mode = l.grouped ? TileMode::kRows : TileMode::kDense;
-      c.a = z;
-      c.b = w;
-      c.b_mn = l.w_cols;
-      c.m = l.m;
-      c.n = l.k;
-      c.k = wide;
-      c.zero_padding = l.grouped && !l.gather;
-      c.experts = l.x;
-      c.epi.out_f32 = l.gather;
-      c.epi.Y = l.gather ? static_cast<void*>(rows) : a.dX;
+    stage_w(l, a.W, false, ws, dry, &copies, &w, nullptr);
+    if (l.gather) rows = ws.take<float>((size_t)l.m * l.k * 4);
+  }
+  if (want_dw) stage_x(l, a.X, l.gather, ws, dry, &copies, &x);
+  if (!ws.base) return MORELLO_OK;
+  if ((rc = copies.launch(s, launches)) != MORELLO_OK) return rc;
+  TileCall calls[2];
+  int count = 0;
+  if (want_dx) {
+    TileCall& c = calls[count++];
+    c.mode = l.grouped ? TileMode::kRows : TileMode::kDense;
+    c.a = z;
+    c.b = w;
+    c.b_mn = l.w_cols;
+    c.m = l.m;
+    c.n = l.k;
+    c.k = wide;
+    c.zero_padding = l.grouped && !l.gather;
+    c.experts = l.x;
+    c.epi.out_f32 = l.gather;
+    c.epi.Y = l.gather ? static_cast<void*>(rows) : a.dX;
+    if (few_rows(l)) {
       if ((rc = product(dev, l, c, s, launches)) != MORELLO_OK) return rc;
-      if (l.gather) {
-        e = combine_launch(l.x, true, l.k, l.k, nullptr, rows, nullptr, static_cast<uint16_t*>(a.dX), s, launches);
-        if (e != cudaSuccess) return record_cuda_error(e);
-      }
+      count = 0;
     }
   }
   if (want_dw) {
-    MatrixView x;
-    if ((rc = stage_x(l, a.X, l.gather, ws, dry, s, launches, &x)) != MORELLO_OK) return rc;
-    if (ws.base) {
-      TileCall c;
-      c.mode = l.grouped ? TileMode::kContract : TileMode::kDense;
-      c.a = l.w_cols ? z : x;
-      c.b = l.w_cols ? x : z;
-      c.a_mn = c.b_mn = true;
-      c.m = l.w_cols ? wide : l.k;
-      c.n = l.w_cols ? l.k : wide;
-      c.k = l.m;
-      c.experts = l.x;
-      c.epi.out_f32 = a.grad_f32;
-      c.epi.accumulate = a.accumulate;
-      c.epi.Y = a.dW;
-      if ((rc = product(dev, l, c, s, launches)) != MORELLO_OK) return rc;
-    }
+    TileCall& c = calls[count++];
+    c = TileCall{};
+    c.mode = l.grouped ? TileMode::kContract : TileMode::kDense;
+    c.a = l.w_cols ? z : x;
+    c.b = l.w_cols ? x : z;
+    c.a_mn = c.b_mn = true;
+    c.m = l.w_cols ? wide : l.k;
+    c.n = l.w_cols ? l.k : wide;
+    c.k = l.m;
+    c.experts = l.x;
+    c.epi.out_f32 = a.grad_f32;
+    c.epi.accumulate = a.accumulate;
+    c.epi.Y = a.dW;
+  }
+  if (count > 0 && (e = tile_launch(dev, calls, count, s, launches)) != cudaSuccess) return record_cuda_error(e);
+  if (rows) {
+    e = combine_launch(l.x, true, l.k, l.k, nullptr, rows, nullptr, static_cast<uint16_t*>(a.dX), s, launches);
+    if (e != cudaSuccess) return record_cuda_error(e);
   }
   return MORELLO_OK;
 }

@@ -45,18 +45,28 @@ struct CopyParams {
   uint4* dst;
   int64_t rows_in, cols_in, rows_out;
   int octets;                 // 8-column groups of a row of dst
+  int spans;                  // of kThreads octets
   bool vec;
   int topk;
   const int32_t* row_src;     // gather
   const int32_t* live;        // number of live rows, or null
 };
 
-// Grid: x = row groups (all groups of dst one after another), y = spans of kThreads octets.
-__global__ void __launch_bounds__(kThreads) copy_kernel(const CopyParams p) {
-  const int o = blockIdx.y * kThreads + threadIdx.x;
-  const int64_t spans = (p.rows_out + kCopyRows - 1) / kCopyRows;
-  const int64_t g = blockIdx.x / spans;
-  const int64_t r0 = (blockIdx.x - g * spans) * kCopyRows;
+struct CopyBatch {
+  CopyParams job[kMaxCopies];
+  int blocks0;                // blocks of the first job
+};
+
+// Grid: a job's row groups (all groups of dst one after another), each in spans of kThreads octets.
+__global__ void __launch_bounds__(kThreads) copy_kernel(const CopyBatch batch) {
+  const bool second = (int)blockIdx.x >= batch.blocks0;
+  const CopyParams& p = batch.job[second ? 1 : 0];
+  const int block = (int)blockIdx.x - (second ? batch.blocks0 : 0);
+  const int o = block % p.spans * kThreads + threadIdx.x;
+  const int64_t row_group = block / p.spans;
+  const int64_t groups_of_rows = (p.rows_out + kCopyRows - 1) / kCopyRows;
+  const int64_t g = row_group / groups_of_rows;
+  const int64_t r0 = (row_group - g * groups_of_rows) * kCopyRows;
   pdl_wait();
   pdl_release();
   if (o >= p.octets || (p.live && r0 >= *p.live)) return;
@@ -290,27 +300,38 @@ cudaError_t grid_for(int64_t threads, unsigned* blocks) {
 
 }  // namespace
 
-cudaError_t copy_launch(const CopyJob& j, cudaStream_t stream, uint64_t* launches) {
-  CopyParams p{};
-  p.src = j.src;
-  p.dst = reinterpret_cast<uint4*>(j.dst);
-  p.rows_in = j.rows_in;
-  p.cols_in = j.cols_in;
-  p.rows_out = j.rows_out;
-  p.octets = (int)(j.cols_out / 8);
-  p.vec = j.cols_in % 8 == 0 && aligned16(j.src);
-  if (j.experts) {
-    p.live = j.experts->offsets + j.experts->experts;
-    if (j.gather) {
-      p.row_src = j.experts->row_src;
-      p.topk = (int)j.experts->topk;
+cudaError_t copy_launch(const CopyJob* jobs, int count, cudaStream_t stream, uint64_t* launches) {
+  if (count > kMaxCopies) return cudaErrorInvalidValue;
+  CopyBatch batch{};
+  int64_t blocks = 0;
+  int at = 0;
+  for (int i = 0; i < count; ++i) {
+    const CopyJob& j = jobs[i];
+    CopyParams p{};
+    p.src = j.src;
+    p.dst = reinterpret_cast<uint4*>(j.dst);
+    p.rows_in = j.rows_in;
+    p.cols_in = j.cols_in;
+    p.rows_out = j.rows_out;
+    p.octets = (int)(j.cols_out / 8);
+    p.spans = (p.octets + kThreads - 1) / kThreads;
+    p.vec = j.cols_in % 8 == 0 && aligned16(j.src);
+    if (j.experts) {
+      p.live = j.experts->offsets + j.experts->experts;
+      if (j.gather) {
+        p.row_src = j.experts->row_src;
+        p.topk = (int)j.experts->topk;
+      }
     }
+    const int64_t mine = j.groups * ((j.rows_out + kCopyRows - 1) / kCopyRows) * p.spans;
+    if (mine <= 0) continue;
+    if (at == 0) batch.blocks0 = (int)std::min<int64_t>(mine, (1ll << 31) - 1);
+    batch.job[at++] = p;
+    blocks += mine;
   }
-  const int64_t blocks = j.groups * ((j.rows_out + kCopyRows - 1) / kCopyRows);
-  const int64_t spans = (p.octets + kThreads - 1) / kThreads;
-  if (blocks <= 0 || spans <= 0) return cudaSuccess;
-  if (blocks >= (1ll << 31) || spans > 65535) return cudaErrorInvalidValue;
-  const cudaError_t e = launch_pdl(copy_kernel, dim3((unsigned)blocks, (unsigned)spans), dim3(kThreads), 0, stream, 1, p);
+  if (blocks == 0) return cudaSuccess;
+  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
+  const cudaError_t e = launch_pdl(copy_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, 1, batch);
   if (e == cudaSuccess) ++*launches;
   return e;
 }

@@ -570,11 +570,18 @@ __device__ __forceinline__ bool epilogue_plain(const TileParams& p, const Epilog
   return true;
 }
 
-template <bool kPair, int kTileN, bool kGated>
-__global__ void __launch_bounds__(kThreads, 1)
-linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                   const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_z,
-                   const TileParams p) {
+// The products of a launch: one, or the two of a backward pass, whose tiles share the units out between them.
+constexpr int kMaxProducts = 2;
+struct TileBatch {
+  CUtensorMap a[kMaxProducts], b[kMaxProducts], y[kMaxProducts];
+  CUtensorMap z;                // of the first product
+  TileParams p[kMaxProducts];
+};
+
+// kTwo: the batch has two products.  One is a form of its own so that its parameters are constants at fixed
+// addresses (through an index the epilogue of a 64-deep product took 92 instead of 79 us).
+template <bool kPair, int kTileN, bool kGated, bool kTwo>
+__global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_constant__ TileBatch batch) {
   using S = Shape<kPair, kTileN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* stages = reinterpret_cast<uint8_t*>(
@@ -600,9 +607,9 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     }
     bars->abort_flag = 0;
     mbar_fence_init();
-    tma_prefetch_descriptor(&map_a);
-    tma_prefetch_descriptor(&map_b);
-    if (p.tma) tma_prefetch_descriptor(&map_y);
+    tma_prefetch_descriptor(&batch.a[0]);
+    tma_prefetch_descriptor(&batch.b[0]);
+    if (batch.p[0].tma) tma_prefetch_descriptor(&batch.y[0]);
   }
   if (warp == 1) {
     if constexpr (kPair) {
@@ -617,8 +624,9 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   pdl_wait();
   pdl_release();
 
-  // The experts' rows that are live are known on the device only.
-  if (kPair && p.mode == (int)TileMode::kRows && warp == 2) {
+  // The experts' rows that are live are known on the device only (the first product's, if any).
+  if (kPair && batch.p[0].mode == (int)TileMode::kRows && warp == 2) {
+    const TileParams& p = batch.p[0];
     int before = 0;
     for (int e0 = 0; e0 < p.experts; e0 += 32) {
       const int e = e0 + lane;
@@ -640,18 +648,22 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_after_sync();
   const uint32_t tmem_base = bars->tmem_base;
 
-  Walk w;
-  w.m_tiles = p.m_tiles;
-  w.n_tiles = p.n_tiles;
-  int tiles = (int)p.tiles;
-  if (p.mode == (int)TileMode::kRows) {
-    w.m_tiles = kPair ? bars->pairs_before[p.experts] : p.offsets[p.experts] / kExpertBlock;
-    tiles = w.m_tiles * p.n_tiles;
-  }
-  // The tiles of a last wave that would occupy at most half the units are cut into column halves.
-  const int tail = tiles % units;
-  w.whole = p.halves && tiles > units && tail > 0 && 2 * tail <= units ? tiles - tail : tiles;
-  w.items = w.whole + 2 * (tiles - w.whole);
+  // Where a product's walk begins for this unit: the second goes on where the first left off.
+  auto walk_of = [&](int q, Walk* w) {
+    const TileParams& p = batch.p[q];
+    w->m_tiles = p.m_tiles;
+    w->n_tiles = p.n_tiles;
+    int tiles = (int)p.tiles;
+    if (p.mode == (int)TileMode::kRows) {
+      w->m_tiles = kPair ? bars->pairs_before[p.experts] : p.offsets[p.experts] / kExpertBlock;
+      tiles = w->m_tiles * p.n_tiles;
+    }
+    // The tiles of a last wave that would occupy at most half the units are cut into column halves.
+    const int tail = tiles % units;
+    w->whole = p.halves && tiles > units && tail > 0 && 2 * tail <= units ? tiles - tail : tiles;
+    w->items = w->whole + 2 * (tiles - w->whole);
+  };
+  auto next_unit = [&](int unit_now, const Walk& w) { return (unit_now + units - w.items % units) % units; };
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
@@ -661,102 +673,118 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       bool ok = true;
       const uint32_t leader_full = kPair ? map_to_cta(smem_u32(&bars->full[0]), 0) : 0u;
       (void)leader_full;
-      // The k loop is kept short: one thread issues it, and everything in it delays the next load.
-      const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
-      for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units); at.valid() && ok; at.next()) {
-        const Item it = at.item();
-        const int row0 = it.row0 + (int)rank * kRowsPerCta;
-        const int z_b = p.mode == (int)TileMode::kRows ? it.group : 0;
-        const int cols_b = it.cols / S::kCtas, boxes_b = cols_b / 64;
-        const uint32_t tx = (uint32_t)(kBytesA + boxes_b * kBoxBytes);
-        const int col0 = kGated ? (it.nt * kTileN + it.n_off) / 2 : it.nt * kTileN + it.n_off;
-        int cols[S::kBoxesB];      // stored column of every 64-column box of B
+      int from = unit;
+      for (int q = 0; q < (kTwo ? 2 : 1); ++q) {
+      const TileParams& p = batch.p[q];
+      const CUtensorMap* map_a   = &batch.a[q];
+        const CUtensorMap* map_b = &batch.b[q];
+        Walk w;
+        walk_of(q, &w);
+        // The k loop is kept short: one thread issues it, and everything in it delays the next load.
+        const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
+        for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, from, units); at.valid() && ok; at.next()) {
+          const Item it = at.item();
+          const int row0 = it.row0 + (int)rank * kRowsPerCta;
+          const int z_b = p.mode == (int)TileMode::kRows ? it.group : 0;
+          const int cols_b = it.cols / S::kCtas, boxes_b = cols_b / 64;
+          const uint32_t tx = (uint32_t)(kBytesA + boxes_b * kBoxBytes);
+          const int col0 = kGated ? (it.nt * kTileN + it.n_off) / 2 : it.nt * kTileN + it.n_off;
+          int cols[S::kBoxesB];      // stored column of every 64-column box of B
 #pragma unroll
-        for (int j = 0; j < S::kBoxesB; ++j) {
-          const int at = (int)rank * cols_b + j * 64;      // accumulator column
-          if constexpr (kGated) cols[j] = at < it.cols / 2 ? col0 + at : p.b_up + col0 + at - it.cols / 2;
-          else cols[j] = col0 + at;
-        }
-        int kc = it.k_row0;
-        for (int kb = 0; kb < it.k_blocks; ++kb, kc += kTileK) {
-          if (!(ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 33))) break;
-          uint8_t* sa = stages + (size_t)stage * S::kStageBytes;
-          uint8_t* sb = sa + kBytesA;
-          const uint32_t full = leader_full + (uint32_t)stage * 8u;
-          (void)full;
-          if constexpr (kPair) {
-            if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * tx);
-          } else {
-            mbar_arrive_expect_tx(&bars->full[stage], tx);
+          for (int j = 0; j < S::kBoxesB; ++j) {
+            const int at = (int)rank * cols_b + j * 64;      // accumulator column
+            if constexpr (kGated) cols[j] = at < it.cols / 2 ? col0 + at : p.b_up + col0 + at - it.cols / 2;
+            else cols[j] = col0 + at;
           }
-          auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1, int c2) {
-            if constexpr (kPair) tma_load_3d_pair(dst, map, full, c0, c1, c2);
-            else tma_load_3d(dst, map, &bars->full[stage], c0, c1, c2);
-          };
-          if (a_mn) {
-            load(sa, &map_a, row0, kc, 0);
-            load(sa + kBoxBytes, &map_a, row0 + 64, kc, 0);
-          } else {
-            load(sa, &map_a, kc, row0, 0);
-          }
+          int kc = it.k_row0;
+          for (int kb = 0; kb < it.k_blocks; ++kb, kc += kTileK) {
+            if (!(ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 33))) break;
+            uint8_t* sa = stages + (size_t)stage * S::kStageBytes;
+            uint8_t* sb = sa + kBytesA;
+            const uint32_t full = leader_full + (uint32_t)stage * 8u;
+            (void)full;
+            if constexpr (kPair) {
+              if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * tx);
+            } else {
+              mbar_arrive_expect_tx(&bars->full[stage], tx);
+            }
+            auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1, int c2) {
+              if constexpr (kPair) tma_load_3d_pair(dst, map, full, c0, c1, c2);
+              else tma_load_3d(dst, map, &bars->full[stage], c0, c1, c2);
+            };
+            if (a_mn) {
+              load(sa, map_a, row0, kc, 0);
+              load(sa + kBoxBytes, map_a, row0 + 64, kc, 0);
+            } else {
+              load(sa, map_a, kc, row0, 0);
+            }
 #pragma unroll
-          for (int j = 0; j < S::kBoxesB; ++j)
-            if (j < boxes_b) load(sb + j * kBoxBytes, &map_b, b_mn ? cols[j] : kc, b_mn ? kc : cols[j], z_b);
-          if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+            for (int j = 0; j < S::kBoxesB; ++j)
+              if (j < boxes_b) load(sb + j * kBoxBytes, map_b, b_mn ? cols[j] : kc, b_mn ? kc : cols[j], z_b);
+            if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+          }
         }
+      from = next_unit(from, w);
       }
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (rank == 0 && elect_one()) {
-      const uint32_t idesc_tile = instr_desc_bf16(S::kTileM, kTileN, p.a_mn != 0, p.b_mn != 0);
-      const uint32_t idesc_half = instr_desc_bf16(S::kTileM, kTileN / 2, p.a_mn != 0, p.b_mn != 0);
-      // Across the contraction: 64-column groups one box apart, 16 contraction rows = 2048 bytes.
-      // Along it: 8-row groups 1024 bytes apart, 16 elements = 32 bytes along the row.
-      const uint32_t step_a = p.a_mn ? 2048u : 32u, step_b = p.b_mn ? 2048u : 32u;
-      const uint32_t lbo_a = p.a_mn ? kBoxBytes : 16u, lbo_b = p.b_mn ? kBoxBytes : 16u;
       int stage = 0;
       uint32_t phase = 0;
       int buf = 0;
       uint32_t acc_phase = 0;
       bool ok = true;
-      for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units); at.valid() && ok; at.next()) {
-        // The place of the tile does not matter here; its width and, by expert, its depth do.
-        int k_blocks = p.k_blocks, k_steps = kTileK / 16;
-        if (p.mode == (int)TileMode::kContract) {
-          const Item it = at.item();
-          k_blocks = it.k_blocks;
-          k_steps = it.k_steps;
-        }
-        const uint32_t idesc = at.is_half() ? idesc_half : idesc_tile;
-        if (!(ok = mbar_wait(&bars->acc_empty[buf], acc_phase ^ 1, abort_flag, p.status, 34))) break;
-        tc_fence_after_sync();
-        const uint32_t d_tmem = tmem_base + (uint32_t)buf * kAccStride;
-        for (int kb = 0; kb < k_blocks; ++kb) {
-          if (!(ok = mbar_wait(&bars->full[stage], phase, abort_flag, p.status, 35))) break;
-          tc_fence_after_sync();
-          const uint32_t sa = smem_u32(stages + (size_t)stage * S::kStageBytes);
-          const uint32_t sb = sa + kBytesA;
-          auto mma = [&](int j) {
-            const uint64_t da = smem_desc_sw128(sa + j * step_a, lbo_a, 1024);
-            const uint64_t db = smem_desc_sw128(sb + j * step_b, lbo_b, 1024);
-            if constexpr (kPair) mma_bf16_ss_pair(d_tmem, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
-            else mma_bf16_ss(d_tmem, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
-          };
-          if (kb + 1 < k_blocks || k_steps == kTileK / 16) {
-#pragma unroll
-            for (int j = 0; j < kTileK / 16; ++j) mma(j);
-          } else {
-            for (int j = 0; j < k_steps; ++j) mma(j);
+      int from = unit;
+      for (int q = 0; q < (kTwo ? 2 : 1); ++q) {
+        const TileParams& p = batch.p[q];
+        Walk w;
+        walk_of(q, &w);
+        const uint32_t idesc_tile = instr_desc_bf16(S::kTileM, kTileN, p.a_mn != 0, p.b_mn != 0);
+        const uint32_t idesc_half = instr_desc_bf16(S::kTileM, kTileN / 2, p.a_mn != 0, p.b_mn != 0);
+        // Across the contraction: 64-column groups one box apart, 16 contraction rows = 2048 bytes.
+        // Along it: 8-row groups 1024 bytes apart, 16 elements = 32 bytes along the row.
+        const uint32_t step_a = p.a_mn ? 2048u : 32u, step_b = p.b_mn ? 2048u : 32u;
+        const uint32_t lbo_a = p.a_mn ? kBoxBytes : 16u, lbo_b = p.b_mn ? kBoxBytes : 16u;
+        for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, from, units); at.valid() && ok; at.next()) {
+          // The place of the tile does not matter here; its width and, by expert, its depth do.
+          int k_blocks = p.k_blocks, k_steps = kTileK / 16;
+          if (p.mode == (int)TileMode::kContract) {
+            const Item it = at.item();
+            k_blocks = it.k_blocks;
+            k_steps = it.k_steps;
           }
-          if constexpr (kPair) mma_commit_pair(&bars->empty[stage], 3);
-          else mma_commit(&bars->empty[stage]);
-          if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+          const uint32_t idesc = at.is_half() ? idesc_half : idesc_tile;
+          if (!(ok = mbar_wait(&bars->acc_empty[buf], acc_phase ^ 1, abort_flag, p.status, 34))) break;
+          tc_fence_after_sync();
+          const uint32_t d_tmem = tmem_base + (uint32_t)buf * kAccStride;
+          for (int kb = 0; kb < k_blocks; ++kb) {
+            if (!(ok = mbar_wait(&bars->full[stage], phase, abort_flag, p.status, 35))) break;
+            tc_fence_after_sync();
+            const uint32_t sa = smem_u32(stages + (size_t)stage * S::kStageBytes);
+            const uint32_t sb = sa + kBytesA;
+            auto mma = [&](int j) {
+              const uint64_t da = smem_desc_sw128(sa + j * step_a, lbo_a, 1024);
+              const uint64_t db = smem_desc_sw128(sb + j * step_b, lbo_b, 1024);
+              if constexpr (kPair) mma_bf16_ss_pair(d_tmem, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
+              else mma_bf16_ss(d_tmem, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
+            };
+            if (kb + 1 < k_blocks || k_steps == kTileK / 16) {
+#pragma unroll
+              for (int j = 0; j < kTileK / 16; ++j) mma(j);
+            } else {
+              for (int j = 0; j < k_steps; ++j) mma(j);
+            }
+            if constexpr (kPair) mma_commit_pair(&bars->empty[stage], 3);
+            else mma_commit(&bars->empty[stage]);
+            if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+          }
+          if (!ok) break;
+          if constexpr (kPair) mma_commit_pair(&bars->acc_full[buf], 3);
+          else mma_commit(&bars->acc_full[buf]);
+          if (++buf == 2) { buf = 0; acc_phase ^= 1; }
         }
-        if (!ok) break;
-        if constexpr (kPair) mma_commit_pair(&bars->acc_full[buf], 3);
-        else mma_commit(&bars->acc_full[buf]);
-        if (++buf == 2) { buf = 0; acc_phase ^= 1; }
+        from = next_unit(from, w);
       }
     }
   } else {
@@ -767,44 +795,56 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     int buf = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
-    Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units);
-    Item ahead{};
-    if (at.valid()) ahead = at.item();
-    bool more = at.valid();
-    while (more && ok) {
-      // The next item is decoded before this one's steps: its loads (an expert's rows) return under them.
-      const Item it = ahead;
-      at.next();
+    int from = unit;
+    for (int q = 0; q < (kTwo ? 2 : 1); ++q) {
+      const TileParams& p = batch.p[q];
+      const CUtensorMap& map_y = batch.y[q];
+      const CUtensorMap& map_z = batch.z;
+      Walk w;
+      walk_of(q, &w);
+      Cursor<kPair, kTileN> at(p, w, bars->pairs_before, from, units);
+      Item ahead{};
       if (at.valid()) ahead = at.item();
-      more = at.valid();
-      EpilogueItem e;
-      e.row0 = it.row0 + (int)rank * kRowsPerCta + quarter * 32;
-      e.row_end = it.row_end;
-      e.col0 = kGated ? (it.nt * kTileN + it.n_off) / 2 : it.nt * kTileN + it.n_off;
-      e.width = kGated ? it.cols / 2 : it.cols;
-      e.taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)buf * kAccStride;
-      e.bias = p.bias ? p.bias + (int64_t)it.group * p.z_pitch : nullptr;
-      e.live_end = it.live_end;
-      e.empty_sum = it.k_blocks == 0;
-      e.group = p.mode == (int)TileMode::kContract ? it.group : 0;
-      auto wait_sums = [&] {
-        bool done = mbar_wait(&bars->acc_full[buf], acc_phase, abort_flag, p.status, 36);
-        done = __all_sync(kFullMask, done);
-        tc_fence_after_sync();
-        return done;
-      };
-      auto release_sums = [&] {
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) {
-          if constexpr (kPair) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&bars->acc_empty[buf]), 0));
-          else mbar_arrive(&bars->acc_empty[buf]);
-        }
-      };
-      if (p.copy) ok = epilogue_copy(p, e, map_y, mine, part, lane, wait_sums, release_sums);
-      else if (p.tma) ok = epilogue_tma<kGated>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums);
-      else ok = epilogue_plain<kGated>(p, e, smem_u32(mine), part, lane, wait_sums, release_sums);
-      if (++buf == 2) { buf = 0; acc_phase ^= 1; }
+      bool more = at.valid();
+      while (more && ok) {
+        // The next item is decoded before this one's steps: its loads (an expert's rows) return under them.
+        const Item it = ahead;
+        at.next();
+        if (at.valid()) ahead = at.item();
+        more = at.valid();
+        EpilogueItem e;
+        e.row0 = it.row0 + (int)rank * kRowsPerCta + quarter * 32;
+        e.row_end = it.row_end;
+        e.col0 = kGated ? (it.nt * kTileN + it.n_off) / 2 : it.nt * kTileN + it.n_off;
+        e.width = kGated ? it.cols / 2 : it.cols;
+        e.taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)buf * kAccStride;
+        e.bias = p.bias ? p.bias + (int64_t)it.group * p.z_pitch : nullptr;
+        e.live_end = it.live_end;
+        e.empty_sum = it.k_blocks == 0;
+        e.group = p.mode == (int)TileMode::kContract ? it.group : 0;
+        auto wait_sums = [&] {
+          bool done = mbar_wait(&bars->acc_full[buf], acc_phase, abort_flag, p.status, 36);
+          done = __all_sync(kFullMask, done);
+          tc_fence_after_sync();
+          return done;
+        };
+        auto release_sums = [&] {
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (kPair) mbar_arrive_cluster_relaxed(map_to_cta(smem_u32(&bars->acc_empty[buf]), 0));
+            else mbar_arrive(&bars->acc_empty[buf]);
+          }
+        };
+        if (p.copy) ok = epilogue_copy(p, e, map_y, mine, part, lane, wait_sums, release_sums);
+        else if (p.tma) ok = epilogue_tma<kGated>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums);
+        else ok = epilogue_plain<kGated>(p, e, smem_u32(mine), part, lane, wait_sums, release_sums);
+        if (++buf == 2) { buf = 0; acc_phase ^= 1; }
+      }
+      // A product's blocks are laid out as its outputs need them: none is pending when the next begins.
+      if (lane == 0) bulk_wait_group_read<0>();
+      __syncwarp();
+      from = next_unit(from, w);
     }
     // Shared memory must outlive the engine's reads, and the stores must have been performed before the
     // kernel counts as complete.
@@ -822,23 +862,27 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   }
 }
 
-struct Maps {
-  CUtensorMap a{}, b{}, y{}, z{};
-};
-
-template <bool kPair, int kTileN, bool kGated>
-cudaError_t launch_tile(const DeviceInfo& dev, const Maps& maps, const TileParams& p, int64_t max_items,
-                        cudaStream_t stream) {
+template <bool kPair, int kTileN, bool kGated, bool kTwo>
+cudaError_t launch_form(const DeviceInfo& dev, const TileBatch& batch, int64_t max_items, cudaStream_t stream) {
   using S = Shape<kPair, kTileN>;
   static PerDeviceOnce once;
   const cudaError_t e = once.run_current([] {
-    return cudaFuncSetAttribute(linear_tile_kernel<kPair, kTileN, kGated>,
+    return cudaFuncSetAttribute(linear_tile_kernel<kPair, kTileN, kGated, kTwo>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmemBytes);
   });
   if (e != cudaSuccess) return e;
   const int64_t units = std::min<int64_t>(max_items, kPair ? gemm_pair_units(dev.sms) : dev.sms);
-  return launch_pdl(linear_tile_kernel<kPair, kTileN, kGated>, dim3((unsigned)(units * S::kCtas)), dim3(kThreads),
-                    S::kSmemBytes, stream, S::kCtas, maps.a, maps.b, maps.y, maps.z, p);
+  return launch_pdl(linear_tile_kernel<kPair, kTileN, kGated, kTwo>, dim3((unsigned)(units * S::kCtas)), dim3(kThreads),
+                    S::kSmemBytes, stream, S::kCtas, batch);
+}
+template <bool kPair, int kTileN>
+cudaError_t launch_tile(const DeviceInfo& dev, const TileBatch& batch, bool gated, bool two, int64_t max_items,
+                        cudaStream_t stream) {
+  if (two) return gated ? cudaErrorInvalidValue : launch_form<kPair, kTileN, false, true>(dev, batch, max_items, stream);
+  if constexpr (kTileN > 64) {
+    if (gated) return launch_form<kPair, kTileN, true, false>(dev, batch, max_items, stream);
+  }
+  return launch_form<kPair, kTileN, false, false>(dev, batch, max_items, stream);
 }
 
 // A tile's column halves are whole 64-column boxes in every CTA (gated: of both halves of W).
@@ -846,105 +890,147 @@ bool can_halve(int pair, int tile_n, bool gated) { return tile_n / (pair || gate
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
+// What a tile costs, in microseconds at full clocks: a contraction block (the MMAs of a 256-column tile, or what the
+// roles' loops take for a narrower one) and the epilogue (which the next tile's main loop hides, if it is longer).
+struct TileForm {
+  int pair, tile_n;
+  double block, epilogue;
+};
+constexpr TileForm kForms[] = {{1, 256, 0.28, 2.2}, {0, 256, 0.31, 2.2}, {1, 128, 0.19, 1.1}, {0, 128, 0.18, 1.1}, {0, 64, 0.175, 0.7}};
+
+// Tiles of a product in a form, and the blocks of the contraction (experts: their numbers are the device's; half a
+// tile of padding per expert, and an even share of the rows, are the guess).
+int64_t tiles_of(const TileCall& c, const TileForm& f, double* blocks) {
+  const int64_t out_cols = c.epi.gated ? f.tile_n / 2 : f.tile_n, tile_m = kRowsPerCta << f.pair;
+  const int64_t pairs = c.experts.tokens * c.experts.topk;
+  const int64_t live = std::max<int64_t>(1, std::min(pairs, c.experts.experts));
+  int64_t m_tiles = (c.m + tile_m - 1) / tile_m, groups = 1;
+  *blocks = (double)((c.k + kTileK - 1) / kTileK);
+  if (c.mode == TileMode::kRows) m_tiles = std::max<int64_t>(1, (pairs + live * tile_m / 2) / tile_m);
+  if (c.mode == TileMode::kContract) {
+    groups = c.experts.experts;
+    *blocks = (double)pairs / live / kTileK + 0.5;
+  }
+  return groups * m_tiles * ((c.n + out_cols - 1) / out_cols);
+}
+
+bool form_allowed(const TileCall& c, const TileForm& f) {
+  if (f.pair && c.m <= kRowsPerCta) return false;
+  if (f.pair && c.mode == TileMode::kRows && c.experts.experts >= kPairTable) return false;
+  return f.tile_n > 64 || !c.epi.gated;
+}
+
+// The form with the least estimated time: whole waves of every product, then what is left of them -- side by side where
+// the units hold it, cut into column halves (about 0.6 of a wave) where a single product's leftover allows.
+TileForm choose_form(const DeviceInfo& dev, const TileCall* calls, int count) {
+  double best = 0;
+  int at = -1;
+  for (int i = 0; i < (int)(sizeof(kForms) / sizeof(kForms[0])); ++i) {
+    const TileForm& f = kForms[i];
+    const int64_t units = std::max(1, f.pair ? gemm_pair_units(dev.sms) : dev.sms);
+    double cost = 0, last = 0;
+    int64_t left = 0;
+    bool allowed = true;
+    for (int q = 0; q < count; ++q) {
+      allowed = allowed && form_allowed(calls[q], f);
+      double blocks = 0;
+      const int64_t items = tiles_of(calls[q], f, &blocks), tail = items % units;
+      const double each = std::max(blocks * f.block, f.epilogue) + 0.2;
+      cost += (double)(items / units) * each;
+      if (tail > 0) {
+        const bool cut = count == 1 && can_halve(f.pair, f.tile_n, calls[q].epi.gated) && items > units && 2 * tail <= units;
+        last = left + tail <= units ? std::max(last, cut ? 0.625 * each : each) : last + each;
+        left += tail;
+      }
+    }
+    cost += last;
+    if (allowed && (at < 0 || cost < best)) { best = cost; at = i; }
+  }
+  return kForms[at < 0 ? 3 : at];
+}
+
 }  // namespace
 
-cudaError_t tile_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t stream, uint64_t* launches) {
-  if (c.m <= 0 || c.n <= 0) return cudaSuccess;
-  const LinearEpilogue& ep = c.epi;
-  const int width = ep.gated ? 2 : 1;
-  TileParams p{};
-  p.m = c.m;
-  p.n = (int)c.n;
-  p.k_blocks = (int)((c.k + kTileK - 1) / kTileK);
-  p.b_up = (int)c.b_up;
-  p.mode = (uint8_t)c.mode;
-  p.a_mn = c.a_mn;
-  p.b_mn = c.b_mn;
-  p.zero_padding = c.zero_padding;
-  p.block_expert = c.experts.block_expert;
-  p.offsets = c.experts.offsets;
-  p.counts = c.experts.counts;
-  p.experts = (int)c.experts.experts;
-  p.act = (uint8_t)ep.act;
-  p.out_f32 = ep.out_f32;
-  p.accumulate = ep.accumulate;
-  p.vec = c.n % 8 == 0 && aligned16(ep.Y) && aligned16(ep.Z) && aligned16(ep.bias) && aligned16(ep.residual);
-  p.tma = p.vec;
-  p.copy = p.vec && !ep.gated && ep.act == kActNone && !ep.bias && !ep.residual && !ep.Z && !ep.out_f32;
-  p.z_pitch = (int)(c.n * width);
-  p.bias = ep.bias;
-  p.residual = ep.residual;
-  p.Y = ep.Y;
-  p.Z = ep.Z;
-  p.status = dev.status;
+cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count, cudaStream_t stream,
+                        uint64_t* launches) {
+  if (count < 1 || count > kMaxProducts) return cudaErrorInvalidValue;
+  for (int q = 0; q < count; ++q)
+    if (calls[q].m <= 0 || calls[q].n <= 0 || (q > 0 && calls[q].mode == TileMode::kRows)) return cudaErrorInvalidValue;
+  const bool gated = calls[0].epi.gated;
+  const TileForm form = choose_form(dev, calls, count);
+  TileBatch batch{};
+  int64_t items = 0;
+  for (int q = 0; q < count; ++q) {
+    const TileCall& c = calls[q];
+    const LinearEpilogue& ep = c.epi;
+    if (ep.gated != gated || (q > 0 && ep.Z)) return cudaErrorInvalidValue;
+    const int width = ep.gated ? 2 : 1;
+    const int64_t groups = c.mode == TileMode::kContract ? c.experts.experts : 1;
+    TileParams& p = batch.p[q];
+    p.m = c.m;
+    p.n = (int)c.n;
+    p.k_blocks = (int)((c.k + kTileK - 1) / kTileK);
+    p.b_up = (int)c.b_up;
+    p.mode = (uint8_t)c.mode;
+    p.a_mn = c.a_mn;
+    p.b_mn = c.b_mn;
+    p.zero_padding = c.zero_padding;
+    p.block_expert = c.experts.block_expert;
+    p.offsets = c.experts.offsets;
+    p.counts = c.experts.counts;
+    p.experts = (int)c.experts.experts;
+    p.act = (uint8_t)ep.act;
+    p.out_f32 = ep.out_f32;
+    p.accumulate = ep.accumulate;
+    p.vec = c.n % 8 == 0 && aligned16(ep.Y) && aligned16(ep.Z) && aligned16(ep.bias) && aligned16(ep.residual);
+    p.tma = p.vec;
+    p.copy = p.vec && !ep.gated && ep.act == kActNone && !ep.bias && !ep.residual && !ep.Z && !ep.out_f32;
+    p.z_pitch = (int)(c.n * width);
+    p.bias = ep.bias;
+    p.residual = ep.residual;
+    p.Y = ep.Y;
+    p.Z = ep.Z;
+    p.status = dev.status;
+    p.halves = can_halve(form.pair, form.tile_n, ep.gated);
+    const int64_t tile_m = kRowsPerCta << form.pair, out_cols = ep.gated ? form.tile_n / 2 : form.tile_n;
+    const int64_t m_tiles = (c.m + tile_m - 1) / tile_m, n_tiles = (c.n + out_cols - 1) / out_cols;
+    // Experts' pairs of blocks: up to one per block.
+    const int64_t most = c.mode == TileMode::kRows ? (c.m / kExpertBlock) * n_tiles : groups * m_tiles * n_tiles;
+    if (most >= (1ll << 30) || n_tiles >= (1 << 27)) return cudaErrorInvalidValue;   // items are ints
+    p.m_tiles = (int)m_tiles;
+    p.n_tiles = (int)n_tiles;
+    p.tiles = groups * m_tiles * n_tiles;
+    items += most;
 
-  // The tile: the least waves x columns, weighted by what the narrower and the one-CTA tiles cost per
-  // column.  A last wave that is cut into column halves costs about 0.6 of a whole one.
-  const int64_t groups = c.mode == TileMode::kContract ? c.experts.experts : 1;
-  const int64_t pairs = c.experts.tokens * c.experts.topk;
-  double best = 0;
-  int best_pair = -1, best_n = 0;
-  for (int pair = 0; pair < 2; ++pair) {
-    if (pair && c.m <= kRowsPerCta) continue;
-    if (pair && c.mode == TileMode::kRows && c.experts.experts >= kPairTable) continue;
-    const int64_t units = std::max(1, pair ? gemm_pair_units(dev.sms) : dev.sms);
-    for (int tn = 256; tn >= 64; tn >>= 1) {
-      if (tn == 64 && (pair || ep.gated)) continue;
-      const int64_t out_cols = ep.gated ? tn / 2 : tn;
-      const int64_t tile_m = kRowsPerCta << pair;
-      // Experts' rows: their number per expert is the device's; half a tile of padding each is the guess.
-      const int64_t m_tiles = c.mode == TileMode::kRows
-                                  ? std::max<int64_t>(1, (pairs + std::min(pairs, c.experts.experts) * tile_m / 2) / tile_m)
-                                  : (c.m + tile_m - 1) / tile_m;
-      const int64_t items = groups * m_tiles * ((c.n + out_cols - 1) / out_cols);
-      const int64_t tail = items % units;
-      const bool cut = can_halve(pair, tn, ep.gated) && items > units && tail > 0 && 2 * tail <= units;
-      const double waves = (double)(items / units) + (tail == 0 ? 0.0 : cut ? 0.625 : 1.0);
-      const double cost = waves * tn * (pair ? 1.0 : 1.15) * (tn == 256 ? 1.0 : tn == 128 ? 1.25 : 1.6);
-      if (best_n == 0 || cost < best) { best = cost; best_pair = pair; best_n = tn; }
+    cudaError_t e = cudaSuccess;
+    if (c.mode == TileMode::kContract || c.k > 0) {
+      e = make_tensor_map_3d(&batch.a[q], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.a.p, (uint64_t)c.a.cols,
+                             (uint64_t)c.a.rows, (uint64_t)c.a.groups, 64, c.a_mn ? 64u : (uint32_t)kRowsPerCta,
+                             CU_TENSOR_MAP_SWIZZLE_128B);
+      if (e == cudaSuccess)
+        e = make_tensor_map_3d(&batch.b[q], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.b.p, (uint64_t)c.b.cols,
+                               (uint64_t)c.b.rows, (uint64_t)c.b.groups, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+      if (e != cudaSuccess) return e;
+    }
+    if (p.tma) {
+      e = make_tensor_map_3d(&batch.y[q], ep.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                             ep.out_f32 ? 4 : 2, ep.Y, (uint64_t)c.n, (uint64_t)c.m, (uint64_t)groups, p.copy ? 64 : 32, 32,
+                             ep.out_f32 || p.copy ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+      // Z's halves are a dimension of their own: a block at the right edge of the first must not reach the second.
+      if (e == cudaSuccess && ep.Z)
+        e = make_tensor_map_3d_box(&batch.z, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ep.Z, (uint64_t)c.n, (uint64_t)width,
+                                   (uint64_t)c.m, 32, 1, 32, CU_TENSOR_MAP_SWIZZLE_64B);
+      if (e != cudaSuccess) return e;
     }
   }
-  p.halves = can_halve(best_pair, best_n, ep.gated);
-  const int64_t tile_m = kRowsPerCta << best_pair, out_cols = ep.gated ? best_n / 2 : best_n;
-  p.m_tiles = (int)((c.m + tile_m - 1) / tile_m);
-  p.n_tiles = (int)((c.n + out_cols - 1) / out_cols);
-  p.tiles = groups * p.m_tiles * (int64_t)p.n_tiles;
-  // Experts' pairs of blocks: up to one per block.
-  const int64_t most = c.mode == TileMode::kRows ? (c.m / kExpertBlock) * (int64_t)p.n_tiles : p.tiles;
-  if (p.tiles >= (1ll << 30) || p.n_tiles >= (1 << 27)) return cudaErrorInvalidValue;   // items are ints
-
-  Maps maps;
-  cudaError_t e = cudaSuccess;
-  if (c.mode == TileMode::kContract || c.k > 0) {
-    e = make_tensor_map_3d(&maps.a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.a.p, (uint64_t)c.a.cols, (uint64_t)c.a.rows,
-                           (uint64_t)c.a.groups, 64, c.a_mn ? 64u : (uint32_t)kRowsPerCta, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (e == cudaSuccess)
-      e = make_tensor_map_3d(&maps.b, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.b.p, (uint64_t)c.b.cols, (uint64_t)c.b.rows,
-                             (uint64_t)c.b.groups, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (e != cudaSuccess) return e;
-  }
-  if (p.tma) {
-    const uint64_t out_groups = (uint64_t)groups;
-    e = make_tensor_map_3d(&maps.y, ep.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                           ep.out_f32 ? 4 : 2, ep.Y, (uint64_t)c.n, (uint64_t)c.m, out_groups, p.copy ? 64 : 32, 32,
-                           ep.out_f32 || p.copy ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
-    // Z's halves are a dimension of their own: a block at the right edge of the first must not reach the second.
-    if (e == cudaSuccess && ep.Z)
-      e = make_tensor_map_3d_box(&maps.z, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ep.Z, (uint64_t)c.n, (uint64_t)width,
-                                 (uint64_t)c.m, 32, 1, 32, CU_TENSOR_MAP_SWIZZLE_64B);
-    if (e != cudaSuccess) return e;
-  }
-  const int code = best_pair * 10000 + best_n * 10 + (ep.gated ? 1 : 0);
-  switch (code) {
-    case 640: e = launch_tile<false, 64, false>(dev, maps, p, most, stream); break;
-    case 1280: e = launch_tile<false, 128, false>(dev, maps, p, most, stream); break;
-    case 2560: e = launch_tile<false, 256, false>(dev, maps, p, most, stream); break;
-    case 1281: e = launch_tile<false, 128, true>(dev, maps, p, most, stream); break;
-    case 2561: e = launch_tile<false, 256, true>(dev, maps, p, most, stream); break;
-    case 11280: e = launch_tile<true, 128, false>(dev, maps, p, most, stream); break;
-    case 12560: e = launch_tile<true, 256, false>(dev, maps, p, most, stream); break;
-    case 11281: e = launch_tile<true, 128, true>(dev, maps, p, most, stream); break;
-    case 12561: e = launch_tile<true, 256, true>(dev, maps, p, most, stream); break;
+  cudaError_t e;
+  const bool two = count == 2;
+  switch (form.pair * 1000 + form.tile_n) {
+    case 64: e = launch_tile<false, 64>(dev, batch, gated, two, items, stream); break;
+    case 128: e = launch_tile<false, 128>(dev, batch, gated, two, items, stream); break;
+    case 256: e = launch_tile<false, 256>(dev, batch, gated, two, items, stream); break;
+    case 1128: e = launch_tile<true, 128>(dev, batch, gated, two, items, stream); break;
+    case 1256: e = launch_tile<true, 256>(dev, batch, gated, two, items, stream); break;
     default: return cudaErrorInvalidValue;
   }
   if (e == cudaSuccess) ++*launches;
