@@ -896,7 +896,7 @@ struct TileForm {
   int pair, tile_n;
   double block, epilogue;
 };
-constexpr TileForm kForms[] = {{1, 256, 0.28, 2.2}, {0, 256, 0.31, 2.2}, {1, 128, 0.19, 1.1}, {0, 128, 0.18, 1.1}, {0, 64, 0.175, 0.7}};
+constexpr TileForm kForms[] = {{1, 256, 0.28, 2.2}, {0, 256, 0.33, 2.2}, {1, 128, 0.19, 1.1}, {0, 128, 0.18, 1.1}, {0, 64, 0.175, 0.7}};
 
 // Tiles of a product in a form, and the blocks of the contraction (experts: their numbers are the device's; half a
 // tile of padding per expert, and an even share of the rows, are the guess).
