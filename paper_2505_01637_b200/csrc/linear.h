@@ -83,6 +83,7 @@ struct CopyJob {
   int64_t groups = 1, rows_in = 0, cols_in = 0, rows_out = 0, cols_out = 0;
   const ExpertRows* experts = nullptr;  // rows past the live ones are left alone
   bool gather = false;                  // with experts: row r of dst is token row_src[r] / topk of src
+  const ExpertRows* by_expert = nullptr;  // groups are experts: those without rows are left alone
 };
 constexpr int kMaxCopies = 2;
 cudaError_t copy_launch(const CopyJob* jobs, int count, cudaStream_t stream, uint64_t* launches);   // one launch

@@ -149,6 +149,7 @@ void stage_w(const Layer& l, const void* W, bool halves_apart, Carver& ws, bool 
   j.src = src;
   j.dst = dst;
   j.groups = l.groups;
+  if (l.grouped) j.by_expert = &l.x;
   j.rows_in = rows;
   j.rows_out = rows;
   j.cols_in = cols_in;

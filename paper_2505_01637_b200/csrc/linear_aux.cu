@@ -20,8 +20,26 @@ constexpr int kSlopeLanes = 8;      // rows a block takes at a time
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-__device__ __forceinline__ uint4 load8_raw(const uint16_t* src, bool vec, int64_t cols) {
-  if (vec) return *reinterpret_cast<const uint4*>(src);
+// Elements per access that rows of `cols` elements from p on allow: 8, 4, 2 or 1.
+int access_width(int64_t cols, const void* p) {
+  for (int w = 8; w > 1; w /= 2)
+    if (cols % w == 0 && reinterpret_cast<uintptr_t>(p) % (2 * w) == 0) return w;
+  return 1;
+}
+
+// Eight elements from src on, of which `cols` exist, in accesses of `width` elements.
+__device__ __forceinline__ uint4 load8_raw(const uint16_t* src, int width, int64_t cols) {
+  if (cols >= 8) {
+    if (width == 8) return *reinterpret_cast<const uint4*>(src);
+    if (width == 4) {
+      const uint2 a = reinterpret_cast<const uint2*>(src)[0], b = reinterpret_cast<const uint2*>(src)[1];
+      return make_uint4(a.x, a.y, b.x, b.y);
+    }
+    if (width == 2) {
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(src);
+      return make_uint4(q[0], q[1], q[2], q[3]);
+    }
+  }
   uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -29,6 +47,22 @@ __device__ __forceinline__ uint4 load8_raw(const uint16_t* src, bool vec, int64_
     w[e >> 1] |= v << ((e & 1) * 16);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store8_raw(uint16_t* dst, int width, int64_t cols, const uint4& w) {
+  if (cols >= 8 && width == 8) {
+    *reinterpret_cast<uint4*>(dst) = w;
+  } else if (cols >= 8 && width == 4) {
+    reinterpret_cast<uint2*>(dst)[0] = make_uint2(w.x, w.y);
+    reinterpret_cast<uint2*>(dst)[1] = make_uint2(w.z, w.w);
+  } else if (cols >= 8 && width == 2) {
+    uint32_t* q = reinterpret_cast<uint32_t*>(dst);
+    q[0] = w.x; q[1] = w.y; q[2] = w.z; q[3] = w.w;
+  } else {
+    const uint32_t q[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < cols) dst[e] = (uint16_t)(q[e >> 1] >> ((e & 1) * 16));
+  }
 }
 __device__ __forceinline__ void unpack8(const uint4& w, float (&v)[8]) {
   v[0] = bf16_low(w.x); v[1] = bf16_high(w.x); v[2] = bf16_low(w.y); v[3] = bf16_high(w.y);
@@ -45,11 +79,13 @@ struct CopyParams {
   uint4* dst;
   int64_t rows_in, cols_in, rows_out;
   int octets;                 // 8-column groups of a row of dst
-  int spans;                  // of kThreads octets
-  bool vec;
+  int width;                  // elements per access of src
+  int row_groups;             // of kCopyRows rows in a group of dst
+  int64_t threads;            // groups * row_groups * octets
   int topk;
   const int32_t* row_src;     // gather
   const int32_t* live;        // number of live rows, or null
+  const int32_t* counts;      // by group of dst: a group without rows is left alone, or null
 };
 
 struct CopyBatch {
@@ -57,19 +93,19 @@ struct CopyBatch {
   int blocks0;                // blocks of the first job
 };
 
-// Grid: a job's row groups (all groups of dst one after another), each in spans of kThreads octets.
 __global__ void __launch_bounds__(kThreads) copy_kernel(const CopyBatch batch) {
   const bool second = (int)blockIdx.x >= batch.blocks0;
   const CopyParams& p = batch.job[second ? 1 : 0];
-  const int block = (int)blockIdx.x - (second ? batch.blocks0 : 0);
-  const int o = block % p.spans * kThreads + threadIdx.x;
-  const int64_t row_group = block / p.spans;
-  const int64_t groups_of_rows = (p.rows_out + kCopyRows - 1) / kCopyRows;
-  const int64_t g = row_group / groups_of_rows;
-  const int64_t r0 = (row_group - g * groups_of_rows) * kCopyRows;
+  const int64_t idx = (int64_t)((int)blockIdx.x - (second ? batch.blocks0 : 0)) * kThreads + threadIdx.x;
+  // 32-bit divisions where they do (64-bit ones are a hundred instructions each).
+  const bool small = p.threads < (1ll << 31);
+  const int64_t row_group = small ? (int64_t)((uint32_t)idx / (uint32_t)p.octets) : idx / p.octets;
+  const int o = (int)(idx - row_group * p.octets);
+  const int64_t g = small ? (int64_t)((uint32_t)row_group / (uint32_t)p.row_groups) : row_group / p.row_groups;
+  const int64_t r0 = (row_group - g * p.row_groups) * kCopyRows;
   pdl_wait();
   pdl_release();
-  if (o >= p.octets || (p.live && r0 >= *p.live)) return;
+  if (idx >= p.threads || (p.live && r0 >= *p.live) || (p.counts && p.counts[g] == 0)) return;
   const int64_t left = p.cols_in - (int64_t)o * 8;
   uint4 w[kCopyRows];
 #pragma unroll
@@ -82,7 +118,7 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(const CopyBatch batch) {
     }
     w[i] = make_uint4(0u, 0u, 0u, 0u);
     if (r < p.rows_out && from >= 0 && from < p.rows_in && left > 0)
-      w[i] = load8_raw(p.src + (g * p.rows_in + from) * p.cols_in + (int64_t)o * 8, p.vec && left >= 8, left);
+      w[i] = load8_raw(p.src + (g * p.rows_in + from) * p.cols_in + (int64_t)o * 8, p.width, left);
   }
 #pragma unroll
   for (int i = 0; i < kCopyRows; ++i)
@@ -95,14 +131,15 @@ struct SlopeParams {
   uint16_t* dZ;
   float* partial;
   int64_t rows, n, pitch;      // pitch: columns of a row of dZ, the width rounded up to 8
-  bool vec;
+  int width_y, width_z, width_up;   // elements per access of dY, of Z, and of dZ's second half
   const int32_t* row_src;
   const int32_t* live;
 };
 
 // A block: 256 columns (32 groups of 8) x kSlopeRows rows, eight rows at a time.
-template <int kAct, bool kGated, bool kSums>
-__global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeParams p) {
+// kOctets: every row is in 16-byte accesses (a test per access kept the loads from going out together).
+template <int kAct, bool kGated, bool kSums, bool kOctets>
+__global__ void __launch_bounds__(kThreads, kSums ? 3 : 4) slope_kernel(const SlopeParams p) {
   __shared__ float sums[kSums ? kSlopeLanes : 1][kGated ? 2 : 1][256 + 8];
   const int group = threadIdx.x & 31, lane = threadIdx.x >> 5;
   const int64_t col = (int64_t)blockIdx.y * 256 + group * 8;
@@ -112,8 +149,6 @@ __global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeParams p)
   if (p.live && row_begin >= *p.live) return;
   const int64_t row_end = min(p.rows, row_begin + kSlopeRows);
   const int64_t left = p.n - col;
-  const bool vec = p.vec && left >= 8;
-  const bool vec_out = (p.n & 7) == 0;
   float s0[8], s1[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) s0[e] = s1[e] = 0.f;
@@ -132,9 +167,9 @@ __global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeParams p)
         wd[i] = w0[i] = make_uint4(0u, 0u, 0u, 0u);
         if constexpr (kGated) w1[i] = make_uint4(0u, 0u, 0u, 0u);
         if (row >= row_end) continue;
-        wd[i] = load8_raw(p.dY + row * p.n + col, vec, left);
-        if (wants_z) w0[i] = load8_raw(p.Z + row * width + col, vec, left);
-        if constexpr (kGated) w1[i] = load8_raw(p.Z + row * width + p.n + col, vec, left);
+        wd[i] = load8_raw(p.dY + row * p.n + col, kOctets ? 8 : p.width_y, kOctets ? 8 : left);
+        if (wants_z) w0[i] = load8_raw(p.Z + row * width + col, kOctets ? 8 : p.width_z, kOctets ? 8 : left);
+        if constexpr (kGated) w1[i] = load8_raw(p.Z + row * width + p.n + col, kOctets ? 8 : p.width_z, kOctets ? 8 : left);
       }
 #pragma unroll
       for (int i = 0; i < kSlopeUnroll; ++i) {
@@ -159,19 +194,10 @@ __global__ void __launch_bounds__(kThreads, 4) slope_kernel(const SlopeParams p)
         }
         if (p.dZ) {
           uint16_t* dst = p.dZ + row * p.pitch + col;
-          if (vec_out) {
-            *reinterpret_cast<uint4*>(dst) = pack8(d0);
-            if constexpr (kGated) *reinterpret_cast<uint4*>(dst + p.n) = pack8(d1);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              if (e >= left) continue;
-              dst[e] = bf16_round(d0[e]);
-              if constexpr (kGated) dst[p.n + e] = bf16_round(d1[e]);
-            }
-            if (left <= 8)       // the columns that round the row up to eight
-              for (int64_t c = width; c < p.pitch; ++c) p.dZ[row * p.pitch + c] = 0;
-          }
+          store8_raw(dst, 8, kOctets ? 8 : left, pack8(d0));        // rows of dZ are multiples of eight
+          if constexpr (kGated) store8_raw(dst + p.n, kOctets ? 8 : p.width_up, kOctets ? 8 : left, pack8(d1));
+          if (!kOctets && left <= 8)       // the columns that round the row up to eight
+            for (int64_t c = width; c < p.pitch; ++c) p.dZ[row * p.pitch + c] = 0;
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -239,7 +265,9 @@ struct CombineParams {
   int64_t n, y_pitch;
   int topk;
   int64_t octets, threads;
-  bool vec_y, vec;
+  int width;                  // elements per access of residual and out
+  bool vec_y;                 // f32 Y in 16-byte accesses
+  int width_y;                // elements per access of bf16 Y
 };
 
 template <bool kF32>
@@ -248,9 +276,10 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineParams p
   pdl_wait();
   pdl_release();
   if (idx >= p.threads) return;
-  const int64_t o = idx % p.octets, t = idx / p.octets;
+  const int64_t t = p.threads < (1ll << 31) ? (int64_t)((uint32_t)idx / (uint32_t)p.octets) : idx / p.octets;
+  const int64_t o = idx - t * p.octets;
   const int64_t col = o * 8, left = p.n - col;
-  const bool vec_y = p.vec_y && left >= 8, vec = p.vec && left >= 8;
+  const bool vec_y = p.vec_y && left >= 8;
   float sum[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) sum[e] = 0.f;
@@ -270,25 +299,18 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineParams p
         for (int e = 0; e < 8; ++e) v[e] = e < left ? y[e] : 0.f;
       }
     } else {
-      unpack8(load8_raw(static_cast<const uint16_t*>(p.Y) + (int64_t)row * p.y_pitch + col, vec_y, left), v);
+      unpack8(load8_raw(static_cast<const uint16_t*>(p.Y) + (int64_t)row * p.y_pitch + col, p.width_y, left), v);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = fmaf(w, v[e], sum[e]);
   }
   if (p.residual) {
     float r[8];
-    unpack8(load8_raw(p.residual + t * p.n + col, vec, left), r);
+    unpack8(load8_raw(p.residual + t * p.n + col, p.width, left), r);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += r[e];
   }
-  uint16_t* dst = p.out + t * p.n + col;
-  if (vec) {
-    *reinterpret_cast<uint4*>(dst) = pack8(sum);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < left) dst[e] = bf16_round(sum[e]);
-  }
+  store8_raw(p.out + t * p.n + col, p.width, left, pack8(sum));
 }
 
 cudaError_t grid_for(int64_t threads, unsigned* blocks) {
@@ -314,8 +336,10 @@ cudaError_t copy_launch(const CopyJob* jobs, int count, cudaStream_t stream, uin
     p.cols_in = j.cols_in;
     p.rows_out = j.rows_out;
     p.octets = (int)(j.cols_out / 8);
-    p.spans = (p.octets + kThreads - 1) / kThreads;
-    p.vec = j.cols_in % 8 == 0 && aligned16(j.src);
+    p.width = access_width(j.cols_in, j.src);
+    p.row_groups = (int)((j.rows_out + kCopyRows - 1) / kCopyRows);
+    p.threads = j.groups * p.row_groups * (int64_t)p.octets;
+    if (j.by_expert) p.counts = j.by_expert->counts;
     if (j.experts) {
       p.live = j.experts->offsets + j.experts->experts;
       if (j.gather) {
@@ -323,7 +347,7 @@ cudaError_t copy_launch(const CopyJob* jobs, int count, cudaStream_t stream, uin
         p.topk = (int)j.experts->topk;
       }
     }
-    const int64_t mine = j.groups * ((j.rows_out + kCopyRows - 1) / kCopyRows) * p.spans;
+    const int64_t mine = (p.threads + kThreads - 1) / kThreads;
     if (mine <= 0) continue;
     if (at == 0) batch.blocks0 = (int)std::min<int64_t>(mine, (1ll << 31) - 1);
     batch.job[at++] = p;
@@ -355,7 +379,9 @@ cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& c, cudaStream_t
     p.rows = c.rows;
     p.n = c.n;
     p.pitch = (width + 7) / 8 * 8;
-    p.vec = c.n % 8 == 0 && aligned16(c.dY) && aligned16(c.Z);
+    p.width_y = access_width(c.n, c.dY);
+    p.width_z = access_width(c.n, c.Z);
+    p.width_up = access_width(c.n, nullptr);
     if (c.experts) {
       p.row_src = c.experts->row_src;
       p.live = c.experts->offsets + c.experts->experts;
@@ -364,18 +390,31 @@ cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& c, cudaStream_t
     if (parts >= (1ll << 31) || strips > 65535) return cudaErrorInvalidValue;
     const dim3 grid((unsigned)parts, (unsigned)strips);
     const bool with = p.partial != nullptr;
-    auto go = [&](auto sums, auto none) { return launch_pdl(with ? sums : none, grid, dim3(kThreads), 0, stream, 1, p); };
+    const bool octets = p.width_y == 8 && p.width_z == 8;
+    auto go = [&](auto sums, auto none, auto sums_any, auto none_any) {
+      return launch_pdl(octets ? (with ? sums : none) : (with ? sums_any : none_any), grid, dim3(kThreads), 0, stream, 1, p);
+    };
     switch (c.act * 2 + (c.gated ? 1 : 0)) {
-      case 0: e = go(slope_kernel<kActNone, false, true>, slope_kernel<kActNone, false, false>); break;
-      case 1: e = go(slope_kernel<kActNone, true, true>, slope_kernel<kActNone, true, false>); break;
-      case 2: e = go(slope_kernel<kActRelu, false, true>, slope_kernel<kActRelu, false, false>); break;
-      case 3: e = go(slope_kernel<kActRelu, true, true>, slope_kernel<kActRelu, true, false>); break;
-      case 4: e = go(slope_kernel<kActGelu, false, true>, slope_kernel<kActGelu, false, false>); break;
-      case 5: e = go(slope_kernel<kActGelu, true, true>, slope_kernel<kActGelu, true, false>); break;
-      case 6: e = go(slope_kernel<kActGeluTanh, false, true>, slope_kernel<kActGeluTanh, false, false>); break;
-      case 7: e = go(slope_kernel<kActGeluTanh, true, true>, slope_kernel<kActGeluTanh, true, false>); break;
-      case 8: e = go(slope_kernel<kActSilu, false, true>, slope_kernel<kActSilu, false, false>); break;
-      default: e = go(slope_kernel<kActSilu, true, true>, slope_kernel<kActSilu, true, false>); break;
+      case 0: e = go(slope_kernel<kActNone, false, true, true>, slope_kernel<kActNone, false, false, true>, slope_kernel<kActNone, false, true, false>,
+                         slope_kernel<kActNone, false, false, false>); break;
+      case 1: e = go(slope_kernel<kActNone, true, true, true>, slope_kernel<kActNone, true, false, true>, slope_kernel<kActNone, true, true, false>,
+                         slope_kernel<kActNone, true, false, false>); break;
+      case 2: e = go(slope_kernel<kActRelu, false, true, true>, slope_kernel<kActRelu, false, false, true>, slope_kernel<kActRelu, false, true, false>,
+                         slope_kernel<kActRelu, false, false, false>); break;
+      case 3: e = go(slope_kernel<kActRelu, true, true, true>, slope_kernel<kActRelu, true, false, true>, slope_kernel<kActRelu, true, true, false>,
+                         slope_kernel<kActRelu, true, false, false>); break;
+      case 4: e = go(slope_kernel<kActGelu, false, true, true>, slope_kernel<kActGelu, false, false, true>, slope_kernel<kActGelu, false, true, false>,
+                         slope_kernel<kActGelu, false, false, false>); break;
+      case 5: e = go(slope_kernel<kActGelu, true, true, true>, slope_kernel<kActGelu, true, false, true>, slope_kernel<kActGelu, true, true, false>,
+                         slope_kernel<kActGelu, true, false, false>); break;
+      case 6: e = go(slope_kernel<kActGeluTanh, false, true, true>, slope_kernel<kActGeluTanh, false, false, true>, slope_kernel<kActGeluTanh, false, true, false>,
+                         slope_kernel<kActGeluTanh, false, false, false>); break;
+      case 7: e = go(slope_kernel<kActGeluTanh, true, true, true>, slope_kernel<kActGeluTanh, true, false, true>, slope_kernel<kActGeluTanh, true, true, false>,
+                         slope_kernel<kActGeluTanh, true, false, false>); break;
+      case 8: e = go(slope_kernel<kActSilu, false, true, true>, slope_kernel<kActSilu, false, false, true>, slope_kernel<kActSilu, false, true, false>,
+                         slope_kernel<kActSilu, false, false, false>); break;
+      default: e = go(slope_kernel<kActSilu, true, true, true>, slope_kernel<kActSilu, true, false, true>, slope_kernel<kActSilu, true, true, false>,
+                         slope_kernel<kActSilu, true, false, false>); break;
     }
     if (e != cudaSuccess) return e;
     ++*launches;
@@ -404,8 +443,9 @@ cudaError_t combine_launch(const ExpertRows& x, bool y_f32, int64_t n, int64_t y
   p.topk = (int)x.topk;
   p.octets = (n + 7) / 8;
   p.threads = x.tokens * p.octets;
-  p.vec = n % 8 == 0 && aligned16(out) && aligned16(residual);
+  p.width = std::min(access_width(n, out), access_width(n, residual));
   p.vec_y = y_pitch % 8 == 0 && aligned16(Y);
+  p.width_y = access_width(y_pitch, Y);
   if (p.threads <= 0) return cudaSuccess;
   unsigned blocks = 0;
   cudaError_t e = grid_for(p.threads, &blocks);

@@ -19,9 +19,8 @@
 // Epilogue: eight warps, two per quarter of the rows, which take its 32-column steps in turn; a thread
 // holds one row of 32 columns.  Where the TMA engine can address Y and Z they leave through shared memory
 // in blocks of 32 rows x 32 columns (64- or 128-byte swizzle), two of which a warp uses in turn; the residual is
-// read straight into registers while the accumulator is awaited.  Anything else (n % 8 != 0, odd addresses): a
-// warp parks 32 rows x 32 accumulator columns (f32) and reads them back with four (gated: two) lanes to a row, so
-// that any n and alignment is a matter of predicates.
+// read straight into registers while the accumulator is awaited.  Anything else (n % 8 != 0, odd addresses) goes
+// through the same blocks, which the warp then copies out (and the residual's in) a row at a time.
 // A step is a chain of tensor-memory load, conversion, shared store, proxy fence and TMA store, about 1,100
 // cycles; eight warps keep it under a main loop of 8 contraction blocks or more.  Twelve and sixteen warps were
 // measured slower (their share of the registers spills: 4096 x 4096 x 4096 with GELU, bias, residual and Z
@@ -81,7 +80,7 @@ struct TileParams {
   const int32_t* counts;
   int experts;
   // epilogue
-  uint8_t act, out_f32, accumulate, vec, tma, copy;   // copy: bf16 Y is the sums, nothing else
+  uint8_t act, out_f32, accumulate, tma, copy;   // copy: bf16 Y is the sums, nothing else
   int z_pitch;           // columns of a row of Z and of the bias: n or 2 n
   const uint16_t* bias;
   const uint16_t* residual;
@@ -201,55 +200,6 @@ class Cursor {
   int t_, at_ = 0, grp_ = 0, expert_ = 0;
 };
 
-// Eight columns of one row, on their way out.
-template <int kAct>
-__device__ __forceinline__ void act8(float (&v)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = act_value<kAct>(v[e]);
-}
-__device__ __forceinline__ void act8_by(int act, float (&v)[8]) {
-  if (act == kActNone) return;
-  if (act == kActRelu) act8<kActRelu>(v);
-  else if (act == kActGelu) act8<kActGelu>(v);
-  else if (act == kActGeluTanh) act8<kActGeluTanh>(v);
-  else act8<kActSilu>(v);
-}
-__device__ __forceinline__ void load8(const uint16_t* src, bool vec, int cols, float (&v)[8]) {
-  if (vec) {
-    const uint4 w = *reinterpret_cast<const uint4*>(src);
-    v[0] = bf16_low(w.x); v[1] = bf16_high(w.x); v[2] = bf16_low(w.y); v[3] = bf16_high(w.y);
-    v[4] = bf16_low(w.z); v[5] = bf16_high(w.z); v[6] = bf16_low(w.w); v[7] = bf16_high(w.w);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < cols ? bf16_value(src[e]) : 0.f;
-  }
-}
-__device__ __forceinline__ void store8(uint16_t* dst, bool vec, int cols, const float (&v)[8]) {
-  if (vec) {
-    *reinterpret_cast<uint4*>(dst) = make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]),
-                                                bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7]));
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < cols) dst[e] = bf16_round(v[e]);
-  }
-}
-__device__ __forceinline__ void store8_f32(float* dst, bool vec, int cols, bool accumulate, float (&v)[8]) {
-  if (vec) {
-    float4* q = reinterpret_cast<float4*>(dst);
-    if (accumulate) {
-      const float4 a = q[0], b = q[1];
-      v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-      v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
-    }
-    q[0] = make_float4(v[0], v[1], v[2], v[3]);
-    q[1] = make_float4(v[4], v[5], v[6], v[7]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < cols) dst[e] = accumulate ? dst[e] + v[e] : v[e];
-  }
-}
 constexpr uint32_t kFullMask = 0xffffffffu;
 
 struct EpilogueItem {
@@ -304,10 +254,62 @@ __device__ __forceinline__ void add_octet(const uint4& w, float* v) {
   v[0] += bf16_low(w.x); v[1] += bf16_high(w.x); v[2] += bf16_low(w.y); v[3] += bf16_high(w.y);
   v[4] += bf16_low(w.z); v[5] += bf16_high(w.z); v[6] += bf16_low(w.w); v[7] += bf16_high(w.w);
 }
-__device__ __forceinline__ void add_bias32(const uint16_t* bias, int cols, float (&v)[32]) {
+__device__ __forceinline__ void add_bias32(const uint16_t* bias, int cols, bool octets, float (&v)[32]) {
+  if (octets) {        // cols % 8 == 0, 16-byte-aligned
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (8 * j < cols) add_octet(reinterpret_cast<const uint4*>(bias)[j], v + 8 * j);   // cols % 8 == 0 here
+    for (int j = 0; j < 4; ++j)
+      if (8 * j < cols) add_octet(reinterpret_cast<const uint4*>(bias)[j], v + 8 * j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (j < cols) v[j] += bf16_value(bias[j]);
+  }
+}
+
+// Where the TMA engine cannot address a tensor (n % 8 != 0, odd addresses) its 32 x 32 blocks move between shared
+// and global memory a row at a time, a lane to a column: 64 or 128 contiguous bytes an access.
+struct PlainBlock {
+  int64_t at;        // the block's first element, this lane's column
+  int64_t pitch;
+  int rows;          // of the block that exist; 0 for a lane past the last column
+};
+__device__ __forceinline__ uint32_t place16(uint32_t block, int row, int lane) {
+  return block + (uint32_t)row * 64u + ((((uint32_t)lane >> 3) ^ (((uint32_t)row >> 1) & 3u)) << 4) + ((uint32_t)lane & 7u) * 2u;
+}
+__device__ __forceinline__ void block_in16(uint32_t block, int lane, const uint16_t* src, const PlainBlock& g) {
+#pragma unroll 8
+  for (int r = 0; r < 32; ++r) {
+    const uint16_t v = r < g.rows ? src[g.at + r * g.pitch] : (uint16_t)0;
+    asm volatile("st.shared.u16 [%0], %1;" ::"r"(place16(block, r, lane)), "h"(v) : "memory");
+  }
+}
+__device__ __forceinline__ void block_out16(uint32_t block, int lane, uint16_t* dst, const PlainBlock& g) {
+#pragma unroll 8
+  for (int r = 0; r < 32; ++r) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(place16(block, r, lane)) : "memory");
+    if (r < g.rows) dst[g.at + r * g.pitch] = v;
+  }
+}
+__device__ __forceinline__ void block_out32(uint32_t block, int lane, float* dst, const PlainBlock& g, bool accumulate) {
+#pragma unroll 8
+  for (int r = 0; r < 32; ++r) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v)
+                 : "r"(block + (uint32_t)r * 128u + ((((uint32_t)lane >> 2) ^ ((uint32_t)r & 7u)) << 4) + ((uint32_t)lane & 3u) * 4u)
+                 : "memory");
+    if (r < g.rows) dst[g.at + r * g.pitch] = accumulate ? dst[g.at + r * g.pitch] + v : v;
+  }
+}
+__device__ __forceinline__ void add_row16(uint32_t block, int lane, float (&v)[32]) {
+  const uint32_t at = block + (uint32_t)lane * 64u, sw = (uint32_t)(lane >> 1) & 3u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint4 w;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                 : "r"(at + (((uint32_t)j ^ sw) << 4)) : "memory");
+    add_octet(w, v + 8 * j);
+  }
 }
 
 // bf16 Y by TMA with nothing to be done to the sums (the gradients): steps of 64 columns, one block of 32 rows x 128
@@ -351,9 +353,9 @@ __device__ __forceinline__ bool epilogue_copy(const TileParams& p, const Epilogu
   return true;
 }
 
-// Y and Z by TMA: steps part, part + kParts, ... of 32 columns.
+// Everything else: steps part, part + kParts, ... of 32 columns; Y and Z by TMA, or row by row.
 template <bool kGated, typename Wait, typename Release>
-__device__ __forceinline__ bool epilogue_tma(const TileParams& p, const EpilogueItem& e, const CUtensorMap& map_y,
+__device__ __forceinline__ bool epilogue_full(const TileParams& p, const EpilogueItem& e, const CUtensorMap& map_y,
                                              const CUtensorMap& map_z, uint8_t* mine, int part, int lane,
                                              Wait&& wait_sums, Release&& release_sums) {
   const int row = e.row0 + lane;
@@ -366,7 +368,7 @@ __device__ __forceinline__ bool epilogue_tma(const TileParams& p, const Epilogue
     for (int j = 0; j < 4; ++j)
       res[j] = row < e.row_end && col + 8 * j < p.n ? src[j] : make_uint4(0u, 0u, 0u, 0u);
   };
-  if (p.residual && part < steps) load_residual(part);
+  if (p.residual && p.tma && part < steps) load_residual(part);
   if (!wait_sums()) return false;
   const bool padding = p.zero_padding && row >= e.live_end;
   // The two blocks take turns; a block may be rewritten once the store from it has been read.
@@ -404,8 +406,8 @@ __device__ __forceinline__ bool epilogue_tma(const TileParams& p, const Epilogue
     bool free_block = true;      // the wait above covers the first block of the step
     if (s + kParts >= steps) release_sums();
     if (e.bias) {
-      add_bias32(e.bias + col, p.n - col, v);
-      if constexpr (kGated) add_bias32(e.bias + p.n + col, p.n - col, u);
+      add_bias32(e.bias + col, p.n - col, p.tma, v);
+      if constexpr (kGated) add_bias32(e.bias + p.n + col, p.n - col, p.tma, u);
     }
     if (padding) {
 #pragma unroll
@@ -415,11 +417,19 @@ __device__ __forceinline__ bool epilogue_tma(const TileParams& p, const Epilogue
         for (int i = 0; i < 32; ++i) u[i] = 0.f;
       }
     }
+    const int rows_here = col + lane < p.n ? min(32, e.row_end - e.row0) : 0;
+    const int64_t out_row = (int64_t)e.group * p.m + e.row0;
     if (p.Z) {
       auto send = [&](const float (&x)[32], int half) {
         uint8_t* b = next_block(free_block);
         free_block = false;
         put_row16(smem_u32(b), lane, x);
+        if (!p.tma) {
+          __syncwarp();
+          block_out16(smem_u32(b), lane, p.Z, PlainBlock{out_row * p.z_pitch + half * p.n + col + lane, p.z_pitch, rows_here});
+          __syncwarp();
+          return;
+        }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
@@ -435,10 +445,26 @@ __device__ __forceinline__ bool epilogue_tma(const TileParams& p, const Epilogue
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] *= u[i];
     }
-    if (p.residual) {
+    const PlainBlock plain{out_row * p.n + col + lane, p.n, rows_here};
+    if (p.residual && p.tma) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) add_octet(res[j], v + 8 * j);
       if (s + kParts < steps) load_residual(s + kParts);
+    } else if (p.residual) {
+      __syncwarp();
+      block_in16(smem_u32(mine), lane, p.residual, plain);
+      __syncwarp();
+      add_row16(smem_u32(mine), lane, v);
+      __syncwarp();
+    }
+    if (!p.tma) {
+      if (p.out_f32) put_row32(smem_u32(mine), lane, v);
+      else put_row16(smem_u32(mine), lane, v);
+      __syncwarp();
+      if (p.out_f32) block_out32(smem_u32(mine), lane, static_cast<float*>(p.Y), plain, p.accumulate);
+      else block_out16(smem_u32(mine), lane, static_cast<uint16_t*>(p.Y), plain);
+      __syncwarp();
+      continue;
     }
     uint8_t* b = mine;
     if (p.out_f32) {
@@ -462,111 +488,6 @@ __device__ __forceinline__ bool epilogue_tma(const TileParams& p, const Epilogue
   }
   // The next item begins with the first block again: nothing but the last store may be pending from the second.
   if (slot == 1u && lane == 0) bulk_wait_group_read<0>();
-  return true;
-}
-
-// v += the eight staged columns at 16-byte chunks c0, c0 + 1 of the row.
-__device__ __forceinline__ void staged8(uint32_t row_addr, uint32_t c0, uint32_t sw, float (&v)[8]) {
-  float x[8];
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
-               : "r"(row_addr + ((c0 ^ sw) << 4)));
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
-               : "r"(row_addr + (((c0 + 1u) ^ sw) << 4)));
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] += x[e];
-}
-
-// Plain loads and stores, any n and alignment.
-template <bool kGated, typename Wait, typename Release>
-__device__ __forceinline__ bool epilogue_plain(const TileParams& p, const EpilogueItem& e, uint32_t block, int part, int lane,
-                                               Wait&& wait_sums, Release&& release_sums) {
-  constexpr int kStep = kGated ? 16 : 32;            // output columns per block (gated: of either half)
-  constexpr int kLanes = kStep / 8, kRowsAt = 32 / kLanes;
-  const int steps = e.row0 < e.row_end ? (min(e.width, p.n - e.col0) + kStep - 1) / kStep : 0;
-  const int sub = lane % kLanes, row_in = lane / kLanes;
-  if (!wait_sums()) return false;
-  const int64_t out_row0 = (int64_t)e.group * p.m;
-  if (part >= steps) release_sums();
-#pragma unroll 1
-  for (int s = part; s < steps; s += kParts) {
-    const int c = s * kStep;
-    {
-      // 32 accumulator columns: the step's own, or its gate's and its partner's 16 each.
-      uint32_t r[2][16];
-      if (!e.empty_sum) {
-        tmem_ld_32x16(e.taddr + (uint32_t)c, r[0]);
-        tmem_ld_32x16(e.taddr + (kGated ? (uint32_t)(e.width + c) : (uint32_t)(c + 16)), r[1]);
-        tmem_ld_wait();
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) r[0][i] = r[1][i] = 0u;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        st_shared_v4(block + (uint32_t)lane * 128u + (((uint32_t)j ^ (uint32_t)(lane & 7)) << 4), r[j >> 2][4 * (j & 3)],
-                     r[j >> 2][4 * (j & 3) + 1], r[j >> 2][4 * (j & 3) + 2], r[j >> 2][4 * (j & 3) + 3]);
-    }
-    if (s + kParts >= steps) release_sums();
-    __syncwarp();
-    const int col = e.col0 + c + sub * 8;
-    const int cols = p.n - col;                  // columns left from here (may be <= 0 or >= 8)
-    const bool vec = p.vec && cols >= 8;
-    if (cols > 0) {
-      float b0[8], b1[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) b0[i] = b1[i] = 0.f;
-      if (e.bias) {
-        load8(e.bias + col, vec, cols, b0);
-        if constexpr (kGated) load8(e.bias + p.n + col, vec, cols, b1);
-      }
-#pragma unroll 2
-      for (int i = 0; i < 32 / kRowsAt; ++i) {
-        const int r_in = i * kRowsAt + row_in;
-        const int row = e.row0 + r_in;
-        if (row >= e.row_end) continue;
-        const uint32_t row_addr = block + (uint32_t)r_in * 128u, sw = (uint32_t)(r_in & 7);
-        const int64_t out_row = out_row0 + row;
-        float x[8];
-        if (p.residual) load8(p.residual + out_row * p.n + col, vec, cols, x);
-        float v[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = b0[q];
-        staged8(row_addr, 2u * sub, sw, v);
-        const bool padding = p.zero_padding && row >= e.live_end;
-        if constexpr (kGated) {
-          float u[8];
-#pragma unroll
-          for (int q = 0; q < 8; ++q) u[q] = b1[q];
-          staged8(row_addr, 4u + 2u * sub, sw, u);
-          if (padding) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = u[q] = 0.f;
-          }
-          if (p.Z) {
-            store8(p.Z + out_row * p.z_pitch + col, vec, cols, v);
-            store8(p.Z + out_row * p.z_pitch + p.n + col, vec, cols, u);
-          }
-          act8_by(p.act, v);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) v[q] *= u[q];
-        } else {
-          if (padding) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = 0.f;
-          }
-          if (p.Z) store8(p.Z + out_row * p.z_pitch + col, vec, cols, v);
-          act8_by(p.act, v);
-        }
-        if (p.residual) {
-#pragma unroll
-          for (int q = 0; q < 8; ++q) v[q] += x[q];
-        }
-        if (p.out_f32) store8_f32(static_cast<float*>(p.Y) + out_row * p.n + col, vec, cols, p.accumulate, v);
-        else store8(static_cast<uint16_t*>(p.Y) + out_row * p.n + col, vec, cols, v);
-      }
-    }
-    __syncwarp();      // the block is rewritten by the next step
-  }
   return true;
 }
 
@@ -837,8 +758,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
           }
         };
         if (p.copy) ok = epilogue_copy(p, e, map_y, mine, part, lane, wait_sums, release_sums);
-        else if (p.tma) ok = epilogue_tma<kGated>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums);
-        else ok = epilogue_plain<kGated>(p, e, smem_u32(mine), part, lane, wait_sums, release_sums);
+        else ok = epilogue_full<kGated>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums);
         if (++buf == 2) { buf = 0; acc_phase ^= 1; }
       }
       // A product's blocks are laid out as its outputs need them: none is pending when the next begins.
@@ -982,9 +902,8 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count,
     p.act = (uint8_t)ep.act;
     p.out_f32 = ep.out_f32;
     p.accumulate = ep.accumulate;
-    p.vec = c.n % 8 == 0 && aligned16(ep.Y) && aligned16(ep.Z) && aligned16(ep.bias) && aligned16(ep.residual);
-    p.tma = p.vec;
-    p.copy = p.vec && !ep.gated && ep.act == kActNone && !ep.bias && !ep.residual && !ep.Z && !ep.out_f32;
+    p.tma = c.n % 8 == 0 && aligned16(ep.Y) && aligned16(ep.Z) && aligned16(ep.bias) && aligned16(ep.residual);
+    p.copy = p.tma && !ep.gated && ep.act == kActNone && !ep.bias && !ep.residual && !ep.Z && !ep.out_f32;
     p.z_pitch = (int)(c.n * width);
     p.bias = ep.bias;
     p.residual = ep.residual;
