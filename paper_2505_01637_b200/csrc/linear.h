@@ -64,6 +64,7 @@ struct TileCall {
   int64_t m = 0, n = 0, k = 0;   // extents of one output (gated: n columns, B has 2 n); k unused by kContract
   int64_t b_up = 0;        // gated: where the second half of B's columns begins in its stored order
   bool zero_padding = false;     // kRows: rows that hold no token are written as zeros
+  bool precise = false;          // f32 output whose sums are wanted as near as f32 allows
   bool gather_a = false;         // few-rows kernel: A is [tokens][cols], its rows fetched through the plan
   ExpertRows experts;
   LinearEpilogue epi;

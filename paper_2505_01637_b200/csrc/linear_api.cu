@@ -194,6 +194,7 @@ int forward(const DeviceInfo& dev, const Layer& l, const ForwardArgs& a, Carver&
   c.epi.act = l.act;
   c.epi.gated = l.gated;
   c.epi.out_f32 = a.y_f32;
+  c.precise = a.y_f32;
   c.epi.bias = static_cast<const uint16_t*>(a.bias);
   c.epi.residual = static_cast<const uint16_t*>(a.R);
   c.epi.Y = a.Y;
@@ -282,6 +283,7 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
     c.k = l.m;
     c.experts = l.x;
     c.epi.out_f32 = a.grad_f32;
+    c.precise = a.grad_f32;
     c.epi.accumulate = a.accumulate;
     c.epi.Y = a.dW;
   }

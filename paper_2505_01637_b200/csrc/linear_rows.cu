@@ -9,6 +9,7 @@
 // through distributed shared memory, then the epilogue: one launch, no scratch, a fixed order.
 // Experts: grid.y is the block of the row layout; a block past the live ones leaves at once.
 #include <algorithm>
+#include <type_traits>
 
 #include "activation.cuh"
 #include "linear.h"
@@ -35,7 +36,6 @@ struct Shape {
   static constexpr int kRing = 108 * 1024;
   static constexpr int kFit = kRing / kStageBytes;
   static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
-  static constexpr int kTmemCols = kRows <= 32 ? 32 : 64;
   static constexpr size_t kSmemBytes = (size_t)kStages * kStageBytes + 1024 + 256;
   static_assert(kRows * kStrip * 4 <= kStages * kStageBytes, "the parked sums reuse the stages");
 };
@@ -43,6 +43,8 @@ struct Shape {
 struct RowsParams {
   int m, n;              // rows (dense) and output columns
   int k_blocks, split, per_slice;
+  int chunks, chunk;     // accumulators the slice's sums are spread over, and contraction blocks of each
+  int tmem_cols;
   int b_up;
   uint8_t b_mn, gated, grouped, zero_padding, gather;
   int topk, tokens;
@@ -147,7 +149,9 @@ struct Column {
 };
 
 // One slice and no gate: the sums come straight from tensor memory.
-__device__ __forceinline__ void finish_direct(Column& c, int act, uint32_t taddr, int rows, bool live) {
+template <bool kPrecise>
+__device__ __forceinline__ void finish_direct(Column& c, int act, uint32_t taddr, int chunks, uint32_t apart, int rows,
+                                              bool live) {
 #pragma unroll 1
   for (int g = 0; g < rows; g += kBatch) {
     uint32_t r[kBatch];
@@ -156,6 +160,12 @@ __device__ __forceinline__ void finish_direct(Column& c, int act, uint32_t taddr
     float v[kBatch], u[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) v[i] = __uint_as_float(r[i]);
+    for (int k = 1; kPrecise && k < chunks; ++k) {
+      tmem_ld_32x4(taddr + k * apart + g, r);
+      tmem_ld_wait();
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) v[i] += __uint_as_float(r[i]);
+    }
     if (live) c.finish<false>(act, rows - g, v, u);
   }
 }
@@ -193,7 +203,9 @@ __device__ __forceinline__ void finish_parked(Column& c, int act, uint32_t part,
   }
 }
 
-template <int kRows>
+// kPrecise: the slice's sums are spread over p.chunks accumulators (the tensor cores add by truncation: see the tile
+// kernel) and added up on the way out.
+template <int kRows, bool kPrecise>
 __global__ void __launch_bounds__(kThreads, 2)       // two blocks to an SM, registers included
 linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const RowsParams p) {
@@ -252,7 +264,7 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const int chunks = (rows + kRows - 1) / kRows;     // of rows; more than one only when an expert has many
 
   if (warp == 1) {
-    tmem_alloc(&bars->tmem_base, S::kTmemCols);
+    tmem_alloc(&bars->tmem_base, (uint32_t)p.tmem_cols);
     tmem_relinquish();
   }
   tc_fence_before_sync();
@@ -322,6 +334,8 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       if (elect_one()) {
         const uint32_t idesc = instr_desc_bf16(kStrip, kRows, p.b_mn != 0, false);
         const uint32_t step = p.b_mn ? 2048u : 32u, lbo = p.b_mn ? (uint32_t)kBoxBytes : 16u;
+        uint32_t d_tmem = tmem_base;
+        int in_chunk = 0;
         for (int kb = kb0; kb < kb1 && ok; ++kb) {
           if (!(ok = mbar_wait(&bars->full[stage], phase, abort_flag, p.status, 42))) break;
           tc_fence_after_sync();
@@ -329,8 +343,13 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           const uint32_t sa = sb + 2 * kBoxBytes;
 #pragma unroll
           for (int j = 0; j < kTileK / 16; ++j)
-            mma_bf16_ss(tmem_base, smem_desc_sw128(sb + j * step, lbo, 1024), smem_desc_sw128(sa + j * 32, 16, 1024),
-                        idesc, ((kb - kb0) | j) != 0 ? 1u : 0u);
+            mma_bf16_ss(d_tmem, smem_desc_sw128(sb + j * step, lbo, 1024), smem_desc_sw128(sa + j * 32, 16, 1024),
+                        idesc, (in_chunk | j) != 0 ? 1u : 0u);
+          ++in_chunk;
+          if (kPrecise && in_chunk == p.chunk) {
+            in_chunk = 0;
+            d_tmem += kRows;
+          }
           mma_commit(&bars->empty[stage]);
           if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         }
@@ -371,11 +390,12 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         float* part = reinterpret_cast<float*>(stages);
         const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16);
         if (direct && kb1 > kb0) {
-          finish_direct(c, p.act, taddr, rows_here, live);
+          finish_direct<kPrecise>(c, p.act, taddr, p.chunks, kRows, rows_here, live);
         } else {
 #pragma unroll 1
           for (int g = 0; g < rows_here; g += 16) {
             uint32_t r[16];
+            float sum[16];
             if (kb1 > kb0) {
               tmem_ld_32x16(taddr + g, r);
               tmem_ld_wait();
@@ -384,7 +404,16 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
               for (int i = 0; i < 16; ++i) r[i] = 0u;     // an empty sum
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) part[(g + i) * kStrip + quarter * 32 + lane] = __uint_as_float(r[i]);
+            for (int i = 0; i < 16; ++i) sum[i] = __uint_as_float(r[i]);
+            // The last slice may have fewer accumulators than the others.
+            for (int k = 1; kPrecise && k < p.chunks && kb0 + k * p.chunk < kb1; ++k) {
+              tmem_ld_32x16(taddr + k * kRows + g, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) sum[i] += __uint_as_float(r[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) part[(g + i) * kStrip + quarter * 32 + lane] = sum[i];
           }
         }
         tc_fence_before_sync();
@@ -434,16 +463,16 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_after_sync();
   if (warp == 1) {
     __syncwarp();
-    tmem_dealloc(tmem_base, S::kTmemCols);
+    tmem_dealloc(tmem_base, (uint32_t)p.tmem_cols);
   }
 }
 
-template <int kRows>
+template <int kRows, bool kPrecise>
 cudaError_t launch(const DeviceInfo& dev, const TileCall& c, RowsParams p, cudaStream_t stream) {
   using S = Shape<kRows>;
   static PerDeviceOnce once;
   cudaError_t e = once.run_current([] {
-    return cudaFuncSetAttribute(linear_rows_kernel<kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(linear_rows_kernel<kRows, kPrecise>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)S::kSmemBytes);
   });
   if (e != cudaSuccess) return e;
@@ -458,6 +487,13 @@ cudaError_t launch(const DeviceInfo& dev, const TileCall& c, RowsParams p, cudaS
   while (split > 1 && (p.k_blocks + split - 1) / split * (split - 1) >= p.k_blocks) split /= 2;   // no empty slice
   p.split = split;
   p.per_slice = (p.k_blocks + split - 1) / split;
+  // Precise sums: an accumulator for every 8 contraction blocks, added up on the way out; at most 256 columns of
+  // tensor memory, half of it, so that two blocks fit.
+  p.chunk = std::max(1, p.per_slice);
+  if (kPrecise) p.chunk = std::max(8, (p.per_slice + 256 / kRows - 1) / (256 / kRows));
+  p.chunks = std::max(1, (p.per_slice + p.chunk - 1) / p.chunk);
+  p.tmem_cols = 32;
+  while (p.tmem_cols < p.chunks * kRows) p.tmem_cols *= 2;
   if (blocks > 65535 || strips * split >= (1ll << 31)) return cudaErrorInvalidValue;
   CUtensorMap ma{}, mb{};
   if (c.k > 0) {
@@ -469,7 +505,7 @@ cudaError_t launch(const DeviceInfo& dev, const TileCall& c, RowsParams p, cudaS
                              (uint64_t)c.b.groups, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
     if (e != cudaSuccess) return e;
   }
-  return launch_pdl(linear_rows_kernel<kRows>, dim3((unsigned)(strips * split), (unsigned)blocks), dim3(kThreads),
+  return launch_pdl(linear_rows_kernel<kRows, kPrecise>, dim3((unsigned)(strips * split), (unsigned)blocks), dim3(kThreads),
                     S::kSmemBytes, stream, split, ma, mb, p);
 }
 
@@ -506,10 +542,14 @@ cudaError_t rows_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   p.Z = ep.Z;
   p.status = dev.status;
   cudaError_t e;
-  if (rows <= 16) e = launch<16>(dev, c, p, stream);
-  else if (rows <= 32) e = launch<32>(dev, c, p, stream);
-  else if (rows <= 48) e = launch<48>(dev, c, p, stream);
-  else e = launch<64>(dev, c, p, stream);
+  auto go = [&](auto kernel_rows) {
+    constexpr int kRows = decltype(kernel_rows)::value;
+    return c.precise && c.k > 8 * kTileK ? launch<kRows, true>(dev, c, p, stream) : launch<kRows, false>(dev, c, p, stream);
+  };
+  if (rows <= 16) e = go(std::integral_constant<int, 16>{});
+  else if (rows <= 32) e = go(std::integral_constant<int, 32>{});
+  else if (rows <= 48) e = go(std::integral_constant<int, 48>{});
+  else e = go(std::integral_constant<int, 64>{});
   if (e == cudaSuccess) ++*launches;
   return e;
 }

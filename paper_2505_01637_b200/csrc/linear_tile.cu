@@ -211,6 +211,7 @@ struct EpilogueItem {
   int live_end;
   int group;             // third coordinate of Y
   bool empty_sum;
+  int chunks;            // parts the contraction's sums come in
 };
 
 template <int kAct>
@@ -354,10 +355,11 @@ __device__ __forceinline__ bool epilogue_copy(const TileParams& p, const Epilogu
 }
 
 // Everything else: steps part, part + kParts, ... of 32 columns; Y and Z by TMA, or row by row.
-template <bool kGated, typename Wait, typename Release>
+// kPrecise (tiles of at most 128 columns): the sums come in e.chunks parts of the contraction, which are added here.
+template <bool kGated, bool kPrecise, typename Wait, typename Release, typename Next>
 __device__ __forceinline__ bool epilogue_full(const TileParams& p, const EpilogueItem& e, const CUtensorMap& map_y,
-                                             const CUtensorMap& map_z, uint8_t* mine, int part, int lane,
-                                             Wait&& wait_sums, Release&& release_sums) {
+                                              const CUtensorMap& map_z, uint8_t* mine, int part, int lane,
+                                              Wait&& wait_sums, Release&& release_sums, Next&& next_sums) {
   const int row = e.row0 + lane;
   const int steps = e.row0 < e.row_end ? min(e.width, (p.n - e.col0 + 31) & ~31) / 32 : 0;
   uint4 res[4];
@@ -369,7 +371,6 @@ __device__ __forceinline__ bool epilogue_full(const TileParams& p, const Epilogu
       res[j] = row < e.row_end && col + 8 * j < p.n ? src[j] : make_uint4(0u, 0u, 0u, 0u);
   };
   if (p.residual && p.tma && part < steps) load_residual(part);
-  if (!wait_sums()) return false;
   const bool padding = p.zero_padding && row >= e.live_end;
   // The two blocks take turns; a block may be rewritten once the store from it has been read.
   uint32_t slot = 0;
@@ -380,31 +381,10 @@ __device__ __forceinline__ bool epilogue_full(const TileParams& p, const Epilogu
     slot ^= 1u;
     return b;
   };
-  if (part >= steps) release_sums();
-#pragma unroll 1
-  for (int s = part; s < steps; s += kParts) {
-    const int c = 32 * s, col = e.col0 + c;
-    float v[32];
-    [[maybe_unused]] float u[kGated ? 32 : 1];
-    {
-      uint32_t r[32];
-      [[maybe_unused]] uint32_t q[32];
-      start_sums32(e.taddr + (uint32_t)c, e.empty_sum, r);
-      if constexpr (kGated) start_sums32(e.taddr + (uint32_t)(e.width + c), e.empty_sum, q);
-      // Meanwhile: the block this step writes first must have been read.
-      if (lane == 0) {
-        if (p.out_f32) bulk_wait_group_read<0>(); else bulk_wait_group_read<1>();
-      }
-      tmem_ld_wait();
-#pragma unroll
-      for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-      if constexpr (kGated) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) u[i] = __uint_as_float(q[i]);
-      }
-    }
-    bool free_block = true;      // the wait above covers the first block of the step
-    if (s + kParts >= steps) release_sums();
+  // One step from its sums (and its gate's partner's).
+  auto finish = [&](int s, float (&v)[32], float (&u)[kGated ? 32 : 1]) {
+    const int col = e.col0 + 32 * s;
+    bool free_block = true;      // the block this step writes first has been read: waited for with the sums
     if (e.bias) {
       add_bias32(e.bias + col, p.n - col, p.tma, v);
       if constexpr (kGated) add_bias32(e.bias + p.n + col, p.n - col, p.tma, u);
@@ -464,7 +444,7 @@ __device__ __forceinline__ bool epilogue_full(const TileParams& p, const Epilogu
       if (p.out_f32) block_out32(smem_u32(mine), lane, static_cast<float*>(p.Y), plain, p.accumulate);
       else block_out16(smem_u32(mine), lane, static_cast<uint16_t*>(p.Y), plain);
       __syncwarp();
-      continue;
+      return;
     }
     uint8_t* b = mine;
     if (p.out_f32) {
@@ -485,6 +465,61 @@ __device__ __forceinline__ bool epilogue_full(const TileParams& p, const Epilogu
       // With f32 the next block written may be the upper half of this one.
       if (p.out_f32 && p.Z) bulk_wait_group_read<0>();
     }
+  };
+  auto free_first_block = [&] {
+    if (lane == 0) {
+      if (p.out_f32) bulk_wait_group_read<0>(); else bulk_wait_group_read<1>();
+    }
+  };
+  if constexpr (kPrecise) {
+    float sums[2][32];         // steps part and part + kParts; gated: the step's gate and its partner
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sums[0][i] = sums[1][i] = 0.f;
+#pragma unroll 1
+    for (int chunk = 0; chunk < e.chunks; ++chunk) {
+      if (!wait_sums()) return false;
+      const uint32_t taddr = next_sums(chunk + 1 == e.chunks, false);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t r[32];
+        start_sums32(taddr + 32u * part + (uint32_t)i * (kGated ? (uint32_t)e.width : 32u * kParts), e.empty_sum, r);
+        tmem_ld_wait();
+#pragma unroll
+        for (int q = 0; q < 32; ++q) sums[i][q] += __uint_as_float(r[q]);
+      }
+      release_sums();
+      next_sums(chunk + 1 == e.chunks, true);
+    }
+#pragma unroll
+    for (int i = 0; i < (kGated ? 1 : 2); ++i) {
+      const int s = part + i * kParts;
+      if (s >= steps) break;
+      free_first_block();
+      if constexpr (kGated) finish(s, sums[0], sums[1]);
+      else { float none[1]; finish(s, sums[i], none); }
+    }
+  } else {
+    if (!wait_sums()) return false;
+    if (part >= steps) release_sums();
+#pragma unroll 1
+    for (int s = part; s < steps; s += kParts) {
+      const uint32_t c = 32u * s;
+      float v[32], u[kGated ? 32 : 1];
+      uint32_t r[32];
+      [[maybe_unused]] uint32_t q[32];
+      start_sums32(e.taddr + c, e.empty_sum, r);
+      if constexpr (kGated) start_sums32(e.taddr + (uint32_t)e.width + c, e.empty_sum, q);
+      free_first_block();        // meanwhile
+      tmem_ld_wait();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+      if constexpr (kGated) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) u[i] = __uint_as_float(q[i]);
+      }
+      if (s + kParts >= steps) release_sums();
+      finish(s, v, u);
+    }
   }
   // The next item begins with the first block again: nothing but the last store may be pending from the second.
   if (slot == 1u && lane == 0) bulk_wait_group_read<0>();
@@ -501,7 +536,12 @@ struct TileBatch {
 
 // kTwo: the batch has two products.  One is a form of its own so that its parameters are constants at fixed
 // addresses (through an index the epilogue of a 64-deep product took 92 instead of 79 us).
-template <bool kPair, int kTileN, bool kGated, bool kTwo>
+// kPrecise: the tensor cores add to their f32 accumulator by truncation, an error of about 1e-9 of the result per
+// element of the contraction (4e-6 at 4096), one way.  Where the output is f32 and the contraction long, the sums are
+// taken out every kChunk blocks and added up in registers (to nearest): a few 1e-7 whatever the length.  A warp's
+// share of a 128-column tile's sums fits its registers; wider tiles' would not.
+constexpr int kChunk = 8;
+template <bool kPair, int kTileN, bool kGated, bool kTwo, bool kPrecise>
 __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_constant__ TileBatch batch) {
   using S = Shape<kPair, kTileN>;
   extern __shared__ uint8_t smem_raw[];
@@ -678,17 +718,28 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
           const uint32_t idesc = at.is_half() ? idesc_half : idesc_tile;
           if (!(ok = mbar_wait(&bars->acc_empty[buf], acc_phase ^ 1, abort_flag, p.status, 34))) break;
           tc_fence_after_sync();
-          const uint32_t d_tmem = tmem_base + (uint32_t)buf * kAccStride;
+          uint32_t d_tmem = tmem_base + (uint32_t)buf * kAccStride;
           for (int kb = 0; kb < k_blocks; ++kb) {
+            if constexpr (kPrecise) {
+              if (kb > 0 && kb % kChunk == 0) {      // this part of the sums is complete: on to the other accumulator
+                if constexpr (kPair) mma_commit_pair(&bars->acc_full[buf], 3);
+                else mma_commit(&bars->acc_full[buf]);
+                if (++buf == 2) { buf = 0; acc_phase ^= 1; }
+                if (!(ok = mbar_wait(&bars->acc_empty[buf], acc_phase ^ 1, abort_flag, p.status, 38))) break;
+                tc_fence_after_sync();
+                d_tmem = tmem_base + (uint32_t)buf * kAccStride;
+              }
+            }
             if (!(ok = mbar_wait(&bars->full[stage], phase, abort_flag, p.status, 35))) break;
             tc_fence_after_sync();
             const uint32_t sa = smem_u32(stages + (size_t)stage * S::kStageBytes);
             const uint32_t sb = sa + kBytesA;
+            const int at_kb = kPrecise ? kb % kChunk : kb;
             auto mma = [&](int j) {
               const uint64_t da = smem_desc_sw128(sa + j * step_a, lbo_a, 1024);
               const uint64_t db = smem_desc_sw128(sb + j * step_b, lbo_b, 1024);
-              if constexpr (kPair) mma_bf16_ss_pair(d_tmem, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
-              else mma_bf16_ss(d_tmem, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
+              if constexpr (kPair) mma_bf16_ss_pair(d_tmem, da, db, idesc, (at_kb | j) != 0 ? 1u : 0u);
+              else mma_bf16_ss(d_tmem, da, db, idesc, (at_kb | j) != 0 ? 1u : 0u);
             };
             if (kb + 1 < k_blocks || k_steps == kTileK / 16) {
 #pragma unroll
@@ -742,6 +793,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
         e.bias = p.bias ? p.bias + (int64_t)it.group * p.z_pitch : nullptr;
         e.live_end = it.live_end;
         e.empty_sum = it.k_blocks == 0;
+        e.chunks = kPrecise ? max(1, (it.k_blocks + kChunk - 1) / kChunk) : 1;
         e.group = p.mode == (int)TileMode::kContract ? it.group : 0;
         auto wait_sums = [&] {
           bool done = mbar_wait(&bars->acc_full[buf], acc_phase, abort_flag, p.status, 36);
@@ -757,8 +809,13 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
             else mbar_arrive(&bars->acc_empty[buf]);
           }
         };
-        if (p.copy) ok = epilogue_copy(p, e, map_y, mine, part, lane, wait_sums, release_sums);
-        else ok = epilogue_full<kGated>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums);
+        // Where the current part of the sums is; or, done with it, on to the next part's accumulator.
+        auto next_sums = [&](bool last, bool done) {
+          if (done && !last && ++buf == 2) { buf = 0; acc_phase ^= 1; }
+          return tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)buf * kAccStride;
+        };
+        if (!kPrecise && p.copy) ok = epilogue_copy(p, e, map_y, mine, part, lane, wait_sums, release_sums);
+        else ok = epilogue_full<kGated, kPrecise>(p, e, map_y, map_z, mine, part, lane, wait_sums, release_sums, next_sums);
         if (++buf == 2) { buf = 0; acc_phase ^= 1; }
       }
       // A product's blocks are laid out as its outputs need them: none is pending when the next begins.
@@ -782,33 +839,38 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   }
 }
 
-template <bool kPair, int kTileN, bool kGated, bool kTwo>
+template <bool kPair, int kTileN, bool kGated, bool kTwo, bool kPrecise>
 cudaError_t launch_form(const DeviceInfo& dev, const TileBatch& batch, int64_t max_items, cudaStream_t stream) {
   using S = Shape<kPair, kTileN>;
   static PerDeviceOnce once;
   const cudaError_t e = once.run_current([] {
-    return cudaFuncSetAttribute(linear_tile_kernel<kPair, kTileN, kGated, kTwo>,
+    return cudaFuncSetAttribute(linear_tile_kernel<kPair, kTileN, kGated, kTwo, kPrecise>,
                                 cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmemBytes);
   });
   if (e != cudaSuccess) return e;
   const int64_t units = std::min<int64_t>(max_items, kPair ? gemm_pair_units(dev.sms) : dev.sms);
-  return launch_pdl(linear_tile_kernel<kPair, kTileN, kGated, kTwo>, dim3((unsigned)(units * S::kCtas)), dim3(kThreads),
+  return launch_pdl(linear_tile_kernel<kPair, kTileN, kGated, kTwo, kPrecise>, dim3((unsigned)(units * S::kCtas)), dim3(kThreads),
                     S::kSmemBytes, stream, S::kCtas, batch);
 }
-template <bool kPair, int kTileN>
+template <bool kPair, int kTileN, bool kPrecise>
 cudaError_t launch_tile(const DeviceInfo& dev, const TileBatch& batch, bool gated, bool two, int64_t max_items,
                         cudaStream_t stream) {
-  if (two) return gated ? cudaErrorInvalidValue : launch_form<kPair, kTileN, false, true>(dev, batch, max_items, stream);
+  if (two)
+    return gated ? cudaErrorInvalidValue : launch_form<kPair, kTileN, false, true, kPrecise>(dev, batch, max_items, stream);
   if constexpr (kTileN > 64) {
-    if (gated) return launch_form<kPair, kTileN, true, false>(dev, batch, max_items, stream);
+    if (gated) return launch_form<kPair, kTileN, true, false, kPrecise>(dev, batch, max_items, stream);
   }
-  return launch_form<kPair, kTileN, false, false>(dev, batch, max_items, stream);
+  return launch_form<kPair, kTileN, false, false, kPrecise>(dev, batch, max_items, stream);
 }
 
 // A tile's column halves are whole 64-column boxes in every CTA (gated: of both halves of W).
 bool can_halve(int pair, int tile_n, bool gated) { return tile_n / (pair || gated ? 2 : 1) / 2 >= 64; }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Up to these lengths the truncation stays within 1e-6 of the result (a gated layer multiplies two sums).  Parts cost
+// 130 instead of 98 us on a cube of 4096.
+constexpr int kPreciseFrom = 1024, kPreciseGated = 512;
 
 // What a tile costs, in microseconds at full clocks: a contraction block (the MMAs of a 256-column tile, or what the
 // roles' loops take for a narrower one) and the epilogue (which the next tile's main loop hides, if it is longer).
@@ -842,7 +904,7 @@ bool form_allowed(const TileCall& c, const TileForm& f) {
 
 // The form with the least estimated time: whole waves of every product, then what is left of them -- side by side where
 // the units hold it, cut into column halves (about 0.6 of a wave) where a single product's leftover allows.
-TileForm choose_form(const DeviceInfo& dev, const TileCall* calls, int count) {
+TileForm choose_form(const DeviceInfo& dev, const TileCall* calls, int count, bool precise) {
   double best = 0;
   int at = -1;
   for (int i = 0; i < (int)(sizeof(kForms) / sizeof(kForms[0])); ++i) {
@@ -850,7 +912,7 @@ TileForm choose_form(const DeviceInfo& dev, const TileCall* calls, int count) {
     const int64_t units = std::max(1, f.pair ? gemm_pair_units(dev.sms) : dev.sms);
     double cost = 0, last = 0;
     int64_t left = 0;
-    bool allowed = true;
+    bool allowed = !precise || f.tile_n == 128;
     for (int q = 0; q < count; ++q) {
       allowed = allowed && form_allowed(calls[q], f);
       double blocks = 0;
@@ -877,7 +939,11 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count,
   for (int q = 0; q < count; ++q)
     if (calls[q].m <= 0 || calls[q].n <= 0 || (q > 0 && calls[q].mode == TileMode::kRows)) return cudaErrorInvalidValue;
   const bool gated = calls[0].epi.gated;
-  const TileForm form = choose_form(dev, calls, count);
+  // f32 results of a long contraction are summed in parts (see kPrecise).
+  bool precise = false;
+  for (int q = 0; q < count; ++q)
+    precise = precise || (calls[q].precise && calls[q].k > (calls[q].epi.gated ? kPreciseGated : kPreciseFrom));
+  const TileForm form = choose_form(dev, calls, count, precise);
   TileBatch batch{};
   int64_t items = 0;
   for (int q = 0; q < count; ++q) {
@@ -944,12 +1010,14 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count,
   }
   cudaError_t e;
   const bool two = count == 2;
-  switch (form.pair * 1000 + form.tile_n) {
-    case 64: e = launch_tile<false, 64>(dev, batch, gated, two, items, stream); break;
-    case 128: e = launch_tile<false, 128>(dev, batch, gated, two, items, stream); break;
-    case 256: e = launch_tile<false, 256>(dev, batch, gated, two, items, stream); break;
-    case 1128: e = launch_tile<true, 128>(dev, batch, gated, two, items, stream); break;
-    case 1256: e = launch_tile<true, 256>(dev, batch, gated, two, items, stream); break;
+  switch (form.pair * 1000 + form.tile_n + (precise ? 1 : 0)) {
+    case 64: e = launch_tile<false, 64, false>(dev, batch, gated, two, items, stream); break;
+    case 128: e = launch_tile<false, 128, false>(dev, batch, gated, two, items, stream); break;
+    case 256: e = launch_tile<false, 256, false>(dev, batch, gated, two, items, stream); break;
+    case 1128: e = launch_tile<true, 128, false>(dev, batch, gated, two, items, stream); break;
+    case 1256: e = launch_tile<true, 256, false>(dev, batch, gated, two, items, stream); break;
+    case 129: e = launch_tile<false, 128, true>(dev, batch, gated, two, items, stream); break;
+    case 1129: e = launch_tile<true, 128, true>(dev, batch, gated, two, items, stream); break;
     default: return cudaErrorInvalidValue;
   }
   if (e == cudaSuccess) ++*launches;
