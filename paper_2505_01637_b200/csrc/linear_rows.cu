@@ -22,23 +22,46 @@ namespace {
 using namespace sm100;
 
 constexpr int kStrip = 128;
-constexpr int kTileK = 64;
-constexpr int kBoxBytes = 64 * kTileK * 2;
+constexpr int kPart = 512;             // contraction elements an accumulator of precise sums takes
+constexpr int kSpan = 64;              // contraction elements of one 128-byte swizzle span
 constexpr int kThreads = 192;
 constexpr int kMaxStages = 8;
-constexpr int kPrefetchBlocks = 6;     // contraction blocks asked into L2 before the wait
+constexpr int kPrefetch = 384;         // contraction elements asked into L2 before the wait
 
 template <int kRows>
 struct Shape {
-  static constexpr int kStageBytes = 2 * kBoxBytes + kRows * kTileK * 2;
+  // Contraction elements of a stage.  The loops that issue loads and MMAs are one thread's each and take about 0.2 us
+  // a stage, so stages are deep where two blocks' rings still hold three of them.
+  static constexpr int kTileK = kRows <= 16 ? 128 : 64;
+  static constexpr int kSpans = kTileK / kSpan;
+  static constexpr int kStripBytes = kStrip * kTileK * 2;        // of W
+  static constexpr int kRowsSpan = kRows * kSpan * 2;            // the rows of X, one span of them
+  static constexpr int kStageBytes = kStripBytes + kSpans * kRowsSpan;
   // Two blocks fit an SM: another strip, or the next launch's, streams beside this one, and clusters of half-SM
   // blocks pack well (200 KiB rings: 8192 x 2048 on 32 rows in clusters of eight took two waves, 26 us).
-  static constexpr int kRing = 108 * 1024;
+  static constexpr int kRing = 109 * 1024;
   static constexpr int kFit = kRing / kStageBytes;
   static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
   static constexpr size_t kSmemBytes = (size_t)kStages * kStageBytes + 1024 + 256;
   static_assert(kRows * kStrip * 4 <= kStages * kStageBytes, "the parked sums reuse the stages");
 };
+
+// The strip's columns in one stage, as boxes: W across the contraction ([k][n]) two of 64 columns x kTileK; along it
+// ([n][k]) one of 128 columns (gated: two of 64) per span.
+template <int kRows, typename Box>
+__device__ __forceinline__ void strip_boxes(bool b_mn, bool gated, int col0, int col1, int kc, Box&& box) {
+  using S = Shape<kRows>;
+  if (b_mn) {
+    box(0, col0, kc);
+    box(S::kStripBytes / 2, col1, kc);
+  } else {
+#pragma unroll
+    for (int h = 0; h < S::kSpans; ++h) {
+      box(h * kStrip * kSpan * 2, kc + h * kSpan, col0);
+      if (gated) box(h * kStrip * kSpan * 2 + kStrip * kSpan, kc + h * kSpan, col1);
+    }
+  }
+}
 
 struct RowsParams {
   int m, n;              // rows (dense) and output columns
@@ -237,15 +260,9 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     tma_prefetch_descriptor(&map_b);
     if (!p.grouped) {
       // The weights' first blocks into L2 while the predecessor drains.
-      for (int kb = kb0; kb < min(kb1, kb0 + kPrefetchBlocks); ++kb) {
-        if (p.b_mn) {
-          tma_prefetch_l2_3d(&map_b, col0, kb * kTileK, 0);
-          tma_prefetch_l2_3d(&map_b, col1, kb * kTileK, 0);
-        } else {
-          tma_prefetch_l2_3d(&map_b, kb * kTileK, col0, 0);
-          tma_prefetch_l2_3d(&map_b, kb * kTileK, col1, 0);
-        }
-      }
+      for (int kb = kb0; kb < min(kb1, kb0 + kPrefetch / S::kTileK); ++kb)
+        strip_boxes<kRows>(p.b_mn, p.gated, col0, col1, kb * S::kTileK,
+                           [&](int, int x, int y) { tma_prefetch_l2_3d(&map_b, x, y, 0); });
     }
   }
   // Which rows, and whose weights.  An expert's are known once the predecessor is done; a dense layer has set
@@ -307,22 +324,20 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           if (p.gather) ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           uint8_t* sb = stages + (size_t)stage * S::kStageBytes;
-          const int kc = kb * kTileK;
+          uint64_t* full = &bars->full[stage];
+          const int kc = kb * S::kTileK;
           if (lead) {
-            mbar_arrive_expect_tx(&bars->full[stage], S::kStageBytes);
-            if (p.b_mn) {
-              tma_load_3d(sb, &map_b, &bars->full[stage], col0, kc, group);
-              tma_load_3d(sb + kBoxBytes, &map_b, &bars->full[stage], col1, kc, group);
-            } else {
-              tma_load_3d(sb, &map_b, &bars->full[stage], kc, col0, group);
-              tma_load_3d(sb + kBoxBytes, &map_b, &bars->full[stage], kc, col1, group);
-            }
-            if (!p.gather) tma_load_3d(sb + 2 * kBoxBytes, &map_a, &bars->full[stage], kc, first, 0);
+            mbar_arrive_expect_tx(full, S::kStageBytes);
+            strip_boxes<kRows>(p.b_mn, p.gated, col0, col1, kc,
+                               [&](int at, int x, int y) { tma_load_3d(sb + at, &map_b, full, x, y, group); });
           }
-          if (p.gather) {
-            __syncwarp();
-            if (lane < kRows / 4)
-              tma_gather4(sb + 2 * kBoxBytes + lane * 512, &map_a, &bars->full[stage], kc, from[0], from[1], from[2], from[3]);
+          if (p.gather) __syncwarp();
+#pragma unroll
+          for (int h = 0; h < S::kSpans; ++h) {
+            uint8_t* sa = sb + S::kStripBytes + h * S::kRowsSpan;
+            if (!p.gather) tma_load_3d(sa, &map_a, full, kc + h * kSpan, first, 0);
+            else if (lane < kRows / 4)
+              tma_gather4(sa + lane * 512, &map_a, full, kc + h * kSpan, from[0], from[1], from[2], from[3]);
           }
           if (++stage == S::kStages) { stage = 0; phase ^= 1; }
         }
@@ -333,18 +348,22 @@ linear_rows_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       // -------------------------------------------------------------- MMA issuer
       if (elect_one()) {
         const uint32_t idesc = instr_desc_bf16(kStrip, kRows, p.b_mn != 0, false);
-        const uint32_t step = p.b_mn ? 2048u : 32u, lbo = p.b_mn ? (uint32_t)kBoxBytes : 16u;
+        // W across the contraction: 64-column groups half a strip apart, 16 contraction rows = 2048 bytes.  Along it,
+        // like the rows of X: 8-row groups 1024 bytes apart, 16 elements = 32 bytes, a span's rows after another's.
+        const uint32_t step = p.b_mn ? 2048u : 32u, lbo = p.b_mn ? (uint32_t)(S::kStripBytes / 2) : 16u;
+        const uint32_t span = p.b_mn ? 4u * 2048u : (uint32_t)(kStrip * kSpan * 2);
         uint32_t d_tmem = tmem_base;
         int in_chunk = 0;
         for (int kb = kb0; kb < kb1 && ok; ++kb) {
           if (!(ok = mbar_wait(&bars->full[stage], phase, abort_flag, p.status, 42))) break;
           tc_fence_after_sync();
           const uint32_t sb = smem_u32(stages + (size_t)stage * S::kStageBytes);
-          const uint32_t sa = sb + 2 * kBoxBytes;
+          const uint32_t sa = sb + S::kStripBytes;
 #pragma unroll
-          for (int j = 0; j < kTileK / 16; ++j)
-            mma_bf16_ss(d_tmem, smem_desc_sw128(sb + j * step, lbo, 1024), smem_desc_sw128(sa + j * 32, 16, 1024),
-                        idesc, (in_chunk | j) != 0 ? 1u : 0u);
+          for (int j = 0; j < S::kTileK / 16; ++j)
+            mma_bf16_ss(d_tmem, smem_desc_sw128(sb + (j / 4) * span + (j % 4) * step, lbo, 1024),
+                        smem_desc_sw128(sa + (j / 4) * S::kRowsSpan + (j % 4) * 32, 16, 1024), idesc,
+                        (in_chunk | j) != 0 ? 1u : 0u);
           ++in_chunk;
           if (kPrecise && in_chunk == p.chunk) {
             in_chunk = 0;
@@ -479,18 +498,19 @@ cudaError_t launch(const DeviceInfo& dev, const TileCall& c, RowsParams p, cudaS
   const int64_t out_cols = c.epi.gated ? kStrip / 2 : kStrip;
   const int64_t strips = (c.n + out_cols - 1) / out_cols;
   const int64_t blocks = p.grouped ? c.experts.rows / kExpertBlock : 1;
-  // Slices: as many as keep every block slot of the device busy with at least four contraction blocks.
+  // Slices: as many as keep every block slot of the device busy with at least 256 elements of the contraction.
   const int64_t live = p.grouped ? std::min(c.experts.experts, c.experts.tokens * c.experts.topk) : 1;
   const int64_t slots = (int64_t)dev.sms * 2;
+  p.k_blocks = (int)((c.k + S::kTileK - 1) / S::kTileK);
   int split = 1;
-  while (split < 8 && strips * live * split * 2 <= slots && p.k_blocks >= split * 2 * 4) split *= 2;
+  while (split < 8 && strips * live * split * 2 <= slots && p.k_blocks >= split * 2 * (256 / S::kTileK)) split *= 2;
   while (split > 1 && (p.k_blocks + split - 1) / split * (split - 1) >= p.k_blocks) split /= 2;   // no empty slice
   p.split = split;
   p.per_slice = (p.k_blocks + split - 1) / split;
-  // Precise sums: an accumulator for every 8 contraction blocks, added up on the way out; at most 256 columns of
-  // tensor memory, half of it, so that two blocks fit.
+  // Precise sums: an accumulator for every 512 elements, added up on the way out; at most 256 columns of tensor memory,
+  // half of it, so that two blocks fit.
   p.chunk = std::max(1, p.per_slice);
-  if (kPrecise) p.chunk = std::max(8, (p.per_slice + 256 / kRows - 1) / (256 / kRows));
+  if (kPrecise) p.chunk = std::max(kPart / S::kTileK, (p.per_slice + 256 / kRows - 1) / (256 / kRows));
   p.chunks = std::max(1, (p.per_slice + p.chunk - 1) / p.chunk);
   p.tmem_cols = 32;
   while (p.tmem_cols < p.chunks * kRows) p.tmem_cols *= 2;
@@ -499,10 +519,11 @@ cudaError_t launch(const DeviceInfo& dev, const TileCall& c, RowsParams p, cudaS
   if (c.k > 0) {
     e = c.gather_a ? make_gather_map(&ma, c.a.p, (uint64_t)c.a.cols, (uint64_t)c.a.rows)
                    : make_tensor_map_3d(&ma, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.a.p, (uint64_t)c.a.cols,
-                                        (uint64_t)c.a.rows, 1, kTileK, kRows, CU_TENSOR_MAP_SWIZZLE_128B);
+                                        (uint64_t)c.a.rows, 1, kSpan, kRows, CU_TENSOR_MAP_SWIZZLE_128B);
     if (e == cudaSuccess)
       e = make_tensor_map_3d(&mb, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.b.p, (uint64_t)c.b.cols, (uint64_t)c.b.rows,
-                             (uint64_t)c.b.groups, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+                             (uint64_t)c.b.groups, kSpan, c.b_mn ? S::kTileK : c.epi.gated ? kStrip / 2 : kStrip,
+                             CU_TENSOR_MAP_SWIZZLE_128B);
     if (e != cudaSuccess) return e;
   }
   return launch_pdl(linear_rows_kernel<kRows, kPrecise>, dim3((unsigned)(strips * split), (unsigned)blocks), dim3(kThreads),
@@ -520,7 +541,6 @@ cudaError_t rows_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   if (rows > kLinearFewRows || c.a_mn || c.mode == TileMode::kContract) return cudaErrorInvalidValue;
   p.m = (int)c.m;
   p.n = (int)c.n;
-  p.k_blocks = (int)((c.k + kTileK - 1) / kTileK);
   p.b_up = (int)c.b_up;
   p.b_mn = c.b_mn;
   p.gated = ep.gated;
@@ -544,7 +564,7 @@ cudaError_t rows_launch(const DeviceInfo& dev, const TileCall& c, cudaStream_t s
   cudaError_t e;
   auto go = [&](auto kernel_rows) {
     constexpr int kRows = decltype(kernel_rows)::value;
-    return c.precise && c.k > 8 * kTileK ? launch<kRows, true>(dev, c, p, stream) : launch<kRows, false>(dev, c, p, stream);
+    return c.precise && c.k > kPart ? launch<kRows, true>(dev, c, p, stream) : launch<kRows, false>(dev, c, p, stream);
   };
   if (rows <= 16) e = go(std::integral_constant<int, 16>{});
   else if (rows <= 32) e = go(std::integral_constant<int, 32>{});
