@@ -645,7 +645,10 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
         const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
         for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, from, units); at.valid() && ok; at.next()) {
           const Item it = at.item();
-          const int row0 = it.row0 + (int)rank * kRowsPerCta;
+          int row0 = it.row0 + (int)rank * kRowsPerCta;
+          // An expert's odd block leaves the pair's second CTA without rows: zeros cost less power than the next
+          // expert's rows, and nothing is fetched for them.
+          if (kPair && p.mode == (int)TileMode::kRows && row0 >= it.row_end) row0 = (int)p.m;
           const int z_b = p.mode == (int)TileMode::kRows ? it.group : 0;
           const int cols_b = it.cols / S::kCtas, boxes_b = cols_b / 64;
           const uint32_t tx = (uint32_t)(kBytesA + boxes_b * kBoxBytes);
