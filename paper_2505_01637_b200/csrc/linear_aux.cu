@@ -283,26 +283,43 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(const CombineParams p
   float sum[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < p.topk; ++k) {
-    const int32_t row = p.slot[t * p.topk + k];
-    if (row < 0) continue;
-    const float w = p.weights ? p.weights[t * p.topk + k] : 1.f;
-    float v[8];
-    if constexpr (kF32) {
-      const float* y = static_cast<const float*>(p.Y) + (int64_t)row * p.y_pitch + col;
-      if (vec_y) {
-        const float4 a = reinterpret_cast<const float4*>(y)[0], b = reinterpret_cast<const float4*>(y)[1];
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-      } else {
+  // Four places at a time, their rows' loads in flight together.
+  for (int k0 = 0; k0 < p.topk; k0 += 4) {
+    int32_t row[4];
+    float w[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < left ? y[e] : 0.f;
+    for (int i = 0; i < 4; ++i) {
+      const bool there = k0 + i < p.topk;
+      row[i] = there ? p.slot[t * p.topk + k0 + i] : -1;
+      w[i] = there && p.weights ? p.weights[t * p.topk + k0 + i] : 1.f;
+    }
+    float v[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+      if (row[i] < 0) continue;
+      if constexpr (kF32) {
+        const float* y = static_cast<const float*>(p.Y) + (int64_t)row[i] * p.y_pitch + col;
+        if (vec_y) {
+          const float4 a = reinterpret_cast<const float4*>(y)[0], b = reinterpret_cast<const float4*>(y)[1];
+          v[i][0] = a.x; v[i][1] = a.y; v[i][2] = a.z; v[i][3] = a.w;
+          v[i][4] = b.x; v[i][5] = b.y; v[i][6] = b.z; v[i][7] = b.w;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < left) v[i][e] = y[e];
+        }
+      } else {
+        unpack8(load8_raw(static_cast<const uint16_t*>(p.Y) + (int64_t)row[i] * p.y_pitch + col, p.width_y, left), v[i]);
       }
-    } else {
-      unpack8(load8_raw(static_cast<const uint16_t*>(p.Y) + (int64_t)row * p.y_pitch + col, p.width_y, left), v);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] = fmaf(w, v[e], sum[e]);
+    for (int i = 0; i < 4; ++i) {
+      if (row[i] < 0) continue;        // not routed: nothing is added, whatever the weight
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] = fmaf(w[i], v[i][e], sum[e]);
+    }
   }
   if (p.residual) {
     float r[8];
