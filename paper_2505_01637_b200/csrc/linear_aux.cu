@@ -79,6 +79,7 @@ struct CopyParams {
   uint4* dst;
   int64_t rows_in, cols_in, rows_out;
   int octets;                 // 8-column groups of a row of dst
+  int spans;                  // > 0: blocks to a row group
   int width;                  // elements per access of src
   int row_groups;             // of kCopyRows rows in a group of dst
   int64_t threads;            // groups * row_groups * octets
@@ -95,19 +96,31 @@ struct CopyBatch {
 
 __global__ void __launch_bounds__(kThreads) copy_kernel(const CopyBatch batch) {
   const bool second = (int)blockIdx.x >= batch.blocks0;
-  const CopyParams& p = batch.job[second ? 1 : 0];
-  const int64_t idx = (int64_t)((int)blockIdx.x - (second ? batch.blocks0 : 0)) * kThreads + threadIdx.x;
-  // 32-bit divisions where they do (64-bit ones are a hundred instructions each).
+  const CopyParams p = second ? batch.job[1] : batch.job[0];     // by value: through an index every field is a load
+  const int block = (int)blockIdx.x - (second ? batch.blocks0 : 0);
+  // Long rows: a block is a span of kThreads octets of a row group, one division for all its threads.  Short ones:
+  // row groups and octets are numbered through (a 64-bit division is a hundred instructions, so 32 bits where they do).
   const bool small = p.threads < (1ll << 31);
-  const int64_t row_group = small ? (int64_t)((uint32_t)idx / (uint32_t)p.octets) : idx / p.octets;
-  const int o = (int)(idx - row_group * p.octets);
+  int64_t row_group;
+  int o;
+  bool mine = true;
+  if (p.spans > 0) {
+    row_group = (uint32_t)block / (uint32_t)p.spans;
+    o = (block - (int)row_group * p.spans) * kThreads + threadIdx.x;
+    mine = o < p.octets;
+  } else {
+    const int64_t idx = (int64_t)block * kThreads + threadIdx.x;
+    row_group = small ? (int64_t)((uint32_t)idx / (uint32_t)p.octets) : idx / p.octets;
+    o = (int)(idx - row_group * p.octets);
+    mine = idx < p.threads;
+  }
   const int64_t g = small ? (int64_t)((uint32_t)row_group / (uint32_t)p.row_groups) : row_group / p.row_groups;
   const int64_t r0 = (row_group - g * p.row_groups) * kCopyRows;
   pdl_wait();
   pdl_release();
-  if (idx >= p.threads || (p.live && r0 >= *p.live) || (p.counts && p.counts[g] == 0)) return;
+  if (!mine || (p.live && r0 >= *p.live) || (p.counts && p.counts[g] == 0)) return;
   const int64_t left = p.cols_in - (int64_t)o * 8;
-  uint4 w[kCopyRows];
+  const uint16_t* src[kCopyRows];
 #pragma unroll
   for (int i = 0; i < kCopyRows; ++i) {
     const int64_t r = r0 + i;
@@ -116,9 +129,21 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(const CopyBatch batch) {
       const int32_t s = p.row_src[r];
       from = s < 0 ? -1 : s / p.topk;
     }
-    w[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (r < p.rows_out && from >= 0 && from < p.rows_in && left > 0)
-      w[i] = load8_raw(p.src + (g * p.rows_in + from) * p.cols_in + (int64_t)o * 8, p.width, left);
+    const bool there = r < p.rows_out && from >= 0 && from < p.rows_in && left > 0;
+    src[i] = there ? p.src + (g * p.rows_in + from) * p.cols_in + (int64_t)o * 8 : nullptr;
+  }
+  uint4 w[kCopyRows];
+  const bool octets = p.width == 8;        // one test for all rows, so that their loads go out together
+#pragma unroll
+  for (int i = 0; i < kCopyRows; ++i) w[i] = make_uint4(0u, 0u, 0u, 0u);
+  if (octets) {
+#pragma unroll
+    for (int i = 0; i < kCopyRows; ++i)
+      if (src[i]) w[i] = *reinterpret_cast<const uint4*>(src[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kCopyRows; ++i)
+      if (src[i]) w[i] = load8_raw(src[i], p.width, left);
   }
 #pragma unroll
   for (int i = 0; i < kCopyRows; ++i)
@@ -364,7 +389,9 @@ cudaError_t copy_launch(const CopyJob* jobs, int count, cudaStream_t stream, uin
         p.topk = (int)j.experts->topk;
       }
     }
-    const int64_t mine = (p.threads + kThreads - 1) / kThreads;
+    // Spans where they leave few threads of a block without work.
+    p.spans = p.octets % kThreads == 0 || p.octets > 4 * kThreads ? (p.octets + kThreads - 1) / kThreads : 0;
+    const int64_t mine = p.spans > 0 ? j.groups * (int64_t)p.row_groups * p.spans : (p.threads + kThreads - 1) / kThreads;
     if (mine <= 0) continue;
     if (at == 0) batch.blocks0 = (int)std::min<int64_t>(mine, (1ll << 31) - 1);
     batch.job[at++] = p;
