@@ -35,10 +35,15 @@ __device__ __forceinline__ uint4 load8_raw(const uint16_t* src, int width, int64
       const uint2 a = reinterpret_cast<const uint2*>(src)[0], b = reinterpret_cast<const uint2*>(src)[1];
       return make_uint4(a.x, a.y, b.x, b.y);
     }
-    if (width == 2) {
+    // Rows of odd length start on 4-byte boundaries and off them in turn.
+    if (width == 2 || (reinterpret_cast<uintptr_t>(src) & 2u) == 0) {
       const uint32_t* q = reinterpret_cast<const uint32_t*>(src);
       return make_uint4(q[0], q[1], q[2], q[3]);
     }
+    const uint32_t first = src[0], last = src[7];
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(src + 1);
+    const uint32_t a = q[0], b = q[1], c = q[2];
+    return make_uint4(first | (a << 16), (a >> 16) | (b << 16), (b >> 16) | (c << 16), (c >> 16) | (last << 16));
   }
   uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
