@@ -69,9 +69,18 @@ struct TileCall {
   ExpertRows experts;
   LinearEpilogue epi;
 };
-// One product, or two (of which only the first may be kRows), in one launch.
-cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count, cudaStream_t stream,
-                        uint64_t* launches);
+// Column sums from partial sums of kSlopeRows rows each: db[g][c] = the partial sums of group g's rows, in a fixed order.
+constexpr int kSlopeRows = 32;
+struct ColumnSums {
+  const float* partial = nullptr;    // [parts][width]
+  float* db = nullptr;               // [groups][width]
+  int64_t width = 0, parts = 0, groups = 1;
+  const int32_t* offsets = nullptr;  // first row of every group (multiples of kSlopeRows), or null: one group
+  bool accumulate = false;
+};
+// One product, or two (of which only the first may be kRows), in one launch; two take the column sums with them.
+cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count, const ColumnSums* sums,
+                        cudaStream_t stream, uint64_t* launches);
 
 // The few-rows kernel: at most kLinearFewRows rows (per expert), B streamed once.
 constexpr int kLinearFewRows = 64;
@@ -87,25 +96,27 @@ struct CopyJob {
   const ExpertRows* by_expert = nullptr;  // groups are experts: those without rows are left alone
 };
 constexpr int kMaxCopies = 2;
-cudaError_t copy_launch(const CopyJob* jobs, int count, cudaStream_t stream, uint64_t* launches);   // one launch
+// One launch.  beside: the launch before it, of the same call, writes nothing that the copies read or overwrite, and
+// they are made while it runs.
+cudaError_t copy_launch(const CopyJob* jobs, int count, bool beside, cudaStream_t stream, uint64_t* launches);
 
 // dZ = dY . act'(Z) into dZ [rows][width rounded up to 8] (bf16, the added columns zero; width = n or
-// 2 n), and, when db is given, the column sums of dZ (per expert with experts) in f32, in a fixed order through
-// `partial`.  z may be null for act none without gating.
+// 2 n), and, when `partial` is given, the partial column sums of dZ in f32, of kSlopeRows
+// rows each.  z may be null for act none without gating.
 struct SlopeCall {
   int act = 0;
   bool gated = false;
   const uint16_t* dY = nullptr;
   const uint16_t* Z = nullptr;
   uint16_t* dZ = nullptr;     // null: only the column sums are wanted
-  float* db = nullptr;
-  float* partial = nullptr;
-  bool accumulate = false;
+  float* partial = nullptr;   // the column sums' parts, or null
   int64_t rows = 0, n = 0;    // rows of dY (with experts: the layout's rows)
   const ExpertRows* experts = nullptr;  // rows past the live ones are left alone
 };
 size_t slope_partial_bytes(int64_t rows, int64_t n, bool gated);
-cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& call, cudaStream_t stream, uint64_t* launches);
+cudaError_t slope_launch(const SlopeCall& call, cudaStream_t stream, uint64_t* launches);
+// The column sums alone.
+cudaError_t slope_sum_launch(const ColumnSums& sums, cudaStream_t stream, uint64_t* launches);
 
 // out[t] = residual[t] + sum_k weight[t][k] * Y[slot[t][k]]
 cudaError_t combine_launch(const ExpertRows& x, bool y_f32, int64_t n, int64_t y_pitch, const float* weights,

@@ -95,8 +95,8 @@ int check_experts(int64_t tokens, int64_t topk, int64_t experts) {
 struct Copies {
   CopyJob job[kMaxCopies];
   int count = 0;
-  int launch(cudaStream_t s, uint64_t* launches) {
-    const cudaError_t e = copy_launch(job, count, s, launches);
+  int launch(bool beside, cudaStream_t s, uint64_t* launches) {
+    const cudaError_t e = copy_launch(job, count, beside, s, launches);
     return e == cudaSuccess ? MORELLO_OK : record_cuda_error(e);
   }
 };
@@ -163,7 +163,7 @@ struct ForwardArgs {
 };
 
 int product(const DeviceInfo& dev, const Layer& l, const TileCall& c, cudaStream_t s, uint64_t* launches) {
-  const cudaError_t e = few_rows(l) ? rows_launch(dev, c, s, launches) : tile_launch(dev, &c, 1, s, launches);
+  const cudaError_t e = few_rows(l) ? rows_launch(dev, c, s, launches) : tile_launch(dev, &c, 1, nullptr, s, launches);
   return e == cudaSuccess ? MORELLO_OK : record_cuda_error(e);
 }
 
@@ -178,7 +178,7 @@ int forward(const DeviceInfo& dev, const Layer& l, const ForwardArgs& a, Carver&
     stage_w(l, a.W, true, ws, dry, &copies, &w, &up);
   }
   if (!ws.base) return MORELLO_OK;
-  if (const int rc = copies.launch(s, launches)) return rc;
+  if (const int rc = copies.launch(false, s, launches)) return rc;
   TileCall c;
   c.mode = l.grouped ? TileMode::kRows : TileMode::kDense;
   c.a = x;
@@ -225,20 +225,31 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
     dz = dz_own;
   }
   float* partial = a.db || dry ? ws.take<float>(slope_partial_bytes(l.m, l.n, l.gated)) : nullptr;
-  if (ws.base && (dz_own || a.db)) {
+  // The slopes' launch writes dZ and the partial sums; the copies of X and W run beside it.  The bias gradient's last sums
+  // go with the products where those are one launch.
+  const bool slopes = dz_own || a.db, one_launch = want_dx && want_dw && !few_rows(l);
+  ColumnSums sums;
+  if (ws.base && slopes) {
     SlopeCall c;
     c.act = l.act;
     c.gated = l.gated;
     c.dY = static_cast<const uint16_t*>(a.dY);
     c.Z = plain ? nullptr : static_cast<const uint16_t*>(a.Z);
     c.dZ = dz_own;
-    c.db = a.db;
-    c.partial = partial;
-    c.accumulate = a.accumulate;
+    c.partial = a.db ? partial : nullptr;
     c.rows = l.m;
     c.n = l.n;
     c.experts = l.grouped ? &l.x : nullptr;
-    if ((e = slope_launch(dev, c, s, launches)) != cudaSuccess) return record_cuda_error(e);
+    if ((e = slope_launch(c, s, launches)) != cudaSuccess) return record_cuda_error(e);
+    sums.partial = partial;
+    sums.db = a.db;
+    sums.width = wide;
+    sums.parts = (l.m + kSlopeRows - 1) / kSlopeRows;
+    sums.accumulate = a.accumulate;
+    if (l.grouped) {
+      sums.groups = l.groups;
+      sums.offsets = l.x.offsets;
+    }
   }
   const MatrixView z{dz, direct ? l.n : wide8, l.m, 1};
   MatrixView x, w;
@@ -250,7 +261,8 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
   }
   if (want_dw) stage_x(l, a.X, l.gather, ws, dry, &copies, &x);
   if (!ws.base) return MORELLO_OK;
-  if ((rc = copies.launch(s, launches)) != MORELLO_OK) return rc;
+  if ((rc = copies.launch(slopes, s, launches)) != MORELLO_OK) return rc;
+  if (a.db && !one_launch && (e = slope_sum_launch(sums, s, launches)) != cudaSuccess) return record_cuda_error(e);
   TileCall calls[2];
   int count = 0;
   if (want_dx) {
@@ -287,7 +299,8 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
     c.epi.accumulate = a.accumulate;
     c.epi.Y = a.dW;
   }
-  if (count > 0 && (e = tile_launch(dev, calls, count, s, launches)) != cudaSuccess) return record_cuda_error(e);
+  const ColumnSums* with = a.db && one_launch ? &sums : nullptr;
+  if (count > 0 && (e = tile_launch(dev, calls, count, with, s, launches)) != cudaSuccess) return record_cuda_error(e);
   if (rows) {
     e = combine_launch(l.x, true, l.k, l.k, nullptr, rows, nullptr, static_cast<uint16_t*>(a.dX), s, launches);
     if (e != cudaSuccess) return record_cuda_error(e);

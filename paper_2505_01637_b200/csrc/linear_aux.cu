@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "activation.cuh"
+#include "column_sums.cuh"
 #include "linear.h"
 #include "sm100.cuh"
 
@@ -13,7 +14,6 @@ namespace {
 using namespace sm100;
 
 constexpr int kThreads = 256;
-constexpr int kSlopeRows = 32;      // rows per partial sum of the bias gradient
 constexpr int kSlopeUnroll = 2;     // rows a thread has in flight: four blocks fit an SM's registers (with four rows, two
                                     // blocks, and 48 instead of 39 us on 18,400 x 2 x 1024)
 constexpr int kSlopeLanes = 8;      // rows a block takes at a time
@@ -97,33 +97,11 @@ struct CopyParams {
 struct CopyBatch {
   CopyParams job[kMaxCopies];
   int blocks0;                // blocks of the first job
+  bool beside;                // made while the launch before runs: waits for it at the end
 };
 
-__global__ void __launch_bounds__(kThreads) copy_kernel(const CopyBatch batch) {
-  const bool second = (int)blockIdx.x >= batch.blocks0;
-  const CopyParams p = second ? batch.job[1] : batch.job[0];     // by value: through an index every field is a load
-  const int block = (int)blockIdx.x - (second ? batch.blocks0 : 0);
-  // Long rows: a block is a span of kThreads octets of a row group, one division for all its threads.  Short ones:
-  // row groups and octets are numbered through (a 64-bit division is a hundred instructions, so 32 bits where they do).
-  const bool small = p.threads < (1ll << 31);
-  int64_t row_group;
-  int o;
-  bool mine = true;
-  if (p.spans > 0) {
-    row_group = (uint32_t)block / (uint32_t)p.spans;
-    o = (block - (int)row_group * p.spans) * kThreads + threadIdx.x;
-    mine = o < p.octets;
-  } else {
-    const int64_t idx = (int64_t)block * kThreads + threadIdx.x;
-    row_group = small ? (int64_t)((uint32_t)idx / (uint32_t)p.octets) : idx / p.octets;
-    o = (int)(idx - row_group * p.octets);
-    mine = idx < p.threads;
-  }
-  const int64_t g = small ? (int64_t)((uint32_t)row_group / (uint32_t)p.row_groups) : row_group / p.row_groups;
-  const int64_t r0 = (row_group - g * p.row_groups) * kCopyRows;
-  pdl_wait();
-  pdl_release();
-  if (!mine || (p.live && r0 >= *p.live) || (p.counts && p.counts[g] == 0)) return;
+// Rows r0 .. of group g, columns 8 o .. of dst.
+__device__ __forceinline__ void copy_rows(const CopyParams& p, int64_t g, int64_t r0, int o) {
   const int64_t left = p.cols_in - (int64_t)o * 8;
   const uint16_t* src[kCopyRows];
 #pragma unroll
@@ -153,6 +131,36 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(const CopyBatch batch) {
 #pragma unroll
   for (int i = 0; i < kCopyRows; ++i)
     if (r0 + i < p.rows_out) p.dst[(g * p.rows_out + r0 + i) * p.octets + o] = w[i];
+}
+
+__global__ void __launch_bounds__(kThreads) copy_kernel(const CopyBatch batch) {
+  const bool second = (int)blockIdx.x >= batch.blocks0;
+  const CopyParams p = second ? batch.job[1] : batch.job[0];     // by value: through an index every field is a load
+  const int block = (int)blockIdx.x - (second ? batch.blocks0 : 0);
+  // Long rows: a block is a span of kThreads octets of a row group, one division for all its threads.  Short ones:
+  // row groups and octets are numbered through (a 64-bit division is a hundred instructions, so 32 bits where they do).
+  const bool small = p.threads < (1ll << 31);
+  int64_t row_group;
+  int o;
+  bool mine = true;
+  if (p.spans > 0) {
+    row_group = (uint32_t)block / (uint32_t)p.spans;
+    o = (block - (int)row_group * p.spans) * kThreads + threadIdx.x;
+    mine = o < p.octets;
+  } else {
+    const int64_t idx = (int64_t)block * kThreads + threadIdx.x;
+    row_group = small ? (int64_t)((uint32_t)idx / (uint32_t)p.octets) : idx / p.octets;
+    o = (int)(idx - row_group * p.octets);
+    mine = idx < p.threads;
+  }
+  const int64_t g = small ? (int64_t)((uint32_t)row_group / (uint32_t)p.row_groups) : row_group / p.row_groups;
+  const int64_t r0 = (row_group - g * p.row_groups) * kCopyRows;
+  // beside: what came before the launch that this one follows is complete, since this one starts when all blocks of that
+  // one are past their own wait.  The wait at the end makes this one's end the end of both.
+  if (!batch.beside) pdl_wait();
+  pdl_release();
+  if (mine && !(p.live && r0 >= *p.live) && !(p.counts && p.counts[g] == 0)) copy_rows(p, g, r0, o);
+  if (batch.beside) pdl_wait();
 }
 
 struct SlopeParams {
@@ -258,32 +266,10 @@ __global__ void __launch_bounds__(kThreads, kSums ? 3 : 4) slope_kernel(const Sl
   }
 }
 
-// db[g][c] = the partial sums of group g's rows, in order: eight strided runs, then the eight.
-__global__ void __launch_bounds__(kThreads)
-slope_sum_kernel(const float* partial, float* db, int64_t width, int64_t parts, const int32_t* offsets, bool accumulate) {
-  __shared__ float sums[8][33];
-  const int x = threadIdx.x & 31, lane = threadIdx.x >> 5;
-  const int64_t c = (int64_t)blockIdx.x * 32 + x;
+__global__ void __launch_bounds__(kThreads) slope_sum_kernel(const ColumnSums c) {
   pdl_wait();
   pdl_release();
-  const int64_t g = blockIdx.y;
-  int64_t first = 0, last = parts;
-  if (offsets) {
-    first = offsets[g] / kSlopeRows;
-    last = offsets[g + 1] / kSlopeRows;
-  }
-  float s = 0.f;
-  if (c < width)
-    for (int64_t i = first + lane; i < last; i += 8) s += partial[i * width + c];
-  sums[lane][x] = s;
-  __syncthreads();
-  if (lane == 0 && c < width) {
-    float total = 0.f;
-#pragma unroll
-    for (int l = 0; l < 8; ++l) total += sums[l][x];
-    float* dst = db + g * width + c;
-    *dst = accumulate ? *dst + total : total;
-  }
+  column_sums(c, (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), (int64_t)gridDim.x * (kThreads / 32), threadIdx.x & 31);
 }
 
 struct CombineParams {
@@ -369,9 +355,10 @@ cudaError_t grid_for(int64_t threads, unsigned* blocks) {
 
 }  // namespace
 
-cudaError_t copy_launch(const CopyJob* jobs, int count, cudaStream_t stream, uint64_t* launches) {
+cudaError_t copy_launch(const CopyJob* jobs, int count, bool beside, cudaStream_t stream, uint64_t* launches) {
   if (count > kMaxCopies) return cudaErrorInvalidValue;
   CopyBatch batch{};
+  batch.beside = beside;
   int64_t blocks = 0;
   int at = 0;
   for (int i = 0; i < count; ++i) {
@@ -413,8 +400,7 @@ size_t slope_partial_bytes(int64_t rows, int64_t n, bool gated) {
   return (size_t)((rows + kSlopeRows - 1) / kSlopeRows) * n * (gated ? 2 : 1) * 4;
 }
 
-cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& c, cudaStream_t stream, uint64_t* launches) {
-  (void)dev;
+cudaError_t slope_launch(const SlopeCall& c, cudaStream_t stream, uint64_t* launches) {
   if (c.n <= 0) return cudaSuccess;
   const int64_t parts = (c.rows + kSlopeRows - 1) / kSlopeRows;
   const int64_t width = c.gated ? 2 * c.n : c.n;
@@ -424,7 +410,7 @@ cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& c, cudaStream_t
     p.dY = c.dY;
     p.Z = c.Z;
     p.dZ = c.dZ;
-    p.partial = c.db ? c.partial : nullptr;
+    p.partial = c.partial;
     p.rows = c.rows;
     p.n = c.n;
     p.pitch = (width + 7) / 8 * 8;
@@ -468,13 +454,15 @@ cudaError_t slope_launch(const DeviceInfo& dev, const SlopeCall& c, cudaStream_t
     if (e != cudaSuccess) return e;
     ++*launches;
   }
-  if (c.db) {
-    const int64_t groups = c.experts ? c.experts->experts : 1;
-    e = launch_pdl(slope_sum_kernel, dim3((unsigned)((width + 31) / 32), (unsigned)groups), dim3(kThreads), 0, stream, 1,
-                   (const float*)c.partial, c.db, width, parts,
-                   c.experts ? c.experts->offsets : (const int32_t*)nullptr, c.accumulate);
-    if (e == cudaSuccess) ++*launches;
-  }
+  return e;
+}
+
+cudaError_t slope_sum_launch(const ColumnSums& c, cudaStream_t stream, uint64_t* launches) {
+  const int64_t items = c.groups * ((c.width + kSumColumns - 1) / kSumColumns);
+  if (items <= 0) return cudaSuccess;
+  const int64_t blocks = std::min<int64_t>((items + kThreads / 32 - 1) / (kThreads / 32), 1 << 20);
+  const cudaError_t e = launch_pdl(slope_sum_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, stream, 1, c);
+  if (e == cudaSuccess) ++*launches;
   return e;
 }
 
