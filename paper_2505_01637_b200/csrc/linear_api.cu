@@ -1,5 +1,6 @@
 // C entry points of the feed-forward operators: argument checks, workspaces and the sequence of launches.
 #include <algorithm>
+#include <utility>
 
 #include "../../include/morello.h"
 #include "activation.cuh"
@@ -299,6 +300,8 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
     c.epi.accumulate = a.accumulate;
     c.epi.Y = a.dW;
   }
+  // The product with the longer tiles first: the other's fill up what its last wave leaves (experts: their rows first).
+  if (count == 2 && !l.grouped && calls[1].k > calls[0].k) std::swap(calls[0], calls[1]);
   const ColumnSums* with = a.db && one_launch ? &sums : nullptr;
   if (count > 0 && (e = tile_launch(dev, calls, count, with, s, launches)) != cudaSuccess) return record_cuda_error(e);
   if (rows) {

@@ -26,6 +26,7 @@
 // measured slower (their share of the registers spills: 4096 x 4096 x 4096 with GELU, bias, residual and Z
 // 116, 123 and 127 us).
 #include <algorithm>
+#include <cmath>
 
 #include "activation.cuh"
 #include "column_sums.cuh"
@@ -73,6 +74,7 @@ struct TileParams {
   int k_blocks;          // contraction blocks (kContract: of the expert, from counts)
   int m_tiles, n_tiles;
   int64_t tiles;         // kRows: decided on the device
+  int lead;              // second product: its items that a unit takes in place of one of the first's
   int b_up;
   uint8_t mode, a_mn, b_mn, zero_padding, halves;
   // experts
@@ -115,10 +117,12 @@ struct Item {
 // flight share a few rows of A and a few columns of B in L2.
 constexpr int kRasterLog = 3, kRaster = 1 << kRasterLog;
 
-// What the tile loop walks: whole tiles, then the column halves of the last wave's.
+// What the tile loop walks: whole tiles, then the column halves of the last wave's.  The units take turns, but the first
+// `lead` items go to the units from `idle` on, which the product before left without a share of its last wave.
 struct Walk {
   int m_tiles, n_tiles;
   int whole, items;
+  int lead, idle;
 };
 
 // A role's place in the walk.  It moves by additions: an item is decoded by every role of a block, and with
@@ -127,21 +131,25 @@ template <bool kPair, int kTileN>
 class Cursor {
  public:
   __device__ __forceinline__ Cursor(const TileParams& p, const Walk& w, const int* pairs_before, int unit, int units)
-      : p_(p), w_(w), pairs_before_(pairs_before), units_(units), t_(unit) {
-    at_ = unit;
-    settle();
+      : p_(p), w_(w), pairs_before_(pairs_before), unit_(unit), units_(units) {
+    const bool leads = unit >= w.idle && w.lead > 0;
+    t_ = leads ? unit - w.idle : w.lead + unit;
+    step_ = leads ? units - w.idle : units;
+    if (leads && t_ >= w.lead) join();
+    place();
   }
   __device__ __forceinline__ bool valid() const { return t_ < w_.items; }
   __device__ __forceinline__ bool is_half() const { return t_ >= w_.whole; }
   __device__ __forceinline__ void next() {
-    t_ += units_;
-    if (t_ < w_.whole) {
-      at_ += units_;
+    t_ += step_;
+    if (step_ != units_ && t_ >= w_.lead) {
+      join();
+      place();
+    } else if (t_ < w_.whole) {
+      at_ += step_;
       settle();
-    } else if (t_ < w_.items) {      // once or twice a launch
-      at_ = w_.whole + ((t_ - w_.whole) >> 1);
-      expert_ = grp_ = 0;
-      settle();
+    } else {                         // once or twice a launch
+      place();
     }
   }
   __device__ __forceinline__ Item item() const {
@@ -184,6 +192,17 @@ class Cursor {
   }
 
  private:
+  // From the leading items on to the turns of all units.
+  __device__ __forceinline__ void join() {
+    t_ = w_.lead + unit_;
+    step_ = units_;
+  }
+  __device__ __forceinline__ void place() {
+    if (t_ >= w_.items) return;
+    at_ = t_ < w_.whole ? t_ : w_.whole + ((t_ - w_.whole) >> 1);
+    expert_ = grp_ = 0;
+    settle();
+  }
   // Carries at_ into the expert (kContract) and the group of rows of tiles it lies in.
   __device__ __forceinline__ void settle() {
     if (p_.mode == (int)TileMode::kContract) {
@@ -197,8 +216,8 @@ class Cursor {
   const TileParams& p_;
   const Walk& w_;
   const int* pairs_before_;
-  const int units_;
-  int t_, at_ = 0, grp_ = 0, expert_ = 0;
+  const int unit_, units_;
+  int t_, step_, at_ = 0, grp_ = 0, expert_ = 0;
 };
 
 constexpr uint32_t kFullMask = 0xffffffffu;
@@ -611,8 +630,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
   tc_fence_after_sync();
   const uint32_t tmem_base = bars->tmem_base;
 
-  // Where a product's walk begins for this unit: the second goes on where the first left off.
-  auto walk_of = [&](int q, Walk* w) {
+  // A product's walk; before: the items of the product before it.
+  auto walk_of = [&](int q, int before, Walk* w) {
     const TileParams& p = batch.p[q];
     w->m_tiles = p.m_tiles;
     w->n_tiles = p.n_tiles;
@@ -621,12 +640,13 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
       w->m_tiles = kPair ? bars->pairs_before[p.experts] : p.offsets[p.experts] / kExpertBlock;
       tiles = w->m_tiles * p.n_tiles;
     }
+    w->idle = before % units;
+    w->lead = w->idle > 0 ? min(p.lead * (units - w->idle), tiles) : 0;
     // The tiles of a last wave that would occupy at most half the units are cut into column halves.
-    const int tail = tiles % units;
+    const int tail = (tiles - w->lead) % units;
     w->whole = p.halves && tiles > units && tail > 0 && 2 * tail <= units ? tiles - tail : tiles;
     w->items = w->whole + 2 * (tiles - w->whole);
   };
-  auto next_unit = [&](int unit_now, const Walk& w) { return (unit_now + units - w.items % units) % units; };
 
   if (warp == 0) {
     // ------------------------------------------------------------------ producer
@@ -636,16 +656,16 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
       bool ok = true;
       const uint32_t leader_full = kPair ? map_to_cta(smem_u32(&bars->full[0]), 0) : 0u;
       (void)leader_full;
-      int from = unit;
+      int before = 0;
       for (int q = 0; q < (kTwo ? 2 : 1); ++q) {
       const TileParams& p = batch.p[q];
       const CUtensorMap* map_a   = &batch.a[q];
         const CUtensorMap* map_b = &batch.b[q];
         Walk w;
-        walk_of(q, &w);
+        walk_of(q, before, &w);
         // The k loop is kept short: one thread issues it, and everything in it delays the next load.
         const bool a_mn = p.a_mn != 0, b_mn = p.b_mn != 0;
-        for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, from, units); at.valid() && ok; at.next()) {
+        for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units); at.valid() && ok; at.next()) {
           const Item it = at.item();
           int row0 = it.row0 + (int)rank * kRowsPerCta;
           // An expert's odd block leaves the pair's second CTA without rows: zeros cost less power than the next
@@ -690,7 +710,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
             if (++stage == S::kStages) { stage = 0; phase ^= 1; }
           }
         }
-      from = next_unit(from, w);
+      before = w.items;
       }
     }
   } else if (warp == 1) {
@@ -701,18 +721,18 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
       int buf = 0;
       uint32_t acc_phase = 0;
       bool ok = true;
-      int from = unit;
+      int before = 0;
       for (int q = 0; q < (kTwo ? 2 : 1); ++q) {
         const TileParams& p = batch.p[q];
         Walk w;
-        walk_of(q, &w);
+        walk_of(q, before, &w);
         const uint32_t idesc_tile = instr_desc_bf16(S::kTileM, kTileN, p.a_mn != 0, p.b_mn != 0);
         const uint32_t idesc_half = instr_desc_bf16(S::kTileM, kTileN / 2, p.a_mn != 0, p.b_mn != 0);
         // Across the contraction: 64-column groups one box apart, 16 contraction rows = 2048 bytes.
         // Along it: 8-row groups 1024 bytes apart, 16 elements = 32 bytes along the row.
         const uint32_t step_a = p.a_mn ? 2048u : 32u, step_b = p.b_mn ? 2048u : 32u;
         const uint32_t lbo_a = p.a_mn ? kBoxBytes : 16u, lbo_b = p.b_mn ? kBoxBytes : 16u;
-        for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, from, units); at.valid() && ok; at.next()) {
+        for (Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units); at.valid() && ok; at.next()) {
           // The place of the tile does not matter here; its width and, by expert, its depth do.
           int k_blocks = p.k_blocks, k_steps = kTileK / 16;
           if (p.mode == (int)TileMode::kContract) {
@@ -761,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
           else mma_commit(&bars->acc_full[buf]);
           if (++buf == 2) { buf = 0; acc_phase ^= 1; }
         }
-        from = next_unit(from, w);
+        before = w.items;
       }
     }
   } else {
@@ -777,14 +797,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
     int buf = 0;
     uint32_t acc_phase = 0;
     bool ok = true;
-    int from = unit;
+    int before = 0;
     for (int q = 0; q < (kTwo ? 2 : 1); ++q) {
       const TileParams& p = batch.p[q];
       const CUtensorMap& map_y = batch.y[q];
       const CUtensorMap& map_z = batch.z;
       Walk w;
-      walk_of(q, &w);
-      Cursor<kPair, kTileN> at(p, w, bars->pairs_before, from, units);
+      walk_of(q, before, &w);
+      Cursor<kPair, kTileN> at(p, w, bars->pairs_before, unit, units);
       Item ahead{};
       if (at.valid()) ahead = at.item();
       bool more = at.valid();
@@ -831,7 +851,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
       // A product's blocks are laid out as its outputs need them: none is pending when the next begins.
       if (lane == 0) bulk_wait_group_read<0>();
       __syncwarp();
-      from = next_unit(from, w);
+      before = w.items;
     }
     // Shared memory must outlive the engine's reads, and the stores must have been performed before the
     // kernel counts as complete.
@@ -912,31 +932,47 @@ bool form_allowed(const TileCall& c, const TileForm& f) {
   return f.tile_n > 64 || !c.epi.gated;
 }
 
-// The form with the least estimated time: whole waves of every product, then what is left of them -- side by side where
-// the units hold it, cut into column halves (about 0.6 of a wave) where a single product's leftover allows.
-TileForm choose_form(const DeviceInfo& dev, const TileCall* calls, int count, bool precise) {
+// Estimated time of a call's tiles in a form; lead: see TileParams.
+double form_time(const DeviceInfo& dev, const TileCall* calls, int count, const TileForm& f, int* lead) {
+  const int64_t units = std::max(1, f.pair ? gemm_pair_units(dev.sms) : dev.sms);
+  double each[kMaxProducts];
+  int64_t items[kMaxProducts];
+  for (int q = 0; q < count; ++q) {
+    double blocks = 0;
+    items[q] = tiles_of(calls[q], f, &blocks);
+    each[q] = std::max(blocks * f.block, f.epilogue) + 0.2;
+  }
+  *lead = count > 1 ? (int)std::min(1000.0, std::max(1.0, std::floor(each[0] / each[1] + 0.5))) : 0;
+  // The units that hold a tile of the first product's last wave, and those that do not.
+  const int64_t first = count > 1 ? items[0] : 0, held = first % units;
+  double busy = 0, idle = 0;
+  int64_t leading = 0;
+  if (count > 1) {
+    idle = (double)(first / units) * each[0];
+    busy = idle + (held > 0 ? each[0] : 0);
+    if (held > 0) {
+      leading = std::min<int64_t>(*lead * (units - held), items[1]);
+      idle += (double)((leading + units - held - 1) / (units - held)) * each[1];
+    }
+  }
+  const int q = count - 1;
+  const int64_t rest = items[q] - leading, tail = rest % units;
+  const bool cut = can_halve(f.pair, f.tile_n, calls[q].epi.gated) && items[q] > units && 2 * tail <= units;
+  const double last = tail == 0 ? 0 : cut ? 0.625 * each[q] : each[q];
+  busy += (double)(rest / units) * each[q] + last;
+  idle += (double)(rest / units) * each[q] + (tail > held ? last : 0);
+  return std::max(busy, idle);
+}
+
+TileForm choose_form(const DeviceInfo& dev, const TileCall* calls, int count, bool precise, int* lead) {
   double best = 0;
   int at = -1;
   for (int i = 0; i < (int)(sizeof(kForms) / sizeof(kForms[0])); ++i) {
-    const TileForm& f = kForms[i];
-    const int64_t units = std::max(1, f.pair ? gemm_pair_units(dev.sms) : dev.sms);
-    double cost = 0, last = 0;
-    int64_t left = 0;
-    bool allowed = !precise || f.tile_n == 128;
-    for (int q = 0; q < count; ++q) {
-      allowed = allowed && form_allowed(calls[q], f);
-      double blocks = 0;
-      const int64_t items = tiles_of(calls[q], f, &blocks), tail = items % units;
-      const double each = std::max(blocks * f.block, f.epilogue) + 0.2;
-      cost += (double)(items / units) * each;
-      if (tail > 0) {
-        const bool cut = count == 1 && can_halve(f.pair, f.tile_n, calls[q].epi.gated) && items > units && 2 * tail <= units;
-        last = left + tail <= units ? std::max(last, cut ? 0.625 * each : each) : last + each;
-        left += tail;
-      }
-    }
-    cost += last;
-    if (allowed && (at < 0 || cost < best)) { best = cost; at = i; }
+    bool allowed = !precise || kForms[i].tile_n == 128;
+    for (int q = 0; q < count; ++q) allowed = allowed && form_allowed(calls[q], kForms[i]);
+    int turn = 0;
+    const double cost = form_time(dev, calls, count, kForms[i], &turn);
+    if (allowed && (at < 0 || cost < best)) { best = cost; at = i; *lead = turn; }
   }
   return kForms[at < 0 ? 3 : at];
 }
@@ -953,7 +989,8 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count,
   bool precise = false;
   for (int q = 0; q < count; ++q)
     precise = precise || (calls[q].precise && calls[q].k > (calls[q].epi.gated ? kPreciseGated : kPreciseFrom));
-  const TileForm form = choose_form(dev, calls, count, precise);
+  int lead = 0;
+  const TileForm form = choose_form(dev, calls, count, precise, &lead);
   TileBatch batch{};
   if (sums) batch.sums = *sums;
   int64_t items = 0;
@@ -987,7 +1024,8 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count,
     p.Y = ep.Y;
     p.Z = ep.Z;
     p.status = dev.status;
-    p.halves = can_halve(form.pair, form.tile_n, ep.gated);
+    p.halves = q + 1 == count && can_halve(form.pair, form.tile_n, ep.gated);
+    p.lead = q > 0 ? lead : 0;
     const int64_t tile_m = kRowsPerCta << form.pair, out_cols = ep.gated ? form.tile_n / 2 : form.tile_n;
     const int64_t m_tiles = (c.m + tile_m - 1) / tile_m, n_tiles = (c.n + out_cols - 1) / out_cols;
     // Experts' pairs of blocks: up to one per block.
