@@ -617,16 +617,17 @@ __global__ void __launch_bounds__(1024) plan_place_kernel(const PlanParams p) {
   int32_t* first = hist + hist_stride() * p.experts;
   int32_t* mine = first + p.experts;
   int32_t* sums = mine + p.experts;
-  pdl_wait();
+  // The pairs were there before the launch that this one follows, which has passed its own wait by now, and that one
+  // writes neither them nor what is read here: the histograms are made beside it.
   pdl_release();
   const Span span = load_span(p, blockIdx.x);
   clear_histograms(p, hist);
+  fill_histograms(span, hist);
+  pdl_wait();
   if (p.chunks > kPlanDirect) {
-    fill_histograms(span, hist);
     warp_starts(p, hist, p.scratch + (int64_t)blockIdx.x * p.experts);
   } else {
     add_chunks(p, blockIdx.x, first, mine);
-    fill_histograms(span, hist);
     scan_experts(p, first, first, sums, blockIdx.x == 0);
     for (int e = threadIdx.x; e < p.experts; e += blockDim.x) first[e] += mine[e];
     __syncthreads();
