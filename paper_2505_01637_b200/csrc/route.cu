@@ -58,12 +58,15 @@ struct RouteParams {
   float scale;
 };
 
+// From this many experts per lane on the choice is among candidates.
+constexpr int kFewest = 4;
+
 // kPer: experts per lane.
-template <int kPer, bool kF32>
+template <int kPer, bool kF32, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
   extern __shared__ uint32_t group_keys[];       // [kWarps][experts] when experts are grouped
-  __shared__ uint2 candidates[kWarps][32];       // key and expert
-  __shared__ float candidate_x[kWarps][32];
+  __shared__ uint64_t candidates[kWarps][32];    // key and ~expert: among equal keys the lower expert is the larger
+  __shared__ int chosen[kWarps][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t t = (int64_t)blockIdx.x * kWarps + warp;
   pdl_wait();
@@ -76,13 +79,16 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
     const int e = i * 32 + lane;
     x[i] = e < p.experts ? load_logit<kF32>(p.logits, t * p.experts + e) : 0.f;
   }
+  float s[kPer];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int e = i * 32 + lane;
-    float s = p.sigmoid ? 1.f / (1.f + expf(-x[i])) : x[i];
-    if (p.bias && e < p.experts) s += p.bias[e];
-    key[i] = e < p.experts ? order_of(s) : 0u;
+  for (int i = 0; i < kPer; ++i) s[i] = kSigmoid ? 1.f / (1.f + expf(-x[i])) : x[i];
+  if (p.bias) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (i * 32 + lane < p.experts) s[i] += p.bias[i * 32 + lane];
   }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) key[i] = i * 32 + lane < p.experts ? order_of(s[i]) : 0u;
   if (p.groups > 1) {
     // Lane g scores group g: the sum of its two largest keys (sigmoid) or its largest (softmax).
     uint32_t* mine = group_keys + (size_t)warp * p.experts;
@@ -100,7 +106,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
         first = max(first, v);
       }
       score = first;
-      if (p.sigmoid) {
+      if constexpr (kSigmoid) {
         auto value = [](uint32_t o) {
           return o <= 1u ? __uint_as_float(0x7fc00000u) : __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
         };
@@ -122,57 +128,45 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
 
   // Lane j ends up with the j-th choice.
   int my_idx = -1;
-  float my_x = 0.f;
-  bool chosen = false;
-  if constexpr (kPer >= 4) {
-    uint32_t most = 0u;
+  bool done = false;
+  if constexpr (kPer >= kFewest) {
+    uint32_t left = 0u, bound = 0u;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) most = max(most, key[i]);
-    uint32_t bound = 0u, left = most;
+    for (int i = 0; i < kPer; ++i) left = max(left, key[i]);
+    // Equal maxima go together, which only lowers the bound.
     for (int j = 0; j < p.topk; ++j) {
       bound = __reduce_max_sync(kFull, left);
-      const uint32_t who = __ballot_sync(kFull, left == bound);
-      if (lane == __ffs(who) - 1) left = 0u;
+      if (left == bound) left = 0u;
     }
     // At least topk keys are >= bound (0 when lanes ran out: everything still in the choice is a candidate).
     bound = max(bound, 1u);
-    int count = 0;
+    int mine = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const uint32_t who = __ballot_sync(kFull, key[i] >= bound);
-      if (key[i] >= bound) {
-        const int at = count + __popc(who & ((1u << lane) - 1u));
-        if (at < 32) {
-          candidates[warp][at] = make_uint2(key[i], (uint32_t)(i * 32 + lane));
-          candidate_x[warp][at] = x[i];
-        }
-      }
-      count += __popc(who);
+    for (int i = 0; i < kPer; ++i) mine += key[i] >= bound ? 1 : 0;
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(kFull, upto, d);
+      if (lane >= d) upto += o;
     }
-    __syncwarp();
+    const int count = __shfl_sync(kFull, upto, 31);
     if (count <= 32) {
-      // In order of expert by construction, so among equal keys the earlier candidate comes first.
-      const uint2 mine = lane < count ? candidates[warp][lane] : make_uint2(0u, kNone);
+      uint64_t* at = &candidates[warp][upto - mine];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (key[i] >= bound) *at++ = (uint64_t)key[i] << 32 | ~(uint32_t)(i * 32 + lane);
+      __syncwarp();
+      const uint64_t own = candidates[warp][lane];       // past count: what an earlier use left, not looked at
       int place = 0;
-      for (int j = 0; j < count; ++j) {
-        const uint32_t other = __shfl_sync(kFull, mine.x, j);
-        place += (other > mine.x || (other == mine.x && j < lane)) ? 1 : 0;
-      }
-      const float x_mine = lane < count ? candidate_x[warp][lane] : 0.f;
+#pragma unroll 4
+      for (int j = 0; j < count; ++j) place += candidates[warp][j] > own ? 1 : 0;
+      if (lane < count && place < p.topk) chosen[warp][place] = (int)~(uint32_t)own;
       __syncwarp();
-      if (lane < count && place < p.topk) {
-        candidates[warp][place] = mine;
-        candidate_x[warp][place] = x_mine;
-      }
-      __syncwarp();
-      if (lane < p.topk) {
-        my_idx = (int)candidates[warp][lane].y;
-        my_x = candidate_x[warp][lane];
-      }
-      chosen = true;
+      if (lane < p.topk) my_idx = chosen[warp][lane];
+      done = true;
     }
   }
-  for (int j = 0; j < p.topk && !chosen; ++j) {
+  for (int j = 0; j < p.topk && !done; ++j) {
     uint32_t best = 0u;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) best = max(best, key[i]);
@@ -182,28 +176,24 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
     for (int i = kPer - 1; i >= 0; --i)
       if (key[i] == best) at = (uint32_t)(i * 32 + lane);
     at = __reduce_min_sync(kFull, at);
-    float v = 0.f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      if (at == (uint32_t)(i * 32 + lane)) {
-        key[i] = 0u;
-        v = x[i];
-      }
-    v = __shfl_sync(kFull, v, (int)(at & 31u));
-    if (lane == j) {
-      my_idx = (int)at;
-      my_x = v;
-    }
+      if (at == (uint32_t)(i * 32 + lane)) key[i] = 0u;
+    if (lane == j) my_idx = (int)at;
   }
+  const bool holds = lane < p.topk && my_idx >= 0 && my_idx < p.experts;
+  const float my_x = holds ? load_logit<kF32>(p.logits, t * p.experts + my_idx) : -INFINITY;
 
   float w = 0.f;
-  if (p.sigmoid) {
+  if constexpr (kSigmoid) {
     w = lane < p.topk ? 1.f / (1.f + expf(-my_x)) : 0.f;
   } else {
-    float m = -INFINITY;
+    float m = my_x;                        // among the chosen, whatever the others are, when only their shares count
+    if (!p.renorm) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (i * 32 + lane < p.experts) m = fmaxf(m, x[i]);
+      for (int i = 0; i < kPer; ++i)
+        if (i * 32 + lane < p.experts) m = fmaxf(m, x[i]);
+    }
     m = warp_max(m);
     if (m == -INFINITY) m = 0.f;           // nothing but masked logits: every weight is 0
     w = lane < p.topk ? expf(my_x - m) : 0.f;
@@ -348,16 +338,16 @@ __global__ void __launch_bounds__(kThreads) route_backward_kernel(const RouteBac
   }
 }
 
-template <bool kF32>
+template <bool kF32, bool kSigmoid>
 cudaError_t launch_route(const RouteParams& p, unsigned blocks, cudaStream_t stream) {
   const size_t smem = p.groups > 1 ? (size_t)kWarps * p.experts * 4 : 0;
   const dim3 g(blocks), b(kThreads);
-  if (p.experts <= 32) return launch_pdl(route_kernel<1, kF32>, g, b, smem, stream, 1, p);
-  if (p.experts <= 64) return launch_pdl(route_kernel<2, kF32>, g, b, smem, stream, 1, p);
-  if (p.experts <= 128) return launch_pdl(route_kernel<4, kF32>, g, b, smem, stream, 1, p);
-  if (p.experts <= 256) return launch_pdl(route_kernel<8, kF32>, g, b, smem, stream, 1, p);
-  if (p.experts <= 512) return launch_pdl(route_kernel<16, kF32>, g, b, smem, stream, 1, p);
-  return launch_pdl(route_kernel<32, kF32>, g, b, smem, stream, 1, p);
+  if (p.experts <= 32) return launch_pdl(route_kernel<1, kF32, kSigmoid>, g, b, smem, stream, 1, p);
+  if (p.experts <= 64) return launch_pdl(route_kernel<2, kF32, kSigmoid>, g, b, smem, stream, 1, p);
+  if (p.experts <= 128) return launch_pdl(route_kernel<4, kF32, kSigmoid>, g, b, smem, stream, 1, p);
+  if (p.experts <= 256) return launch_pdl(route_kernel<8, kF32, kSigmoid>, g, b, smem, stream, 1, p);
+  if (p.experts <= 512) return launch_pdl(route_kernel<16, kF32, kSigmoid>, g, b, smem, stream, 1, p);
+  return launch_pdl(route_kernel<32, kF32, kSigmoid>, g, b, smem, stream, 1, p);
 }
 template <bool kF32>
 cudaError_t launch_route_backward(const RouteBackParams& p, unsigned blocks, cudaStream_t stream) {
@@ -735,8 +725,9 @@ cudaError_t route_launch(const RouteCall& c, cudaStream_t stream, uint64_t* laun
   if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
   RouteParams p{c.logits, c.bias, c.idx, c.weights, c.tokens, (int)c.experts, (int)c.topk, (int)c.groups,
                 (int)c.topk_groups, c.sigmoid, c.renorm, c.scale};
-  const cudaError_t e = c.logits_f32 ? launch_route<true>(p, (unsigned)blocks, stream)
-                                     : launch_route<false>(p, (unsigned)blocks, stream);
+  const cudaError_t e =
+      c.logits_f32 ? (c.sigmoid ? launch_route<true, true> : launch_route<true, false>)(p, (unsigned)blocks, stream)
+                   : (c.sigmoid ? launch_route<false, true> : launch_route<false, false>)(p, (unsigned)blocks, stream);
   if (e == cudaSuccess) ++*launches;
   return e;
 }
