@@ -117,31 +117,42 @@ def lib() -> ctypes.CDLL:
 def _addr(x):
     if x is None:
         return None
-    if isinstance(x, int):
+    if type(x) is int:
         return x or None
-    if hasattr(x, "data_ptr"):
+    try:
         return x.data_ptr() or None
+    except AttributeError:
+        pass
     if hasattr(x, "ctypes"):          # numpy array (host entry point)
         return x.ctypes.data or None
+    if isinstance(x, int):
+        return x or None
     raise TypeError("expected a tensor, an array or an integer address, got %r" % type(x))
+
+
+_raw_stream = _device = None          # torch's own calls, once it has set the GPU up
 
 
 def _stream(stream):
     if stream is None:
-        torch = sys.modules.get("torch")
-        if torch is None:
-            return None
-        if not torch.cuda.is_initialized() and not torch.cuda.is_available():
-            return None
-        # The raw handle of the current device's current stream, where torch has a call for it: building a
-        # Stream object costs microseconds, as much as a small call's launch.
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is not None:
-            return raw(torch.cuda.current_device()) or None
-        return torch.cuda.current_stream().cuda_stream or None
+        return _raw_stream(_device()) or None if _raw_stream is not None else _torch_stream()
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
+
+
+def _torch_stream():
+    global _raw_stream, _device
+    torch = sys.modules.get("torch")
+    if torch is None or not (torch.cuda.is_initialized() or torch.cuda.is_available()):
+        return None
+    # The raw handle of the current device's current stream, where torch has the calls for it: building a Stream
+    # object, and the wrappers around these, cost microseconds, as much as a small call's launch.
+    now = torch.cuda.current_stream().cuda_stream or None
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is not None and device is not None:
+        _raw_stream, _device = raw, device
+    return now
 
 
 def _check(status: int, where: str) -> None:

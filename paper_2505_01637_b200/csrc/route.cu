@@ -61,14 +61,16 @@ struct RouteParams {
 // From this many experts per lane on the choice is among candidates.
 constexpr int kFewest = 4;
 
-// kPer: experts per lane.
-template <int kPer, bool kF32, bool kSigmoid>
+// kPer: experts per lane.  kWhole: every lane holds that many (a test per expert and phase: 10.7 instead of 9.2 us on
+// 16384 x 256).
+template <int kPer, bool kWhole, bool kF32, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
   extern __shared__ uint32_t group_keys[];       // [kWarps][experts] when experts are grouped
   __shared__ uint64_t candidates[kWarps][32];    // key and ~expert: among equal keys the lower expert is the larger
   __shared__ int chosen[kWarps][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t t = (int64_t)blockIdx.x * kWarps + warp;
+  const int experts = kWhole ? 32 * kPer : p.experts;
   pdl_wait();
   pdl_release();
   if (t >= p.tokens) return;
@@ -77,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int e = i * 32 + lane;
-    x[i] = e < p.experts ? load_logit<kF32>(p.logits, t * p.experts + e) : 0.f;
+    x[i] = e < experts ? load_logit<kF32>(p.logits, t * experts + e) : 0.f;
   }
   float s[kPer];
 #pragma unroll
@@ -85,18 +87,18 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
   if (p.bias) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      if (i * 32 + lane < p.experts) s[i] += p.bias[i * 32 + lane];
+      if (i * 32 + lane < experts) s[i] += p.bias[i * 32 + lane];
   }
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) key[i] = i * 32 + lane < p.experts ? order_of(s[i]) : 0u;
+  for (int i = 0; i < kPer; ++i) key[i] = i * 32 + lane < experts ? order_of(s[i]) : 0u;
   if (p.groups > 1) {
     // Lane g scores group g: the sum of its two largest keys (sigmoid) or its largest (softmax).
-    uint32_t* mine = group_keys + (size_t)warp * p.experts;
+    uint32_t* mine = group_keys + (size_t)warp * experts;
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      if (i * 32 + lane < p.experts) mine[i * 32 + lane] = key[i];
+      if (i * 32 + lane < experts) mine[i * 32 + lane] = key[i];
     __syncwarp();
-    const int per = p.experts / p.groups;
+    const int per = experts / p.groups;
     uint32_t score = 0u;
     if (lane < p.groups) {
       uint32_t first = 0u, second = 0u;
@@ -122,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int e = i * 32 + lane;
-      if (e < p.experts && !((keep >> (e / per)) & 1u)) key[i] = 0u;
+      if (e < experts && !((keep >> (e / per)) & 1u)) key[i] = 0u;
     }
   }
 
@@ -181,8 +183,8 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
       if (at == (uint32_t)(i * 32 + lane)) key[i] = 0u;
     if (lane == j) my_idx = (int)at;
   }
-  const bool holds = lane < p.topk && my_idx >= 0 && my_idx < p.experts;
-  const float my_x = holds ? load_logit<kF32>(p.logits, t * p.experts + my_idx) : -INFINITY;
+  const bool holds = lane < p.topk && my_idx >= 0 && my_idx < experts;
+  const float my_x = holds ? load_logit<kF32>(p.logits, t * experts + my_idx) : -INFINITY;
 
   float w = 0.f;
   if constexpr (kSigmoid) {
@@ -192,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
     if (!p.renorm) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
-        if (i * 32 + lane < p.experts) m = fmaxf(m, x[i]);
+        if (i * 32 + lane < experts) m = fmaxf(m, x[i]);
     }
     m = warp_max(m);
     if (m == -INFINITY) m = 0.f;           // nothing but masked logits: every weight is 0
@@ -201,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const RouteParams p) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
-        if (i * 32 + lane < p.experts) sum += expf(x[i] - m);
+        if (i * 32 + lane < experts) sum += expf(x[i] - m);
       sum = warp_sum(sum);
       w = sum == 0.f ? 0.f : w / sum;
     }
@@ -338,16 +340,20 @@ __global__ void __launch_bounds__(kThreads) route_backward_kernel(const RouteBac
   }
 }
 
+template <int kPer, bool kF32, bool kSigmoid>
+cudaError_t launch_route_form(const RouteParams& p, unsigned blocks, cudaStream_t stream) {
+  const size_t smem = p.groups > 1 ? (size_t)kWarps * p.experts * 4 : 0;
+  return launch_pdl(p.experts == 32 * kPer ? route_kernel<kPer, true, kF32, kSigmoid> : route_kernel<kPer, false, kF32, kSigmoid>,
+                    dim3(blocks), dim3(kThreads), smem, stream, 1, p);
+}
 template <bool kF32, bool kSigmoid>
 cudaError_t launch_route(const RouteParams& p, unsigned blocks, cudaStream_t stream) {
-  const size_t smem = p.groups > 1 ? (size_t)kWarps * p.experts * 4 : 0;
-  const dim3 g(blocks), b(kThreads);
-  if (p.experts <= 32) return launch_pdl(route_kernel<1, kF32, kSigmoid>, g, b, smem, stream, 1, p);
-  if (p.experts <= 64) return launch_pdl(route_kernel<2, kF32, kSigmoid>, g, b, smem, stream, 1, p);
-  if (p.experts <= 128) return launch_pdl(route_kernel<4, kF32, kSigmoid>, g, b, smem, stream, 1, p);
-  if (p.experts <= 256) return launch_pdl(route_kernel<8, kF32, kSigmoid>, g, b, smem, stream, 1, p);
-  if (p.experts <= 512) return launch_pdl(route_kernel<16, kF32, kSigmoid>, g, b, smem, stream, 1, p);
-  return launch_pdl(route_kernel<32, kF32, kSigmoid>, g, b, smem, stream, 1, p);
+  if (p.experts <= 32) return launch_route_form<1, kF32, kSigmoid>(p, blocks, stream);
+  if (p.experts <= 64) return launch_route_form<2, kF32, kSigmoid>(p, blocks, stream);
+  if (p.experts <= 128) return launch_route_form<4, kF32, kSigmoid>(p, blocks, stream);
+  if (p.experts <= 256) return launch_route_form<8, kF32, kSigmoid>(p, blocks, stream);
+  if (p.experts <= 512) return launch_route_form<16, kF32, kSigmoid>(p, blocks, stream);
+  return launch_route_form<32, kF32, kSigmoid>(p, blocks, stream);
 }
 template <bool kF32>
 cudaError_t launch_route_backward(const RouteBackParams& p, unsigned blocks, cudaStream_t stream) {
