@@ -17,7 +17,7 @@ __device__ __forceinline__ void column_sums(const ColumnSums& c, int64_t warp, i
     int64_t first = 0, last = c.parts;
     if (c.offsets) {
       first = c.offsets[g] / kSlopeRows;
-      last = c.offsets[g + 1] / kSlopeRows;
+      last = first + (c.counts[g] + kSlopeRows - 1) / kSlopeRows;
     }
     float s = 0.f;
     if (col < c.width) {

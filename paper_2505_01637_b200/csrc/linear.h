@@ -75,7 +75,8 @@ struct ColumnSums {
   const float* partial = nullptr;    // [parts][width]
   float* db = nullptr;               // [groups][width]
   int64_t width = 0, parts = 0, groups = 1;
-  const int32_t* offsets = nullptr;  // first row of every group (multiples of kSlopeRows), or null: one group
+  const int32_t* offsets = nullptr;  // first row of every group (multiples of kSlopeRows) and
+  const int32_t* counts = nullptr;   // rows of every group, or null: one group
   bool accumulate = false;
 };
 // One product, or two (of which only the first may be kRows), in one launch; two take the column sums with them.
@@ -111,7 +112,7 @@ struct SlopeCall {
   uint16_t* dZ = nullptr;     // null: only the column sums are wanted
   float* partial = nullptr;   // the column sums' parts, or null
   int64_t rows = 0, n = 0;    // rows of dY (with experts: the layout's rows)
-  const ExpertRows* experts = nullptr;  // rows past the live ones are left alone
+  const ExpertRows* experts = nullptr;  // rows past the live ones are left alone, as are sums of kSlopeRows without a token
 };
 size_t slope_partial_bytes(int64_t rows, int64_t n, bool gated);
 cudaError_t slope_launch(const SlopeCall& call, cudaStream_t stream, uint64_t* launches);

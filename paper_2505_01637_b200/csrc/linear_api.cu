@@ -250,6 +250,7 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
     if (l.grouped) {
       sums.groups = l.groups;
       sums.offsets = l.x.offsets;
+      sums.counts = l.x.counts;
     }
   }
   const MatrixView z{dz, direct ? l.n : wide8, l.m, 1};

@@ -184,7 +184,19 @@ __global__ void __launch_bounds__(kThreads, kSums ? 3 : 4) slope_kernel(const Sl
   const int64_t row_begin = (int64_t)blockIdx.x * kSlopeRows;
   pdl_wait();
   pdl_release();
-  if (p.live && row_begin >= *p.live) return;
+  if (p.live) {
+    // An expert's tokens come first among its rows, which begin at a multiple of kSlopeRows: a first row without one means
+    // none.  Nothing is read then, but zeros are left for the products, which run over such rows.
+    const int32_t token = p.row_src[row_begin];
+    if (row_begin >= *p.live) return;
+    if (token < 0) {
+      const int64_t octets = p.pitch / 8, end = min(p.rows, row_begin + kSlopeRows);
+      uint4* dst = reinterpret_cast<uint4*>(p.dZ);
+      for (int64_t r = row_begin + lane; p.dZ && r < end; r += kSlopeLanes)
+        for (int64_t o = blockIdx.y * 32 + group; o < octets; o += gridDim.y * 32) dst[r * octets + o] = make_uint4(0u, 0u, 0u, 0u);
+      return;
+    }
+  }
   const int64_t row_end = min(p.rows, row_begin + kSlopeRows);
   const int64_t left = p.n - col;
   float s0[8], s1[8];
