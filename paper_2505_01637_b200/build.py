@@ -17,7 +17,7 @@ SOURCES = ["api.cu", "skinny.cu", "gemv_stream.cu", "gemm_tcgen05.cu", "f32_spli
            "linear_api.cu", "linear_tile.cu", "linear_rows.cu", "linear_aux.cu", "route.cu"]
 HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "sm100.cuh"),
            os.path.join(CSRC, "tensormap.h"), os.path.join(CSRC, "linear.h"), os.path.join(CSRC, "route.h"),
-           os.path.join(CSRC, "activation.cuh", "column_sums.cuh"),
+           os.path.join(CSRC, "activation.cuh"), os.path.join(CSRC, "column_sums.cuh"),
            os.path.join(os.path.dirname(HERE), "include", "morello.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
