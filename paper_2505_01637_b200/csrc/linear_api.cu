@@ -327,7 +327,6 @@ size_t dry_bytes(Pass&& pass) {
 }
 
 int run_forward(const Layer& l, const ForwardArgs& a, void* workspace, size_t workspace_bytes, void* stream) {
-  const int64_t wide = l.wide();
   if (workspace && !aligned(workspace, 16)) return MORELLO_ERR_MISALIGNED;
   if (l.m > 0 && l.n > 0) {
     if (!a.Y || (l.k > 0 && (!a.X || !a.W))) return MORELLO_ERR_NULL_POINTER;
@@ -335,7 +334,6 @@ int run_forward(const Layer& l, const ForwardArgs& a, void* workspace, size_t wo
         !aligned(a.Y, a.y_f32 ? 4 : 2))
       return MORELLO_ERR_MISALIGNED;
   }
-  (void)wide;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   Carver size;
   uint64_t launches = 0;

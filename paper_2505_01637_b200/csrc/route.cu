@@ -59,7 +59,8 @@ struct RouteParams {
   float scale;
 };
 
-// From this many experts per lane on the choice is among candidates.
+// From this many experts per lane on the choice is among candidates (at two per lane, 64 experts, that took 3.03 instead of
+// 2.79 us on 16 tokens and 3.2 instead of 3.1 on 4096).
 constexpr int kFewest = 4;
 
 // kPer: experts per lane.  kWhole: every lane holds that many (a test per expert and phase: 10.7 instead of 9.2 us on
