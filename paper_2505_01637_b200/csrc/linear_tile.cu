@@ -83,7 +83,7 @@ struct TileParams {
   const int32_t* counts;
   int experts;
   // epilogue
-  uint8_t act, out_f32, accumulate, tma, copy;   // copy: bf16 Y is the sums, nothing else
+  uint8_t act, out_f32, accumulate, tma, copy;   // copy: bf16 Y is the sums, nothing else, by epilogue_copy
   int z_pitch;           // columns of a row of Z and of the bias: n or 2 n
   const uint16_t* bias;
   const uint16_t* residual;
@@ -1017,7 +1017,8 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count,
     p.out_f32 = ep.out_f32;
     p.accumulate = ep.accumulate;
     p.tma = c.n % 8 == 0 && aligned16(ep.Y) && aligned16(ep.Z) && aligned16(ep.bias) && aligned16(ep.residual);
-    p.copy = p.tma && !ep.gated && ep.act == kActNone && !ep.bias && !ep.residual && !ep.Z && !ep.out_f32;
+    // Y's map below goes by it, and so does the kernel's choice of epilogue: never in a launch that is summed in parts.
+    p.copy = !precise && p.tma && !ep.gated && ep.act == kActNone && !ep.bias && !ep.residual && !ep.Z && !ep.out_f32;
     p.z_pitch = (int)(c.n * width);
     p.bias = ep.bias;
     p.residual = ep.residual;
