@@ -345,8 +345,8 @@ int morello_route_backward(int score, int renorm, float scale, int logits_type, 
  *
  * A tensor "in the layout" is [R][columns]; rows past offsets[experts] are neither read nor written.  Rows before
  * it that hold no pair: from an expert's last pair up to the next multiple of 16 rows they are written as zeros by
- * every entry point below and have to be zeros (or at least finite)
- * in the tensors they read; from there to the multiple of 128 they may hold anything.  Both functions return -1 for sizes that no entry point takes.
+ * every entry point below and may hold any finite number in the tensors they read (no result depends on it); from
+ * there to the multiple of 128 they may hold anything.  Both functions return -1 for sizes that no entry point takes.
  */
 int64_t morello_expert_plan_rows(int64_t tokens, int64_t topk, int64_t experts);
 int64_t morello_expert_plan_words(int64_t tokens, int64_t topk, int64_t experts);

@@ -65,6 +65,7 @@ struct TileCall {
   int64_t b_up = 0;        // gated: where the second half of B's columns begins in its stored order
   bool zero_padding = false;     // kRows: rows that hold no token are written as zeros
   bool precise = false;          // f32 output whose sums are wanted as near as f32 allows
+  bool masked_a = false;         // kContract: rows of A that hold no pair are taken as zeros (both operands are the caller's)
   bool gather_a = false;         // few-rows kernel: A is [tokens][cols], its rows fetched through the plan
   ExpertRows experts;
   LinearEpilogue epi;

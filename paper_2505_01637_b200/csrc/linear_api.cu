@@ -296,6 +296,8 @@ int backward(const DeviceInfo& dev, const Layer& l, const BackwardArgs& a, Carve
     c.n = l.w_cols ? l.k : wide;
     c.k = l.m;
     c.experts = l.x;
+    // Gathered rows and slopes are written with zeros where there is no pair; X and dY as they came may hold any number there.
+    c.masked_a = l.grouped && direct && !l.gather;
     c.epi.out_f32 = a.grad_f32;
     c.precise = a.grad_f32;
     c.epi.accumulate = a.accumulate;

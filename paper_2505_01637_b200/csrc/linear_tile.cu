@@ -2,7 +2,7 @@
 // gradient of linear layers, dense or with the weights of every row's expert.
 //
 // Persistent thread blocks walk output tiles, one CTA (cta_group::1, 128 x N) or a CTA pair
-// (cta_group::2, 256 x N) per tile, warps specialised into a TMA producer, an MMA issuer and four
+// (cta_group::2, 256 x N) per tile, warps specialised into a TMA producer, an MMA issuer and eight
 // epilogue warps; the two TMEM accumulators let the epilogue of one tile run under the main loop of
 // the next.
 //
@@ -14,7 +14,9 @@
 // Gated layers: a tile of N accumulator columns holds N / 2 columns of either half of W, so the gate and
 // its partner meet in one thread's registers.
 // Experts: their rows begin at multiples of 128, so a 128-row tile belongs to one expert and the weight
-// gradient's contraction runs over its rows alone (rounded up to 16, where padding rows are zero).
+// gradient's contraction runs over its rows alone, rounded up to 16.  The rows that round it up are zeros in one operand at
+// least: where neither was written by this library, the last contraction block of A comes in gathers of four rows, and those
+// without a pair are asked for past the tensor's end, which reads as zeros.
 //
 // Epilogue: eight warps, two per quarter of the rows, which take its 32-column steps in turn; a thread
 // holds one row of 32 columns.  Where the TMA engine can address Y and Z they leave through shared memory
@@ -76,7 +78,9 @@ struct TileParams {
   int64_t tiles;         // kRows: decided on the device
   int lead;              // second product: its items that a unit takes in place of one of the first's
   int b_up;
+  int a_rows;            // masked_a: rows of A, the first that it does not have
   uint8_t mode, a_mn, b_mn, zero_padding, halves;
+  uint8_t masked_a;      // kContract: see TileCall
   // experts
   const int32_t* block_expert;
   const int32_t* offsets;
@@ -108,7 +112,8 @@ struct Item {
   int n_off, cols;  // first accumulator column inside the tile's, and how many: the tile or half of it
   int group;        // expert (bias, weights, output of kContract)
   int k_blocks;
-  int k_row0;       // kContract: first row of the contraction
+  int k_row0;       // kContract: first row of the contraction,
+  int k_row_end;    // and the first past it that holds no pair
   int k_steps;      // 16-deep steps of the last contraction block
   int live_end;     // rows of the output from here on hold no token (kRows)
 };
@@ -155,7 +160,7 @@ class Cursor {
   __device__ __forceinline__ Item item() const {
     constexpr int kTileM = kPair ? 2 * kRowsPerCta : kRowsPerCta;
     Item it;
-    it.k_row0 = 0;
+    it.k_row0 = it.k_row_end = 0;
     it.k_blocks = p_.k_blocks;
     it.k_steps = kTileK / 16;
     it.group = 0;
@@ -170,6 +175,7 @@ class Cursor {
       it.group = expert_;
       it.k_row0 = p_.offsets[expert_];
       const int count = p_.counts[expert_];
+      it.k_row_end = it.k_row0 + count;
       it.k_blocks = (count + kTileK - 1) / kTileK;
       // Rows past the next multiple of 16 are never multiplied: they may hold anything.
       it.k_steps = (count - (it.k_blocks - 1) * kTileK + 15) / 16;
@@ -551,6 +557,7 @@ constexpr int kMaxProducts = 2;
 struct TileBatch {
   CUtensorMap a[kMaxProducts], b[kMaxProducts], y[kMaxProducts];
   CUtensorMap z;                // of the first product
+  CUtensorMap a_rows;           // A of the product with masked_a, by single rows
   TileParams p[kMaxProducts];
   ColumnSums sums;              // of two products, or empty
 };
@@ -658,8 +665,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
       (void)leader_full;
       int before = 0;
       for (int q = 0; q < (kTwo ? 2 : 1); ++q) {
-      const TileParams& p = batch.p[q];
-      const CUtensorMap* map_a   = &batch.a[q];
+        const TileParams& p = batch.p[q];
+        const CUtensorMap* map_a = &batch.a[q];
         const CUtensorMap* map_b = &batch.b[q];
         Walk w;
         walk_of(q, before, &w);
@@ -682,6 +689,10 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
             if constexpr (kGated) cols[j] = at < it.cols / 2 ? col0 + at : p.b_up + col0 + at - it.cols / 2;
             else cols[j] = col0 + at;
           }
+          // From this block on A's rows are masked.  (The up to 32 gathers of a tile cost the backward pass of 16,384 rows,
+          // 1024 -> 2048 on 32 experts, 1 %: 139.1 -> 140.6 us; 1554 rows on 16 experts 30.7 -> 31.2.  A copy of dY with
+          // zeros, which layers with an activation make anyway, would read and write 150 MB there.)
+          const int masked_from = p.masked_a && it.k_row_end % 16 != 0 ? it.k_blocks - 1 : it.k_blocks;
           int kc = it.k_row0;
           for (int kb = 0; kb < it.k_blocks; ++kb, kc += kTileK) {
             if (!(ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 33))) break;
@@ -689,16 +700,32 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
             uint8_t* sb = sa + kBytesA;
             const uint32_t full = leader_full + (uint32_t)stage * 8u;
             (void)full;
+            const bool masked = kb >= masked_from;
+            // Of a masked block only the steps that are multiplied come: two boxes of 16 rows x 128 bytes each.
+            const uint32_t expected = masked ? tx - (uint32_t)(kTileK / 16 - it.k_steps) * 4096u : tx;
             if constexpr (kPair) {
-              if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * tx);
+              if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * expected);
             } else {
-              mbar_arrive_expect_tx(&bars->full[stage], tx);
+              mbar_arrive_expect_tx(&bars->full[stage], expected);
             }
             auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1, int c2) {
               if constexpr (kPair) tma_load_3d_pair(dst, map, full, c0, c1, c2);
               else tma_load_3d(dst, map, &bars->full[stage], c0, c1, c2);
             };
-            if (a_mn) {
+            if (masked) {
+              const int none = p.a_rows;
+              for (int r = 0; r < 16 * it.k_steps; r += 4) {
+                int from[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) from[i] = kc + r + i < it.k_row_end ? kc + r + i : none;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  uint8_t* dst = sa + h * kBoxBytes + r * 128;
+                  if constexpr (kPair) tma_gather4_pair(dst, &batch.a_rows, full, row0 + 64 * h, from[0], from[1], from[2], from[3]);
+                  else tma_gather4(dst, &batch.a_rows, &bars->full[stage], row0 + 64 * h, from[0], from[1], from[2], from[3]);
+                }
+              }
+            } else if (a_mn) {
               load(sa, map_a, row0, kc, 0);
               load(sa + kBoxBytes, map_a, row0 + 64, kc, 0);
             } else {
@@ -710,7 +737,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
             if (++stage == S::kStages) { stage = 0; phase ^= 1; }
           }
         }
-      before = w.items;
+        before = w.items;
       }
     }
   } else if (warp == 1) {
@@ -1009,6 +1036,8 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count,
     p.a_mn = c.a_mn;
     p.b_mn = c.b_mn;
     p.zero_padding = c.zero_padding;
+    p.masked_a = c.masked_a;
+    p.a_rows = (int)c.a.rows;
     p.block_expert = c.experts.block_expert;
     p.offsets = c.experts.offsets;
     p.counts = c.experts.counts;
@@ -1045,6 +1074,7 @@ cudaError_t tile_launch(const DeviceInfo& dev, const TileCall* calls, int count,
       if (e == cudaSuccess)
         e = make_tensor_map_3d(&batch.b[q], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.b.p, (uint64_t)c.b.cols,
                                (uint64_t)c.b.rows, (uint64_t)c.b.groups, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+      if (e == cudaSuccess && c.masked_a) e = make_gather_map(&batch.a_rows, c.a.p, (uint64_t)c.a.cols, (uint64_t)c.a.rows);
       if (e != cudaSuccess) return e;
     }
     if (p.tma) {
