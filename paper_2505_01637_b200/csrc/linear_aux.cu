@@ -204,12 +204,14 @@ struct SlopeParams {
 };
 
 // A block: 256 columns (32 groups of 8) x kSlopeRows rows, eight rows at a time.
-// kOctets: every row is in 16-byte accesses (a test per access kept the loads from going out together).
+// kOctets: every row is in 16-byte accesses (a test per access kept the loads from going out together), and the strips fit
+// the grid's second dimension, 65,535 of them: the third, for layers of more than 16.7 million columns, costs registers (spills in
+// five forms).
 template <int kAct, bool kGated, bool kSums, bool kOctets>
 __global__ void __launch_bounds__(kThreads, kSums ? 3 : 4) slope_kernel(const SlopeParams p) {
   __shared__ float sums[kSums ? kSlopeLanes : 1][kGated ? 2 : 1][256 + 8];
   const int group = threadIdx.x & 31, lane = threadIdx.x >> 5;
-  const int64_t col = (int64_t)blockIdx.y * 256 + group * 8;
+  const int64_t col = (int64_t)(kOctets ? blockIdx.y : blockIdx.z * gridDim.y + blockIdx.y) * 256 + group * 8;
   const int64_t row_begin = (int64_t)blockIdx.x * kSlopeRows;
   pdl_wait();
   pdl_release();
@@ -293,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, kSums ? 3 : 4) slope_kernel(const Sl
       if constexpr (kGated) sums[lane][1][group * 8 + e] = s1[e];
     }
     __syncthreads();
-    const int64_t c = (int64_t)blockIdx.y * 256 + threadIdx.x;
+    const int64_t c = (int64_t)(kOctets ? blockIdx.y : blockIdx.z * gridDim.y + blockIdx.y) * 256 + threadIdx.x;
     if (c < p.n) {
       const int64_t width = kGated ? 2 * p.n : p.n;
 #pragma unroll
@@ -464,10 +466,11 @@ cudaError_t slope_launch(const SlopeCall& c, cudaStream_t stream, uint64_t* laun
       p.live = c.experts->offsets + c.experts->experts;
     }
     const int64_t strips = (c.n + 255) / 256;
-    if (parts >= (1ll << 31) || strips > 65535) return cudaErrorInvalidValue;
-    const dim3 grid((unsigned)parts, (unsigned)strips);
+    if (parts >= (1ll << 31)) return cudaErrorInvalidValue;
+    const unsigned deep = (unsigned)((strips + 65534) / 65535), wide = (unsigned)((strips + deep - 1) / deep);
+    const dim3 grid((unsigned)parts, wide, deep);
     const bool with = p.partial != nullptr;
-    const bool octets = p.width_y == 8 && p.width_z == 8;
+    const bool octets = p.width_y == 8 && p.width_z == 8 && deep == 1;
     auto go = [&](auto sums, auto none, auto sums_any, auto none_any) {
       return launch_pdl(octets ? (with ? sums : none) : (with ? sums_any : none_any), grid, dim3(kThreads), 0, stream, 1, p);
     };
