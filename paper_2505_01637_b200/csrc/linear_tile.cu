@@ -689,43 +689,26 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
             if constexpr (kGated) cols[j] = at < it.cols / 2 ? col0 + at : p.b_up + col0 + at - it.cols / 2;
             else cols[j] = col0 + at;
           }
-          // From this block on A's rows are masked.  (The up to 32 gathers of a tile cost the backward pass of 16,384 rows,
-          // 1024 -> 2048 on 32 experts, 1 %: 139.1 -> 140.6 us; 1554 rows on 16 experts 30.7 -> 31.2.  A copy of dY with
-          // zeros, which layers with an activation make anyway, would read and write 150 MB there.)
-          const int masked_from = p.masked_a && it.k_row_end % 16 != 0 ? it.k_blocks - 1 : it.k_blocks;
+          auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1, int c2) {
+            if constexpr (kPair) tma_load_3d_pair(dst, map, leader_full + (uint32_t)stage * 8u, c0, c1, c2);
+            else tma_load_3d(dst, map, &bars->full[stage], c0, c1, c2);
+          };
+          auto expect = [&](uint32_t bytes) {
+            if constexpr (kPair) {
+              if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * bytes);
+            } else {
+              mbar_arrive_expect_tx(&bars->full[stage], bytes);
+            }
+          };
+          const bool masked = !kGated && p.masked_a && it.k_row_end % 16 != 0;
+          const int whole_blocks = masked ? it.k_blocks - 1 : it.k_blocks;
           int kc = it.k_row0;
-          for (int kb = 0; kb < it.k_blocks; ++kb, kc += kTileK) {
+          for (int kb = 0; kb < whole_blocks; ++kb, kc += kTileK) {
             if (!(ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 33))) break;
             uint8_t* sa = stages + (size_t)stage * S::kStageBytes;
             uint8_t* sb = sa + kBytesA;
-            const uint32_t full = leader_full + (uint32_t)stage * 8u;
-            (void)full;
-            const bool masked = kb >= masked_from;
-            // Of a masked block only the steps that are multiplied come: two boxes of 16 rows x 128 bytes each.
-            const uint32_t expected = masked ? tx - (uint32_t)(kTileK / 16 - it.k_steps) * 4096u : tx;
-            if constexpr (kPair) {
-              if (rank == 0) mbar_arrive_expect_tx(&bars->full[stage], 2 * expected);
-            } else {
-              mbar_arrive_expect_tx(&bars->full[stage], expected);
-            }
-            auto load = [&](void* dst, const CUtensorMap* map, int c0, int c1, int c2) {
-              if constexpr (kPair) tma_load_3d_pair(dst, map, full, c0, c1, c2);
-              else tma_load_3d(dst, map, &bars->full[stage], c0, c1, c2);
-            };
-            if (masked) {
-              const int none = p.a_rows;
-              for (int r = 0; r < 16 * it.k_steps; r += 4) {
-                int from[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) from[i] = kc + r + i < it.k_row_end ? kc + r + i : none;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  uint8_t* dst = sa + h * kBoxBytes + r * 128;
-                  if constexpr (kPair) tma_gather4_pair(dst, &batch.a_rows, full, row0 + 64 * h, from[0], from[1], from[2], from[3]);
-                  else tma_gather4(dst, &batch.a_rows, &bars->full[stage], row0 + 64 * h, from[0], from[1], from[2], from[3]);
-                }
-              }
-            } else if (a_mn) {
+            expect(tx);
+            if (a_mn) {
               load(sa, map_a, row0, kc, 0);
               load(sa + kBoxBytes, map_a, row0 + 64, kc, 0);
             } else {
@@ -734,6 +717,30 @@ __global__ void __launch_bounds__(kThreads, 1) linear_tile_kernel(const __grid_c
 #pragma unroll
             for (int j = 0; j < S::kBoxesB; ++j)
               if (j < boxes_b) load(sb + j * kBoxBytes, map_b, b_mn ? cols[j] : kc, b_mn ? kc : cols[j], z_b);
+            if (++stage == S::kStages) { stage = 0; phase ^= 1; }
+          }
+          // The last block with A's rows masked.  Only the steps that are multiplied come: two boxes of 16 rows x 128 bytes
+          // each.  (The up to 32 gathers of a tile cost the backward pass of 16,384 rows, 1024 -> 2048 on 32 experts, 1 %:
+          // 139.1 -> 140.6 us; 1554 rows on 16 experts 30.7 -> 31.2.  A copy of dY with zeros, which layers with an
+          // activation make anyway, would read and write 150 MB there.)
+          if (masked && ok && (ok = mbar_wait(&bars->empty[stage], phase ^ 1, abort_flag, p.status, 33))) {
+            uint8_t* sa = stages + (size_t)stage * S::kStageBytes;
+            expect(tx - (uint32_t)(kTileK / 16 - it.k_steps) * 4096u);
+#pragma unroll 1
+            for (int r = 0; r < 16 * it.k_steps; r += 4) {
+              int from[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) from[i] = kc + r + i < it.k_row_end ? kc + r + i : p.a_rows;
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                uint8_t* dst = sa + h * kBoxBytes + r * 128;
+                if constexpr (kPair) tma_gather4_pair(dst, &batch.a_rows, leader_full + (uint32_t)stage * 8u, row0 + 64 * h, from[0], from[1], from[2], from[3]);
+                else tma_gather4(dst, &batch.a_rows, &bars->full[stage], row0 + 64 * h, from[0], from[1], from[2], from[3]);
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < S::kBoxesB; ++j)
+              if (j < boxes_b) load(sa + kBytesA + j * kBoxBytes, map_b, cols[j], kc, z_b);
             if (++stage == S::kStages) { stage = 0; phase ^= 1; }
           }
         }
