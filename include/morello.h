@@ -325,7 +325,8 @@ int morello_route(int score, int renorm, float scale, int logits_type, int64_t t
                   int64_t topk, int64_t groups, int64_t topk_groups, const void* logits, const float* bias,
                   int32_t* idx, float* weights, void* stream);
 /* Gradient of the logits (their type; every element is written) from that of the weights; the choice is
- * constant.  idx entries outside 0 .. experts - 1 are skipped. */
+ * constant.  idx entries outside 0 .. experts - 1 are skipped; the terms of an expert that a token names more
+ * than once add up. */
 int morello_route_backward(int score, int renorm, float scale, int logits_type, int64_t tokens,
                            int64_t experts, int64_t topk, const void* logits, const int32_t* idx,
                            const float* dweights, void* dlogits, void* stream);
