@@ -298,7 +298,10 @@ size_t morello_linear_workspace_bytes(int gated, int w_layout, int64_t m, int64_
  * dX, dW and dbias may each be NULL (not wanted).  accumulate == 1 (f32 gradients only) adds to dW and
  * dbias instead of setting them.  Z may be NULL for MORELLO_ACT_NONE without gating.  The gradient of R is
  * dY itself.  dz is rounded to bf16 for the two products (they run on the bf16 tensor cores) and kept in
- * f32 for dbias.  m == 0 and k == 0 or n == 0 sums are empty: zero, or nothing added.  Workspace as in morello_linear.
+ * f32 for dbias.  m == 0 and k == 0 or n == 0 sums are empty: zero, or nothing added.  accumulate adds to a dW that
+ * is 16-byte aligned with rows of multiples of 8 elements in L2, which takes subnormal numbers as zero.  Workspace as
+ * in morello_linear; without activation and gating a dY that is not 16-byte aligned needs its own bytes besides, too
+ * (m rows of n rounded up to 8 elements, the whole to 256 bytes).
  */
 int morello_linear_backward(int act, int gated, int grad_type, int accumulate, int w_layout,
                             int64_t m, int64_t k, int64_t n,
@@ -316,9 +319,10 @@ size_t morello_linear_backward_workspace_bytes(int act, int gated, int w_layout,
  *     idx[t][0 .. topk): the experts of the topk largest keys, largest first
  *     weights[t][j] = scale * p, p = softmax(x)_e or s_e of the chosen; renorm == 1: divided by their sum
  *
- * The bias steers the choice alone.  Ties go to the lowest index, among groups too; -0 equals +0 and a NaN key
- * is below every number.  A logit of -inf has weight 0 (it is chosen only when nothing else is left); a row of
- * nothing else, and a sum of 0, give weights of 0.  Otherwise infinities and NaN follow the formulas.
+ * The bias steers the choice alone; with softmax scores it is added to the logits, not to the probabilities.  Ties
+ * go to the lowest index, among groups too; -0 equals +0 and a NaN key is below every number.  A logit of -inf has
+ * weight 0 (it is chosen only when nothing else is left); a row of nothing else, and a sum of 0, give weights of 0.
+ * Otherwise infinities and NaN follow the formulas.
  * experts <= 1024, topk <= 32, groups <= 32 and dividing experts, topk <= topk_groups * experts / groups.
  */
 int morello_route(int score, int renorm, float scale, int logits_type, int64_t tokens, int64_t experts,

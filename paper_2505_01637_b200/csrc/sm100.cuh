@@ -124,9 +124,10 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
                : "memory");
 }
 
-// The same without release semantics, for arrivals that hand back tensor memory alone: what must be done before
-// them (tcgen05.wait::ld) is done in program order, and a release at cluster scope waits for every store of the
-// thread's block besides (1,300 cycles where this takes 150).
+// The same without release semantics, for arrivals that hand back tensor memory alone.  Its accesses are ordered by
+// tcgen05.fence::before_thread_sync ahead of the arrival and ::after_thread_sync behind the wait, for which a relaxed
+// arrival is enough; no other memory is passed on.  A release at cluster scope waits for every store of the block besides
+// (weight gradients of 16 experts with 1,554 rows and their call: 59.6 instead of 54.9 us).
 __device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
