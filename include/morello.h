@@ -85,7 +85,9 @@ enum {
  * frees and allocates device memory, which a stream capture does not allow: a call
  * that would have to grow it while `stream` is being captured returns
  * MORELLO_ERR_WORKSPACE and touches nothing -- size the buffer with an ordinary call
- * on the same shape first, or capture morello_matmul_accum_ws.  The same holds for
+ * on the same shape first, or capture morello_matmul_accum_ws.  A buffer that captured
+ * work uses is not freed when a larger one takes its place, so that the graph stays valid
+ * (replays of it and calls on another stream must not overlap).  The same holds for
  * every entry point below that uses the library's own buffers, and the library's first
  * call on a device (which allocates a 256-byte status block) must come before any capture.
  */

@@ -17,16 +17,21 @@ namespace {
 constexpr int kMaxDevices = 64;
 constexpr int kSkinnyMaxRows = 16;
 
+// A library-owned device buffer that grows on demand.
+struct OwnedBuffer {
+  void* p = nullptr;
+  size_t bytes = 0;
+  bool captured = false;         // a graph may replay work on it
+};
+
 struct DeviceState {
   bool ready = false;
   int status_code = MORELLO_OK;  // result of the one-time set-up
   DeviceInfo info;
-  void* scratch = nullptr;       // library-owned workspace, grown on demand
-  size_t scratch_bytes = 0;
+  OwnedBuffer scratch;           // workspace
   void* stage = nullptr;         // device staging for the host-buffer entry point
   size_t stage_bytes = 0;
-  void* split = nullptr;         // bf16 terms of float32 operands (morello_matmul_accum_f32)
-  size_t split_bytes = 0;
+  OwnedBuffer split;             // bf16 terms of float32 operands (morello_matmul_accum_f32)
 };
 
 std::mutex g_mutex;
@@ -80,23 +85,31 @@ int device_state(DeviceState** out) {
   return st.status_code;
 }
 
-// Makes the library-owned scratch at least `need` bytes, under g_mutex.
-int grow_scratch(DeviceState* st, size_t need, cudaStream_t stream) {
-  if (st->scratch_bytes >= need) return MORELLO_OK;
-  if (capturing(stream)) return MORELLO_ERR_WORKSPACE;
+// Makes a buffer at least `need` bytes, under g_mutex.  One that work on it has been captured from is not freed when a
+// larger one takes its place, since the graph can still be replayed: it stays for the rest of the process.
+int grow_buffer(OwnedBuffer* b, size_t need, size_t smallest, cudaStream_t stream) {
+  const bool in_capture = (b->bytes < need || !b->captured) && capturing(stream);
+  if (b->bytes >= need) {
+    b->captured = b->captured || in_capture;
+    return MORELLO_OK;
+  }
+  if (in_capture) return MORELLO_ERR_WORKSPACE;
   // Work already enqueued may still be using the old buffer.
   cudaError_t e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return cuda_fail(e);
-  if (st->scratch) cudaFree(st->scratch);
-  st->scratch = nullptr;
-  st->scratch_bytes = 0;
-  const size_t grow = std::max(need, (size_t)(8u << 20));
-  if ((e = cudaMalloc(&st->scratch, grow)) != cudaSuccess) {
+  if (b->p && !b->captured) cudaFree(b->p);
+  *b = OwnedBuffer{};
+  const size_t grow = std::max(need, smallest);
+  if ((e = cudaMalloc(&b->p, grow)) != cudaSuccess) {
+    b->p = nullptr;
     cuda_fail(e);
     return MORELLO_ERR_WORKSPACE;
   }
-  st->scratch_bytes = grow;
+  b->bytes = grow;
   return MORELLO_OK;
+}
+int grow_scratch(DeviceState* st, size_t need, cudaStream_t stream) {
+  return grow_buffer(&st->scratch, need, (size_t)(8u << 20), stream);
 }
 
 // Bounded text output for morello_describe_route.
@@ -336,7 +349,7 @@ int run(int path, int split_k, int64_t b, int64_t m, int64_t k, int64_t n, const
     if (own_scratch) {
       std::lock_guard<std::mutex> lock(g_mutex);
       if ((rc = grow_scratch(st, need, static_cast<cudaStream_t>(stream))) != MORELLO_OK) return rc;
-      ws = static_cast<float*>(st->scratch);
+      ws = static_cast<float*>(st->scratch.p);
     } else if (!ws || workspace_bytes < need) {
       return MORELLO_ERR_WORKSPACE;
     }
@@ -409,7 +422,7 @@ int operator_workspace(size_t need, void* given, size_t given_bytes, cudaStream_
     return MORELLO_OK;
   }
   if ((rc = grow_scratch(st, need, stream)) != MORELLO_OK) return rc;
-  *out = st->scratch;
+  *out = st->scratch.p;
   return MORELLO_OK;
 }
 
@@ -546,19 +559,7 @@ int run_f32(int64_t b, int64_t m, int64_t k, int64_t n, const float* A, const fl
   const size_t need = f32_split_bytes(b, m, k, n);
   {
     std::lock_guard<std::mutex> lock(g_mutex);
-    if (st->split_bytes < need) {
-      if (capturing(static_cast<cudaStream_t>(stream))) return MORELLO_ERR_WORKSPACE;
-      cudaError_t e = cudaDeviceSynchronize();   // work in flight may still read the old buffer
-      if (e != cudaSuccess) return cuda_fail(e);
-      if (st->split) cudaFree(st->split);
-      st->split = nullptr;
-      st->split_bytes = 0;
-      if ((e = cudaMalloc(&st->split, need)) != cudaSuccess) {
-        cuda_fail(e);
-        return MORELLO_ERR_WORKSPACE;
-      }
-      st->split_bytes = need;
-    }
+    if ((rc = grow_buffer(&st->split, need, 0, static_cast<cudaStream_t>(stream))) != MORELLO_OK) return rc;
   }
   // When the bf16 problem goes to the tensor-core kernels directly and k is a whole number of
   // their 64-element blocks, only the three terms are stored and the kernels visit them in the
@@ -569,7 +570,7 @@ int run_f32(int64_t b, int64_t m, int64_t k, int64_t n, const float* A, const fl
                      select_path(st->info.sms, b, m, k6, n, aligned, aligned, C) == MORELLO_PATH_TCGEN05;
   uint16_t *A6 = nullptr, *B6 = nullptr;
   uint64_t launches = 0;
-  const cudaError_t e = f32_split_launch(b, m, k, n, A, B, st->split, !three, &A6, &B6,
+  const cudaError_t e = f32_split_launch(b, m, k, n, A, B, st->split.p, !three, &A6, &B6,
                                          static_cast<cudaStream_t>(stream), &launches);
   g_launches.fetch_add(launches, std::memory_order_relaxed);
   if (e != cudaSuccess) return cuda_fail(e);
