@@ -393,6 +393,42 @@ int morello_expert_combine_backward(int y_type, int64_t tokens, int64_t topk, in
                                     const int32_t* plan, const float* weights, const void* Y, const void* dout,
                                     void* dY, float* dweights, void* stream);
 
+/* --- norms ------------------------------------------------------------------- */
+
+/*
+ * Layer norm of every row of X[m][n] (bf16 or f32, x_type):
+ *
+ *     mu = mean(x) (rms == 1: 0),   r = 1 / sqrt(mean((x - mu)^2) + eps)
+ *     Y[i,j] = (X[i,j] - mu_i) * r_i * gamma[j] + beta[j]
+ *
+ * gamma[n] bf16 or NULL (ones), beta[n] bf16 or NULL (zeros), Y[m][n] bf16, rounded once; mean[m] and rstd[m] f32 or NULL:
+ * mu and r, for the backward pass (rms == 1 writes no mean).  Means, squares and differences are f32, the squares those of
+ * differences from the mean.  Y may be X itself when both are bf16; no other overlap is allowed.  eps >= 0.  A row that
+ * holds a NaN or (rms == 0) an infinity is NaN throughout.  m == 0 or n == 0 does nothing.  Any extent up to 2^31 - 1024
+ * and alignment runs; n % 8 == 0 with 16-byte-aligned tensors is read in 16-byte accesses.  Needs no workspace.
+ * Asynchronous on `stream`.
+ */
+int morello_layer_norm(int rms, int x_type, int64_t m, int64_t n, float eps, const void* X, const void* gamma,
+                       const void* beta, void* Y, float* mean, float* rstd, void* stream);
+
+/*
+ * Gradients of morello_layer_norm from dY[m][n] (bf16) and the kept mean and rstd.  With h = (X - mean) * rstd, g = dY * gamma:
+ *
+ *     dX[i,j] = rstd_i * (g[i,j] - mean_j(g[i,:]) - h[i,j] * mean_j(g[i,:] * h[i,:])) + R[i,j]    (rms == 1: without mean(g))
+ *     dgamma[j] = sum_i dY[i,j] * h[i,j],   dbeta[j] = sum_i dY[i,j]                               (f32)
+ *
+ * dX and R are of X's type; R, the gradient that reaches X past the norm, may be NULL, and may be dX itself.  dX, dgamma
+ * and dbeta may each be NULL (not wanted); mean is not read when rms == 1.  accumulate == 1 adds to dgamma and dbeta
+ * instead of setting them.  m == 0 sums are empty: zero, or nothing added.  Sums are f32, in an order that is fixed for a
+ * shape.  `workspace` (for dgamma and dbeta): morello_layer_norm_backward_workspace_bytes() bytes, 16-byte aligned, or
+ * NULL and 0 for the library's own scratch (rules as in morello_matmul_accum).  Asynchronous on `stream`.
+ */
+int morello_layer_norm_backward(int rms, int x_type, int accumulate, int64_t m, int64_t n, const void* X,
+                                const void* gamma, const float* mean, const float* rstd, const void* dY, const void* R,
+                                void* dX, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
+                                void* stream);
+size_t morello_layer_norm_backward_workspace_bytes(int64_t m, int64_t n);
+
 /* --- introspection and experiments (tests and benchmarks) ------------------ */
 
 /* The path the selector picks for this shape with 16-byte-aligned operands:

@@ -77,6 +77,9 @@ SIGNATURES = {
     "morello_expert_linear_backward_workspace_bytes": (_sz, [_int] * 4 + [_i64] * 5),
     "morello_expert_combine": (_int, [_int] + [_i64] * 4 + [_vp] * 6),
     "morello_expert_combine_backward": (_int, [_int] + [_i64] * 4 + [_vp] * 7),
+    "morello_layer_norm": (_int, [_int] * 2 + [_i64] * 2 + [ctypes.c_float] + [_vp] * 7),
+    "morello_layer_norm_backward": (_int, [_int] * 3 + [_i64] * 2 + [_vp] * 10 + [_sz, _vp]),
+    "morello_layer_norm_backward_workspace_bytes": (_sz, [_i64] * 2),
     "morello_read_device_status": (_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "morello_device_limits": (_int, [ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]),
     "morello_launch_count": (ctypes.c_uint64, []),
@@ -371,6 +374,26 @@ def morello_selftest_wait_timeout(limit_ms, stream=None) -> None:
     """Makes one bounded device-side wait run out on purpose (see the header); raises unless it
     gave up as designed.  The device status word is set afterwards."""
     _check(lib().morello_selftest_wait_timeout(limit_ms, _stream(stream)), "morello_selftest_wait_timeout")
+
+
+def morello_layer_norm(rms, x_type, m, n, eps, X, gamma, beta, Y, mean=None, rstd=None, stream=None) -> None:
+    """Y = (X - mean) * rstd * gamma + beta of every row; gamma, beta, mean and rstd may be None."""
+    _check(lib().morello_layer_norm(rms, x_type, m, n, eps, _addr(X), _addr(gamma), _addr(beta), _addr(Y), _addr(mean),
+                                    _addr(rstd), _stream(stream)),
+           "morello_layer_norm")
+
+
+def morello_layer_norm_backward(rms, x_type, accumulate, m, n, X, gamma, mean, rstd, dY, R, dX, dgamma, dbeta,
+                                workspace=None, workspace_bytes=0, stream=None) -> None:
+    """Gradients of morello_layer_norm; gamma, R, dX, dgamma and dbeta may be None (with rms: mean too)."""
+    _check(lib().morello_layer_norm_backward(rms, x_type, accumulate, m, n, _addr(X), _addr(gamma), _addr(mean),
+                                             _addr(rstd), _addr(dY), _addr(R), _addr(dX), _addr(dgamma), _addr(dbeta),
+                                             _addr(workspace), workspace_bytes, _stream(stream)),
+           "morello_layer_norm_backward")
+
+
+def morello_layer_norm_backward_workspace_bytes(m, n) -> int:
+    return int(lib().morello_layer_norm_backward_workspace_bytes(m, n))
 
 
 def morello_read_device_status(stream=None):
