@@ -429,6 +429,69 @@ int morello_layer_norm_backward(int rms, int x_type, int accumulate, int64_t m, 
                                 void* stream);
 size_t morello_layer_norm_backward_workspace_bytes(int64_t m, int64_t n);
 
+/* --- microscaled 4-bit tensors -------------------------------------------------- */
+
+/* Formats: blocks of 32 elements with a power of two as scale (one byte e: 2^(e - 127), 255 NaN), or of 16 with a scale
+ * in e4m3 (1 sign, 4 exponent, 3 fraction bits; the sign is 0, 127 NaN). */
+enum { MORELLO_MXFP4 = 0, MORELLO_NVFP4 = 1 };
+
+/*
+ * A 4-bit tensor of `rows` rows and k columns, blocks along k, is two device buffers, 16-byte aligned:
+ *
+ *     Q[rows][P], P = 16 ceil(k / 32) bytes: elements 2 i and 2 i + 1 of a row in the low and the high half of byte i,
+ *         zeros past k.  An element is e2m1: a sign bit and three bits for 0, 1/2, 1, 3/2, 2, 3, 4, 6.
+ *     scales[parts][ceil(rows / parts / 128)][ceil(k / (4 block))][32][4][4] bytes: block j of row r of a part at
+ *         [r / 128][j / 4][r % 32][(r % 128) / 32][j % 4], zeros where there is no such row or block.
+ *
+ * The rows are `parts` equal parts (rows % parts == 0), each with scales of its own from a multiple of 128 rows on:
+ * 1, or 2 for the two halves of a gated layer's weights.  A weight matrix of k inputs and w outputs is a tensor of w
+ * rows, activations of m tokens one of m rows.  Sizes: morello_fp4_bytes() = rows P and morello_fp4_scale_bytes(); -1 for
+ * sizes that no entry point takes.
+ */
+int64_t morello_fp4_bytes(int64_t rows, int64_t k);
+int64_t morello_fp4_scale_bytes(int format, int64_t rows, int64_t parts, int64_t k);
+
+/*
+ * Quantises X (bf16 or f32, x_type): [rows][k] with x_layout = MORELLO_W_COLMAJOR (activations, and weights stored
+ * [w][k]) or [k][rows] with MORELLO_W_ROWMAJOR (weights stored [k][w]).  With x the element, times the one f32 at `mult`
+ * (device memory, NULL: 1; the product is rounded to f32), and amax the largest |x| of its block:
+ *
+ *     s = 2^(floor(log2 amax) - 2), exponent at least -127;    or s = amax / 6 rounded to e4m3, at most 448
+ *     Q = x / s rounded to e2m1, at most 6; 0 where s is 0
+ *
+ * All roundings are to nearest, ties to even, of the exact quotient.  A block that holds a NaN or an infinity has a NaN
+ * scale.  `mult` keeps e4m3 scales in range for the tensor as a whole (448 * 6 / the tensor's amax, say); its
+ * inverse goes into the product's alpha.  rows == 0 or k == 0 does nothing.  Any extent up to 2^31 - 1024 and alignment
+ * of X.  Needs no workspace.  Deterministic, asynchronous on `stream`.
+ */
+int morello_fp4_quantize(int format, int x_type, int x_layout, int64_t rows, int64_t parts, int64_t k, const void* X,
+                         const float* mult, void* Q, void* scales, void* stream);
+
+/* Y[rows][k] (bf16 or f32, y_type) = the tensor's values times the one f32 at `alpha` (device memory, NULL: 1); without
+ * alpha exact in either type.  What a NaN scale serves is NaN. */
+int morello_fp4_dequantize(int format, int y_type, int64_t rows, int64_t parts, int64_t k, const void* Q,
+                           const void* scales, const float* alpha, void* Y, void* stream);
+
+/*
+ * morello_linear on 4-bit tensors of one format:
+ *
+ *     z[i,j] = alpha * sum_{p<k} X[i,p] * W[j,p] + bias[j]
+ *     gated == 0:  Y[i,j] = act(z[i,j]) + R[i,j]
+ *     gated == 1:  Y[i,j] = act(z[i,j]) * z[i,n+j] + R[i,j]          (W and bias have 2 n rows)
+ *
+ *     X: a tensor of m rows, one part;  W: of n rows, one part, or (gated) of 2 n rows in two parts;
+ *     alpha: one f32 in device memory, or NULL (1);  bias[n or 2 n] bf16 or NULL;  R[m][n] bf16 or NULL;
+ *     Y[m][n] bf16 or f32 (y_type).
+ *
+ * Products of elements and scales are exact, sums f32, Y is rounded once.  k == 0 is an empty sum (Y = act(bias) + R);
+ * m == 0 or n == 0 does nothing.  R may be Y itself when both are bf16; no other overlap is allowed.  X, W and their
+ * scales are 16-byte aligned, other tensors to their elements.  A NaN scale makes the results it reaches NaN.  Needs no
+ * workspace.  Deterministic, asynchronous on `stream`.
+ */
+int morello_fp4_linear(int format, int act, int gated, int y_type, int64_t m, int64_t k, int64_t n, const void* X,
+                       const void* X_scales, const void* W, const void* W_scales, const float* alpha, const void* bias,
+                       const void* R, void* Y, void* stream);
+
 /* --- introspection and experiments (tests and benchmarks) ------------------ */
 
 /* The path the selector picks for this shape with 16-byte-aligned operands:

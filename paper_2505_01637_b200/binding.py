@@ -35,6 +35,7 @@ MORELLO_ACT_NONE, MORELLO_ACT_RELU, MORELLO_ACT_GELU, MORELLO_ACT_GELU_TANH, MOR
 MORELLO_BF16, MORELLO_F32 = 0, 1
 MORELLO_W_ROWMAJOR, MORELLO_W_COLMAJOR = 0, 1
 MORELLO_SCORE_SOFTMAX, MORELLO_SCORE_SIGMOID = 0, 1
+MORELLO_MXFP4, MORELLO_NVFP4 = 0, 1
 
 _i64, _vp, _int, _sz = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
 
@@ -80,6 +81,11 @@ SIGNATURES = {
     "morello_layer_norm": (_int, [_int] * 2 + [_i64] * 2 + [ctypes.c_float] + [_vp] * 7),
     "morello_layer_norm_backward": (_int, [_int] * 3 + [_i64] * 2 + [_vp] * 10 + [_sz, _vp]),
     "morello_layer_norm_backward_workspace_bytes": (_sz, [_i64] * 2),
+    "morello_fp4_bytes": (_i64, [_i64] * 2),
+    "morello_fp4_scale_bytes": (_i64, [_int] + [_i64] * 3),
+    "morello_fp4_quantize": (_int, [_int] * 3 + [_i64] * 3 + [_vp] * 5),
+    "morello_fp4_dequantize": (_int, [_int] * 2 + [_i64] * 3 + [_vp] * 5),
+    "morello_fp4_linear": (_int, [_int] * 4 + [_i64] * 3 + [_vp] * 9),
     "morello_read_device_status": (_int, [_vp, ctypes.POINTER(ctypes.c_uint32)]),
     "morello_device_limits": (_int, [ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]),
     "morello_launch_count": (ctypes.c_uint64, []),
@@ -394,6 +400,36 @@ def morello_layer_norm_backward(rms, x_type, accumulate, m, n, X, gamma, mean, r
 
 def morello_layer_norm_backward_workspace_bytes(m, n) -> int:
     return int(lib().morello_layer_norm_backward_workspace_bytes(m, n))
+
+
+def morello_fp4_bytes(rows, k) -> int:
+    return int(lib().morello_fp4_bytes(rows, k))
+
+
+def morello_fp4_scale_bytes(format, rows, parts, k) -> int:
+    return int(lib().morello_fp4_scale_bytes(format, rows, parts, k))
+
+
+def morello_fp4_quantize(format, x_type, x_layout, rows, parts, k, X, mult, Q, scales, stream=None) -> None:
+    """X (times the one f32 at mult, if any) to 4-bit blocks along k with a scale each."""
+    _check(lib().morello_fp4_quantize(format, x_type, x_layout, rows, parts, k, _addr(X), _addr(mult), _addr(Q),
+                                      _addr(scales), _stream(stream)),
+           "morello_fp4_quantize")
+
+
+def morello_fp4_dequantize(format, y_type, rows, parts, k, Q, scales, alpha, Y, stream=None) -> None:
+    """Y[rows][k] = the values of a 4-bit tensor (times the one f32 at alpha, if any)."""
+    _check(lib().morello_fp4_dequantize(format, y_type, rows, parts, k, _addr(Q), _addr(scales), _addr(alpha), _addr(Y),
+                                        _stream(stream)),
+           "morello_fp4_dequantize")
+
+
+def morello_fp4_linear(format, act, gated, y_type, m, k, n, X, X_scales, W, W_scales, alpha, bias, R, Y,
+                       stream=None) -> None:
+    """morello_linear on 4-bit X and W: z = alpha * (X W) + bias; alpha, bias and R may be None."""
+    _check(lib().morello_fp4_linear(format, act, gated, y_type, m, k, n, _addr(X), _addr(X_scales), _addr(W),
+                                    _addr(W_scales), _addr(alpha), _addr(bias), _addr(R), _addr(Y), _stream(stream)),
+           "morello_fp4_linear")
 
 
 def morello_read_device_status(stream=None):

@@ -1,0 +1,463 @@
+// Microscaled 4-bit tensors: quantisation and reading back.
+//
+// A block of 32 (or 16) elements along k shares a scale s, elements are e2m1: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives.
+//   mx   s = 2^(floor(log2 amax) - 2): amax / s is in [4, 8), and what is beyond 6 becomes 6
+//   nv   s = amax / 6 rounded to e4m3 (at most 448)
+// and every element is x / s rounded to the nearest e2m1 value, ties to the even code.
+//
+// Rounding is exact: the result is that of the real quotient.  By a power of two a product is exact.  An e4m3 scale
+// has at most 4 significant bits, a midpoint of two e2m1 values 3: x / s equals a midpoint t only if x = t s, 7 bits.
+// An f32 quotient rounded to nearest never moves from beside a midpoint onto it, since x differs from t s by an ulp of x
+// at least, half an ulp of t s or more.  A bf16 x (8 bits) differs from t s by 2^-8 of it at least, so a product with the
+// rounded reciprocal of s, itself rounded to 2^-13, is on the same side too, and on the midpoint where x / s is: one
+// fma and an addition instead of a division.  The same holds for amax / 6, whose midpoints have 5 bits.
+//
+// Bound by memory: one read of X, one write.  A lane takes eight elements of a row of the [rows][k] layout, a warp 256
+// columns of four rows 32 apart, which share the 16 contiguous bytes of an atom's scales.  The [k][rows] layout is
+// turned in registers: a lane takes two rows and 32 elements of each, a warp reads 64 columns' pairs side by side.
+#include <algorithm>
+
+#include "../../include/morello.h"
+#include "fp4.h"
+#include "octets.cuh"
+#include "sm100.cuh"
+
+namespace morello {
+namespace {
+
+using namespace sm100;
+
+constexpr uint32_t kFull = 0xffffffffu;
+constexpr int kThreads = 256;
+
+struct QuantizeParams {
+  const void* X;
+  const float* mult;
+  uint8_t* q;
+  uint8_t* scales;
+  int64_t each, parts, k;      // rows of a part
+  int64_t pitch;               // bytes of a row of q
+  int down, across;            // atoms of a part
+  int segments;                // 256-column pieces of a row
+  int width;                   // elements of X per access
+  int64_t items;
+};
+
+// Eight e2m1 codes, the first in the lowest four bits; beyond 6 is 6.
+__device__ __forceinline__ uint32_t e2m1_codes(const float (&v)[8]) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return r;
+}
+__device__ __forceinline__ uint32_t e4m3_code(float v) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(v));
+  return r & 0xffu;
+}
+__device__ __forceinline__ float f16_low(uint32_t h) {
+  float f;
+  asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %1;\n\tcvt.f32.f16 %0, l;\n\t}" : "=f"(f) : "r"(h));
+  return f;
+}
+__device__ __forceinline__ float f16_high(uint32_t h) {
+  float f;
+  asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %1;\n\tcvt.f32.f16 %0, u;\n\t}" : "=f"(f) : "r"(h));
+  return f;
+}
+__device__ __forceinline__ float e4m3_value(uint32_t code) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)code));
+  return f16_low(h);
+}
+constexpr uint32_t kInfinity = 0x7f800000u;
+
+// The scale's byte of a block whose largest magnitude has these bits; an infinity or a NaN in the block: NaN.
+template <bool kNv>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
+  if constexpr (kNv) return amax >= kInfinity ? 0x7fu : e4m3_code(__fdiv_rn(__uint_as_float(amax), 6.f));
+  else return amax >= kInfinity ? 0xffu : (uint32_t)max((int)(amax >> 23) - 2, 0);
+}
+// What an element is multiplied with (or divided by) before it is rounded.
+template <bool kNv, bool kDivide>
+struct Scaler {
+  float f;
+  // From the scale's byte.  A scale of 0 leaves codes of 0; behind a NaN scale the codes mean nothing.
+  __device__ __forceinline__ explicit Scaler(uint32_t byte) {
+    if constexpr (!kNv) {
+      f = byte == 0xffu ? 0.f : __uint_as_float((254u - byte) << 23);       // 2^(127 - byte)
+    } else {
+      const float s = e4m3_value(byte);
+      const bool none = byte == 0u || byte == 0x7fu;
+      if constexpr (kDivide) f = none ? __uint_as_float(kInfinity) : s;
+      else f = none ? 0.f : __fdiv_rn(1.f, s);
+    }
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    if constexpr (!kNv) return x * f;
+    if constexpr (kDivide) return __fdiv_rn(x, f);
+    constexpr float kSnap = 1536.f;      // sums with it are multiples of 2^-13
+    return fmaf(x, f, kSnap) - kSnap;
+  }
+};
+
+// Eight elements of X, f32, times the tensor's factor; bits of the largest magnitude.
+template <bool kF32>
+__device__ __forceinline__ void load_octet(const void* X, int64_t at, int64_t cols, int width, float (&v)[8]) {
+  if constexpr (kF32) {
+    const float* src = static_cast<const float*>(X) + at;
+    if (cols >= 8 && width >= 4) {
+      const float4 a = reinterpret_cast<const float4*>(src)[0], b = reinterpret_cast<const float4*>(src)[1];
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = e < cols ? src[e] : 0.f;
+    }
+  } else {
+    const uint4 w = cols > 0 ? load8_raw(static_cast<const uint16_t*>(X) + at, width, cols) : make_uint4(0u, 0u, 0u, 0u);
+    unpack8(w, v);
+  }
+}
+
+constexpr int kRowsAtOnce = 4;      // 32 apart: an atom's rows of the same 16 bytes
+
+template <bool kNv, bool kF32, bool kMult>
+__global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeParams p) {
+  constexpr int kLanes = kNv ? 2 : 4;            // of a block
+  const int lane = threadIdx.x % 32;
+  const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  pdl_wait();
+  pdl_release();
+  if (item >= p.items) return;
+  const int r32 = (int)(item & 31);
+  const int64_t band = item >> 5;                // (part, atom down, segment)
+  const int segment = (int)(band % p.segments);
+  const int64_t atom_row = band / p.segments;    // part * down + atom
+  const int64_t part = atom_row / p.down;
+  const int64_t row0 = (atom_row - part * p.down) * kAtomRows + r32;      // inside the part
+  const int64_t col = (int64_t)segment * 256 + lane * 8;
+  const float mult = kMult ? *p.mult : 1.f;
+  float v[kRowsAtOnce][8];
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i) {
+    const int64_t row = row0 + 32 * i;
+    load_octet<kF32>(p.X, (part * p.each + row) * p.k + col, row < p.each ? p.k - col : 0, p.width, v[i]);
+  }
+  uint32_t words[kRowsAtOnce];
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i) {
+    uint32_t amax = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (kMult) v[i][e] = __fmul_rn(v[i][e], mult);
+      amax = max(amax, __float_as_uint(v[i][e]) & 0x7fffffffu);
+    }
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) amax = max(amax, __shfl_xor_sync(kFull, amax, d));
+    const bool there = row0 + 32 * i < p.each && col / (kNv ? 16 : 32) * (kNv ? 16 : 32) < p.k;
+    const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
+    const Scaler<kNv, kF32 || kMult> scaled(byte);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[i][e] = scaled(v[i][e]);
+    if (there || (row0 + 32 * i < p.each && col < 2 * p.pitch))
+      *reinterpret_cast<uint32_t*>(p.q + (part * p.each + row0 + 32 * i) * p.pitch + col / 2) = e2m1_codes(v[i]);
+    uint32_t word = byte << (8 * (lane / kLanes % 4));
+    word |= __shfl_xor_sync(kFull, word, kLanes);
+    words[i] = word | __shfl_xor_sync(kFull, word, 2 * kLanes);
+  }
+  const int across = segment * (kNv ? 4 : 2) + lane / (4 * kLanes);
+  if (lane % (4 * kLanes) == 0 && across < p.across)
+    *reinterpret_cast<uint4*>(p.scales + (atom_row * p.across + across) * kAtomBytes + r32 * 16) =
+        make_uint4(words[0], words[1], words[2], words[3]);
+}
+
+// X[k][rows]: a block turns 64 rows x 256 elements, a warp 32 elements of each.
+constexpr int kTurnRows = 64;
+template <bool kNv, bool kF32, bool kMult>
+__global__ void __launch_bounds__(kThreads) quantize_turned_kernel(const QuantizeParams p) {
+  constexpr int kBlocks = kNv ? 2 : 1;           // blocks of 32 elements
+  constexpr int kBlock = 32 / kBlocks;
+  __shared__ __align__(16) uint8_t bytes[kTurnRows][16 + 4];   // rows 20 bytes apart: words of different rows in different banks
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int64_t halves = 2 * (int64_t)p.down;    // tiles of a part
+  const int64_t tile = (int64_t)blockIdx.x / p.segments;
+  const int segment = (int)((int64_t)blockIdx.x % p.segments);
+  const int64_t part = tile / halves, row0 = (tile - part * halves) * kTurnRows;      // inside the part
+  const int64_t col = (int64_t)segment * 256 + warp * 32;
+  pdl_wait();
+  pdl_release();
+  const float mult = kMult ? *p.mult : 1.f;
+  const int64_t rows = p.each * p.parts;         // of X's rows of memory
+  const int64_t mine = row0 + 2 * lane;
+  const int64_t left = p.each - mine;            // of this lane's rows that exist
+  const int64_t at = part * p.each + mine;
+  float v[2][32];
+  if (p.width >= 2) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const bool has = left > 0 && col + i < p.k;      // rows and parts are even: both rows exist or neither
+      if constexpr (kF32) {
+        const float2 w = has ? *reinterpret_cast<const float2*>(static_cast<const float*>(p.X) + (col + i) * rows + at) : make_float2(0.f, 0.f);
+        v[0][i] = w.x;
+        v[1][i] = w.y;
+      } else {
+        const uint32_t w = has ? *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.X) + (col + i) * rows + at) : 0u;
+        v[0][i] = bf16_low(w);
+        v[1][i] = bf16_high(w);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool has = left > h && col + i < p.k;
+        if constexpr (kF32) v[h][i] = has ? static_cast<const float*>(p.X)[(col + i) * rows + at + h] : 0.f;
+        else v[h][i] = has ? bf16_value(static_cast<const uint16_t*>(p.X)[(col + i) * rows + at + h]) : 0.f;
+      }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t codes[4];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      uint32_t amax = 0;
+#pragma unroll
+      for (int i = 0; i < kBlock; ++i) {
+        float& x = v[h][b * kBlock + i];
+        if constexpr (kMult) x = __fmul_rn(x, mult);
+        amax = max(amax, __float_as_uint(x) & 0x7fffffffu);
+      }
+      const bool there = left > h && col + b * kBlock < p.k;
+      const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
+      bytes[2 * lane + h][warp * kBlocks + b] = (uint8_t)byte;
+      const Scaler<kNv, kF32 || kMult> scaled(byte);
+#pragma unroll
+      for (int o = 0; o < kBlock / 8; ++o) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = scaled(v[h][b * kBlock + o * 8 + e]);
+        codes[b * (kBlock / 8) + o] = e2m1_codes(w);
+      }
+    }
+    if (left > h && col < p.k)
+      *reinterpret_cast<uint4*>(p.q + (at + h) * p.pitch + col / 2) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+  }
+  __syncthreads();
+  // The tile's scales, an atom's four bytes of a row at a time.
+  const int row = threadIdx.x % kTurnRows, word = threadIdx.x / kTurnRows;
+  const int across = segment * (kNv ? 4 : 2) + word;
+  if (word < (kNv ? 4 : 2) && across < p.across) {
+    const int64_t r = row0 + row;
+    const int64_t atom = part * p.down + r / kAtomRows;
+    *reinterpret_cast<uint32_t*>(p.scales + (atom * p.across + across) * kAtomBytes + (r % 32) * 16 + r % kAtomRows / 32 * 4) =
+        *reinterpret_cast<const uint32_t*>(&bytes[row][word * 4]);
+  }
+}
+
+struct DequantizeParams {
+  const uint8_t* q;
+  const uint8_t* scales;
+  const float* alpha;
+  void* Y;
+  int64_t rows, each, k, pitch;
+  int down, across, segments;
+  int width;                   // elements of Y per access
+  int64_t items;
+};
+// A lane reads eight codes and their scale and writes eight values; a warp 256 columns of kRowsAtOnce rows.
+template <bool kNv, bool kF32>
+__global__ void __launch_bounds__(kThreads) dequantize_kernel(const DequantizeParams p) {
+  const int lane = threadIdx.x % 32;
+  const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  pdl_wait();
+  pdl_release();
+  if (item >= p.items) return;
+  const int64_t row0 = item / p.segments * kRowsAtOnce;
+  const int64_t col = (item % p.segments) * 256 + lane * 8;
+  if (col >= p.k) return;
+  const float alpha = p.alpha ? *p.alpha : 1.f;
+  const int block = (int)(col / (kNv ? 16 : 32));
+  uint32_t codes[kRowsAtOnce], byte[kRowsAtOnce];
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i) {
+    const int64_t row = row0 + i;
+    codes[i] = byte[i] = 0u;
+    if (row < p.rows) {
+      codes[i] = *reinterpret_cast<const uint32_t*>(p.q + row * p.pitch + col / 2);
+      const int64_t part = row / p.each, r = row - part * p.each;
+      byte[i] = p.scales[((part * p.down + r / kAtomRows) * p.across + block / 4) * kAtomBytes + (r % 32) * 16 +
+                         r % kAtomRows / 32 * 4 + block % 4];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kRowsAtOnce; ++i) {
+    const int64_t row = row0 + i;
+    if (row >= p.rows) return;
+    float s;
+    if constexpr (kNv) s = byte[i] == 0x7fu ? __uint_as_float(0x7fffffffu) : e4m3_value(byte[i]);
+    else s = byte[i] == 0xffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte[i] == 0u ? 0x400000u : byte[i] << 23);
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(codes[i]));
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = f16_low(h[j]) * s * alpha;
+      v[2 * j + 1] = f16_high(h[j]) * s * alpha;
+    }
+    const int64_t at = row * p.k + col, left = p.k - col;
+    if constexpr (kF32) {
+      float* dst = static_cast<float*>(p.Y) + at;
+      if (left >= 8 && p.width >= 4) {
+        reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < left) dst[e] = v[e];
+      }
+    } else {
+      store8_raw(static_cast<uint16_t*>(p.Y) + at, p.width, left, pack8(v));
+    }
+  }
+}
+
+// --- host -----------------------------------------------------------------------------------
+
+constexpr int64_t kMaxExtent = (1ll << 31) - 1024;
+
+bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int check_tensor(int format, int type, int64_t rows, int64_t parts, int64_t k) {
+  if (format < 0 || format > 1 || type < 0 || type > 1) return MORELLO_ERR_INVALID_ARGUMENT;
+  if (rows < 0 || k < 0 || parts < 1 || rows > kMaxExtent || k > kMaxExtent || rows % parts != 0) return MORELLO_ERR_INVALID_SHAPE;
+  int64_t t;
+  if (__builtin_mul_overflow(parts * fp4_atoms_down(rows / parts), fp4_atoms_across(format == MORELLO_NVFP4, k) * kAtomBytes, &t) ||
+      __builtin_mul_overflow(rows, k * 4, &t))
+    return MORELLO_ERR_INVALID_SHAPE;
+  return MORELLO_OK;
+}
+
+// Elements per access that f32 rows of `cols` elements allow: 4, 2 or 1.
+int access_width_f32(int64_t cols, const void* p) {
+  for (int w = 4; w > 1; w /= 2)
+    if (cols % w == 0 && aligned(p, 4 * w)) return w;
+  return 1;
+}
+
+template <bool kNv, bool kF32, bool kMult>
+cudaError_t quantize_launch(const QuantizeParams& p, bool turned, cudaStream_t s) {
+  const int64_t blocks = turned ? p.parts * p.down * 2 * p.segments : (p.items + kThreads / 32 - 1) / (kThreads / 32);
+  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
+  return turned ? launch_pdl(quantize_turned_kernel<kNv, kF32, kMult>, dim3((unsigned)blocks), dim3(kThreads), 0, s, 1, p)
+                : launch_pdl(quantize_kernel<kNv, kF32, kMult>, dim3((unsigned)blocks), dim3(kThreads), 0, s, 1, p);
+}
+
+}  // namespace
+}  // namespace morello
+
+using namespace morello;
+
+#pragma GCC visibility push(default)
+extern "C" {
+
+int64_t morello_fp4_bytes(int64_t rows, int64_t k) {
+  return check_tensor(MORELLO_MXFP4, 0, rows, 1, k) == MORELLO_OK ? rows * fp4_pitch(k) : -1;
+}
+
+int64_t morello_fp4_scale_bytes(int format, int64_t rows, int64_t parts, int64_t k) {
+  if (check_tensor(format, 0, rows, parts, k) != MORELLO_OK) return -1;
+  return parts * fp4_atoms_down(rows / parts) * fp4_atoms_across(format == MORELLO_NVFP4, k) * kAtomBytes;
+}
+
+int morello_fp4_quantize(int format, int x_type, int x_layout, int64_t rows, int64_t parts, int64_t k, const void* X,
+                         const float* mult, void* Q, void* scales, void* stream) {
+  int rc;
+  if (x_layout != MORELLO_W_ROWMAJOR && x_layout != MORELLO_W_COLMAJOR) return MORELLO_ERR_INVALID_ARGUMENT;
+  if ((rc = check_tensor(format, x_type, rows, parts, k)) != MORELLO_OK) return rc;
+  const bool empty = rows == 0 || k == 0, nv = format == MORELLO_NVFP4, f32 = x_type == MORELLO_F32;
+  const bool turned = x_layout == MORELLO_W_ROWMAJOR;
+  if (!empty && (!X || !Q || !scales)) return MORELLO_ERR_NULL_POINTER;
+  if (!aligned(X, f32 ? 4 : 2) || !aligned(mult, 4) || !aligned(Q, 16) || !aligned(scales, 16)) return MORELLO_ERR_MISALIGNED;
+  DeviceInfo dev;
+  void* none = nullptr;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((rc = operator_workspace(0, nullptr, 0, s, &none, &dev)) != MORELLO_OK || empty) return rc;
+  QuantizeParams p;
+  p.X = X;
+  p.mult = mult;
+  p.q = static_cast<uint8_t*>(Q);
+  p.scales = static_cast<uint8_t*>(scales);
+  p.each = rows / parts;
+  p.parts = parts;
+  p.k = k;
+  p.pitch = fp4_pitch(k);
+  p.down = (int)fp4_atoms_down(p.each);
+  p.across = (int)fp4_atoms_across(nv, k);
+  p.segments = (int)((k + 255) / 256);
+  // In the turned layout a lane's two rows are read together where every part begins on an even row.
+  const int64_t contiguous = turned ? (p.each % 2 == 0 ? rows : 1) : k;
+  p.width = f32 ? access_width_f32(contiguous, X) : access_width(contiguous, X);
+  p.items = parts * p.down * 32 * p.segments;
+  cudaError_t e;
+  switch (nv * 4 + f32 * 2 + (mult ? 1 : 0)) {
+    case 0: e = quantize_launch<false, false, false>(p, turned, s); break;
+    case 1: e = quantize_launch<false, false, true>(p, turned, s); break;
+    case 2: e = quantize_launch<false, true, false>(p, turned, s); break;
+    case 3: e = quantize_launch<false, true, true>(p, turned, s); break;
+    case 4: e = quantize_launch<true, false, false>(p, turned, s); break;
+    case 5: e = quantize_launch<true, false, true>(p, turned, s); break;
+    case 6: e = quantize_launch<true, true, false>(p, turned, s); break;
+    default: e = quantize_launch<true, true, true>(p, turned, s); break;
+  }
+  if (e != cudaSuccess) return record_cuda_error(e);
+  count_launches(1);
+  return MORELLO_OK;
+}
+
+int morello_fp4_dequantize(int format, int y_type, int64_t rows, int64_t parts, int64_t k, const void* Q,
+                           const void* scales, const float* alpha, void* Y, void* stream) {
+  int rc;
+  if ((rc = check_tensor(format, y_type, rows, parts, k)) != MORELLO_OK) return rc;
+  const bool empty = rows == 0 || k == 0, nv = format == MORELLO_NVFP4, f32 = y_type == MORELLO_F32;
+  if (!empty && (!Q || !scales || !Y)) return MORELLO_ERR_NULL_POINTER;
+  if (!aligned(Q, 16) || !aligned(scales, 16) || !aligned(alpha, 4) || !aligned(Y, f32 ? 4 : 2)) return MORELLO_ERR_MISALIGNED;
+  DeviceInfo dev;
+  void* none = nullptr;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((rc = operator_workspace(0, nullptr, 0, s, &none, &dev)) != MORELLO_OK || empty) return rc;
+  DequantizeParams p;
+  p.q = static_cast<const uint8_t*>(Q);
+  p.scales = static_cast<const uint8_t*>(scales);
+  p.alpha = alpha;
+  p.Y = Y;
+  p.rows = rows;
+  p.each = rows / parts;
+  p.k = k;
+  p.pitch = fp4_pitch(k);
+  p.down = (int)fp4_atoms_down(p.each);
+  p.across = (int)fp4_atoms_across(nv, k);
+  p.segments = (int)((k + 255) / 256);
+  p.width = f32 ? access_width_f32(k, Y) : access_width(k, Y);
+  p.items = (rows + kRowsAtOnce - 1) / kRowsAtOnce * p.segments;
+  const int64_t blocks = (p.items + kThreads / 32 - 1) / (kThreads / 32);
+  if (blocks >= (1ll << 31)) return MORELLO_ERR_INVALID_SHAPE;
+  const dim3 grid((unsigned)blocks), block(kThreads);
+  cudaError_t e;
+  if (nv) e = f32 ? launch_pdl(dequantize_kernel<true, true>, grid, block, 0, s, 1, p) : launch_pdl(dequantize_kernel<true, false>, grid, block, 0, s, 1, p);
+  else e = f32 ? launch_pdl(dequantize_kernel<false, true>, grid, block, 0, s, 1, p) : launch_pdl(dequantize_kernel<false, false>, grid, block, 0, s, 1, p);
+  if (e != cudaSuccess) return record_cuda_error(e);
+  count_launches(1);
+  return MORELLO_OK;
+}
+
+}  // extern "C"
+#pragma GCC visibility pop

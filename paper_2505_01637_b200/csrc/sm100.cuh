@@ -284,6 +284,32 @@ __device__ __forceinline__ void mma_bf16_ss(uint32_t d_tmem, uint64_t a_desc, ui
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// The same for e2m1 x e2m1 with block scales: kBlock 32 (powers of two, two of a row's four scale bytes a step) or 16
+// (e4m3, all four), 64 elements of the contraction a step.  The scales lie in tensor memory, a row's four bytes to a
+// lane, 128 rows to four columns.
+template <bool kPair, bool kNv>
+__device__ __forceinline__ void mma_fp4_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                           uint32_t a_scales, uint32_t b_scales, uint32_t accumulate) {
+#define MORELLO_MMA_FP4(GROUP, VEC)                                                                              \
+  asm volatile(                                                                                                  \
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                                          \
+      "tcgen05.mma.cta_group::" GROUP ".kind::mxf4nvf4.block_scale.scale_vec::" VEC                              \
+      " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), \
+      "r"(b_scales), "r"(accumulate)                                                                             \
+      : "memory")
+  if constexpr (kPair && kNv) MORELLO_MMA_FP4("2", "4X");
+  else if constexpr (kPair) MORELLO_MMA_FP4("2", "2X");
+  else if constexpr (kNv) MORELLO_MMA_FP4("1", "4X");
+  else MORELLO_MMA_FP4("1", "2X");
+#undef MORELLO_MMA_FP4
+}
+// 512 bytes of shared memory, 32 rows of 16, to four columns of tensor memory, in each of its four quarters of 32 lanes
+// (pair: in both CTAs, from the same offset of each).  Runs in order with the MMAs that the same thread issues.
+template <bool kPair>
+__device__ __forceinline__ void tmem_copy_32x16b(uint32_t taddr, uint64_t desc) {
+  if constexpr (kPair) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
 // Arrives on the mbarrier once every MMA issued so far by this thread has completed.
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
@@ -404,6 +430,20 @@ __host__ __device__ constexpr uint32_t instr_desc_bf16(int m, int n, bool a_mn_m
                                                        bool b_mn_major) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn_major ? 1u : 0u) << 15) |
          ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+// Shared-memory matrix descriptor of 8-row groups of 16-byte rows, 128 bytes apart, without a swizzle (as smem_desc_sw128
+// otherwise).
+__device__ __forceinline__ uint64_t smem_desc_rows16(uint32_t smem_addr) {
+  return (uint64_t)((smem_addr >> 4) & 0x3fffu) | (uint64_t)(128u >> 4) << 32 | (uint64_t)1 << 46;
+}
+
+// Instruction descriptor, kind::mxf4nvf4: e2m1 A (bits 7-9 = 1) and B (bits 10-11 = 1), both K-major, N >> 3 in bits
+// 17-22, power-of-two scales in bit 23 (else e4m3), M >> 7 in bits 27-28; the first of the scale bytes that a step uses
+// in bits 29-30 (A) and 4-5 (B).
+__host__ __device__ constexpr uint32_t instr_desc_fp4(int m, int n, bool nv, int scale_byte) {
+  return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((nv ? 0u : 1u) << 23) | ((uint32_t)(m >> 7) << 27) |
+         ((uint32_t)scale_byte << 29) | ((uint32_t)scale_byte << 4);
 }
 
 }  // namespace sm100
