@@ -420,7 +420,7 @@ int morello_layer_norm(int rms, int x_type, int64_t m, int64_t n, float eps, con
  * dX and R are of X's type; R, the gradient that reaches X past the norm, may be NULL, and may be dX itself.  dX, dgamma
  * and dbeta may each be NULL (not wanted); mean is not read when rms == 1.  accumulate == 1 adds to dgamma and dbeta
  * instead of setting them.  m == 0 sums are empty: zero, or nothing added.  Sums are f32, in an order that is fixed for a
- * shape.  `workspace` (for dgamma and dbeta): morello_layer_norm_backward_workspace_bytes() bytes, 16-byte aligned, or
+ * shape, its types and whether all tensors are 16-byte aligned.  `workspace` (for dgamma and dbeta): morello_layer_norm_backward_workspace_bytes() bytes, 16-byte aligned, or
  * NULL and 0 for the library's own scratch (rules as in morello_matmul_accum).  Asynchronous on `stream`.
  */
 int morello_layer_norm_backward(int rms, int x_type, int accumulate, int64_t m, int64_t n, const void* X,

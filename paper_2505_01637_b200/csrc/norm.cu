@@ -38,6 +38,7 @@ struct NormParams {
   uint16_t* Y;
   float* mean;
   float* rstd;
+  uint32_t* status;
 };
 
 struct NormBackwardParams {
@@ -53,12 +54,14 @@ struct NormBackwardParams {
   void* dX;
   float* partial;        // [blocks][2][n]: the blocks' sums for dgamma and dbeta
   bool beta;             // dbeta is wanted
+  uint32_t* status;
 };
 
-// Sum over the 32 lanes, in every lane.
+// Sum over kLanes neighbouring lanes, in every one of them.
+template <int kLanes = 32>
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(kFull, v, d);
+  for (int d = kLanes / 2; d > 0; d >>= 1) v += __shfl_xor_sync(kFull, v, d);
   return v;
 }
 
@@ -73,7 +76,6 @@ __device__ __forceinline__ void team_barrier(int team) {
 // aligned tensors.  kVec 1: single columns t + i T.  Element e of the thread: columns are known to exist by has(e).
 template <int kT, int kVec, int kIter>
 struct Columns {
-  static constexpr int kCount = kVec * kIter;
   int t, n;
   __device__ __forceinline__ int of(int e) const {
     return kVec == 8 ? (t + e / 8 * kT) * 8 + e % 8 : t + e * kT;
@@ -84,10 +86,9 @@ struct Columns {
 // The raw elements of those columns, bf16 or f32, as they came from memory.
 template <int kT, int kVec, int kIter, bool kF32>
 struct Held {
-  using C = Columns<kT, kVec, kIter>;
-  static constexpr int kWords = kVec == 1 ? C::kCount : C::kCount * (kF32 ? 4 : 2) / 4;
+  static constexpr int kWords = kVec == 1 ? kIter : kVec * kIter * (kF32 ? 4 : 2) / 4;
   uint32_t w[kWords];
-  __device__ __forceinline__ void load(const void* row, const C& c) {
+  __device__ __forceinline__ void load(const void* row, const Columns<kT, kVec, kIter>& c) {
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
       const bool has = c.has(i * kVec);
@@ -105,6 +106,14 @@ struct Held {
       } else {
         w[i] = has ? (uint32_t)static_cast<const uint16_t*>(row)[c.t + i * kT] << 16 : 0u;
       }
+    }
+  }
+  // Octet i, as four pairs.
+  __device__ __forceinline__ void pairs(int i, f32x2 (&v)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (kF32) v[j] = pair_of(__uint_as_float(w[i * 8 + 2 * j]), __uint_as_float(w[i * 8 + 2 * j + 1]));
+      else v[j] = pair_of(bf16_low(w[i * 4 + j]), bf16_high(w[i * 4 + j]));
     }
   }
   __device__ __forceinline__ float get(int e) const {
@@ -145,6 +154,51 @@ __device__ __forceinline__ void vector_part(const uint16_t* p, int col, float mi
   }
 }
 
+// Eight elements as four pairs.
+__device__ __forceinline__ void octet_pairs(const uint4& w, f32x2 (&v)[4]) {
+  v[0] = pair_of(bf16_low(w.x), bf16_high(w.x));
+  v[1] = pair_of(bf16_low(w.y), bf16_high(w.y));
+  v[2] = pair_of(bf16_low(w.z), bf16_high(w.z));
+  v[3] = pair_of(bf16_low(w.w), bf16_high(w.w));
+}
+// Eight columns of gamma or beta; `missing` where there is no such vector.
+__device__ __forceinline__ void vector_pairs(const uint16_t* p, int col, float missing, f32x2 (&v)[4]) {
+  if (p) octet_pairs(*reinterpret_cast<const uint4*>(p + col), v);
+  else v[0] = v[1] = v[2] = v[3] = pair_of(missing);
+}
+// An octet of a row in shared memory.
+template <bool kF32>
+__device__ __forceinline__ void shared_octet(const uint8_t* row, int col, f32x2 (&v)[4]) {
+  if constexpr (kF32) {
+    const float4* q = reinterpret_cast<const float4*>(row) + col / 4;
+    const float4 a = q[0], b = q[1];
+    v[0] = pair_of(a.x, a.y);
+    v[1] = pair_of(a.z, a.w);
+    v[2] = pair_of(b.x, b.y);
+    v[3] = pair_of(b.z, b.w);
+  } else {
+    octet_pairs(*reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(row) + col), v);
+  }
+}
+__device__ __forceinline__ uint32_t bf16_pack_pair(f32x2 v) {
+  const float2 f = pair_values(v);
+  return bf16_pack(f.x, f.y);
+}
+template <bool kF32>
+__device__ __forceinline__ void put_octet(void* row, int col, const f32x2 (&v)[4]) {
+  if constexpr (kF32) {
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + col);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float2 a = pair_values(v[2 * q]), b = pair_values(v[2 * q + 1]);
+      o[q] = make_float4(a.x, a.y, b.x, b.y);
+    }
+  } else {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + col) =
+        make_uint4(bf16_pack_pair(v[0]), bf16_pack_pair(v[1]), bf16_pack_pair(v[2]), bf16_pack_pair(v[3]));
+  }
+}
+
 // What a warp knows of its part of a row: count values of mean `mean` + off / count, squares about `mean` with sum `squares`.
 struct Part {
   float mean, off, squares, count;
@@ -162,7 +216,7 @@ template <int kWarps>
 __device__ __forceinline__ float join_parts(const Part* parts, float inv_n, float* base, float* off) {
   const float m0 = parts[0].mean;
   float shift = 0.f, squares = 0.f;
-  if constexpr (kWarps <= 8) {
+  if constexpr (kWarps <= 4) {
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) shift += shift_of(parts[w], m0);
     shift *= inv_n;
@@ -185,11 +239,10 @@ template <int kT, int kVec, int kIter, bool kF32, bool kRms>
 __global__ void __launch_bounds__(kT > kBlockThreads ? kT : kBlockThreads) norm_kernel(const NormParams p) {
   constexpr int kTeams = kT < kBlockThreads ? kBlockThreads / kT : 1;
   constexpr int kWarps = kT / 32;
-  using C = Columns<kT, kVec, kIter>;
-  constexpr int kCount = C::kCount;
+  constexpr int kCount = kVec * kIter;
   __shared__ Part parts[2][kTeams][kWarps];
   const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / 32, lane = (int)threadIdx.x % 32;
-  const C c{(int)threadIdx.x % kT, p.n};
+  const Columns<kT, kVec, kIter> c{(int)threadIdx.x % kT, p.n};
   float here = 0.f;
 #pragma unroll
   for (int e = 0; e < kCount; ++e) here += c.has(e) ? 1.f : 0.f;
@@ -242,6 +295,342 @@ __global__ void __launch_bounds__(kT > kBlockThreads ? kT : kBlockThreads) norm_
         y[j] = fmaf(d * rstd, gamma[j], beta[j]);
       }
       put_part<kVec, false>(p.Y + row * p.n, c.of(i * kVec), y);
+    }
+  }
+}
+
+// The same by octets, two columns an instruction: n % 8 == 0 and 16-byte-aligned tensors.  Teams of 8 to 512 threads; up to
+// kIter octets of a row to a thread, kept as they came.
+template <int kT, int kIter, bool kF32, bool kRms>
+__global__ void __launch_bounds__(kT > kBlockThreads ? kT : kBlockThreads) norm_octets_kernel(const NormParams p) {
+  constexpr int kTeams = kT < kBlockThreads ? kBlockThreads / kT : 1;
+  constexpr int kLanes = kT < 32 ? kT : 32, kWarps = kT / kLanes;
+  __shared__ Part parts[2][kTeams][kWarps];
+  const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / kLanes, lane = (int)threadIdx.x % kLanes;
+  const Columns<kT, 8, kIter> c{(int)threadIdx.x % kT, p.n};
+  float here = 0.f;
+#pragma unroll
+  for (int i = 0; i < kIter; ++i) here += c.has(i * 8) ? 8.f : 0.f;
+  const float count = warp_sum<kLanes>(here), inv_count = count > 0.f ? 1.f / count : 0.f;
+  pdl_wait();
+  pdl_release();
+  int turn = 0;
+  // Teams of less than a warp leave the loop together: a row past the last is worked on like any other, but neither read nor written.
+  for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < p.m; row0 += (int64_t)gridDim.x * kTeams, turn ^= 1) {
+    const int64_t row = row0 + team;
+    const bool live = row < p.m;
+    if (kT >= 32 && !live) break;
+    Held<kT, 8, kIter, kF32> x;
+    const Columns<kT, 8, kIter> mine_of{c.t, live ? p.n : 0};
+    x.load(static_cast<const char*>(p.X) + row * p.n * (kF32 ? 4 : 2), mine_of);
+    Part mine{0.f, 0.f, 0.f, count};
+    if constexpr (!kRms) {
+      f32x2 sums = 0;
+#pragma unroll
+      for (int i = 0; i < kIter; ++i) {
+        f32x2 v[4];
+        x.pairs(i, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums = add2(sums, v[j]);
+      }
+      mine.mean = warp_sum<kLanes>(pair_sum(sums)) * inv_count;
+    }
+    const f32x2 minus_mean = pair_of(-mine.mean);
+    f32x2 off = 0, squares = 0;
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      if (!c.has(i * 8)) continue;
+      f32x2 v[4];
+      x.pairs(i, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 d = kRms ? v[j] : add2(v[j], minus_mean);
+        if constexpr (!kRms) off = add2(off, d);
+        squares = fma2(d, d, squares);
+      }
+    }
+    if constexpr (!kRms) mine.off = warp_sum<kLanes>(pair_sum(off));
+    mine.squares = warp_sum<kLanes>(pair_sum(squares));
+    float base, shift, square;
+    if constexpr (kWarps == 1) {
+      square = join_parts<1>(&mine, p.inv_n, &base, &shift);
+    } else {
+      if (lane == 0) parts[turn][team][warp] = mine;
+      team_barrier<kT>(team);     // the other set of parts is written next: nobody is still reading it behind this barrier
+      square = join_parts<kWarps>(parts[turn][team], p.inv_n, &base, &shift);
+    }
+    const float rstd = 1.f / sqrtf(square + p.eps);
+    if (c.t == 0 && live) {
+      if (!kRms && p.mean) p.mean[row] = base + shift;
+      if (p.rstd) p.rstd[row] = rstd;
+    }
+    const f32x2 factor = pair_of(rstd), minus_base = pair_of(-base), shifted = pair_of(-shift * rstd);
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      if (!mine_of.has(i * 8)) continue;
+      f32x2 v[4], gamma[4], beta[4], y[4];
+      x.pairs(i, v);
+      vector_pairs(p.gamma, c.of(i * 8), 1.f, gamma);
+      vector_pairs(p.beta, c.of(i * 8), 0.f, beta);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 h = kRms ? mul2(v[j], factor) : fma2(add2(v[j], minus_base), factor, shifted);
+        y[j] = fma2(h, gamma[j], beta[j]);
+      }
+      put_octet<false>(p.Y + row * p.n, c.of(i * 8), y);
+    }
+  }
+}
+
+// --- rows through a ring in shared memory ------------------------------------------------------
+//
+// Whole batches: one or two persistent blocks of 16 warps to an SM.  A group is kTeams neighbouring rows, one to a team, and
+// contiguous in memory: one bulk copy per tensor.  The first thread keeps the ring full: behind every group it has worked
+// on it waits until the others are done with the one before, and has the next copied there.  The loads' latency, which a
+// team that loads its own rows waits out at every row, is behind the ring.  (A warp of its own for the copies takes 3 of
+// every 16 registers a thread, since registers are given to four warps at a time.)
+constexpr int kRingThreads = 512;
+constexpr int kMaxStages = 16;
+struct RingBars {
+  uint64_t full[kMaxStages];
+  uint64_t empty[kMaxStages];
+  int abort_flag;
+};
+struct RingShape {
+  int stages;
+  uint32_t stage_bytes;        // a group's rows of every tensor
+};
+
+struct RingTensor {
+  const void* p;
+  uint32_t row_bytes;
+};
+// Starts the copies of the group whose first row is `row` to a stage.
+template <int kTeams, int kTensors>
+__device__ __forceinline__ void ring_fill(RingBars* bars, uint8_t* smem, const RingShape& ring, int stage, int64_t row, int64_t m,
+                                          const RingTensor (&tensors)[kTensors]) {
+  const uint32_t rows = (uint32_t)min((int64_t)kTeams, m - row);
+  uint32_t bytes = 0;
+#pragma unroll
+  for (int i = 0; i < kTensors; ++i) bytes += tensors[i].p ? rows * tensors[i].row_bytes : 0u;
+  mbar_arrive_expect_tx(&bars->full[stage], bytes);
+  uint8_t* dst = smem + (size_t)stage * ring.stage_bytes;
+#pragma unroll
+  for (int i = 0; i < kTensors; ++i) {
+    if (!tensors[i].p) continue;
+    bulk_load(dst, static_cast<const uint8_t*>(tensors[i].p) + row * tensors[i].row_bytes, rows * tensors[i].row_bytes,
+              &bars->full[stage]);
+    dst += kTeams * tensors[i].row_bytes;
+  }
+}
+__device__ __forceinline__ void ring_init(RingBars* bars, int stages) {
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < stages; ++i) {
+      mbar_init(&bars->full[i], 1);
+      mbar_init(&bars->empty[i], kRingThreads / 32);
+    }
+    bars->abort_flag = 0;
+    mbar_fence_init();
+  }
+  __syncthreads();
+}
+// Where a block is in the ring.
+struct RingPlace {
+  int stage = 0, before = -1;        // the group's stage, and the one before it
+  uint32_t phase = 0, phase_before = 0;
+  int64_t fill;                      // first row of the next group to copy
+  __device__ __forceinline__ void next(int stages) {
+    before = stage;
+    phase_before = phase;
+    if (++stage == stages) { stage = 0; phase ^= 1; }
+  }
+};
+template <int kTeams, int kTensors>
+__device__ __forceinline__ void ring_start(RingBars* bars, uint8_t* smem, const RingShape& ring, RingPlace* at, int64_t m,
+                                           const RingTensor (&tensors)[kTensors]) {
+  at->fill = (int64_t)blockIdx.x * kTeams;
+  if (threadIdx.x != 0) return;
+  for (int i = 0; i < ring.stages && at->fill < m; ++i, at->fill += (int64_t)gridDim.x * kTeams)
+    ring_fill<kTeams>(bars, smem, ring, i, at->fill, m, tensors);
+}
+// A warp is done with the group; the first thread has the stage before it filled again.
+template <int kTeams, int kTensors>
+__device__ __forceinline__ bool ring_next(RingBars* bars, uint8_t* smem, const RingShape& ring, RingPlace* at, int64_t m,
+                                          const RingTensor (&tensors)[kTensors], uint32_t* status) {
+  bool ok = true;
+  __syncwarp();
+  if (threadIdx.x % 32 == 0) mbar_arrive(&bars->empty[at->stage]);
+  if (threadIdx.x == 0 && at->before >= 0 && at->fill < m) {
+    ok = mbar_wait(&bars->empty[at->before], at->phase_before, &bars->abort_flag, status, 61);
+    if (ok) ring_fill<kTeams>(bars, smem, ring, at->before, at->fill, m, tensors);
+    at->fill += (int64_t)gridDim.x * kTeams;
+  }
+  at->next(ring.stages);
+  return ok;
+}
+// A thread's octets of gamma or beta, kept through all its rows where registers allow (kIter 2), read again where not.
+template <int kT, int kIter>
+struct HeldVector {
+  static constexpr bool kHold = kIter <= 2;
+  const uint16_t* p;
+  uint4 w[kHold ? kIter : 1];
+  float missing;
+  __device__ __forceinline__ HeldVector(const uint16_t* vector, float instead, const Columns<kT, 8, kIter>& c)
+      : p(vector), missing(instead) {
+    if constexpr (kHold) {
+      const uint32_t pair = __float_as_uint(instead) | (__float_as_uint(instead) >> 16);      // exact in bf16
+#pragma unroll
+      for (int i = 0; i < kIter; ++i)
+        w[i] = p && c.has(i * 8) ? *reinterpret_cast<const uint4*>(p + c.of(i * 8)) : make_uint4(pair, pair, pair, pair);
+    }
+  }
+  __device__ __forceinline__ void get(int i, int col, f32x2 (&v)[4]) const {
+    if constexpr (kHold) {
+      octet_pairs(w[i], v);
+    } else {
+      vector_pairs(p, col, missing, v);
+    }
+  }
+};
+template <int kT>
+__device__ __forceinline__ void ring_team_barrier(int team) {
+  asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(kT) : "memory");
+}
+
+template <int kT, int kIter, bool kF32, bool kRms>
+__global__ void __launch_bounds__(kRingThreads, 1)
+norm_backward_ring_kernel(const NormBackwardParams p, const RingShape ring) {
+  constexpr int kTeams = kRingThreads / kT, kWarps = kT / 32;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ RingBars bars;
+  __shared__ float2 parts[2][kTeams][kWarps];
+  ring_init(&bars, ring.stages);
+  pdl_wait();
+  pdl_release();
+  const uint32_t row16 = (uint32_t)p.n * 2, row_x = kF32 ? 2 * row16 : row16;
+  const RingTensor tensors[3] = {{p.X, row_x}, {p.dY, row16}, {p.dX ? p.R : nullptr, row_x}};
+  RingPlace at;
+  ring_start<kTeams>(&bars, smem, ring, &at, p.m, tensors);
+  const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / 32, lane = (int)threadIdx.x % 32;
+  const Columns<kT, 8, kIter> c{(int)threadIdx.x % kT, p.n};
+  const HeldVector<kT, kIter> gammas(p.gamma, 1.f, c);
+  f32x2 sum_g[kIter][4], sum_b[kIter][4];
+#pragma unroll
+  for (int i = 0; i < kIter; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum_g[i][j] = sum_b[i][j] = 0;
+  int turn = 0;
+  bool ok = true;
+  const int64_t step = (int64_t)gridDim.x * kTeams;
+  int64_t row = (int64_t)blockIdx.x * kTeams + team;
+  // The row's mean and rstd are fetched a row ahead.
+  float mean = 0.f, rstd = 0.f, next_mean = 0.f, next_rstd = 0.f;
+  auto fetch = [&](int64_t r) {
+    if (r < p.m) {
+      if constexpr (!kRms) next_mean = p.mean[r];
+      next_rstd = p.rstd[r];
+    }
+  };
+  fetch(row);
+  for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < p.m; row0 += step, row += step, turn ^= 1) {
+    mean = next_mean;
+    rstd = next_rstd;
+    fetch(row + step);
+    if (ok) ok = mbar_wait(&bars.full[at.stage], at.phase, &bars.abort_flag, p.status, 63);
+    ok = __all_sync(kFull, ok);
+    const bool live = ok && row < p.m;
+    const uint8_t* x_row = smem + (size_t)at.stage * ring.stage_bytes + team * row_x;
+    const uint8_t* dy_row = smem + (size_t)at.stage * ring.stage_bytes + kTeams * row_x + team * row16;
+    const uint8_t* r_row = smem + (size_t)at.stage * ring.stage_bytes + kTeams * (row_x + row16) + team * row_x;
+    f32x2 p1 = 0, p2 = 0;      // sums of g and of g (x - mean)
+    const f32x2 minus_mean = pair_of(-mean), factor = pair_of(rstd);
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < kIter; ++i) {
+        if (!c.has(i * 8)) continue;
+        f32x2 x[4], dy[4], gamma[4];
+        shared_octet<kF32>(x_row, c.of(i * 8), x);
+        shared_octet<false>(dy_row, c.of(i * 8), dy);
+        gammas.get(i, c.of(i * 8), gamma);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x2 d = kRms ? x[j] : add2(x[j], minus_mean), g = mul2(dy[j], gamma[j]);
+          if constexpr (!kRms) p1 = add2(p1, g);
+          p2 = fma2(g, d, p2);
+          sum_g[i][j] = fma2(dy[j], mul2(d, factor), sum_g[i][j]);
+          sum_b[i][j] = add2(sum_b[i][j], dy[j]);
+        }
+      }
+    }
+    if (p.dX) {
+      float s1 = 0.f, s2 = warp_sum(pair_sum(p2));
+      if constexpr (!kRms) s1 = warp_sum(pair_sum(p1));
+      if constexpr (kT > 32) {
+        if (lane == 0) parts[turn][team][warp] = make_float2(s1, s2);
+        ring_team_barrier<kT>(team);
+        s1 = s2 = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          s1 += parts[turn][team][w].x;
+          s2 += parts[turn][team][w].y;
+        }
+      }
+      // dx = rstd g - rstd mean(g) - (mean(g h) rstd) rstd (x - mean) ...
+      const f32x2 constant = pair_of(-rstd * s1 * p.inv_n), slope = pair_of(-(s2 * rstd * p.inv_n * rstd) * rstd);
+      if (live) {
+#pragma unroll
+        for (int i = 0; i < kIter; ++i) {
+          if (!c.has(i * 8)) continue;
+          f32x2 x[4], dy[4], gamma[4], r[4], out[4];
+          shared_octet<kF32>(x_row, c.of(i * 8), x);
+          shared_octet<false>(dy_row, c.of(i * 8), dy);
+          if (p.R) shared_octet<kF32>(r_row, c.of(i * 8), r);
+          gammas.get(i, c.of(i * 8), gamma);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x2 d = kRms ? x[j] : add2(x[j], minus_mean);
+            out[j] = fma2(mul2(dy[j], gamma[j]), factor, kRms ? mul2(d, slope) : fma2(d, slope, constant));
+            if (p.R) out[j] = add2(out[j], r[j]);
+          }
+          put_octet<kF32>(static_cast<char*>(p.dX) + row * row_x, c.of(i * 8), out);
+        }
+      }
+    }
+    ok = ring_next<kTeams>(&bars, smem, ring, &at, p.m, tensors, p.status) && ok;
+  }
+  if (!p.partial) return;
+  // The teams' sums meet in the ring's memory, whose last copies every team has read.
+  if constexpr (kTeams > 1) {
+    float* joined = reinterpret_cast<float*>(smem);        // [team][2][kT * kIter * 8]
+    constexpr int kWide = kT * kIter * 8;
+    asm volatile("bar.sync 15, %0;" ::"n"(kRingThreads) : "memory");     // no team's own
+    float* mine = joined + (size_t)team * 2 * kWide;
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      put_octet<true>(mine, c.of(i * 8), sum_g[i]);
+      put_octet<true>(mine + kWide, c.of(i * 8), sum_b[i]);
+    }
+    asm volatile("bar.sync 15, %0;" ::"n"(kRingThreads) : "memory");     // no team's own
+    if (!ok) return;
+    float* out = p.partial + (int64_t)blockIdx.x * 2 * p.n;
+    for (int col = (int)threadIdx.x; col < p.n; col += kRingThreads) {
+      float g = 0.f, b = 0.f;
+#pragma unroll
+      for (int t = 0; t < kTeams; ++t) {
+        g += joined[(size_t)t * 2 * kWide + col];
+        b += joined[(size_t)t * 2 * kWide + kWide + col];
+      }
+      out[col] = g;
+      if (p.beta) out[p.n + col] = b;
+    }
+  } else {
+    if (!ok) return;
+    float* out = p.partial + (int64_t)blockIdx.x * 2 * p.n;
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      if (!c.has(i * 8)) continue;
+      put_octet<true>(out, c.of(i * 8), sum_g[i]);
+      if (p.beta) put_octet<true>(out + p.n, c.of(i * 8), sum_b[i]);
     }
   }
 }
@@ -301,11 +690,10 @@ template <int kT, int kVec, int kIter, bool kF32, bool kRms, bool kSums>
 __global__ void __launch_bounds__(kBlockThreads) norm_backward_kernel(const NormBackwardParams p) {
   constexpr int kTeams = kBlockThreads / kT;
   constexpr int kWarps = kT / 32;
-  using C = Columns<kT, kVec, kIter>;
-  constexpr int kCount = C::kCount;
+  constexpr int kCount = kVec * kIter;
   __shared__ float2 parts[2][kTeams][kWarps];
   const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / 32, lane = (int)threadIdx.x % 32;
-  const C c{(int)threadIdx.x % kT, p.n};
+  const Columns<kT, kVec, kIter> c{(int)threadIdx.x % kT, p.n};
   float sum_g[kSums ? kCount : 1], sum_b[kSums ? kCount : 1];
   if constexpr (kSums) {
 #pragma unroll
@@ -503,52 +891,90 @@ constexpr int kTeamBackward = 8192;     // columns a team of 256 threads holds b
 
 bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
+// The ring's teams: 16 columns to a thread, 32 in the longest rows.
+int ring_team(int64_t n) {
+  int t = 32;
+  while (t < kRingThreads && n > t * 16) t *= 2;
+  return t;
+}
+// Stages that fit `budget` bytes of shared memory beside the static part; below two the ring does not run.
+RingShape ring_shape(int64_t n, int64_t column_bytes, int budget) {
+  RingShape r;
+  const int64_t bytes = kRingThreads / ring_team(n) * n * column_bytes;
+  r.stage_bytes = (uint32_t)bytes;
+  r.stages = (int)std::min<int64_t>(kMaxStages, budget / bytes);
+  return r;
+}
+
 // Threads of a team: the fewest that hold the row in at most 32 columns each.
 int team_of(int64_t n) { return n <= 1024 ? 32 : n <= 4096 ? 128 : n <= 8192 ? 256 : 512; }
 
+// Blocks at most that leave sums of their own.
 int64_t backward_parts(int64_t m, int64_t n) {
-  if (m == 0) return 0;
-  if (n > kTeamBackward) return std::min<int64_t>(kMaxParts, (m + 127) / 128);
+  if (n > kTeamBackward) return std::min<int64_t>(kMaxParts, m);
   const int64_t teams = kBlockThreads / team_of(n);
   return std::min<int64_t>(kMaxParts, (m + teams - 1) / teams);
 }
 size_t backward_bytes(int64_t m, int64_t n) { return (size_t)backward_parts(m, n) * 2 * n * 4; }
 
+constexpr int kBackwardBudget = 224 * 1024;
+
+template <auto kKernel, int kBudget, typename Params>
+cudaError_t ring_launch(const Params& p, const RingShape& ring, int teams, int64_t most, size_t least_smem, cudaStream_t s) {
+  static PerDeviceOnce once;
+  const cudaError_t e = once.run_current(
+      [] { return cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBudget); });
+  if (e != cudaSuccess) return e;
+  const int64_t blocks = std::min(most, (p.m + teams - 1) / teams);
+  return launch_pdl(kKernel, dim3((unsigned)blocks), dim3(kRingThreads),
+                    std::max(least_smem, (size_t)ring.stages * ring.stage_bytes), s, 1, p, ring);
+}
+template <bool kF32, bool kRms>
+cudaError_t backward_ring(const NormBackwardParams& p, const RingShape& ring, int64_t blocks, cudaStream_t s) {
+#define MORELLO_RING(T, ITER)                                                                                          \
+  return ring_launch<norm_backward_ring_kernel<T, ITER, kF32, kRms>, kBackwardBudget>(p, ring, kRingThreads / T, blocks, \
+                                                                                      (size_t)kRingThreads * ITER * 64, s)
+  if (p.n <= 256) MORELLO_RING(32, 1);
+  if (p.n <= 512) MORELLO_RING(32, 2);
+  if (p.n <= 1024) MORELLO_RING(64, 2);
+  if (p.n <= 2048) MORELLO_RING(128, 2);
+  if (p.n <= 4096) MORELLO_RING(256, 2);
+  if (p.n <= 8192) MORELLO_RING(512, 2);
+  MORELLO_RING(512, 4);
+#undef MORELLO_RING
+}
+
 template <bool kF32, bool kRms>
 cudaError_t forward_launch(const DeviceInfo& dev, const NormParams& p, bool vec, cudaStream_t s) {
-  const int n = p.n, t = team_of(n);
-  auto go = [&](auto kernel, int threads, int rows_per_block, int resident) {
-    const int64_t blocks = std::min<int64_t>((p.m + rows_per_block - 1) / rows_per_block, (int64_t)dev.sms * resident);
+  const int n = p.n;
+  auto go = [&](auto kernel, int team) {
+    const int threads = std::max(team, kBlockThreads), rows = threads / team;
+    const int64_t blocks = std::min<int64_t>((p.m + rows - 1) / rows, (int64_t)dev.sms * 8);
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(threads), 0, s, 1, p);
   };
-  if (n > kTeamForward) return go(norm_long_kernel<kF32, kRms>, kLongThreads, 1, 2);
-#define MORELLO_NORM(T, VEC, ITER) \
-  return go(norm_kernel<T, VEC, ITER, kF32, kRms>, T > kBlockThreads ? T : kBlockThreads, T < kBlockThreads ? kBlockThreads / T : 1, \
-            T > kBlockThreads ? 2 : 8)
+#define MORELLO_NORM(T, ITER) return go(norm_octets_kernel<T, ITER, kF32, kRms>, T)
+#define MORELLO_NORM_ODD(T, ITER) return go(norm_kernel<T, 1, ITER, kF32, kRms>, T)
+  if (n > kTeamForward) return launch_pdl(norm_long_kernel<kF32, kRms>, dim3((unsigned)std::min<int64_t>(p.m, (int64_t)dev.sms * 2)),
+                                          dim3(kLongThreads), 0, s, 1, p);
   if (vec) {
-    if (t == 32) {
-      if (n <= 256) MORELLO_NORM(32, 8, 1);
-      if (n <= 512) MORELLO_NORM(32, 8, 2);
-      MORELLO_NORM(32, 8, 4);
-    }
-    if (t == 128) {
-      if (n <= 2048) MORELLO_NORM(128, 8, 2);
-      MORELLO_NORM(128, 8, 4);
-    }
-    if (t == 256) MORELLO_NORM(256, 8, 4);
-    MORELLO_NORM(512, 8, 4);
+    if (n <= 64) MORELLO_NORM(8, 1);
+    if (n <= 128) MORELLO_NORM(16, 1);
+    if (n <= 256) MORELLO_NORM(32, 1);
+    if (n <= 512) MORELLO_NORM(32, 2);
+    if (n <= 1024) MORELLO_NORM(32, 4);
+    if (n <= 2048) MORELLO_NORM(128, 2);
+    if (n <= 4096) MORELLO_NORM(128, 4);
+    if (n <= 8192) MORELLO_NORM(256, 4);
+    MORELLO_NORM(512, 4);
   }
-  if (t == 32) {
-    if (n <= 256) MORELLO_NORM(32, 1, 8);
-    MORELLO_NORM(32, 1, 32);
-  }
-  if (t == 128) {
-    if (n <= 2048) MORELLO_NORM(128, 1, 16);
-    MORELLO_NORM(128, 1, 32);
-  }
-  if (t == 256) MORELLO_NORM(256, 1, 32);
-  MORELLO_NORM(512, 1, 32);
+  if (n <= 256) MORELLO_NORM_ODD(32, 8);
+  if (n <= 1024) MORELLO_NORM_ODD(32, 32);
+  if (n <= 2048) MORELLO_NORM_ODD(128, 16);
+  if (n <= 4096) MORELLO_NORM_ODD(128, 32);
+  if (n <= 8192) MORELLO_NORM_ODD(256, 32);
+  MORELLO_NORM_ODD(512, 32);
 #undef MORELLO_NORM
+#undef MORELLO_NORM_ODD
 }
 
 template <bool kF32, bool kRms, bool kSums>
@@ -589,27 +1015,32 @@ cudaError_t backward_launch(const DeviceInfo& dev, const NormBackwardParams& p, 
                             bool accumulate, bool vec, cudaStream_t s, uint64_t* launches) {
   cudaError_t e = cudaSuccess;
   const bool sums = dgamma || dbeta;
-  const int parts = (int)backward_parts(p.m, p.n);
-  if (p.n > kTeamBackward) {
+  int parts = (int)backward_parts(p.m, p.n);
+  constexpr int kSize = kF32 ? 4 : 2;
+  // With R or without: what a call asks for besides does not change the order of its sums.
+  if (vec && p.n <= kRingThreads * 32 && ring_shape(p.n, 2 * kSize + 2, kBackwardBudget).stages >= 2) {
+    const RingShape ring = ring_shape(p.n, kSize * (p.R && p.dX ? 2 : 1) + 2, kBackwardBudget);
+    const int64_t teams = kRingThreads / ring_team(p.n);
+    parts = (int)std::min<int64_t>(std::min(parts, dev.sms), (p.m + teams - 1) / teams);
+    e = backward_ring<kF32, kRms>(p, ring, parts, s);
+  } else if (p.n > kTeamBackward) {
+    parts = (int)std::min<int64_t>(kMaxParts, (p.m + 127) / 128);
     if (p.dX) {
       const int64_t blocks = std::min<int64_t>(p.m, (int64_t)dev.sms * 2);
       e = launch_pdl(norm_backward_long_kernel<kF32, kRms>, dim3((unsigned)blocks), dim3(kLongThreads), 0, s, 1, p);
       if (e != cudaSuccess) return e;
       ++*launches;
     }
-    if (sums) {
-      const int64_t per = (p.m + parts - 1) / parts;
-      e = launch_pdl(norm_columns_kernel<kF32>, dim3((unsigned)((p.n + 31) / 32), (unsigned)parts), dim3(1024), 0, s, 1, p, per);
-    }
+    if (!sums) return e;
+    const int64_t per = (p.m + parts - 1) / parts;
+    e = launch_pdl(norm_columns_kernel<kF32>, dim3((unsigned)((p.n + 31) / 32), (unsigned)parts), dim3(1024), 0, s, 1, p, per);
   } else {
     e = sums ? backward_rows_launch<kF32, kRms, true>(p, parts, vec, s)
              : backward_rows_launch<kF32, kRms, false>(p, parts, vec, s);
   }
-  if (e != cudaSuccess || !sums) {
-    if (e == cudaSuccess && p.n <= kTeamBackward) ++*launches;
-    return e;
-  }
+  if (e != cudaSuccess) return e;
   ++*launches;
+  if (!sums) return e;
   const NormSums ns{p.partial, {dgamma, dbeta}, p.n, parts, accumulate};
   e = launch_pdl(norm_sums_kernel, dim3((unsigned)((p.n + 31) / 32), dbeta ? 2u : 1u), dim3(256), 0, s, 1, ns);
   if (e == cudaSuccess) ++*launches;
@@ -645,7 +1076,7 @@ int morello_layer_norm(int rms, int x_type, int64_t m, int64_t n, float eps, con
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((rc = operator_workspace(0, nullptr, 0, s, &none, &dev)) != MORELLO_OK || empty) return rc;
   const NormParams p{m, (int)n, eps, 1.f / (float)n, X, static_cast<const uint16_t*>(gamma),
-                     static_cast<const uint16_t*>(beta), static_cast<uint16_t*>(Y), mean, rstd};
+                     static_cast<const uint16_t*>(beta), static_cast<uint16_t*>(Y), mean, rstd, dev.status};
   const bool vec = n % 8 == 0 && aligned(X, 16) && aligned(gamma, 16) && aligned(beta, 16) && aligned(Y, 16);
   cudaError_t e;
   if (f32) e = rms ? forward_launch<true, true>(dev, p, vec, s) : forward_launch<true, false>(dev, p, vec, s);
@@ -682,7 +1113,7 @@ int morello_layer_norm_backward(int rms, int x_type, int accumulate, int64_t m, 
   }
   if (!dX && !sums) return MORELLO_OK;
   const NormBackwardParams p{m, (int)n, 1.f / (float)n, X, static_cast<const uint16_t*>(gamma), rms ? nullptr : mean, rstd,
-                             static_cast<const uint16_t*>(dY), R, dX, static_cast<float*>(ws), dbeta != nullptr};
+                             static_cast<const uint16_t*>(dY), R, dX, static_cast<float*>(ws), dbeta != nullptr, dev.status};
   const bool vec = n % 8 == 0 && aligned(X, 16) && aligned(gamma, 16) && aligned(dY, 16) && aligned(R, 16) && aligned(dX, 16) &&
                    aligned(ws, 16);
   uint64_t launches = 0;

@@ -66,6 +66,16 @@ def test_backward(m, n, rms, kind):
 
 
 @pytest.mark.parametrize("kind", [BF, F32])
+@pytest.mark.parametrize("m,n", [(20000, 64), (9001, 256), (5000, 520), (2503, 1024), (1701, 2048), (1303, 4096), (799, 8192),
+                                 (601, 16384), (700, 12008), (4000, 2056)])
+def test_batches(m, n, kind):
+    # many rows to a block, the last ones a part of a group
+    for rms in (False, True):
+        test_forward(m, n, rms, kind)
+        test_backward(m, n, rms, kind)
+
+
+@pytest.mark.parametrize("kind", [BF, F32])
 @pytest.mark.parametrize("n", [256, 2048, 8192, 16384])
 def test_unaligned_tensors(n, kind):
     x, gamma, beta, dy, r = (misaligned(t) for t in make(5, n, kind, n))
