@@ -14,6 +14,8 @@
 // registers; the blocks' sums are joined by a second launch in the order of the blocks.  No atomics: the same sums in the
 // same order every time.
 #include <algorithm>
+#include <initializer_list>
+#include <type_traits>
 
 #include "../../include/morello.h"
 #include "activation.cuh"
@@ -27,6 +29,7 @@ using namespace sm100;
 
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kBlockThreads = 256;
+constexpr int kMaxParts = 296;          // blocks that leave sums of their own: two to an SM of 148
 
 struct NormParams {
   int64_t m;
@@ -65,94 +68,46 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// The barrier of one team of a block (all of it: barrier 0).
-template <int kT>
+// The barrier of one team of a block of kThreads.
+template <int kT, int kThreads>
 __device__ __forceinline__ void team_barrier(int team) {
-  if constexpr (kT >= kBlockThreads) __syncthreads();
+  if constexpr (kT == kThreads) __syncthreads();
   else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(kT) : "memory");
 }
 
-// A thread's columns of a row.  kVec 8: octets of columns, 8 (t + i T) ..., 16-byte accesses; needs n % 8 == 0 and
-// aligned tensors.  kVec 1: single columns t + i T.  Element e of the thread: columns are known to exist by has(e).
+// A thread's columns of a row, by eights.  kVec 8: octets of columns, 8 (t + i T) ..., 16-byte accesses; needs n % 8 == 0
+// and aligned tensors.  kVec 1: single columns t + (8 i + e) T, any n and alignment.
 template <int kT, int kVec, int kIter>
 struct Columns {
   int t, n;
-  __device__ __forceinline__ int of(int e) const {
-    return kVec == 8 ? (t + e / 8 * kT) * 8 + e % 8 : t + e * kT;
+  __device__ __forceinline__ int of(int i, int e) const { return first() + past(i, e); }
+  // The same from the thread's first column on: a constant, so that addresses are one register's.
+  static constexpr __device__ int past(int i, int e) { return kVec == 8 ? i * kT * 8 + e : (8 * i + e) * kT; }
+  __device__ __forceinline__ int first() const { return kVec == 8 ? 8 * t : t; }
+  __device__ __forceinline__ bool any(int i) const { return of(i, 0) < n; }       // of the eight
+  __device__ __forceinline__ bool has(int i, int e) const { return kVec == 8 ? any(i) : of(i, e) < n; }
+  // Whether the whole team has all of the i-th eight.
+  __device__ __forceinline__ bool whole(int i) const { return kVec == 8 || 8 * (i + 1) * kT <= n; }
+  __device__ __forceinline__ float count() const {
+    float k = 0.f;
+#pragma unroll
+    for (int i = 0; i < kIter; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) k += has(i, e) ? 1.f : 0.f;
+    return k;
   }
-  __device__ __forceinline__ bool has(int e) const { return of(e - e % kVec) < n; }
-};
-
-// The raw elements of those columns, bf16 or f32, as they came from memory.
-template <int kT, int kVec, int kIter, bool kF32>
-struct Held {
-  static constexpr int kWords = kVec == 1 ? kIter : kVec * kIter * (kF32 ? 4 : 2) / 4;
-  uint32_t w[kWords];
-  __device__ __forceinline__ void load(const void* row, const Columns<kT, kVec, kIter>& c) {
+  // Zeros where there is no column.
+  __device__ __forceinline__ void clear(int i, f32x2 (&v)[4]) const {
+    if constexpr (kVec == 1) {
+      if (whole(i)) return;
 #pragma unroll
-    for (int i = 0; i < kIter; ++i) {
-      const bool has = c.has(i * kVec);
-      if constexpr (kVec == 8) {
-        constexpr int kQuads = kF32 ? 2 : 1;
-#pragma unroll
-        for (int q = 0; q < kQuads; ++q) {
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (has) v = reinterpret_cast<const uint4*>(row)[(c.t + i * kT) * kQuads + q];
-          uint32_t* o = w + (i * kQuads + q) * 4;
-          o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
-        }
-      } else if constexpr (kF32) {
-        w[i] = has ? __float_as_uint(static_cast<const float*>(row)[c.t + i * kT]) : 0u;
-      } else {
-        w[i] = has ? (uint32_t)static_cast<const uint16_t*>(row)[c.t + i * kT] << 16 : 0u;
+      for (int j = 0; j < 4; ++j) {
+        const float2 f = pair_values(v[j]);
+        v[j] = pair_of(has(i, 2 * j) ? f.x : 0.f, has(i, 2 * j + 1) ? f.y : 0.f);
       }
     }
   }
-  // Octet i, as four pairs.
-  __device__ __forceinline__ void pairs(int i, f32x2 (&v)[4]) const {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if constexpr (kF32) v[j] = pair_of(__uint_as_float(w[i * 8 + 2 * j]), __uint_as_float(w[i * 8 + 2 * j + 1]));
-      else v[j] = pair_of(bf16_low(w[i * 4 + j]), bf16_high(w[i * 4 + j]));
-    }
-  }
-  __device__ __forceinline__ float get(int e) const {
-    if constexpr (kVec == 1 || kF32) return __uint_as_float(w[e]);
-    else return e % 2 ? bf16_high(w[e / 2]) : bf16_low(w[e / 2]);
-  }
 };
-
-// Stores one octet (kVec 8) or one element of a row, column `col` on.
-template <int kVec, bool kF32>
-__device__ __forceinline__ void put_part(void* row, int col, const float* v) {
-  if constexpr (kVec == 8 && kF32) {
-    float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + col);
-    o[0] = make_float4(v[0], v[1], v[2], v[3]);
-    o[1] = make_float4(v[4], v[5], v[6], v[7]);
-  } else if constexpr (kVec == 8) {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + col) =
-        make_uint4(bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3]), bf16_pack(v[4], v[5]), bf16_pack(v[6], v[7]));
-  } else if constexpr (kF32) {
-    static_cast<float*>(row)[col] = v[0];
-  } else {
-    static_cast<uint16_t*>(row)[col] = bf16_round(v[0]);
-  }
-}
-
-// One octet or one element of a bf16 vector (gamma, beta); `missing` where there is none.
-template <int kVec>
-__device__ __forceinline__ void vector_part(const uint16_t* p, int col, float missing, float (&v)[kVec]) {
-  if (!p) {
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = missing;
-  } else if constexpr (kVec == 8) {
-    const uint4 w = __ldg(reinterpret_cast<const uint4*>(p + col));
-    v[0] = bf16_low(w.x); v[1] = bf16_high(w.x); v[2] = bf16_low(w.y); v[3] = bf16_high(w.y);
-    v[4] = bf16_low(w.z); v[5] = bf16_high(w.z); v[6] = bf16_low(w.w); v[7] = bf16_high(w.w);
-  } else {
-    v[0] = bf16_value(__ldg(p + col));
-  }
-}
 
 // Eight elements as four pairs.
 __device__ __forceinline__ void octet_pairs(const uint4& w, f32x2 (&v)[4]) {
@@ -161,41 +116,96 @@ __device__ __forceinline__ void octet_pairs(const uint4& w, f32x2 (&v)[4]) {
   v[2] = pair_of(bf16_low(w.z), bf16_high(w.z));
   v[3] = pair_of(bf16_low(w.w), bf16_high(w.w));
 }
-// Eight columns of gamma or beta; `missing` where there is no such vector.
-__device__ __forceinline__ void vector_pairs(const uint16_t* p, int col, float missing, f32x2 (&v)[4]) {
-  if (p) octet_pairs(*reinterpret_cast<const uint4*>(p + col), v);
-  else v[0] = v[1] = v[2] = v[3] = pair_of(missing);
-}
-// An octet of a row in shared memory.
-template <bool kF32>
-__device__ __forceinline__ void shared_octet(const uint8_t* row, int col, f32x2 (&v)[4]) {
-  if constexpr (kF32) {
-    const float4* q = reinterpret_cast<const float4*>(row) + col / 4;
-    const float4 a = q[0], b = q[1];
-    v[0] = pair_of(a.x, a.y);
-    v[1] = pair_of(a.z, a.w);
-    v[2] = pair_of(b.x, b.y);
-    v[3] = pair_of(b.z, b.w);
-  } else {
-    octet_pairs(*reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(row) + col), v);
-  }
-}
 __device__ __forceinline__ uint32_t bf16_pack_pair(f32x2 v) {
   const float2 f = pair_values(v);
   return bf16_pack(f.x, f.y);
 }
-template <bool kF32>
-__device__ __forceinline__ void put_octet(void* row, int col, const f32x2 (&v)[4]) {
-  if constexpr (kF32) {
-    float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + col);
+
+// The elements of a thread's octets, bf16 or f32, as they came from memory.
+template <int kT, int kIter, bool kF32>
+struct Held {
+  uint32_t w[(kF32 ? 8 : 4) * kIter];
+  __device__ __forceinline__ void load(const void* row, const Columns<kT, 8, kIter>& c) {
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      constexpr int kQuads = kF32 ? 2 : 1;
+#pragma unroll
+      for (int q = 0; q < kQuads; ++q) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (c.any(i)) v = static_cast<const uint4*>(row)[(c.t + i * kT) * kQuads + q];
+        uint32_t* o = w + (i * kQuads + q) * 4;
+        o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+      }
+    }
+  }
+  __device__ __forceinline__ void pairs(int i, f32x2 (&v)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (kF32) v[j] = pair_of(__uint_as_float(w[i * 8 + 2 * j]), __uint_as_float(w[i * 8 + 2 * j + 1]));
+      else v[j] = pair_of(bf16_low(w[i * 4 + j]), bf16_high(w[i * 4 + j]));
+    }
+  }
+};
+
+// Eight of a thread's columns of gamma or beta; `missing` where there is no such vector.
+template <int kT, int kIter>
+__device__ __forceinline__ void vector_pairs(const uint16_t* p, const Columns<kT, 8, kIter>& c, int i, float missing,
+                                             f32x2 (&v)[4]) {
+  if (p) octet_pairs(*reinterpret_cast<const uint4*>(p + c.of(i, 0)), v);
+  else v[0] = v[1] = v[2] = v[3] = pair_of(missing);
+}
+
+// Stores eight columns of a row (kVec 8: they all exist).
+template <bool kF32, int kT, int kVec, int kIter>
+__device__ __forceinline__ void put_eight(void* row, const Columns<kT, kVec, kIter>& c, int i, const f32x2 (&v)[4]) {
+  if constexpr (kVec == 8 && kF32) {
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(row) + c.of(i, 0));
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const float2 a = pair_values(v[2 * q]), b = pair_values(v[2 * q + 1]);
       o[q] = make_float4(a.x, a.y, b.x, b.y);
     }
-  } else {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + col) =
+  } else if constexpr (kVec == 8) {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(row) + c.of(i, 0)) =
         make_uint4(bf16_pack_pair(v[0]), bf16_pack_pair(v[1]), bf16_pack_pair(v[2]), bf16_pack_pair(v[3]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = pair_values(v[j]);
+      if constexpr (kF32) {
+        float* dst = static_cast<float*>(row) + c.t;
+        if (c.has(i, 2 * j)) dst[c.past(i, 2 * j)] = f.x;
+        if (c.has(i, 2 * j + 1)) dst[c.past(i, 2 * j + 1)] = f.y;
+      } else {
+        const uint32_t both = bf16_pack(f.x, f.y);
+        uint16_t* dst = static_cast<uint16_t*>(row) + c.t;
+        if (c.has(i, 2 * j)) dst[c.past(i, 2 * j)] = (uint16_t)both;
+        if (c.has(i, 2 * j + 1)) dst[c.past(i, 2 * j + 1)] = (uint16_t)(both >> 16);
+      }
+    }
+  }
+}
+
+// Eight columns of a row in shared memory.  kVec 1: where the row ends its last column stands in for those that are missing.
+template <bool kF32, int kT, int kVec, int kIter>
+__device__ __forceinline__ void row_eight(const void* row, const Columns<kT, kVec, kIter>& c, int i, f32x2 (&v)[4]) {
+  if constexpr (kVec == 8 && kF32) {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(row) + c.of(i, 0));
+    const float4 a = q[0], b = q[1];
+    v[0] = pair_of(a.x, a.y);
+    v[1] = pair_of(a.z, a.w);
+    v[2] = pair_of(b.x, b.y);
+    v[3] = pair_of(b.z, b.w);
+  } else if constexpr (kVec == 8) {
+    octet_pairs(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(row) + c.of(i, 0)), v);
+  } else {
+    auto one = [&](int e) {
+      const int col = min(c.of(i, e), c.n - 1);
+      if constexpr (kF32) return static_cast<const float*>(row)[col];
+      else return bf16_value(static_cast<const uint16_t*>(row)[col]);
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = pair_of(one(2 * j), one(2 * j + 1));
   }
 }
 
@@ -234,150 +244,102 @@ __device__ __forceinline__ float join_parts(const Part* parts, float inv_n, floa
   return squares * inv_n;
 }
 
-// Teams of kT threads, a row each.
-template <int kT, int kVec, int kIter, bool kF32, bool kRms>
-__global__ void __launch_bounds__(kT > kBlockThreads ? kT : kBlockThreads) norm_kernel(const NormParams p) {
-  constexpr int kTeams = kT < kBlockThreads ? kBlockThreads / kT : 1;
-  constexpr int kWarps = kT / 32;
-  constexpr int kCount = kVec * kIter;
-  __shared__ Part parts[2][kTeams][kWarps];
-  const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / 32, lane = (int)threadIdx.x % 32;
-  const Columns<kT, kVec, kIter> c{(int)threadIdx.x % kT, p.n};
-  float here = 0.f;
+// d = x - mean of eight columns: their sum and their squares.
+template <bool kRms>
+__device__ __forceinline__ void spread(const f32x2 (&x)[4], f32x2 minus_mean, f32x2* off, f32x2* squares) {
 #pragma unroll
-  for (int e = 0; e < kCount; ++e) here += c.has(e) ? 1.f : 0.f;
-  const float count = warp_sum(here), inv_count = count > 0.f ? 1.f / count : 0.f;
-  pdl_wait();
-  pdl_release();
-  int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * kTeams + team; row < p.m; row += (int64_t)gridDim.x * kTeams, turn ^= 1) {
-    Held<kT, kVec, kIter, kF32> x;
-    x.load(static_cast<const char*>(p.X) + row * p.n * (kF32 ? 4 : 2), c);
-    Part mine{0.f, 0.f, 0.f, count};
-    if constexpr (!kRms) {
-      float s = 0.f;
-#pragma unroll
-      for (int e = 0; e < kCount; ++e) s += x.get(e);
-      mine.mean = warp_sum(s) * inv_count;
-    }
-    float off = 0.f, squares = 0.f;
-#pragma unroll
-    for (int e = 0; e < kCount; ++e) {
-      const float d = c.has(e) ? x.get(e) - mine.mean : 0.f;
-      if constexpr (!kRms) off += d;
-      squares = fmaf(d, d, squares);
-    }
-    if constexpr (!kRms) mine.off = warp_sum(off);
-    mine.squares = warp_sum(squares);
-    float base, shift, square;
-    if constexpr (kT == 32) {
-      square = join_parts<1>(&mine, p.inv_n, &base, &shift);
-    } else {
-      if (lane == 0) parts[turn][team][warp] = mine;
-      team_barrier<kT>(team);     // the other set of parts is written next: nobody is still reading it behind this barrier
-      square = join_parts<kWarps>(parts[turn][team], p.inv_n, &base, &shift);
-    }
-    const float rstd = 1.f / sqrtf(square + p.eps);
-    if (c.t == 0) {
-      if (!kRms && p.mean) p.mean[row] = base + shift;
-      if (p.rstd) p.rstd[row] = rstd;
-    }
-#pragma unroll
-    for (int i = 0; i < kIter; ++i) {
-      if (!c.has(i * kVec)) continue;
-      float gamma[kVec], beta[kVec], y[kVec];
-      vector_part<kVec>(p.gamma, c.of(i * kVec), 1.f, gamma);
-      vector_part<kVec>(p.beta, c.of(i * kVec), 0.f, beta);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const float v = x.get(i * kVec + j);
-        const float d = kRms ? v : (v - base) - shift;
-        y[j] = fmaf(d * rstd, gamma[j], beta[j]);
-      }
-      put_part<kVec, false>(p.Y + row * p.n, c.of(i * kVec), y);
-    }
+  for (int j = 0; j < 4; ++j) {
+    const f32x2 d = kRms ? x[j] : add2(x[j], minus_mean);
+    if constexpr (!kRms) *off = add2(*off, d);
+    *squares = fma2(d, d, *squares);
   }
 }
+// y = ((x - base) rstd - shift rstd) gamma + beta
+struct ForwardFactors {
+  f32x2 rstd, minus_base, shifted;
+  template <bool kRms>
+  __device__ __forceinline__ void y(const f32x2 (&x)[4], const f32x2 (&gamma)[4], const f32x2 (&beta)[4], f32x2 (&out)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      out[j] = fma2(kRms ? mul2(x[j], rstd) : fma2(add2(x[j], minus_base), rstd, shifted), gamma[j], beta[j]);
+  }
+};
+// Joins the row's parts; one thread keeps its mean and rstd.
+template <int kT, int kLanes, int kTeams, bool kRms, int kWarps>
+__device__ __forceinline__ ForwardFactors forward_factors(const NormParams& p, Part (&parts)[kTeams][kWarps], const Part& mine, int team,
+                                                          int warp, int lane, int64_t row, bool keeps) {
+  float base, shift, square;
+  if constexpr (kWarps == 1) {
+    square = join_parts<1>(&mine, p.inv_n, &base, &shift);
+  } else {
+    if (lane == 0) parts[team][warp] = mine;
+    team_barrier<kT, kT * kTeams>(team);     // the other set of parts is written next: nobody is still reading it behind this barrier
+    square = join_parts<kWarps>(parts[team], p.inv_n, &base, &shift);
+  }
+  const float rstd = rsqrtf(square + p.eps);
+  if (keeps) {
+    if (!kRms && p.mean) p.mean[row] = base + shift;
+    if (p.rstd) p.rstd[row] = rstd;
+  }
+  return ForwardFactors{pair_of(rstd), pair_of(-base), pair_of(-shift * rstd)};
+}
 
-// The same by octets, two columns an instruction: n % 8 == 0 and 16-byte-aligned tensors.  Teams of 8 to 512 threads; up to
-// kIter octets of a row to a thread, kept as they came.
+// n % 8 == 0 and 16-byte-aligned tensors.  Teams of 8 to 512 threads, a row each and kIter of its octets to a thread, two
+// columns an instruction.  A team's next row is on its way while it works on this one.
 template <int kT, int kIter, bool kF32, bool kRms>
-__global__ void __launch_bounds__(kT > kBlockThreads ? kT : kBlockThreads) norm_octets_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kT > kBlockThreads ? kT : kBlockThreads, kT > kBlockThreads || kIter < 4 ? 1 : kF32 ? 2 : 3)
+norm_kernel(const NormParams p) {
   constexpr int kTeams = kT < kBlockThreads ? kBlockThreads / kT : 1;
   constexpr int kLanes = kT < 32 ? kT : 32, kWarps = kT / kLanes;
   __shared__ Part parts[2][kTeams][kWarps];
   const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / kLanes, lane = (int)threadIdx.x % kLanes;
   const Columns<kT, 8, kIter> c{(int)threadIdx.x % kT, p.n};
-  float here = 0.f;
-#pragma unroll
-  for (int i = 0; i < kIter; ++i) here += c.has(i * 8) ? 8.f : 0.f;
-  const float count = warp_sum<kLanes>(here), inv_count = count > 0.f ? 1.f / count : 0.f;
+  const float count = warp_sum<kLanes>(c.count()), inv_count = count > 0.f ? 1.f / count : 0.f;
   pdl_wait();
   pdl_release();
+  const int64_t step = (int64_t)gridDim.x * kTeams;
+  int64_t row = (int64_t)blockIdx.x * kTeams + team;
+  Held<kT, kIter, kF32> held;
+  auto fetch = [&](int64_t r) {      // past the last row: the last one, to no use
+    held.load(static_cast<const char*>(p.X) + min(r, p.m - 1) * p.n * (kF32 ? 4 : 2), c);
+  };
+  fetch(row);
   int turn = 0;
-  // Teams of less than a warp leave the loop together: a row past the last is worked on like any other, but neither read nor written.
-  for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < p.m; row0 += (int64_t)gridDim.x * kTeams, turn ^= 1) {
-    const int64_t row = row0 + team;
+  // Rows past the last are worked on like any other, but neither read nor written: teams of less than a warp leave together.
+  for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < p.m; row0 += step, row += step, turn ^= 1) {
     const bool live = row < p.m;
     if (kT >= 32 && !live) break;
-    Held<kT, 8, kIter, kF32> x;
-    const Columns<kT, 8, kIter> mine_of{c.t, live ? p.n : 0};
-    x.load(static_cast<const char*>(p.X) + row * p.n * (kF32 ? 4 : 2), mine_of);
-    Part mine{0.f, 0.f, 0.f, count};
-    if constexpr (!kRms) {
-      f32x2 sums = 0;
+    f32x2 x[kIter][4], sums = 0;
 #pragma unroll
-      for (int i = 0; i < kIter; ++i) {
-        f32x2 v[4];
-        x.pairs(i, v);
+    for (int i = 0; i < kIter; ++i) {
+      held.pairs(i, x[i]);
+      if constexpr (!kRms) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sums = add2(sums, v[j]);
+        for (int j = 0; j < 4; ++j) sums = add2(sums, x[i][j]);
       }
-      mine.mean = warp_sum<kLanes>(pair_sum(sums)) * inv_count;
     }
+    fetch(row + step);
+    Part mine{0.f, 0.f, 0.f, count};
+    if constexpr (!kRms) mine.mean = warp_sum<kLanes>(pair_sum(sums)) * inv_count;
     const f32x2 minus_mean = pair_of(-mine.mean);
     f32x2 off = 0, squares = 0;
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      if (!c.has(i * 8)) continue;
-      f32x2 v[4];
-      x.pairs(i, v);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x2 d = kRms ? v[j] : add2(v[j], minus_mean);
-        if constexpr (!kRms) off = add2(off, d);
-        squares = fma2(d, d, squares);
-      }
+      if (!c.any(i)) continue;
+      spread<kRms>(x[i], minus_mean, &off, &squares);
     }
     if constexpr (!kRms) mine.off = warp_sum<kLanes>(pair_sum(off));
     mine.squares = warp_sum<kLanes>(pair_sum(squares));
-    float base, shift, square;
-    if constexpr (kWarps == 1) {
-      square = join_parts<1>(&mine, p.inv_n, &base, &shift);
-    } else {
-      if (lane == 0) parts[turn][team][warp] = mine;
-      team_barrier<kT>(team);     // the other set of parts is written next: nobody is still reading it behind this barrier
-      square = join_parts<kWarps>(parts[turn][team], p.inv_n, &base, &shift);
-    }
-    const float rstd = 1.f / sqrtf(square + p.eps);
-    if (c.t == 0 && live) {
-      if (!kRms && p.mean) p.mean[row] = base + shift;
-      if (p.rstd) p.rstd[row] = rstd;
-    }
-    const f32x2 factor = pair_of(rstd), minus_base = pair_of(-base), shifted = pair_of(-shift * rstd);
+    const ForwardFactors f = forward_factors<kT, kLanes, kTeams, kRms>(p, parts[turn], mine, team, warp, lane, row, live && c.t == 0);
+    if (!live) continue;
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      if (!mine_of.has(i * 8)) continue;
-      f32x2 v[4], gamma[4], beta[4], y[4];
-      x.pairs(i, v);
-      vector_pairs(p.gamma, c.of(i * 8), 1.f, gamma);
-      vector_pairs(p.beta, c.of(i * 8), 0.f, beta);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x2 h = kRms ? mul2(v[j], factor) : fma2(add2(v[j], minus_base), factor, shifted);
-        y[j] = fma2(h, gamma[j], beta[j]);
-      }
-      put_octet<false>(p.Y + row * p.n, c.of(i * 8), y);
+      if (!c.any(i)) continue;
+      f32x2 gamma[4], beta[4], y[4];
+      vector_pairs(p.gamma, c, i, 1.f, gamma);
+      vector_pairs(p.beta, c, i, 0.f, beta);
+      f.y<kRms>(x[i], gamma, beta, y);
+      put_eight<false>(p.Y + row * p.n, c, i, y);
     }
   }
 }
@@ -401,27 +363,78 @@ struct RingShape {
   uint32_t stage_bytes;        // a group's rows of every tensor
 };
 
+// A tensor of rows, and the bytes of a stage that its part of a group takes: 32 more than its rows', so that their first byte
+// can lie where it lies in its 16 bytes of memory, and a multiple of 16.
 struct RingTensor {
   const void* p;
-  uint32_t row_bytes;
+  uint32_t row_bytes, area;
 };
-// Starts the copies of the group whose first row is `row` to a stage.
-template <int kTeams, int kTensors>
+__host__ __device__ constexpr uint32_t ring_area(uint32_t rows, uint32_t row_bytes) { return (rows * row_bytes + 47) / 16 * 16; }
+
+// Starts the copies of the group whose first row is `row` to a stage.  A bulk copy moves whole 16 bytes: those that hold the
+// group's rows, but where they reach past the tensor's ends, there its elements (2 bytes at a time) are copied one by one.
+// kWhole: rows are whole 16 bytes.
+template <int kTeams, bool kWhole, int kTensors>
 __device__ __forceinline__ void ring_fill(RingBars* bars, uint8_t* smem, const RingShape& ring, int stage, int64_t row, int64_t m,
                                           const RingTensor (&tensors)[kTensors]) {
   const uint32_t rows = (uint32_t)min((int64_t)kTeams, m - row);
-  uint32_t bytes = 0;
+  if constexpr (kWhole) {
+    uint32_t bytes = 0;
 #pragma unroll
-  for (int i = 0; i < kTensors; ++i) bytes += tensors[i].p ? rows * tensors[i].row_bytes : 0u;
-  mbar_arrive_expect_tx(&bars->full[stage], bytes);
+    for (int i = 0; i < kTensors; ++i) bytes += tensors[i].p ? rows * tensors[i].row_bytes : 0u;
+    mbar_arrive_expect_tx(&bars->full[stage], bytes);
+    uint8_t* dst = smem + (size_t)stage * ring.stage_bytes;
+#pragma unroll
+    for (int i = 0; i < kTensors; ++i) {
+      if (!tensors[i].p) continue;
+      bulk_load(dst, static_cast<const uint8_t*>(tensors[i].p) + row * tensors[i].row_bytes, rows * tensors[i].row_bytes,
+                &bars->full[stage]);
+      dst += tensors[i].area;
+    }
+    return;
+  }
+  const uint8_t* from[kTensors];
+  uint32_t head[kTensors], size[kTensors], bytes = 0;      // where the copy begins in its area, and how long it is
   uint8_t* dst = smem + (size_t)stage * ring.stage_bytes;
 #pragma unroll
   for (int i = 0; i < kTensors; ++i) {
     if (!tensors[i].p) continue;
-    bulk_load(dst, static_cast<const uint8_t*>(tensors[i].p) + row * tensors[i].row_bytes, rows * tensors[i].row_bytes,
-              &bars->full[stage]);
-    dst += kTeams * tensors[i].row_bytes;
+    const uint8_t* base = static_cast<const uint8_t*>(tensors[i].p);
+    const uint8_t* first = base + row * tensors[i].row_bytes;
+    const uint32_t skew = (uint32_t)reinterpret_cast<uintptr_t>(first) & 15u, end = skew + rows * tensors[i].row_bytes;
+    uint32_t lo = 0u, hi = (end + 15u) & ~15u;
+    auto singly = [&](uint32_t at, uint32_t stop) {
+      for (; at < stop; at += 2) *reinterpret_cast<uint16_t*>(dst + at) = *reinterpret_cast<const uint16_t*>(first + (at - skew));
+      fence_proxy_async_smem();      // a later copy to the same place comes behind it
+    };
+    if (first - skew < base) {
+      lo = 16u;
+      singly(skew, min(lo, end));
+    }
+    if (first - skew + hi > base + m * tensors[i].row_bytes) {
+      hi = end & ~15u;
+      singly(max(max(hi, lo), skew), end);
+    }
+    from[i] = first - skew + lo;
+    head[i] = lo;
+    size[i] = hi > lo ? hi - lo : 0u;
+    bytes += size[i];
+    dst += tensors[i].area;
   }
+  mbar_arrive_expect_tx(&bars->full[stage], bytes);
+  dst = smem + (size_t)stage * ring.stage_bytes;
+#pragma unroll
+  for (int i = 0; i < kTensors; ++i) {
+    if (!tensors[i].p) continue;
+    if (size[i] > 0) bulk_load(dst + head[i], from[i], size[i], &bars->full[stage]);
+    dst += tensors[i].area;
+  }
+}
+// Row `place` of the group whose first row is row0.
+template <bool kWhole>
+__device__ __forceinline__ const uint8_t* ring_row(const uint8_t* area, const RingTensor& t, int64_t row0, int place) {
+  const uint32_t skew = kWhole ? 0u : (uint32_t)(reinterpret_cast<uintptr_t>(t.p) + (uintptr_t)row0 * t.row_bytes) & 15u;
+  return area + skew + (uint32_t)place * t.row_bytes;
 }
 __device__ __forceinline__ void ring_init(RingBars* bars, int stages) {
   if (threadIdx.x == 0) {
@@ -445,61 +458,173 @@ struct RingPlace {
     if (++stage == stages) { stage = 0; phase ^= 1; }
   }
 };
-template <int kTeams, int kTensors>
+template <int kTeams, bool kWhole, int kTensors>
 __device__ __forceinline__ void ring_start(RingBars* bars, uint8_t* smem, const RingShape& ring, RingPlace* at, int64_t m,
                                            const RingTensor (&tensors)[kTensors]) {
   at->fill = (int64_t)blockIdx.x * kTeams;
   if (threadIdx.x != 0) return;
   for (int i = 0; i < ring.stages && at->fill < m; ++i, at->fill += (int64_t)gridDim.x * kTeams)
-    ring_fill<kTeams>(bars, smem, ring, i, at->fill, m, tensors);
+    ring_fill<kTeams, kWhole>(bars, smem, ring, i, at->fill, m, tensors);
 }
-// A warp is done with the group; the first thread has the stage before it filled again.
-template <int kTeams, int kTensors>
+// A warp is done with the group's memory.
+__device__ __forceinline__ void ring_release(RingBars* bars, const RingPlace& at) {
+  __syncwarp();
+  if (threadIdx.x % 32 == 0) mbar_arrive(&bars->empty[at.stage]);
+}
+// On to the next group; the first thread has the stage before this one's filled again.
+template <int kTeams, bool kWhole, int kTensors>
 __device__ __forceinline__ bool ring_next(RingBars* bars, uint8_t* smem, const RingShape& ring, RingPlace* at, int64_t m,
                                           const RingTensor (&tensors)[kTensors], uint32_t* status) {
   bool ok = true;
-  __syncwarp();
-  if (threadIdx.x % 32 == 0) mbar_arrive(&bars->empty[at->stage]);
   if (threadIdx.x == 0 && at->before >= 0 && at->fill < m) {
     ok = mbar_wait(&bars->empty[at->before], at->phase_before, &bars->abort_flag, status, 61);
-    if (ok) ring_fill<kTeams>(bars, smem, ring, at->before, at->fill, m, tensors);
+    if (ok) ring_fill<kTeams, kWhole>(bars, smem, ring, at->before, at->fill, m, tensors);
     at->fill += (int64_t)gridDim.x * kTeams;
   }
   at->next(ring.stages);
   return ok;
 }
-// A thread's octets of gamma or beta, kept through all its rows where registers allow (kIter 2), read again where not.
-template <int kT, int kIter>
-struct HeldVector {
-  static constexpr bool kHold = kIter <= 2;
+// A thread's columns of gamma or beta.  Octets: kept through all its rows where registers allow (kIter 2), read again where not.
+// Single columns: from a copy in shared memory.
+template <int kT, int kVec, int kIter>
+struct RingVector {
+  static constexpr bool kHold = kVec == 8 && kIter <= 2;
   const uint16_t* p;
-  uint4 w[kHold ? kIter : 1];
   float missing;
-  __device__ __forceinline__ HeldVector(const uint16_t* vector, float instead, const Columns<kT, 8, kIter>& c)
+  Held<kT, kHold ? kIter : 1, false> held;
+  __device__ __forceinline__ RingVector(const uint16_t* vector, float instead, uint16_t* copy, const Columns<kT, kVec, kIter>& c)
       : p(vector), missing(instead) {
-    if constexpr (kHold) {
-      const uint32_t pair = __float_as_uint(instead) | (__float_as_uint(instead) >> 16);      // exact in bf16
-#pragma unroll
-      for (int i = 0; i < kIter; ++i)
-        w[i] = p && c.has(i * 8) ? *reinterpret_cast<const uint4*>(p + c.of(i * 8)) : make_uint4(pair, pair, pair, pair);
+    if constexpr (kVec == 1) {
+      for (int col = (int)threadIdx.x; p && col < c.n; col += kRingThreads) copy[col] = p[col];
+      if (p) p = copy;
+    } else if constexpr (kHold) {
+      if (p) held.load(p, c);
     }
   }
-  __device__ __forceinline__ void get(int i, int col, f32x2 (&v)[4]) const {
-    if constexpr (kHold) {
-      octet_pairs(w[i], v);
+  __device__ __forceinline__ void get(const Columns<kT, kVec, kIter>& c, int i, f32x2 (&v)[4]) const {
+    if (!p) {
+      v[0] = v[1] = v[2] = v[3] = pair_of(missing);
+    } else if constexpr (kHold) {
+      held.pairs(i, v);
+    } else if constexpr (kVec == 1) {
+      row_eight<false>(p, c, i, v);
     } else {
-      vector_pairs(p, col, missing, v);
+      vector_pairs(p, c, i, missing, v);
     }
   }
 };
-template <int kT>
-__device__ __forceinline__ void ring_team_barrier(int team) {
-  asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(kT) : "memory");
+
+// The threads of a block of the ring, in a barrier that is no team's own.
+__device__ __forceinline__ void block_barrier() { asm volatile("bar.sync 15, %0;" ::"n"(kRingThreads) : "memory"); }
+
+// The forward pass of rows that are not whole octets.
+template <int kT, int kIter, bool kF32, bool kRms>
+__global__ void __launch_bounds__(kRingThreads, 1) norm_ring_kernel(const NormParams p, const RingShape ring) {
+  constexpr int kTeams = kRingThreads / kT, kWarps = kT / 32;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ RingBars bars;
+  __shared__ Part parts[2][kTeams][kWarps];
+  ring_init(&bars, ring.stages);
+  pdl_wait();
+  pdl_release();
+  const uint32_t row_bytes = (uint32_t)p.n * (kF32 ? 4 : 2);
+  const RingTensor tensors[1] = {{p.X, row_bytes, ring_area(kTeams, row_bytes)}};
+  RingPlace at;
+  ring_start<kTeams, false>(&bars, smem, ring, &at, p.m, tensors);
+  const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / 32, lane = (int)threadIdx.x % 32;
+  const Columns<kT, 1, kIter> c{(int)threadIdx.x % kT, p.n};
+  uint16_t* copies = reinterpret_cast<uint16_t*>(smem + (size_t)ring.stages * ring.stage_bytes);
+  const RingVector<kT, 1, kIter> gammas(p.gamma, 1.f, copies, c), betas(p.beta, 0.f, copies + p.n, c);
+  const float count = warp_sum(c.count()), inv_count = count > 0.f ? 1.f / count : 0.f;
+  __syncthreads();
+  int turn = 0;
+  bool ok = true;          // once a wait gave up the rows go by unread and unwritten: the team's barriers still meet
+  for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < p.m; row0 += (int64_t)gridDim.x * kTeams, turn ^= 1) {
+    const int64_t row = row0 + team;
+    if (ok) ok = mbar_wait(&bars.full[at.stage], at.phase, &bars.abort_flag, p.status, 63);
+    ok = __all_sync(kFull, ok);
+    const bool live = ok && row < p.m;
+    f32x2 x[kIter][4], sums = 0;
+    const uint8_t* src = ring_row<false>(smem + (size_t)at.stage * ring.stage_bytes, tensors[0], row0, team);
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      x[i][0] = x[i][1] = x[i][2] = x[i][3] = 0;
+      if (!live) continue;
+      row_eight<kF32>(src, c, i, x[i]);
+      c.clear(i, x[i]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sums = add2(sums, x[i][j]);
+    }
+    ring_release(&bars, at);
+    Part mine{0.f, 0.f, 0.f, count};
+    if constexpr (!kRms) mine.mean = warp_sum(pair_sum(sums)) * inv_count;
+    f32x2 off = 0, squares = 0;
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      f32x2 d[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) d[j] = kRms ? x[i][j] : add2(x[i][j], pair_of(-mine.mean));
+      c.clear(i, d);
+      spread<kRms>(d, 0, &off, &squares);
+    }
+    if constexpr (!kRms) mine.off = warp_sum(pair_sum(off));
+    mine.squares = warp_sum(pair_sum(squares));
+    const ForwardFactors f = forward_factors<kT, 32, kTeams, kRms>(p, parts[turn], mine, team, warp, lane, row, live && c.t == 0);
+#pragma unroll
+    for (int i = 0; i < kIter; ++i) {
+      if (!live || !c.any(i)) continue;
+      f32x2 gamma[4], beta[4], y[4];
+      gammas.get(c, i, gamma);
+      betas.get(c, i, beta);
+      f.y<kRms>(x[i], gamma, beta, y);
+      put_eight<false>(p.Y + row * p.n, c, i, y);
+    }
+    ok = ring_next<kTeams, false>(&bars, smem, ring, &at, p.m, tensors, p.status) && ok;
+  }
 }
 
-template <int kT, int kIter, bool kF32, bool kRms>
+// A row's x - mean, g = dy gamma and dy, eight columns of them.
+template <bool kRms>
+__device__ __forceinline__ void backward_terms(const f32x2 (&x)[4], const f32x2 (&dy)[4], const f32x2 (&gamma)[4], f32x2 minus_mean,
+                                               f32x2 (&d)[4], f32x2 (&g)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    d[j] = kRms ? x[j] : add2(x[j], minus_mean);
+    g[j] = mul2(dy[j], gamma[j]);
+  }
+}
+// Their part of the row's two sums, and of dgamma and dbeta.
+template <bool kRms>
+__device__ __forceinline__ void backward_sums(const f32x2 (&d)[4], const f32x2 (&g)[4], const f32x2 (&dy)[4], f32x2 rstd, f32x2* p1,
+                                              f32x2* p2, f32x2 (&sum_g)[4], f32x2 (&sum_b)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (!kRms) *p1 = add2(*p1, g[j]);
+    *p2 = fma2(g[j], d[j], *p2);
+    sum_g[j] = fma2(dy[j], mul2(d[j], rstd), sum_g[j]);
+    sum_b[j] = add2(sum_b[j], dy[j]);
+  }
+}
+// dx = rstd g - rstd mean(g) - (mean(g h) rstd) rstd (x - mean), from the row's sums of g (s1) and of g (x - mean) (s2).
+struct BackwardFactors {
+  f32x2 rstd, slope, constant;
+  __device__ __forceinline__ BackwardFactors(float r, float s1, float s2, float inv_n)
+      : rstd(pair_of(r)), slope(pair_of(-(s2 * r * inv_n * r) * r)), constant(pair_of(-r * s1 * inv_n)) {}
+  template <bool kRms>
+  __device__ __forceinline__ void dx(const f32x2 (&d)[4], const f32x2 (&g)[4], f32x2 (&out)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out[j] = fma2(g[j], rstd, kRms ? mul2(d[j], slope) : fma2(d[j], slope, constant));
+  }
+};
+__device__ __forceinline__ void add_four(f32x2 (&v)[4], const f32x2 (&r)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = add2(v[j], r[j]);
+}
+
+// The row is read from shared memory in both sweeps: kept in registers in between it took as long (and spilled with f32).
+template <int kT, int kVec, int kIter, bool kF32, bool kRms>
 __global__ void __launch_bounds__(kRingThreads, 1)
-norm_backward_ring_kernel(const NormBackwardParams p, const RingShape ring) {
+norm_backward_kernel(const NormBackwardParams p, const RingShape ring) {
   constexpr int kTeams = kRingThreads / kT, kWarps = kT / 32;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ RingBars bars;
@@ -508,66 +633,62 @@ norm_backward_ring_kernel(const NormBackwardParams p, const RingShape ring) {
   pdl_wait();
   pdl_release();
   const uint32_t row16 = (uint32_t)p.n * 2, row_x = kF32 ? 2 * row16 : row16;
-  const RingTensor tensors[3] = {{p.X, row_x}, {p.dY, row16}, {p.dX ? p.R : nullptr, row_x}};
+  const uint32_t area_x = ring_area(kTeams, row_x), area16 = ring_area(kTeams, row16);
+  const RingTensor tensors[3] = {{p.X, row_x, area_x}, {p.dY, row16, area16}, {p.dX ? p.R : nullptr, row_x, area_x}};
   RingPlace at;
-  ring_start<kTeams>(&bars, smem, ring, &at, p.m, tensors);
+  ring_start<kTeams, kVec == 8>(&bars, smem, ring, &at, p.m, tensors);
   const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / 32, lane = (int)threadIdx.x % 32;
-  const Columns<kT, 8, kIter> c{(int)threadIdx.x % kT, p.n};
-  const HeldVector<kT, kIter> gammas(p.gamma, 1.f, c);
+  const Columns<kT, kVec, kIter> c{(int)threadIdx.x % kT, p.n};
+  const RingVector<kT, kVec, kIter> gammas(p.gamma, 1.f, reinterpret_cast<uint16_t*>(smem + (size_t)ring.stages * ring.stage_bytes), c);
+  if constexpr (kVec == 1) __syncthreads();
   f32x2 sum_g[kIter][4], sum_b[kIter][4];
 #pragma unroll
   for (int i = 0; i < kIter; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum_g[i][j] = sum_b[i][j] = 0;
   int turn = 0;
-  bool ok = true;
+  bool ok = true;          // once a wait gave up the rows go by unread and unwritten: the team's barriers still meet
   const int64_t step = (int64_t)gridDim.x * kTeams;
   int64_t row = (int64_t)blockIdx.x * kTeams + team;
   // The row's mean and rstd are fetched a row ahead.
-  float mean = 0.f, rstd = 0.f, next_mean = 0.f, next_rstd = 0.f;
+  float next_mean = 0.f, next_rstd = 0.f;
   auto fetch = [&](int64_t r) {
-    if (r < p.m) {
-      if constexpr (!kRms) next_mean = p.mean[r];
-      next_rstd = p.rstd[r];
-    }
+    next_mean = !kRms && r < p.m ? p.mean[r] : 0.f;
+    next_rstd = r < p.m ? p.rstd[r] : 0.f;
   };
   fetch(row);
   for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < p.m; row0 += step, row += step, turn ^= 1) {
-    mean = next_mean;
-    rstd = next_rstd;
+    const float rstd = next_rstd;
+    const f32x2 minus_mean = pair_of(-next_mean);
     fetch(row + step);
-    if (ok) ok = mbar_wait(&bars.full[at.stage], at.phase, &bars.abort_flag, p.status, 63);
+    if (ok) ok = mbar_wait(&bars.full[at.stage], at.phase, &bars.abort_flag, p.status, 62);
     ok = __all_sync(kFull, ok);
     const bool live = ok && row < p.m;
-    const uint8_t* x_row = smem + (size_t)at.stage * ring.stage_bytes + team * row_x;
-    const uint8_t* dy_row = smem + (size_t)at.stage * ring.stage_bytes + kTeams * row_x + team * row16;
-    const uint8_t* r_row = smem + (size_t)at.stage * ring.stage_bytes + kTeams * (row_x + row16) + team * row_x;
-    f32x2 p1 = 0, p2 = 0;      // sums of g and of g (x - mean)
-    const f32x2 minus_mean = pair_of(-mean), factor = pair_of(rstd);
-    if (live) {
+    const uint8_t* area = smem + (size_t)at.stage * ring.stage_bytes;
+    const uint8_t* x_row = ring_row<kVec == 8>(area, tensors[0], row0, team);
+    const uint8_t* dy_row = ring_row<kVec == 8>(area + area_x, tensors[1], row0, team);
+    const uint8_t* r_row = ring_row<kVec == 8>(area + area_x + area16, tensors[2], row0, team);
+    auto terms = [&](int i, f32x2 (&d)[4], f32x2 (&g)[4], f32x2 (&dy)[4]) {
+      f32x2 x[4], gamma[4];
+      gammas.get(c, i, gamma);
+      row_eight<kF32>(x_row, c, i, x);
+      row_eight<false>(dy_row, c, i, dy);
+      c.clear(i, dy);
+      backward_terms<kRms>(x, dy, gamma, minus_mean, d, g);
+    };
+    f32x2 p1 = 0, p2 = 0;
 #pragma unroll
-      for (int i = 0; i < kIter; ++i) {
-        if (!c.has(i * 8)) continue;
-        f32x2 x[4], dy[4], gamma[4];
-        shared_octet<kF32>(x_row, c.of(i * 8), x);
-        shared_octet<false>(dy_row, c.of(i * 8), dy);
-        gammas.get(i, c.of(i * 8), gamma);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x2 d = kRms ? x[j] : add2(x[j], minus_mean), g = mul2(dy[j], gamma[j]);
-          if constexpr (!kRms) p1 = add2(p1, g);
-          p2 = fma2(g, d, p2);
-          sum_g[i][j] = fma2(dy[j], mul2(d, factor), sum_g[i][j]);
-          sum_b[i][j] = add2(sum_b[i][j], dy[j]);
-        }
-      }
+    for (int i = 0; i < kIter; ++i) {
+      if (!live || !c.any(i)) continue;
+      f32x2 d[4], g[4], dy[4];
+      terms(i, d, g, dy);
+      backward_sums<kRms>(d, g, dy, pair_of(rstd), &p1, &p2, sum_g[i], sum_b[i]);
     }
     if (p.dX) {
-      float s1 = 0.f, s2 = warp_sum(pair_sum(p2));
-      if constexpr (!kRms) s1 = warp_sum(pair_sum(p1));
+      float s1 = kRms ? 0.f : warp_sum(pair_sum(p1)), s2 = warp_sum(pair_sum(p2));
       if constexpr (kT > 32) {
         if (lane == 0) parts[turn][team][warp] = make_float2(s1, s2);
-        ring_team_barrier<kT>(team);
+        team_barrier<kT, kRingThreads>(team);
         s1 = s2 = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
@@ -575,44 +696,39 @@ norm_backward_ring_kernel(const NormBackwardParams p, const RingShape ring) {
           s2 += parts[turn][team][w].y;
         }
       }
-      // dx = rstd g - rstd mean(g) - (mean(g h) rstd) rstd (x - mean) ...
-      const f32x2 constant = pair_of(-rstd * s1 * p.inv_n), slope = pair_of(-(s2 * rstd * p.inv_n * rstd) * rstd);
-      if (live) {
+      const BackwardFactors f(rstd, s1, s2, p.inv_n);
 #pragma unroll
-        for (int i = 0; i < kIter; ++i) {
-          if (!c.has(i * 8)) continue;
-          f32x2 x[4], dy[4], gamma[4], r[4], out[4];
-          shared_octet<kF32>(x_row, c.of(i * 8), x);
-          shared_octet<false>(dy_row, c.of(i * 8), dy);
-          if (p.R) shared_octet<kF32>(r_row, c.of(i * 8), r);
-          gammas.get(i, c.of(i * 8), gamma);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f32x2 d = kRms ? x[j] : add2(x[j], minus_mean);
-            out[j] = fma2(mul2(dy[j], gamma[j]), factor, kRms ? mul2(d, slope) : fma2(d, slope, constant));
-            if (p.R) out[j] = add2(out[j], r[j]);
-          }
-          put_octet<kF32>(static_cast<char*>(p.dX) + row * row_x, c.of(i * 8), out);
+      for (int i = 0; i < kIter; ++i) {
+        if (!live || !c.any(i)) continue;
+        f32x2 d[4], g[4], dy[4], out[4];
+        terms(i, d, g, dy);
+        f.dx<kRms>(d, g, out);
+        if (p.R) {
+          f32x2 r[4];
+          row_eight<kF32>(r_row, c, i, r);
+          add_four(out, r);
         }
+        put_eight<kF32>(static_cast<char*>(p.dX) + row * row_x, c, i, out);
       }
     }
-    ok = ring_next<kTeams>(&bars, smem, ring, &at, p.m, tensors, p.status) && ok;
+    ring_release(&bars, at);
+    ok = ring_next<kTeams, kVec == 8>(&bars, smem, ring, &at, p.m, tensors, p.status) && ok;
   }
   if (!p.partial) return;
   // The teams' sums meet in the ring's memory, whose last copies every team has read.
+  constexpr int kWide = kT * kIter * 8;
+  float* joined = reinterpret_cast<float*>(smem);        // [team][2][kWide]
+  float* out = p.partial + (int64_t)blockIdx.x * 2 * p.n;
   if constexpr (kTeams > 1) {
-    float* joined = reinterpret_cast<float*>(smem);        // [team][2][kT * kIter * 8]
-    constexpr int kWide = kT * kIter * 8;
-    asm volatile("bar.sync 15, %0;" ::"n"(kRingThreads) : "memory");     // no team's own
-    float* mine = joined + (size_t)team * 2 * kWide;
+    const Columns<kT, kVec, kIter> all{c.t, kWide};
+    block_barrier();
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      put_octet<true>(mine, c.of(i * 8), sum_g[i]);
-      put_octet<true>(mine + kWide, c.of(i * 8), sum_b[i]);
+      put_eight<true>(joined + (size_t)team * 2 * kWide, all, i, sum_g[i]);
+      put_eight<true>(joined + (size_t)team * 2 * kWide + kWide, all, i, sum_b[i]);
     }
-    asm volatile("bar.sync 15, %0;" ::"n"(kRingThreads) : "memory");     // no team's own
+    block_barrier();
     if (!ok) return;
-    float* out = p.partial + (int64_t)blockIdx.x * 2 * p.n;
     for (int col = (int)threadIdx.x; col < p.n; col += kRingThreads) {
       float g = 0.f, b = 0.f;
 #pragma unroll
@@ -625,12 +741,11 @@ norm_backward_ring_kernel(const NormBackwardParams p, const RingShape ring) {
     }
   } else {
     if (!ok) return;
-    float* out = p.partial + (int64_t)blockIdx.x * 2 * p.n;
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
-      if (!c.has(i * 8)) continue;
-      put_octet<true>(out, c.of(i * 8), sum_g[i]);
-      if (p.beta) put_octet<true>(out + p.n, c.of(i * 8), sum_b[i]);
+      if (!c.any(i)) continue;
+      put_eight<true>(out, c, i, sum_g[i]);
+      if (p.beta) put_eight<true>(out + p.n, c, i, sum_b[i]);
     }
   }
 }
@@ -672,7 +787,7 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormParam
     }
     if constexpr (!kRms) shift = block_sum(off, shared) * p.inv_n;
     const float square = block_sum(squares, shared) * p.inv_n - shift * shift;
-    const float rstd = 1.f / sqrtf(square + p.eps);
+    const float rstd = rsqrtf(square + p.eps);
     if (threadIdx.x == 0) {
       if (!kRms && p.mean) p.mean[row] = base + shift;
       if (p.rstd) p.rstd[row] = rstd;
@@ -681,114 +796,6 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormParam
       const float d = (element<kF32>(p.X, at + j) - base) - shift;
       const float g = p.gamma ? bf16_value(p.gamma[j]) : 1.f, b = p.beta ? bf16_value(p.beta[j]) : 0.f;
       p.Y[at + j] = bf16_round(fmaf(d * rstd, g, b));
-    }
-  }
-}
-
-// The gradients, by the same teams.  kSums: dgamma (and dbeta) are wanted.
-template <int kT, int kVec, int kIter, bool kF32, bool kRms, bool kSums>
-__global__ void __launch_bounds__(kBlockThreads) norm_backward_kernel(const NormBackwardParams p) {
-  constexpr int kTeams = kBlockThreads / kT;
-  constexpr int kWarps = kT / 32;
-  constexpr int kCount = kVec * kIter;
-  __shared__ float2 parts[2][kTeams][kWarps];
-  const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / 32, lane = (int)threadIdx.x % 32;
-  const Columns<kT, kVec, kIter> c{(int)threadIdx.x % kT, p.n};
-  float sum_g[kSums ? kCount : 1], sum_b[kSums ? kCount : 1];
-  if constexpr (kSums) {
-#pragma unroll
-    for (int e = 0; e < kCount; ++e) sum_g[e] = sum_b[e] = 0.f;
-  }
-  pdl_wait();
-  pdl_release();
-  int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * kTeams + team; row < p.m; row += (int64_t)gridDim.x * kTeams, turn ^= 1) {
-    const int64_t at = row * p.n;
-    Held<kT, kVec, kIter, kF32> x;
-    Held<kT, kVec, kIter, false> dy;
-    Held<kT, kVec, kIter, kF32> r;
-    x.load(static_cast<const char*>(p.X) + at * (kF32 ? 4 : 2), c);
-    dy.load(p.dY + at, c);
-    if (p.R) r.load(static_cast<const char*>(p.R) + at * (kF32 ? 4 : 2), c);
-    const float mean = kRms ? 0.f : p.mean[row], rstd = p.rstd[row];
-    float s1 = 0.f, s2 = 0.f;      // sums of g and of g (x - mean)
-#pragma unroll
-    for (int i = 0; i < kIter; ++i) {
-      float gamma[kVec];
-      vector_part<kVec>(c.has(i * kVec) ? p.gamma : nullptr, c.of(i * kVec), 1.f, gamma);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const int e = i * kVec + j;
-        const float v = dy.get(e), d = x.get(e) - mean, g = v * gamma[j];
-        if constexpr (!kRms) s1 += g;
-        s2 = fmaf(g, c.has(e) ? d : 0.f, s2);
-        if constexpr (kSums) {
-          sum_g[e] = fmaf(v, c.has(e) ? d * rstd : 0.f, sum_g[e]);
-          sum_b[e] += v;
-        }
-      }
-    }
-    if (!p.dX) continue;
-    if constexpr (!kRms) s1 = warp_sum(s1);
-    s2 = warp_sum(s2);
-    if constexpr (kT > 32) {
-      if (lane == 0) parts[turn][team][warp] = make_float2(s1, s2);
-      team_barrier<kT>(team);
-      s1 = s2 = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        s1 += parts[turn][team][w].x;
-        s2 += parts[turn][team][w].y;
-      }
-    }
-    const float mean_g = s1 * p.inv_n, slope = s2 * rstd * p.inv_n * rstd;     // slope: mean(g h) r, to go with x - mean
-#pragma unroll
-    for (int i = 0; i < kIter; ++i) {
-      if (!c.has(i * kVec)) continue;
-      float gamma[kVec], out[kVec];
-      vector_part<kVec>(p.gamma, c.of(i * kVec), 1.f, gamma);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const int e = i * kVec + j;
-        const float g = dy.get(e) * gamma[j], d = x.get(e) - mean;
-        const float inner = fmaf(-slope, d, kRms ? g : g - mean_g);
-        out[j] = p.R ? fmaf(rstd, inner, r.get(e)) : rstd * inner;
-      }
-      put_part<kVec, kF32>(static_cast<char*>(p.dX) + at * (kF32 ? 4 : 2), c.of(i * kVec), out);
-    }
-  }
-  if constexpr (kSums) {
-    // The teams of the block one after the other, then the block's row of partial sums.
-    float* mine = p.partial + (int64_t)blockIdx.x * 2 * p.n;
-    extern __shared__ float joined[];      // [2][kT * kCount] when there are several teams
-    if constexpr (kTeams > 1) {
-      for (int turn_of = kTeams - 1; turn_of > 0; --turn_of) {
-        if (team == turn_of) {
-#pragma unroll
-          for (int e = 0; e < kCount; ++e) {
-            const bool first = turn_of == kTeams - 1;
-            float* s = joined + e * kT + c.t;
-            s[0] = first ? sum_g[e] : s[0] + sum_g[e];
-            s[kT * kCount] = first ? sum_b[e] : s[kT * kCount] + sum_b[e];
-          }
-        }
-        __syncthreads();
-      }
-      if (team == 0) {
-#pragma unroll
-        for (int e = 0; e < kCount; ++e) {
-          sum_g[e] += joined[e * kT + c.t];
-          sum_b[e] += joined[e * kT + c.t + kT * kCount];
-        }
-      }
-    }
-    if (team == 0) {
-#pragma unroll
-      for (int i = 0; i < kIter; ++i) {
-        if (!c.has(i * kVec)) continue;
-        put_part<kVec, true>(mine, c.of(i * kVec), sum_g + i * kVec);
-        if (p.beta) put_part<kVec, true>(mine + p.n, c.of(i * kVec), sum_b + i * kVec);
-      }
     }
   }
 }
@@ -852,8 +859,8 @@ __global__ void __launch_bounds__(1024) norm_columns_kernel(const NormBackwardPa
   }
 }
 
-// dgamma and dbeta from the blocks' sums: 32 columns to a block, eight warps that take every eighth part, then the eight
-// in order.  grid.y: 0 dgamma, 1 dbeta.
+// dgamma and dbeta from the blocks' sums: 32 columns to a block, eight warps that take every eighth part, then the eight in
+// order (32 warps: 128 x 4096 7.5 instead of 6.3 us, both launches).  grid.y: 0 dgamma, 1 dbeta.
 struct NormSums {
   const float* partial;
   float* out[2];
@@ -885,128 +892,100 @@ __global__ void __launch_bounds__(256) norm_sums_kernel(const NormSums p) {
 // --- host -----------------------------------------------------------------------------------
 
 constexpr int64_t kMaxExtent = (1ll << 31) - 1024;
-constexpr int kMaxParts = 296;          // blocks whose sums the second launch joins: two to an SM of 148
-constexpr int kTeamForward = 16384;     // columns a team of 512 threads holds
-constexpr int kTeamBackward = 8192;     // columns a team of 256 threads holds beside its sums
+constexpr int64_t kRingColumns = 16384;     // a team of 512 threads with 32 columns each
 
 bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
-// The ring's teams: 16 columns to a thread, 32 in the longest rows.
-int ring_team(int64_t n) {
+// Teams of 16 columns to a thread (32 in the longest rows).
+int team_of(int64_t n) {
   int t = 32;
-  while (t < kRingThreads && n > t * 16) t *= 2;
+  while (t < 512 && n > t * 16) t *= 2;
   return t;
 }
-// Stages that fit `budget` bytes of shared memory beside the static part; below two the ring does not run.
-RingShape ring_shape(int64_t n, int64_t column_bytes, int budget) {
-  RingShape r;
-  const int64_t bytes = kRingThreads / ring_team(n) * n * column_bytes;
-  r.stage_bytes = (uint32_t)bytes;
-  r.stages = (int)std::min<int64_t>(kMaxStages, budget / bytes);
+// Stages of tensors of `sizes` bytes an element that fit shared memory beside `beside` bytes; below two the ring does not run.
+constexpr int kRingBudget = 224 * 1024;
+RingShape ring_shape(int64_t n, std::initializer_list<int> sizes, int64_t beside) {
+  RingShape r{0, 0};
+  if (n > kRingColumns) return r;
+  const int teams = kRingThreads / team_of(n);
+  for (const int size : sizes) r.stage_bytes += size ? ring_area((uint32_t)teams, (uint32_t)(n * size)) : 0u;
+  r.stages = (int)std::min<int64_t>(kMaxStages, (kRingBudget - beside) / r.stage_bytes);
   return r;
 }
 
-// Threads of a team: the fewest that hold the row in at most 32 columns each.
-int team_of(int64_t n) { return n <= 1024 ? 32 : n <= 4096 ? 128 : n <= 8192 ? 256 : 512; }
-
 // Blocks at most that leave sums of their own.
 int64_t backward_parts(int64_t m, int64_t n) {
-  if (n > kTeamBackward) return std::min<int64_t>(kMaxParts, m);
-  const int64_t teams = kBlockThreads / team_of(n);
-  return std::min<int64_t>(kMaxParts, (m + teams - 1) / teams);
+  const int64_t rows = n > kRingColumns ? 1 : kRingThreads / team_of(n);      // long rows: of a block's share
+  return std::min<int64_t>(kMaxParts, (m + rows - 1) / rows);
 }
 size_t backward_bytes(int64_t m, int64_t n) { return (size_t)backward_parts(m, n) * 2 * n * 4; }
 
-constexpr int kBackwardBudget = 224 * 1024;
-
-template <auto kKernel, int kBudget, typename Params>
-cudaError_t ring_launch(const Params& p, const RingShape& ring, int teams, int64_t most, size_t least_smem, cudaStream_t s) {
+template <auto kKernel, typename Params>
+cudaError_t ring_launch(const Params& p, const RingShape& ring, int teams, int64_t most, size_t beside, size_t least_smem, cudaStream_t s) {
   static PerDeviceOnce once;
   const cudaError_t e = once.run_current(
-      [] { return cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBudget); });
+      [] { return cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBudget); });
   if (e != cudaSuccess) return e;
   const int64_t blocks = std::min(most, (p.m + teams - 1) / teams);
   return launch_pdl(kKernel, dim3((unsigned)blocks), dim3(kRingThreads),
-                    std::max(least_smem, (size_t)ring.stages * ring.stage_bytes), s, 1, p, ring);
+                    std::max(least_smem, (size_t)ring.stages * ring.stage_bytes + beside), s, 1, p, ring);
 }
-template <bool kF32, bool kRms>
-cudaError_t backward_ring(const NormBackwardParams& p, const RingShape& ring, int64_t blocks, cudaStream_t s) {
-#define MORELLO_RING(T, ITER)                                                                                          \
-  return ring_launch<norm_backward_ring_kernel<T, ITER, kF32, kRms>, kBackwardBudget>(p, ring, kRingThreads / T, blocks, \
-                                                                                      (size_t)kRingThreads * ITER * 64, s)
-  if (p.n <= 256) MORELLO_RING(32, 1);
-  if (p.n <= 512) MORELLO_RING(32, 2);
-  if (p.n <= 1024) MORELLO_RING(64, 2);
-  if (p.n <= 2048) MORELLO_RING(128, 2);
-  if (p.n <= 4096) MORELLO_RING(256, 2);
-  if (p.n <= 8192) MORELLO_RING(512, 2);
-  MORELLO_RING(512, 4);
-#undef MORELLO_RING
+// Calls go with a team's threads and a thread's eights.
+template <typename Go>
+cudaError_t by_team(int64_t n, Go&& go) {
+  using std::integral_constant;
+  if (n <= 256) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+  if (n <= 512) return go(integral_constant<int, 32>{}, integral_constant<int, 2>{});
+  if (n <= 1024) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  if (n <= 2048) return go(integral_constant<int, 128>{}, integral_constant<int, 2>{});
+  if (n <= 4096) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  if (n <= 8192) return go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+  return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
 }
 
 template <bool kF32, bool kRms>
 cudaError_t forward_launch(const DeviceInfo& dev, const NormParams& p, bool vec, cudaStream_t s) {
   const int n = p.n;
+  // Blocks: as many as are resident together, each with its share of the rows.
   auto go = [&](auto kernel, int team) {
-    const int threads = std::max(team, kBlockThreads), rows = threads / team;
-    const int64_t blocks = std::min<int64_t>((p.m + rows - 1) / rows, (int64_t)dev.sms * 8);
+    const int threads = std::max(team, kBlockThreads), each = threads / team;
+    int resident = 1;
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, 0);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = std::min<int64_t>((p.m + each - 1) / each, (int64_t)dev.sms * resident);
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(threads), 0, s, 1, p);
   };
-#define MORELLO_NORM(T, ITER) return go(norm_octets_kernel<T, ITER, kF32, kRms>, T)
-#define MORELLO_NORM_ODD(T, ITER) return go(norm_kernel<T, 1, ITER, kF32, kRms>, T)
-  if (n > kTeamForward) return launch_pdl(norm_long_kernel<kF32, kRms>, dim3((unsigned)std::min<int64_t>(p.m, (int64_t)dev.sms * 2)),
-                                          dim3(kLongThreads), 0, s, 1, p);
+#define MORELLO_NORM(T, ITER) return go(norm_kernel<T, ITER, kF32, kRms>, T)
+  const int64_t beside = n > kRingColumns ? 0 : 4 * n;       // gamma and beta
+  const RingShape ring = ring_shape(n, {kF32 ? 4 : 2}, beside);
+  if (vec ? n > kRingColumns : ring.stages < 2)
+    return launch_pdl(norm_long_kernel<kF32, kRms>, dim3((unsigned)std::min<int64_t>(p.m, (int64_t)dev.sms * 2)),
+                      dim3(kLongThreads), 0, s, 1, p);
   if (vec) {
+    // 16 columns to a thread; 32 of long rows where there are many: half the teams' joins, and 16 bytes more of every thread
+    // in flight (2048 x 8192: 15.5 instead of 19.0 us, f32 4096 x 4096 18.2 instead of 20.8; 16384 x 4096 53.0 and 53.9,
+    // 4096 x 2048 9.6 and 8.7; 128 x 4096 3.5 and 2.6).
+    const bool many = p.m >= 4 * (int64_t)dev.sms;
     if (n <= 64) MORELLO_NORM(8, 1);
     if (n <= 128) MORELLO_NORM(16, 1);
     if (n <= 256) MORELLO_NORM(32, 1);
     if (n <= 512) MORELLO_NORM(32, 2);
-    if (n <= 1024) MORELLO_NORM(32, 4);
+    if (n <= 1024) MORELLO_NORM(64, 2);
     if (n <= 2048) MORELLO_NORM(128, 2);
-    if (n <= 4096) MORELLO_NORM(128, 4);
-    if (n <= 8192) MORELLO_NORM(256, 4);
+    if (n <= 4096) {
+      if (many) MORELLO_NORM(128, 4);
+      MORELLO_NORM(256, 2);
+    }
+    if (n <= 8192) {
+      if (many) MORELLO_NORM(256, 4);
+      MORELLO_NORM(512, 2);
+    }
     MORELLO_NORM(512, 4);
   }
-  if (n <= 256) MORELLO_NORM_ODD(32, 8);
-  if (n <= 1024) MORELLO_NORM_ODD(32, 32);
-  if (n <= 2048) MORELLO_NORM_ODD(128, 16);
-  if (n <= 4096) MORELLO_NORM_ODD(128, 32);
-  if (n <= 8192) MORELLO_NORM_ODD(256, 32);
-  MORELLO_NORM_ODD(512, 32);
-#undef MORELLO_NORM
-#undef MORELLO_NORM_ODD
-}
-
-template <bool kF32, bool kRms, bool kSums>
-cudaError_t backward_rows_launch(const NormBackwardParams& p, int parts, bool vec, cudaStream_t s) {
-  const int n = p.n, t = team_of(n);
-  auto go = [&](auto kernel, int teams) {
-    // The teams' sums meet in shared memory: kBlockThreads / teams threads of 32 columns at most.
-    const size_t smem = kSums && teams > 1 ? (size_t)2 * (kBlockThreads / teams) * 32 * 4 : 0;
-    return launch_pdl(kernel, dim3((unsigned)parts), dim3(kBlockThreads), smem, s, 1, p);
-  };
-#define MORELLO_NORM(T, VEC, ITER) return go(norm_backward_kernel<T, VEC, ITER, kF32, kRms, kSums>, kBlockThreads / T)
-  if (vec) {
-    if (t == 32) {
-      if (n <= 256) MORELLO_NORM(32, 8, 1);
-      if (n <= 512) MORELLO_NORM(32, 8, 2);
-      MORELLO_NORM(32, 8, 4);
-    }
-    if (t == 128) {
-      if (n <= 2048) MORELLO_NORM(128, 8, 2);
-      MORELLO_NORM(128, 8, 4);
-    }
-    MORELLO_NORM(256, 8, 4);
-  }
-  if (t == 32) {
-    if (n <= 256) MORELLO_NORM(32, 1, 8);
-    MORELLO_NORM(32, 1, 32);
-  }
-  if (t == 128) {
-    if (n <= 2048) MORELLO_NORM(128, 1, 16);
-    MORELLO_NORM(128, 1, 32);
-  }
-  MORELLO_NORM(256, 1, 32);
+  return by_team(n, [&](auto team, auto eights) {
+    return ring_launch<norm_ring_kernel<team.value, eights.value, kF32, kRms>>(p, ring, kRingThreads / team.value, dev.sms,
+                                                                               (size_t)beside, 0, s);
+  });
 #undef MORELLO_NORM
 }
 
@@ -1017,14 +996,20 @@ cudaError_t backward_launch(const DeviceInfo& dev, const NormBackwardParams& p, 
   const bool sums = dgamma || dbeta;
   int parts = (int)backward_parts(p.m, p.n);
   constexpr int kSize = kF32 ? 4 : 2;
+  const int64_t beside = vec || p.n > kRingColumns ? 0 : 2 * p.n;       // gamma
   // With R or without: what a call asks for besides does not change the order of its sums.
-  if (vec && p.n <= kRingThreads * 32 && ring_shape(p.n, 2 * kSize + 2, kBackwardBudget).stages >= 2) {
-    const RingShape ring = ring_shape(p.n, kSize * (p.R && p.dX ? 2 : 1) + 2, kBackwardBudget);
-    const int64_t teams = kRingThreads / ring_team(p.n);
+  if (ring_shape(p.n, {kSize, 2, kSize}, beside).stages >= 2) {
+    const RingShape ring = ring_shape(p.n, {kSize, 2, p.R && p.dX ? kSize : 0}, beside);
+    const int64_t teams = kRingThreads / team_of(p.n);
     parts = (int)std::min<int64_t>(std::min(parts, dev.sms), (p.m + teams - 1) / teams);
-    e = backward_ring<kF32, kRms>(p, ring, parts, s);
-  } else if (p.n > kTeamBackward) {
-    parts = (int)std::min<int64_t>(kMaxParts, (p.m + 127) / 128);
+    e = by_team(p.n, [&](auto team, auto eights) {
+      constexpr int kT = team.value, kIter = eights.value;
+      constexpr size_t kJoined = (size_t)kRingThreads * kIter * 64;      // the teams' sums
+      return vec ? ring_launch<norm_backward_kernel<kT, 8, kIter, kF32, kRms>>(p, ring, kRingThreads / kT, parts, 0, kJoined, s)
+                 : ring_launch<norm_backward_kernel<kT, 1, kIter, kF32, kRms>>(p, ring, kRingThreads / kT, parts, (size_t)beside, kJoined, s);
+    });
+  } else {
+    parts = (int)std::min<int64_t>(parts, (p.m + 127) / 128);
     if (p.dX) {
       const int64_t blocks = std::min<int64_t>(p.m, (int64_t)dev.sms * 2);
       e = launch_pdl(norm_backward_long_kernel<kF32, kRms>, dim3((unsigned)blocks), dim3(kLongThreads), 0, s, 1, p);
@@ -1034,9 +1019,6 @@ cudaError_t backward_launch(const DeviceInfo& dev, const NormBackwardParams& p, 
     if (!sums) return e;
     const int64_t per = (p.m + parts - 1) / parts;
     e = launch_pdl(norm_columns_kernel<kF32>, dim3((unsigned)((p.n + 31) / 32), (unsigned)parts), dim3(1024), 0, s, 1, p, per);
-  } else {
-    e = sums ? backward_rows_launch<kF32, kRms, true>(p, parts, vec, s)
-             : backward_rows_launch<kF32, kRms, false>(p, parts, vec, s);
   }
   if (e != cudaSuccess) return e;
   ++*launches;

@@ -67,7 +67,8 @@ def test_backward(m, n, rms, kind):
 
 @pytest.mark.parametrize("kind", [BF, F32])
 @pytest.mark.parametrize("m,n", [(20000, 64), (9001, 256), (5000, 520), (2503, 1024), (1701, 2048), (1303, 4096), (799, 8192),
-                                 (601, 16384), (700, 12008), (4000, 2056)])
+                                 (601, 16384), (700, 12008), (4000, 2056), (20000, 7), (5000, 333), (4001, 2047), (799, 8191),
+                                 (600, 12001), (3000, 1)])
 def test_batches(m, n, kind):
     # many rows to a block, the last ones a part of a group
     for rms in (False, True):
@@ -76,16 +77,17 @@ def test_batches(m, n, kind):
 
 
 @pytest.mark.parametrize("kind", [BF, F32])
-@pytest.mark.parametrize("n", [256, 2048, 8192, 16384])
-def test_unaligned_tensors(n, kind):
-    x, gamma, beta, dy, r = (misaligned(t) for t in make(5, n, kind, n))
-    y = misaligned(torch.zeros(5, n, device="cuda", dtype=BF))
-    mb.morello_layer_norm(0, int(kind == F32), 5, n, 1e-5, x, gamma, beta, y)
+@pytest.mark.parametrize("m,n", [(5, 256), (5, 2048), (5, 8192), (5, 16384), (5, 3), (17, 1), (40, 1), (100, 5), (1500, 7), (2000, 264),
+                                 (700, 2048)])
+def test_unaligned_tensors(m, n, kind):
+    x, gamma, beta, dy, r = (misaligned(t) for t in make(m, n, kind, n))
+    y = misaligned(torch.zeros(m, n, device="cuda", dtype=BF))
+    mb.morello_layer_norm(0, int(kind == F32), m, n, 1e-5, x, gamma, beta, y)
     check_forward(x, gamma, beta, 1e-5, False, y, None, None)
     mean, rstd, _, _ = norm64(x, None, None, 1e-5, False)
     mean, rstd = mean[:, 0].float(), rstd[:, 0].float()
     dx, dg = misaligned(torch.zeros_like(x)), misaligned(torch.zeros(n, device="cuda"))
-    mb.morello_layer_norm_backward(0, int(kind == F32), 0, 5, n, x, gamma, mean, rstd, dy, r, dx, dg, None)
+    mb.morello_layer_norm_backward(0, int(kind == F32), 0, m, n, x, gamma, mean, rstd, dy, r, dx, dg, None)
     check_backward(x, gamma, mean, rstd, dy, r, False, dx, dg, None)
 
 
