@@ -12,7 +12,9 @@
 // warps take all of a tile's sums into registers, hand the accumulator back, and finish the tile under the next one's main
 // loop.  Gated tiles hold 128 columns of either half of W.
 #include <algorithm>
+#include <type_traits>
 
+#include "activation_pairs.cuh"
 #include "fp4.h"
 #include "tensormap.h"
 #include "tile_epilogue.cuh"
@@ -31,12 +33,16 @@ constexpr int kBytesA = kRowsPerCta * kRowBytes;     // 16 KiB
 constexpr int kAccColumns = 256;
 constexpr int kScaleColumns = 64;                    // of tensor memory, per stage in turn
 constexpr int kTmemColumns = 512;
-constexpr int kEpiWarps = 8;                         // two per quarter of the rows
-constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kEpiWarps = 16;                        // four per quarter of the rows
+constexpr int kParts = kEpiWarps / 4;
+constexpr int kThreads = 128 + 32 * kEpiWarps;       // a warpgroup for the producer and the issuer, two for the epilogue
+// 640 threads are launched with 96 registers each; the epilogue's hold up to 64 sums besides.  (Eight epilogue warps with twice
+// the sums each leave the schedulers short of warps: 4096 x 4096 x 4096 with GELU, bias and residual 46 us.)
+constexpr int kFewRegisters = 32, kManyRegisters = 112;
+static_assert(128 * kFewRegisters + 32 * kEpiWarps * kManyRegisters <= kThreads * 96, "registers of the launch");
 constexpr int kMaxStages = 8;
-constexpr int kEpiBlockBytes = 4 * 1024;             // per warp: two blocks of 32 x 32 bf16, or one of f32
-constexpr int kEpiBytes = kEpiWarps * kEpiBlockBytes;
-constexpr int kBlock16 = 32 * 32 * 2;
+constexpr int kBlockBytes = 32 * 64;                 // per warp: a block of 32 rows of 32 bf16 or 16 f32
+constexpr int kEpiBytes = kEpiWarps * kBlockBytes;
 constexpr int kSmemBudget = 227 * 1024;
 constexpr int kRaster = 8;                           // rows of tiles per group of the tile order
 
@@ -54,7 +60,7 @@ struct Shape {
   static constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
   static constexpr size_t kSmemBytes = (size_t)kStages * kStageBytes + kEpiBytes + 1024 + 512;
   static constexpr int kBuffers = kAccColumns / kTileN;
-  static constexpr int kCols = kTileN / 2;                           // accumulator columns of an epilogue thread
+  static constexpr int kCols = kTileN / kParts;                      // accumulator columns of an epilogue thread
   static_assert(kColsB % kAtomRows == 0 && kAtomsK * 4 * (1 + kAtomsB) <= kScaleColumns, "tile shape");
 };
 
@@ -77,12 +83,14 @@ struct Barriers {
   uint64_t empty[kMaxStages];
   uint64_t acc_full[2];
   uint64_t acc_empty[2];
+  uint64_t res_full[kEpiWarps];      // the residual has come to a warp's block
   uint32_t tmem_base;
   int abort_flag;
 };
 
 // The tile's place: tiles are walked in groups of kRaster rows of tiles, row-fastest inside a group, so that the tiles in
-// flight share a few rows of X and a few columns of W in L2.
+// flight share a few rows of X and a few columns of W in L2.  (The last wave's tiles cut into column halves, where those fill
+// at most half of the units, gained 1 % on a cube of 4096, and lost as much elsewhere: the board's power is the limit.)
 __device__ __forceinline__ void tile_place(const Fp4Params& p, int t, int* mt, int* nt) {
   const int per = kRaster * p.n_tiles, group = t / per, at = t - group * per;
   const int rows = min(kRaster, p.m_tiles - group * kRaster);
@@ -94,7 +102,7 @@ template <bool kPair, int kTileN, bool kGated, bool kNv>
 __global__ void __launch_bounds__(kThreads, 1)
 fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
-                const __grid_constant__ CUtensorMap map_y, const Fp4Params p) {
+                const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_r, const Fp4Params p) {
   using S = Shape<kPair, kTileN, kNv>;
   constexpr int kOutCols = kGated ? kTileN / 2 : kTileN;
   extern __shared__ uint8_t smem_raw[];
@@ -119,6 +127,7 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       mbar_init(&bars->acc_full[i], 1);
       mbar_init(&bars->acc_empty[i], kEpiWarps * S::kCtas);
     }
+    for (int i = 0; i < kEpiWarps; ++i) mbar_init(&bars->res_full[i], 1);
     bars->abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_descriptor(&map_a);
@@ -143,7 +152,9 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   tc_fence_after_sync();
   const uint32_t tmem_base = bars->tmem_base;
 
-  if (warp == 0) {
+  if (warp < 4) {
+    registers_down<kFewRegisters>();
+    if (warp == 0) {
     // ------------------------------------------------------------------ producer
     if (elect_one()) {
       int stage = 0;
@@ -184,7 +195,7 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
       }
     }
-  } else if (warp == 1) {
+    } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (rank == 0 && elect_one()) {
       int stage = 0, buf = 0;
@@ -238,36 +249,61 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if (++buf == S::kBuffers) { buf = 0; acc_phase ^= 1; }
       }
     }
+    }
   } else {
+    registers_up<kManyRegisters>();
     // ------------------------------------------------------------------ epilogue
-    const int ew = warp - 2;
+    const int ew = warp - 4;
     const int quarter = warp & 3, part = ew >> 2;      // TMEM lanes 32 quarter ..; share of the columns
-    uint8_t* mine = epi + (size_t)ew * kEpiBlockBytes;
+    uint8_t* mine = epi + (size_t)ew * kBlockBytes;
+    const uint32_t block = smem_u32(mine);
     const float alpha = p.alpha ? *p.alpha : 1.f;
     // A thread's groups of 32 accumulator columns; gated: the gate's, then their partners'.
     constexpr int kGroups = S::kCols / 32, kOutGroups = kGated ? kGroups / 2 : kGroups;
+    static_assert(kOutGroups == 1 || kOutGroups == 2, "steps of an item");
     auto group_column = [&](int g) {
       return kGated ? (g / kOutGroups) * (kTileN / 2) + part * (32 * kOutGroups) + g % kOutGroups * 32
                     : part * S::kCols + g * 32;
     };
+    auto scale_and_bias = [&](f32x2(&v)[16], float bias) {
+      const f32x2 factor = pair_of(alpha);
+      if (p.bias) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          v[i] = fma2(v[i], factor, pair_of(__shfl_sync(kFullMask, bias, 2 * i), __shfl_sync(kFullMask, bias, 2 * i + 1)));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], factor);
+      }
+    };
     int buf = 0;
-    uint32_t acc_phase = 0, slot = 0;
+    uint32_t acc_phase = 0, res_phase = 0;
     bool ok = true;
     for (int t = unit; t < p.tiles && ok; t += units) {
       int mt, nt;
       tile_place(p, t, &mt, &nt);
-      const int64_t row0 = (int64_t)mt * S::kTileM + rank * kRowsPerCta + quarter * 32, row = row0 + lane;
+      const int64_t row0 = (int64_t)mt * S::kTileM + rank * kRowsPerCta + quarter * 32;
       const int col0 = nt * kOutCols + part * (32 * kOutGroups);      // first output column of this thread
       const int steps = row0 < p.m && col0 < p.n ? min(kOutGroups, (p.n - col0 + 31) / 32) : 0;
-      uint4 res[4];
+      // The residual's blocks come by TMA to where the output's leave from: the first while the sums are awaited, the next
+      // while a step is worked on.  (Read straight into registers, 64 bytes of 32 rows, it cost 15 us of 49 on a cube of 4096.)
+      const bool res_tma = p.residual && p.tma;
       auto load_residual = [&](int s) {
-        const int col = col0 + 32 * s;
-        const uint4* src = reinterpret_cast<const uint4*>(p.residual + row * p.n + col);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) res[j] = row < p.m && col + 8 * j < p.n ? src[j] : make_uint4(0u, 0u, 0u, 0u);
+        if (lane != 0) return;
+        bulk_wait_group_read<0>();
+        mbar_arrive_expect_tx(&bars->res_full[ew], kBlockBytes);
+        tma_load_3d(mine, &map_r, &bars->res_full[ew], col0 + 32 * s, (int)row0, 0);
       };
-      if (p.residual && p.tma && steps > 0) load_residual(0);
-      float sums[S::kCols];
+      if (res_tma && steps > 0) load_residual(0);
+      // The bias of a step's columns, one to a lane.
+      float bias[kOutGroups], bias_up[kGated ? kOutGroups : 1];
+#pragma unroll
+      for (int g = 0; g < kOutGroups; ++g) {
+        const int col = col0 + 32 * g + lane;
+        bias[g] = p.bias && col < p.n ? bf16_value(p.bias[col]) : 0.f;
+        if constexpr (kGated) bias_up[g] = p.bias && col < p.n ? bf16_value(p.bias[p.n + col]) : 0.f;
+      }
+      f32x2 sums[kGroups][16];
       for (int done = 0; done < p.k_blocks && ok; done += p.chunk) {
         ok = mbar_wait(&bars->acc_full[buf], acc_phase, abort_flag, p.status, 54);
         ok = __all_sync(kFullMask, ok);
@@ -275,10 +311,14 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if (!ok) break;
         const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kTileN);
         if (done == 0) {
+          uint32_t r[kGroups][32];
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) tmem_ld_32x32(taddr + group_column(g), r[g]);
+          tmem_ld_wait();
 #pragma unroll
           for (int g = 0; g < kGroups; ++g)
-            tmem_ld_32x32(taddr + group_column(g), *reinterpret_cast<uint32_t(*)[32]>(sums + 32 * g));
-          tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sums[g][i] = pair_of(__uint_as_float(r[g][2 * i]), __uint_as_float(r[g][2 * i + 1]));
         } else {
 #pragma unroll
           for (int g = 0; g < kGroups; ++g) {
@@ -286,7 +326,8 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             tmem_ld_32x32(taddr + group_column(g), r);
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) sums[32 * g + i] += __uint_as_float(r[i]);
+            for (int i = 0; i < 16; ++i)
+              sums[g][i] = add2(sums[g][i], pair_of(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])));
           }
         }
         tc_fence_before_sync();
@@ -300,72 +341,72 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       if (!ok) break;
       if (p.k_blocks == 0) {
 #pragma unroll
-        for (int i = 0; i < S::kCols; ++i) sums[i] = 0.f;
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sums[g][i] = 0;
       }
-      // One step of 32 columns a turn, always from the first registers; the others move up behind it, so that the code of a
-      // step is there once.
-#pragma unroll 1
-      for (int s = 0; s < steps; ++s) {
+      // 32 columns of the output, the s-th of this thread's, from group g of its sums.
+      auto step = [&](int s, auto group) {
+        constexpr int g = decltype(group)::value;
         const int col = col0 + 32 * s;
-        float(&v)[32] = *reinterpret_cast<float(*)[32]>(sums);
-        const int left = p.n - col;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= alpha;
-        if (p.bias) add_bias32(p.bias + col, left, p.tma, v);
-        act32_by(p.act, v);
+        f32x2(&v)[16] = sums[g];
+        if (res_tma && s > 0) load_residual(s);
+        scale_and_bias(v, bias[g]);
+        act_pairs_by(p.act, v);
         if constexpr (kGated) {
-          float u[32];
+          f32x2(&u)[16] = sums[kOutGroups + g];
+          scale_and_bias(u, bias_up[g]);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) u[i] = sums[32 * kOutGroups + i] * alpha;
-          if (p.bias) add_bias32(p.bias + p.n + col, left, p.tma, u);
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] *= u[i];
+          for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], u[i]);
         }
-        const int rows_here = lane < left ? (int)min((int64_t)32, p.m - row0) : 0;
-        const PlainBlock plain{row0 * p.n + col + lane, p.n, rows_here};
-        uint8_t* b = mine;
-        if (p.residual && p.tma) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) add_octet(res[j], v + 8 * j);
-          if (s + 1 < steps) load_residual(s + 1);
+        const int left = p.n - col, rows_here = (int)max((int64_t)0, min((int64_t)32, p.m - row0));
+        const PlainBlock plain{row0 * p.n + col + lane, p.n, lane < left ? rows_here : 0};
+        if (res_tma) {
+          ok = mbar_wait(&bars->res_full[ew], res_phase, abort_flag, p.status, 55);
+          ok = __all_sync(kFullMask, ok);
+          res_phase ^= 1u;
+          if (!ok) return;
+          add_pairs16(block, lane, v);
         } else if (p.residual) {
-          block_in16(smem_u32(b), lane, p.residual, plain);
+          block_in16(block, lane, p.residual, plain);
           __syncwarp();
-          add_row16(smem_u32(b), lane, v);
-          __syncwarp();
+          add_pairs16(block, lane, v);
+        } else if (p.tma) {
+          if (lane == 0) bulk_wait_group_read<0>();      // the block's last store has been read
         }
-        if (p.tma) {
-          // The block's last store has been read: with f32 the only block's, with bf16 that of the other turn may be pending.
-          if (lane == 0) {
-            if (p.out_f32) bulk_wait_group_read<0>(); else bulk_wait_group_read<1>();
+        __syncwarp();
+        // The block out, or (f32) the first and the second half of the columns.
+        auto send = [&](int at) {
+          if (p.tma) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_3d(&map_y, mine, col + at, (int)row0, 0);
+              bulk_commit_group();
+            }
+          } else {
+            __syncwarp();
+            if (p.out_f32) half_block_out32(block, lane, static_cast<float*>(p.Y), PlainBlock{row0 * p.n + col + at, p.n, rows_here}, left - at);
+            else block_out16(block, lane, static_cast<uint16_t*>(p.Y), plain);
+            __syncwarp();
           }
+        };
+        if (p.out_f32) {
+          put_pairs32<0>(block, lane, v);
+          send(0);
+          if (left <= 16) return;
+          if (p.tma && lane == 0) bulk_wait_group_read<0>();
           __syncwarp();
-          if (!p.out_f32) {
-            b += slot * kBlock16;
-            slot ^= 1u;
-          }
-        }
-        if (p.out_f32) put_row32(smem_u32(b), lane, v);
-        else put_row16(smem_u32(b), lane, v);
-        if (p.tma) {
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store_3d(&map_y, b, col, (int)row0, 0);
-            bulk_commit_group();
-          }
+          put_pairs32<1>(block, lane, v);
+          send(16);
         } else {
-          __syncwarp();
-          if (p.out_f32) block_out32(smem_u32(b), lane, static_cast<float*>(p.Y), plain, false);
-          else block_out16(smem_u32(b), lane, static_cast<uint16_t*>(p.Y), plain);
-          __syncwarp();
+          put_pairs16(block, lane, v);
+          send(0);
         }
-#pragma unroll
-        for (int g = 0; g + 1 < kGroups; ++g) {
-          if (g + 1 == kOutGroups) continue;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) sums[32 * g + i] = sums[32 * (g + 1) + i];
-        }
+      };
+      if (steps > 0) step(0, std::integral_constant<int, 0>{});
+      if constexpr (kOutGroups > 1) {
+        if (steps > 1 && ok) step(1, std::integral_constant<int, 1>{});
       }
     }
     // Shared memory must outlive the engine's reads, and the stores must have been performed before the
@@ -405,7 +446,7 @@ cudaError_t launch_form(const DeviceInfo& dev, const Fp4Call& c, Fp4Params p, cu
   p.m_tiles = (int)m_tiles;
   p.n_tiles = (int)n_tiles;
   p.tiles = (int)(m_tiles * n_tiles);
-  CUtensorMap a{}, b{}, sa{}, sb{}, y{};
+  CUtensorMap a{}, b{}, sa{}, sb{}, y{}, r{};
   const int64_t pitch = fp4_pitch(c.k), across = fp4_atoms_across(kNv, c.k);
   auto rows_map = [&](CUtensorMap* m, const void* q, int64_t rows) {
     return make_tensor_map_3d(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, q, (uint64_t)pitch, (uint64_t)rows, 1, kRowBytes, kAtomRows,
@@ -424,19 +465,42 @@ cudaError_t launch_form(const DeviceInfo& dev, const Fp4Call& c, Fp4Params p, cu
   }
   if (p.tma) {
     e = make_tensor_map_3d(&y, c.epi.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                           c.epi.out_f32 ? 4 : 2, c.epi.Y, (uint64_t)c.n, (uint64_t)c.m, 1, 32, 32,
-                           c.epi.out_f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+                           c.epi.out_f32 ? 4 : 2, c.epi.Y, (uint64_t)c.n, (uint64_t)c.m, 1, c.epi.out_f32 ? 16 : 32, 32,
+                           CU_TENSOR_MAP_SWIZZLE_64B);
+    if (e == cudaSuccess && c.epi.residual)
+      e = make_tensor_map_3d(&r, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, c.epi.residual, (uint64_t)c.n, (uint64_t)c.m, 1, 32, 32,
+                             CU_TENSOR_MAP_SWIZZLE_64B);
     if (e != cudaSuccess) return e;
   }
   const int units = std::min(p.tiles, kPair ? gemm_pair_units(dev.sms) : dev.sms);
   return launch_pdl(fp4_tile_kernel<kPair, kTileN, kGated, kNv>, dim3((unsigned)(units * S::kCtas)), dim3(kThreads),
-                    S::kSmemBytes, stream, S::kCtas, a, b, sa, sb, y, p);
+                    S::kSmemBytes, stream, S::kCtas, a, b, sa, sb, y, r, p);
+}
+
+// What a tile costs, in microseconds: a block of 256 elements of the contraction, and the epilogue, which the next tile's
+// main loop hides if it is longer.  Measured, of whole calls: pairs and single CTAs 31 and 38 us on a cube of 4096, 14.4 and
+// 15.2 on 1024 x 4096 x 4096, 11.3 and 10.1 on 700 x 2048 x 4096, 20.0 and 18.7 on 4096 x 512 x 4096.
+struct TileForm {
+  bool pair;
+  int tile_n;
+  double block, epilogue;
+};
+constexpr TileForm kPair256{true, 256, 0.41, 4.0}, kOne256{false, 256, 0.56, 1.5}, kOne128{false, 128, 0.29, 2.0};
+double form_time(const DeviceInfo& dev, const Fp4Call& c, const TileForm& f) {
+  const int64_t tile_m = kRowsPerCta << (f.pair ? 1 : 0), cols = c.epi.gated ? f.tile_n / 2 : f.tile_n;
+  const int64_t tiles = (c.m + tile_m - 1) / tile_m * ((c.n + cols - 1) / cols);
+  const int64_t units = std::max(1, f.pair ? gemm_pair_units(dev.sms) : dev.sms);
+  const double blocks = (double)((c.k + kTileK - 1) / kTileK);
+  return (double)((tiles + units - 1) / units) * std::max(blocks * f.block, f.epilogue) + f.epilogue;
 }
 
 template <bool kNv>
 cudaError_t launch_any(const DeviceInfo& dev, const Fp4Call& c, const Fp4Params& p, cudaStream_t stream) {
-  if (c.epi.gated) return launch_form<false, 256, true, kNv>(dev, c, p, stream);
-  return launch_form<false, 128, false, kNv>(dev, c, p, stream);
+  const TileForm& one = c.epi.gated ? kOne256 : kOne128;
+  const bool pair = c.m > kRowsPerCta && form_time(dev, c, kPair256) < form_time(dev, c, one);
+  if (c.epi.gated)
+    return pair ? launch_form<true, 256, true, kNv>(dev, c, p, stream) : launch_form<false, 256, true, kNv>(dev, c, p, stream);
+  return pair ? launch_form<true, 256, false, kNv>(dev, c, p, stream) : launch_form<false, 128, false, kNv>(dev, c, p, stream);
 }
 
 }  // namespace

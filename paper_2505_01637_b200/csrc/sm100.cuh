@@ -35,6 +35,14 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;"); }
 
+// ---- registers of a warpgroup --------------------------------------------------
+// Hands registers back, or takes handed-back ones: executed by all four warps of a warpgroup.  What the warpgroups of a block
+// hold in the end must not be more than it was launched with.
+template <int kRegisters>
+__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
+template <int kRegisters>
+__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
+
 // ---- pairs of f32 ------------------------------------------------------------
 // Two f32 in one 64-bit register, one instruction for both; every result is rounded as by the single operation.
 using f32x2 = uint64_t;

@@ -112,4 +112,51 @@ __device__ __forceinline__ void add_row16(uint32_t block, int lane, float (&v)[3
   }
 }
 
+// put_row16 and add_row16 of 16 pairs; 16 f32 make a row as long (the lower or the upper eight pairs).
+__device__ __forceinline__ uint32_t bf16_pack_pair(sm100::f32x2 v) {
+  const float2 f = sm100::pair_values(v);
+  return bf16_pack(f.x, f.y);
+}
+__device__ __forceinline__ void put_pairs16(uint32_t block, int lane, const sm100::f32x2 (&v)[16]) {
+  const uint32_t at = block + (uint32_t)lane * 64u, sw = (uint32_t)(lane >> 1) & 3u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    st_shared_v4(at + (((uint32_t)j ^ sw) << 4), bf16_pack_pair(v[4 * j]), bf16_pack_pair(v[4 * j + 1]), bf16_pack_pair(v[4 * j + 2]),
+                 bf16_pack_pair(v[4 * j + 3]));
+}
+template <int kHalf>
+__device__ __forceinline__ void put_pairs32(uint32_t block, int lane, const sm100::f32x2 (&v)[16]) {
+  const uint32_t at = block + (uint32_t)lane * 64u, sw = (uint32_t)(lane >> 1) & 3u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 a = sm100::pair_values(v[8 * kHalf + 2 * j]), b = sm100::pair_values(v[8 * kHalf + 2 * j + 1]);
+    st_shared_v4(at + (((uint32_t)j ^ sw) << 4), __float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+  }
+}
+__device__ __forceinline__ void add_pairs16(uint32_t block, int lane, sm100::f32x2 (&v)[16]) {
+  const uint32_t at = block + (uint32_t)lane * 64u, sw = (uint32_t)(lane >> 1) & 3u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                 : "r"(at + (((uint32_t)j ^ sw) << 4)) : "memory");
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[4 * j + q] = sm100::add2(v[4 * j + q], sm100::pair_of(bf16_low(w[q]), bf16_high(w[q])));
+  }
+}
+// A block of 32 rows of 16 f32 out to memory, two rows at a time: g.at is that of the block's first element here, cols its
+// columns that exist.
+__device__ __forceinline__ void half_block_out32(uint32_t block, int lane, float* dst, const PlainBlock& g, int cols) {
+  const int col = lane & 15;
+#pragma unroll 8
+  for (int r0 = 0; r0 < 32; r0 += 2) {
+    const int r = r0 + (lane >> 4);
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v)
+                 : "r"(block + (uint32_t)r * 64u + ((((uint32_t)col >> 2) ^ (((uint32_t)r >> 1) & 3u)) << 4) + ((uint32_t)col & 3u) * 4u)
+                 : "memory");
+    if (r < g.rows && col < cols) dst[g.at + r * g.pitch + col] = v;
+  }
+}
+
 }  // namespace morello
