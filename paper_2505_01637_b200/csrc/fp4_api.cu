@@ -52,7 +52,7 @@ int morello_fp4_linear(int format, int act, int gated, int y_type, int64_t m, in
   c.epi.residual = static_cast<const uint16_t*>(R);
   c.epi.Y = Y;
   uint64_t launches = 0;
-  const cudaError_t e = fp4_tile_launch(dev, c, s, &launches);
+  const cudaError_t e = m <= kFp4FewRows ? fp4_rows_launch(dev, c, s, &launches) : fp4_tile_launch(dev, c, s, &launches);
   count_launches(launches);
   return e == cudaSuccess ? MORELLO_OK : record_cuda_error(e);
 }

@@ -72,6 +72,14 @@ def test_large(m, k, n, fmt):
 
 
 @pytest.mark.parametrize("fmt", [MX, NV])
+@pytest.mark.parametrize("m", [1, 7, 8, 9, 16, 17, 31, 32, 33, 48, 63, 64])
+def test_few_rows(m, fmt):
+    # one slice, a cluster of every size, slices of different lengths, parts of f32 sums in a slice
+    for k, n in ((200, 2000), (768, 333), (2048, 520), (2400, 128), (4096, 19000), (16384, 250)):
+        run(m, k, n, fmt, "silu", m % 2 == 0 and n < 9000, True, m % 3 == 0, k > 4096 or m % 5 == 0, True)
+
+
+@pytest.mark.parametrize("fmt", [MX, NV])
 @pytest.mark.parametrize("m,k,n", [(1, 300, 40), (20, 1000, 130), (140, 2048, 390), (520, 700, 512)])
 def test_whole_numbers_exactly(m, k, n, fmt):
     # Codes of whole numbers, scales 1 and 2: every sum is a whole number below 2^24.
