@@ -5,12 +5,14 @@
 //   nv   s = amax / 6 rounded to e4m3 (at most 448)
 // and every element is x / s rounded to the nearest e2m1 value, ties to the even code.
 //
-// Rounding is exact: the result is that of the real quotient.  By a power of two a product is exact.  An e4m3 scale
-// has at most 4 significant bits, a midpoint of two e2m1 values 3: x / s equals a midpoint t only if x = t s, 7 bits.
-// An f32 quotient rounded to nearest never moves from beside a midpoint onto it, since x differs from t s by an ulp of x
-// at least, half an ulp of t s or more.  A bf16 x (8 bits) differs from t s by 2^-8 of it at least, so a product with the
-// rounded reciprocal of s, itself rounded to 2^-13, is on the same side too, and on the midpoint where x / s is: one
-// fma and an addition instead of a division.  The same holds for amax / 6, whose midpoints have 5 bits.
+// Rounding is exact: the result is that of the real quotient.  By a power of two a product is exact.  An e4m3 scale has at
+// most 4 significant bits, a midpoint t of two e2m1 values 3, so t s is exact in f32.  q = x (1 / s) rounded to a multiple of 2^-13
+// (by adding and taking away a large number) is t if x / s is t, and on the same side of every t as x / s where it is not t.
+// Where it is t without x / s being t, the remainder x - q s, exact for q = t, tells: q + (x - q s) (1 / s) is x / s but
+// for 2^-38, and rounds to f32 beside t, since x differs from t s by an ulp of x at least, more than half an ulp of t s.  A
+// bf16 x (8 bits) differs from t s by 2^-8 of it at least: it needs no remainder.  Three instructions for two elements, and no
+// division.  amax / 6 is the f32 quotient to nearest (Markstein's correction of a product with the rounded reciprocal),
+// which never meets one of e4m3's midpoints (5 bits) from beside it, by the same argument.
 //
 // Bound by memory: one read of X, one write.  A lane takes eight elements of a row of the [rows][k] layout, a warp 256
 // columns of four rows 32 apart, which share the 16 contiguous bytes of an atom's scales.  The [k][rows] layout is
@@ -44,14 +46,15 @@ struct QuantizeParams {
 };
 
 // Eight e2m1 codes, the first in the lowest four bits; beyond 6 is 6.
-__device__ __forceinline__ uint32_t e2m1_codes(const float (&v)[8]) {
+__device__ __forceinline__ uint32_t e2m1_codes(const f32x2 (&v)[4]) {
+  const float2 a = pair_values(v[0]), b = pair_values(v[1]), c = pair_values(v[2]), d = pair_values(v[3]);
   uint32_t r;
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
       "mov.b32 %0, {a, b, c, d};\n\t}"
       : "=r"(r)
-      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y), "f"(d.x), "f"(d.y));
   return r;
 }
 __device__ __forceinline__ uint32_t e4m3_code(float v) {
@@ -79,48 +82,79 @@ constexpr uint32_t kInfinity = 0x7f800000u;
 // The scale's byte of a block whose largest magnitude has these bits; an infinity or a NaN in the block: NaN.
 template <bool kNv>
 __device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
-  if constexpr (kNv) return amax >= kInfinity ? 0x7fu : e4m3_code(__fdiv_rn(__uint_as_float(amax), 6.f));
+  if constexpr (kNv) {
+    constexpr float kSixth = 1.f / 6.f;
+    const float a = __uint_as_float(amax), q = a * kSixth;
+    return amax >= kInfinity ? 0x7fu : e4m3_code(fmaf(fmaf(-6.f, q, a), kSixth, q));
+  }
   else return amax >= kInfinity ? 0xffu : (uint32_t)max((int)(amax >> 23) - 2, 0);
 }
-// What an element is multiplied with (or divided by) before it is rounded.
-template <bool kNv, bool kDivide>
+// Elements over the scale, before they are rounded to e2m1.  kWide: of more than 8 significant bits.
+template <bool kNv, bool kWide>
 struct Scaler {
-  float f;
+  f32x2 inverse, minus_scale;
   // From the scale's byte.  A scale of 0 leaves codes of 0; behind a NaN scale the codes mean nothing.
   __device__ __forceinline__ explicit Scaler(uint32_t byte) {
     if constexpr (!kNv) {
-      f = byte == 0xffu ? 0.f : __uint_as_float((254u - byte) << 23);       // 2^(127 - byte)
+      inverse = pair_of(byte == 0xffu ? 0.f : __uint_as_float((254u - byte) << 23));       // 2^(127 - byte)
     } else {
       const float s = e4m3_value(byte);
-      const bool none = byte == 0u || byte == 0x7fu;
-      if constexpr (kDivide) f = none ? __uint_as_float(kInfinity) : s;
-      else f = none ? 0.f : __fdiv_rn(1.f, s);
+      inverse = pair_of(byte == 0u || byte == 0x7fu ? 0.f : fast_reciprocal(s));
+      minus_scale = pair_of(-s);
     }
   }
-  __device__ __forceinline__ float operator()(float x) const {
-    if constexpr (!kNv) return x * f;
-    if constexpr (kDivide) return __fdiv_rn(x, f);
+  __device__ __forceinline__ f32x2 operator()(f32x2 x) const {
+    if constexpr (!kNv) return mul2(x, inverse);
     constexpr float kSnap = 1536.f;      // sums with it are multiples of 2^-13
-    return fmaf(x, f, kSnap) - kSnap;
+    const f32x2 q = add2(fma2(x, inverse, pair_of(kSnap)), pair_of(-kSnap));
+    return kWide ? fma2(fma2(q, minus_scale, x), inverse, q) : q;
   }
 };
 
-// Eight elements of X, f32, times the tensor's factor; bits of the largest magnitude.
+// Eight elements of X.
 template <bool kF32>
-__device__ __forceinline__ void load_octet(const void* X, int64_t at, int64_t cols, int width, float (&v)[8]) {
-  if constexpr (kF32) {
-    const float* src = static_cast<const float*>(X) + at;
-    if (cols >= 8 && width >= 4) {
-      const float4 a = reinterpret_cast<const float4*>(src)[0], b = reinterpret_cast<const float4*>(src)[1];
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
+struct Octet {
+  uint4 w[kF32 ? 2 : 1];
+  __device__ __forceinline__ void load(const void* X, int64_t at, int64_t cols, int width) {
+    if constexpr (kF32) {
+      const float* src = static_cast<const float*>(X) + at;
+      if (cols >= 8 && width >= 4) {
+        w[0] = reinterpret_cast<const uint4*>(src)[0];
+        w[1] = reinterpret_cast<const uint4*>(src)[1];
+      } else {
+        uint32_t v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = e < cols ? src[e] : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = e < cols ? __float_as_uint(src[e]) : 0u;
+        w[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        w[1] = make_uint4(v[4], v[5], v[6], v[7]);
+      }
+    } else {
+      w[0] = cols > 0 ? load8_raw(static_cast<const uint16_t*>(X) + at, width, cols) : make_uint4(0u, 0u, 0u, 0u);
     }
-  } else {
-    const uint4 w = cols > 0 ? load8_raw(static_cast<const uint16_t*>(X) + at, width, cols) : make_uint4(0u, 0u, 0u, 0u);
-    unpack8(w, v);
   }
+  __device__ __forceinline__ void pairs(f32x2 (&v)[4]) const {
+    if constexpr (kF32) {
+      v[0] = pair_of(__uint_as_float(w[0].x), __uint_as_float(w[0].y));
+      v[1] = pair_of(__uint_as_float(w[0].z), __uint_as_float(w[0].w));
+      v[2] = pair_of(__uint_as_float(w[1].x), __uint_as_float(w[1].y));
+      v[3] = pair_of(__uint_as_float(w[1].z), __uint_as_float(w[1].w));
+    } else {
+      v[0] = pair_of(bf16_low(w[0].x), bf16_high(w[0].x));
+      v[1] = pair_of(bf16_low(w[0].y), bf16_high(w[0].y));
+      v[2] = pair_of(bf16_low(w[0].z), bf16_high(w[0].z));
+      v[3] = pair_of(bf16_low(w[0].w), bf16_high(w[0].w));
+    }
+  }
+  // Bits of the largest bf16 magnitude, as f32.
+  __device__ __forceinline__ uint32_t amax16() const {
+    const uint32_t m = 0x7fff7fffu;
+    const uint32_t a = __vmaxu2(__vmaxu2(w[0].x & m, w[0].y & m), __vmaxu2(w[0].z & m, w[0].w & m));
+    return max(a << 16, a & 0xffff0000u);
+  }
+};
+__device__ __forceinline__ uint32_t magnitude(f32x2 v) {
+  const float2 f = pair_values(v);
+  return max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu);
 }
 
 constexpr int kRowsAtOnce = 4;      // 32 apart: an atom's rows of the same 16 bytes
@@ -141,20 +175,26 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeParams
   const int64_t row0 = (atom_row - part * p.down) * kAtomRows + r32;      // inside the part
   const int64_t col = (int64_t)segment * 256 + lane * 8;
   const float mult = kMult ? *p.mult : 1.f;
-  float v[kRowsAtOnce][8];
+  Octet<kF32> x[kRowsAtOnce];
 #pragma unroll
   for (int i = 0; i < kRowsAtOnce; ++i) {
     const int64_t row = row0 + 32 * i;
-    load_octet<kF32>(p.X, (part * p.each + row) * p.k + col, row < p.each ? p.k - col : 0, p.width, v[i]);
+    x[i].load(p.X, (part * p.each + row) * p.k + col, row < p.each ? p.k - col : 0, p.width);
   }
   uint32_t words[kRowsAtOnce];
 #pragma unroll
   for (int i = 0; i < kRowsAtOnce; ++i) {
+    f32x2 v[4];
+    x[i].pairs(v);
     uint32_t amax = 0;
+    if constexpr (!kF32 && !kMult) {
+      amax = x[i].amax16();
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (kMult) v[i][e] = __fmul_rn(v[i][e], mult);
-      amax = max(amax, __float_as_uint(v[i][e]) & 0x7fffffffu);
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (kMult) v[j] = mul2(v[j], pair_of(mult));
+        amax = max(amax, magnitude(v[j]));
+      }
     }
 #pragma unroll
     for (int d = 1; d < kLanes; d <<= 1) amax = max(amax, __shfl_xor_sync(kFull, amax, d));
@@ -162,9 +202,9 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeParams
     const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
     const Scaler<kNv, kF32 || kMult> scaled(byte);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = scaled(v[i][e]);
+    for (int j = 0; j < 4; ++j) v[j] = scaled(v[j]);
     if (there || (row0 + 32 * i < p.each && col < 2 * p.pitch))
-      *reinterpret_cast<uint32_t*>(p.q + (part * p.each + row0 + 32 * i) * p.pitch + col / 2) = e2m1_codes(v[i]);
+      *reinterpret_cast<uint32_t*>(p.q + (part * p.each + row0 + 32 * i) * p.pitch + col / 2) = e2m1_codes(v);
     uint32_t word = byte << (8 * (lane / kLanes % 4));
     word |= __shfl_xor_sync(kFull, word, kLanes);
     words[i] = word | __shfl_xor_sync(kFull, word, 2 * kLanes);
@@ -195,42 +235,59 @@ __global__ void __launch_bounds__(kThreads) quantize_turned_kernel(const Quantiz
   const int64_t mine = row0 + 2 * lane;
   const int64_t left = p.each - mine;            // of this lane's rows that exist
   const int64_t at = part * p.each + mine;
-  float v[2][32];
+  f32x2 v[2][16];      // elements 2 i and 2 i + 1 of either row
   if (p.width >= 2) {
+    uint2 w[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const bool has = left > 0 && col + i < p.k;      // rows and parts are even: both rows exist or neither
+      w[i] = make_uint2(0u, 0u);
       if constexpr (kF32) {
-        const float2 w = has ? *reinterpret_cast<const float2*>(static_cast<const float*>(p.X) + (col + i) * rows + at) : make_float2(0.f, 0.f);
-        v[0][i] = w.x;
-        v[1][i] = w.y;
+        if (has) w[i] = *reinterpret_cast<const uint2*>(static_cast<const float*>(p.X) + (col + i) * rows + at);
       } else {
-        const uint32_t w = has ? *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.X) + (col + i) * rows + at) : 0u;
-        v[0][i] = bf16_low(w);
-        v[1][i] = bf16_high(w);
+        if (has) w[i].x = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.X) + (col + i) * rows + at);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if constexpr (kF32) {
+        v[0][i] = pair_of(__uint_as_float(w[2 * i].x), __uint_as_float(w[2 * i + 1].x));
+        v[1][i] = pair_of(__uint_as_float(w[2 * i].y), __uint_as_float(w[2 * i + 1].y));
+      } else {
+        v[0][i] = pair_of(bf16_low(w[2 * i].x), bf16_low(w[2 * i + 1].x));
+        v[1][i] = pair_of(bf16_high(w[2 * i].x), bf16_high(w[2 * i + 1].x));
       }
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
+    for (int h = 0; h < 2; ++h) {
+      uint32_t w[32];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int i = 0; i < 32; ++i) {
         const bool has = left > h && col + i < p.k;
-        if constexpr (kF32) v[h][i] = has ? static_cast<const float*>(p.X)[(col + i) * rows + at + h] : 0.f;
-        else v[h][i] = has ? bf16_value(static_cast<const uint16_t*>(p.X)[(col + i) * rows + at + h]) : 0.f;
+        w[i] = 0u;
+        if constexpr (kF32) {
+          if (has) w[i] = static_cast<const uint32_t*>(p.X)[(col + i) * rows + at + h];
+        } else {
+          if (has) w[i] = static_cast<const uint16_t*>(p.X)[(col + i) * rows + at + h];
+        }
       }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        v[h][i] = pair_of(__uint_as_float(w[2 * i] << (kF32 ? 0 : 16)), __uint_as_float(w[2 * i + 1] << (kF32 ? 0 : 16)));
+    }
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t codes[4];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
+      f32x2(&block)[kBlock / 2] = *reinterpret_cast<f32x2(*)[kBlock / 2]>(&v[h][b * kBlock / 2]);
       uint32_t amax = 0;
 #pragma unroll
-      for (int i = 0; i < kBlock; ++i) {
-        float& x = v[h][b * kBlock + i];
-        if constexpr (kMult) x = __fmul_rn(x, mult);
-        amax = max(amax, __float_as_uint(x) & 0x7fffffffu);
+      for (int i = 0; i < kBlock / 2; ++i) {
+        if constexpr (kMult) block[i] = mul2(block[i], pair_of(mult));
+        amax = max(amax, magnitude(block[i]));
       }
       const bool there = left > h && col + b * kBlock < p.k;
       const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
@@ -238,9 +295,9 @@ __global__ void __launch_bounds__(kThreads) quantize_turned_kernel(const Quantiz
       const Scaler<kNv, kF32 || kMult> scaled(byte);
 #pragma unroll
       for (int o = 0; o < kBlock / 8; ++o) {
-        float w[8];
+        f32x2 w[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = scaled(v[h][b * kBlock + o * 8 + e]);
+        for (int j = 0; j < 4; ++j) w[j] = scaled(block[4 * o + j]);
         codes[b * (kBlock / 8) + o] = e2m1_codes(w);
       }
     }

@@ -14,6 +14,7 @@
 // registers; the blocks' sums are joined by a second launch in the order of the blocks.  No atomics: the same sums in the
 // same order every time.
 #include <algorithm>
+#include <atomic>
 #include <initializer_list>
 #include <type_traits>
 
@@ -943,19 +944,26 @@ cudaError_t by_team(int64_t n, Go&& go) {
   return go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
 }
 
+// Blocks: as many as are resident together, each with its share of the rows.
+template <auto kKernel>
+cudaError_t octets_launch(const DeviceInfo& dev, const NormParams& p, int team, cudaStream_t s) {
+  const int threads = std::max(team, kBlockThreads), each = threads / team;
+  // Of a kernel on devices of one kind, which all are: asked once.
+  static std::atomic<int> resident{0};
+  int r = resident.load(std::memory_order_relaxed);
+  if (r == 0) {
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&r, kKernel, threads, 0);
+    if (e != cudaSuccess) return e;
+    resident.store(r = std::max(r, 1), std::memory_order_relaxed);
+  }
+  const int64_t blocks = std::min<int64_t>((p.m + each - 1) / each, (int64_t)dev.sms * r);
+  return launch_pdl(kKernel, dim3((unsigned)blocks), dim3(threads), 0, s, 1, p);
+}
+
 template <bool kF32, bool kRms>
 cudaError_t forward_launch(const DeviceInfo& dev, const NormParams& p, bool vec, cudaStream_t s) {
   const int n = p.n;
-  // Blocks: as many as are resident together, each with its share of the rows.
-  auto go = [&](auto kernel, int team) {
-    const int threads = std::max(team, kBlockThreads), each = threads / team;
-    int resident = 1;
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, 0);
-    if (e != cudaSuccess) return e;
-    const int64_t blocks = std::min<int64_t>((p.m + each - 1) / each, (int64_t)dev.sms * resident);
-    return launch_pdl(kernel, dim3((unsigned)blocks), dim3(threads), 0, s, 1, p);
-  };
-#define MORELLO_NORM(T, ITER) return go(norm_kernel<T, ITER, kF32, kRms>, T)
+#define MORELLO_NORM(T, ITER) return octets_launch<norm_kernel<T, ITER, kF32, kRms>>(dev, p, T, s)
   const int64_t beside = n > kRingColumns ? 0 : 4 * n;       // gamma and beta
   const RingShape ring = ring_shape(n, {kF32 ? 4 : 2}, beside);
   if (vec ? n > kRingColumns : ring.stages < 2)
