@@ -18,6 +18,7 @@
 // columns of four rows 32 apart, which share the 16 contiguous bytes of an atom's scales.  The [k][rows] layout is
 // turned in registers: a lane takes two rows and 32 elements of each, a warp reads 64 columns' pairs side by side.
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/morello.h"
 #include "fp4.h"
@@ -41,9 +42,12 @@ struct QuantizeParams {
   int64_t pitch;               // bytes of a row of q
   int down, across;            // atoms of a part
   int segments;                // 256-column pieces of a row
+  unsigned bands;              // groups of rows
   int width;                   // elements of X per access
-  int64_t items;
 };
+// Blocks are numbered without long divisions (which took half of all instructions): grid.x along X's contiguous direction,
+// the pieces of a row or (turned) the rows, grid.y across it (in turns, if more than 65,535).  The other way round the
+// DRAM sees 512 bytes of every row, and 8192 x 4096 took 22.7 instead of 21.3 us.
 
 // Eight e2m1 codes, the first in the lowest four bits; beyond 6 is 6.
 __device__ __forceinline__ uint32_t e2m1_codes(const f32x2 (&v)[4]) {
@@ -65,11 +69,6 @@ __device__ __forceinline__ uint32_t e4m3_code(float v) {
 __device__ __forceinline__ float f16_low(uint32_t h) {
   float f;
   asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %1;\n\tcvt.f32.f16 %0, l;\n\t}" : "=f"(f) : "r"(h));
-  return f;
-}
-__device__ __forceinline__ float f16_high(uint32_t h) {
-  float f;
-  asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %1;\n\tcvt.f32.f16 %0, u;\n\t}" : "=f"(f) : "r"(h));
   return f;
 }
 __device__ __forceinline__ float e4m3_value(uint32_t code) {
@@ -145,16 +144,21 @@ struct Octet {
       v[3] = pair_of(bf16_low(w[0].w), bf16_high(w[0].w));
     }
   }
-  // Bits of the largest bf16 magnitude, as f32.
-  __device__ __forceinline__ uint32_t amax16() const {
-    const uint32_t m = 0x7fff7fffu;
-    const uint32_t a = __vmaxu2(__vmaxu2(w[0].x & m, w[0].y & m), __vmaxu2(w[0].z & m, w[0].w & m));
-    return max(a << 16, a & 0xffff0000u);
+  // Bits of the largest magnitude, as f32: NaN above infinity above the numbers.
+  __device__ __forceinline__ uint32_t amax() const {
+    if constexpr (kF32) {
+      const uint32_t m = 0x7fffffffu;
+      return max(max(max(w[0].x & m, w[0].y & m), max(w[0].z & m, w[0].w & m)), max(max(w[1].x & m, w[1].y & m), max(w[1].z & m, w[1].w & m)));
+    } else {
+      const uint32_t m = 0x7fff7fffu;
+      const uint32_t a = __vmaxu2(__vmaxu2(w[0].x & m, w[0].y & m), __vmaxu2(w[0].z & m, w[0].w & m));
+      return max(a << 16, a & 0xffff0000u);
+    }
   }
 };
-__device__ __forceinline__ uint32_t magnitude(f32x2 v) {
-  const float2 f = pair_values(v);
-  return max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu);
+// The largest magnitude of a block's elements times the tensor's factor, from that of the elements: rounding keeps the order.
+__device__ __forceinline__ uint32_t times(uint32_t amax, float mult) {
+  return __float_as_uint(__uint_as_float(amax) * mult) & 0x7fffffffu;
 }
 
 constexpr int kRowsAtOnce = 4;      // 32 apart: an atom's rows of the same 16 bytes
@@ -163,156 +167,160 @@ template <bool kNv, bool kF32, bool kMult>
 __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeParams p) {
   constexpr int kLanes = kNv ? 2 : 4;            // of a block
   const int lane = threadIdx.x % 32;
-  const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
   pdl_wait();
   pdl_release();
-  if (item >= p.items) return;
-  const int r32 = (int)(item & 31);
-  const int64_t band = item >> 5;                // (part, atom down, segment)
-  const int segment = (int)(band % p.segments);
-  const int64_t atom_row = band / p.segments;    // part * down + atom
-  const int64_t part = atom_row / p.down;
-  const int64_t row0 = (atom_row - part * p.down) * kAtomRows + r32;      // inside the part
+  const int segment = (int)blockIdx.x;
   const int64_t col = (int64_t)segment * 256 + lane * 8;
   const float mult = kMult ? *p.mult : 1.f;
-  Octet<kF32> x[kRowsAtOnce];
+  for (unsigned band = blockIdx.y; band < p.bands; band += gridDim.y) {
+    const int r32 = (int)(band & 3u) * 8 + (int)threadIdx.x / 32;
+    const unsigned atom_row = band >> 2;     // part * down + atom
+    const unsigned part = p.parts > 1 ? atom_row / (unsigned)p.down : 0u;
+    const int64_t row0 = (int64_t)(atom_row - part * (unsigned)p.down) * kAtomRows + r32;      // inside the part
+    Octet<kF32> x[kRowsAtOnce];
 #pragma unroll
-  for (int i = 0; i < kRowsAtOnce; ++i) {
-    const int64_t row = row0 + 32 * i;
-    x[i].load(p.X, (part * p.each + row) * p.k + col, row < p.each ? p.k - col : 0, p.width);
-  }
-  uint32_t words[kRowsAtOnce];
-#pragma unroll
-  for (int i = 0; i < kRowsAtOnce; ++i) {
-    f32x2 v[4];
-    x[i].pairs(v);
-    uint32_t amax = 0;
-    if constexpr (!kF32 && !kMult) {
-      amax = x[i].amax16();
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (kMult) v[j] = mul2(v[j], pair_of(mult));
-        amax = max(amax, magnitude(v[j]));
-      }
+    for (int i = 0; i < kRowsAtOnce; ++i) {
+      const int64_t row = row0 + 32 * i;
+      x[i].load(p.X, (part * p.each + row) * p.k + col, row < p.each ? p.k - col : 0, p.width);
     }
+    uint32_t words[kRowsAtOnce];
 #pragma unroll
-    for (int d = 1; d < kLanes; d <<= 1) amax = max(amax, __shfl_xor_sync(kFull, amax, d));
-    const bool there = row0 + 32 * i < p.each && col / (kNv ? 16 : 32) * (kNv ? 16 : 32) < p.k;
-    const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
-    const Scaler<kNv, kF32 || kMult> scaled(byte);
+    for (int i = 0; i < kRowsAtOnce; ++i) {
+      f32x2 v[4];
+      x[i].pairs(v);
+      uint32_t amax = x[i].amax();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = scaled(v[j]);
-    if (there || (row0 + 32 * i < p.each && col < 2 * p.pitch))
-      *reinterpret_cast<uint32_t*>(p.q + (part * p.each + row0 + 32 * i) * p.pitch + col / 2) = e2m1_codes(v);
-    uint32_t word = byte << (8 * (lane / kLanes % 4));
-    word |= __shfl_xor_sync(kFull, word, kLanes);
-    words[i] = word | __shfl_xor_sync(kFull, word, 2 * kLanes);
+      for (int d = 1; d < kLanes; d <<= 1) amax = max(amax, __shfl_xor_sync(kFull, amax, d));
+      if constexpr (kMult) {
+        amax = times(amax, mult);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], pair_of(mult));
+      }
+      const bool there = row0 + 32 * i < p.each && col / (kNv ? 16 : 32) * (kNv ? 16 : 32) < p.k;
+      const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
+      const Scaler<kNv, kF32 || kMult> scaled(byte);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = scaled(v[j]);
+      if (there || (row0 + 32 * i < p.each && col < 2 * p.pitch))
+        *reinterpret_cast<uint32_t*>(p.q + (part * p.each + row0 + 32 * i) * p.pitch + col / 2) = e2m1_codes(v);
+      uint32_t word = byte << (8 * (lane / kLanes % 4));
+      word |= __shfl_xor_sync(kFull, word, kLanes);
+      words[i] = word | __shfl_xor_sync(kFull, word, 2 * kLanes);
+    }
+    const int across = segment * (kNv ? 4 : 2) + lane / (4 * kLanes);
+    if (lane % (4 * kLanes) == 0 && across < p.across)
+      *reinterpret_cast<uint4*>(p.scales + ((int64_t)atom_row * p.across + across) * kAtomBytes + r32 * 16) =
+          make_uint4(words[0], words[1], words[2], words[3]);
   }
-  const int across = segment * (kNv ? 4 : 2) + lane / (4 * kLanes);
-  if (lane % (4 * kLanes) == 0 && across < p.across)
-    *reinterpret_cast<uint4*>(p.scales + (atom_row * p.across + across) * kAtomBytes + r32 * 16) =
-        make_uint4(words[0], words[1], words[2], words[3]);
 }
 
-// X[k][rows]: a block turns 64 rows x 256 elements, a warp 32 elements of each.
-constexpr int kTurnRows = 64;
-template <bool kNv, bool kF32, bool kMult>
-__global__ void __launch_bounds__(kThreads) quantize_turned_kernel(const QuantizeParams p) {
+// X[k][rows]: a block turns 128 rows (f32: 32) x 256 elements, a warp 32 elements of each, a lane four neighbouring rows, which
+// it reads together (one): 256 (128) bytes of memory a warp and element.
+// kTogether: rows and parts are multiples of a lane's rows, and X aligned to them; f32 always.
+template <bool kNv, bool kF32, bool kMult, bool kTogether>
+__global__ void __launch_bounds__(kThreads, 2) quantize_turned_kernel(const QuantizeParams p) {
   constexpr int kBlocks = kNv ? 2 : 1;           // blocks of 32 elements
   constexpr int kBlock = 32 / kBlocks;
-  __shared__ __align__(16) uint8_t bytes[kTurnRows][16 + 4];   // rows 20 bytes apart: words of different rows in different banks
+  constexpr int kLaneRows = kF32 ? 1 : 4, kTile = 32 * kLaneRows, kWords = kNv ? 4 : 2;
+  using Word = std::conditional_t<kF32, uint32_t, uint16_t>;
+  __shared__ __align__(16) uint8_t bytes[kTile][16 + 4];   // rows 20 bytes apart: words of different rows in different banks
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  const int64_t halves = 2 * (int64_t)p.down;    // tiles of a part
-  const int64_t tile = (int64_t)blockIdx.x / p.segments;
-  const int segment = (int)((int64_t)blockIdx.x % p.segments);
-  const int64_t part = tile / halves, row0 = (tile - part * halves) * kTurnRows;      // inside the part
-  const int64_t col = (int64_t)segment * 256 + warp * 32;
+  const unsigned tiles = (unsigned)p.down * (kAtomRows / kTile);      // of a part
+  const unsigned part = p.parts > 1 ? blockIdx.x / tiles : 0u;
+  const int64_t row0 = (int64_t)(blockIdx.x - part * tiles) * kTile;      // inside the part
+  const int64_t left = p.each - row0 - kLaneRows * lane;                  // of this lane's rows that exist
+  const int64_t at = part * p.each + row0 + kLaneRows * lane, rows = p.each * p.parts;
   pdl_wait();
   pdl_release();
   const float mult = kMult ? *p.mult : 1.f;
-  const int64_t rows = p.each * p.parts;         // of X's rows of memory
-  const int64_t mine = row0 + 2 * lane;
-  const int64_t left = p.each - mine;            // of this lane's rows that exist
-  const int64_t at = part * p.each + mine;
-  f32x2 v[2][16];      // elements 2 i and 2 i + 1 of either row
-  if (p.width >= 2) {
-    uint2 w[32];
+#pragma unroll 1
+  for (int segment = (int)blockIdx.y; segment < p.segments; segment += (int)gridDim.y) {
+    const int64_t col = (int64_t)segment * 256 + warp * 32;
+    uint2 w[32];      // an element of the lane's rows
+    const int here = (int)min((int64_t)32, p.k - col);      // elements that exist
+    if constexpr (kTogether) {
+      const Word* src = static_cast<const Word*>(p.X) + col * rows + at;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const bool has = left > 0 && col + i < p.k;      // rows and parts are even: both rows exist or neither
-      w[i] = make_uint2(0u, 0u);
-      if constexpr (kF32) {
-        if (has) w[i] = *reinterpret_cast<const uint2*>(static_cast<const float*>(p.X) + (col + i) * rows + at);
-      } else {
-        if (has) w[i].x = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.X) + (col + i) * rows + at);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if constexpr (kF32) {
-        v[0][i] = pair_of(__uint_as_float(w[2 * i].x), __uint_as_float(w[2 * i + 1].x));
-        v[1][i] = pair_of(__uint_as_float(w[2 * i].y), __uint_as_float(w[2 * i + 1].y));
-      } else {
-        v[0][i] = pair_of(bf16_low(w[2 * i].x), bf16_low(w[2 * i + 1].x));
-        v[1][i] = pair_of(bf16_high(w[2 * i].x), bf16_high(w[2 * i + 1].x));
-      }
-    }
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t w[32];
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const bool has = left > h && col + i < p.k;
-        w[i] = 0u;
-        if constexpr (kF32) {
-          if (has) w[i] = static_cast<const uint32_t*>(p.X)[(col + i) * rows + at + h];
-        } else {
-          if (has) w[i] = static_cast<const uint16_t*>(p.X)[(col + i) * rows + at + h];
+      for (int i = 0; i < 32; ++i, src += rows) {
+        w[i] = make_uint2(0u, 0u);
+        if (left > 0 && i < here) {
+          if constexpr (kF32) w[i].x = *src;
+          else w[i] = *reinterpret_cast<const uint2*>(src);
         }
       }
+    } else {
+      static_assert(!kF32, "single rows");
+      // Single elements, the last row's and the last element's in place of those that are missing: loads without a condition.
+      const Word* src[kLaneRows];
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        v[h][i] = pair_of(__uint_as_float(w[2 * i] << (kF32 ? 0 : 16)), __uint_as_float(w[2 * i + 1] << (kF32 ? 0 : 16)));
+      for (int h = 0; h < kLaneRows; ++h)
+        src[h] = static_cast<const Word*>(p.X) + min(col, p.k - 1) * rows + part * p.each + min(row0 + kLaneRows * lane + h, p.each - 1);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        uint32_t e[kLaneRows];
+#pragma unroll
+        for (int h = 0; h < kLaneRows; ++h) {
+          e[h] = *src[h];
+          if (i + 1 < here) src[h] += rows;
+        }
+        w[i] = make_uint2(e[0] | e[1] << 16, e[2] | e[3] << 16);
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i >= here) w[i] = make_uint2(0u, 0u);
     }
-  }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint32_t codes[4];
+    // Bits of the largest magnitude of every row's blocks (bf16: two rows a word).
+    uint2 most[kBlocks];
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      f32x2(&block)[kBlock / 2] = *reinterpret_cast<f32x2(*)[kBlock / 2]>(&v[h][b * kBlock / 2]);
-      uint32_t amax = 0;
+      most[b] = make_uint2(0u, 0u);
 #pragma unroll
-      for (int i = 0; i < kBlock / 2; ++i) {
-        if constexpr (kMult) block[i] = mul2(block[i], pair_of(mult));
-        amax = max(amax, magnitude(block[i]));
-      }
-      const bool there = left > h && col + b * kBlock < p.k;
-      const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
-      bytes[2 * lane + h][warp * kBlocks + b] = (uint8_t)byte;
-      const Scaler<kNv, kF32 || kMult> scaled(byte);
-#pragma unroll
-      for (int o = 0; o < kBlock / 8; ++o) {
-        f32x2 w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = scaled(block[4 * o + j]);
-        codes[b * (kBlock / 8) + o] = e2m1_codes(w);
+      for (int i = b * kBlock; i < (b + 1) * kBlock; ++i) {
+        if constexpr (kF32) most[b].x = max(most[b].x, w[i].x & 0x7fffffffu);
+        else most[b] = make_uint2(__vmaxu2(most[b].x, w[i].x & 0x7fff7fffu), __vmaxu2(most[b].y, w[i].y & 0x7fff7fffu));
       }
     }
-    if (left > h && col < p.k)
-      *reinterpret_cast<uint4*>(p.q + (at + h) * p.pitch + col / 2) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
-  }
-  __syncthreads();
-  // The tile's scales, an atom's four bytes of a row at a time.
-  const int row = threadIdx.x % kTurnRows, word = threadIdx.x / kTurnRows;
-  const int across = segment * (kNv ? 4 : 2) + word;
-  if (word < (kNv ? 4 : 2) && across < p.across) {
-    const int64_t r = row0 + row;
-    const int64_t atom = part * p.down + r / kAtomRows;
-    *reinterpret_cast<uint32_t*>(p.scales + (atom * p.across + across) * kAtomBytes + (r % 32) * 16 + r % kAtomRows / 32 * 4) =
-        *reinterpret_cast<const uint32_t*>(&bytes[row][word * 4]);
+#pragma unroll
+    for (int h = 0; h < kLaneRows; ++h) {
+      auto value = [&](const uint2& word) {
+        if constexpr (kF32) return __uint_as_float(word.x);
+        else return h % 2 ? bf16_high(h < 2 ? word.x : word.y) : bf16_low(h < 2 ? word.x : word.y);
+      };
+      uint32_t codes[4];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        uint32_t amax = __float_as_uint(value(most[b]));
+        if constexpr (kMult) amax = times(amax, mult);
+        const bool there = left > h && col + b * kBlock < p.k;
+        const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
+        bytes[kLaneRows * lane + h][warp * kBlocks + b] = (uint8_t)byte;
+        const Scaler<kNv, kF32 || kMult> scaled(byte);
+#pragma unroll
+        for (int o = 0; o < kBlock / 8; ++o) {
+          f32x2 v[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = b * kBlock + 8 * o + 2 * j;
+            v[j] = pair_of(value(w[i]), value(w[i + 1]));
+            if constexpr (kMult) v[j] = mul2(v[j], pair_of(mult));
+            v[j] = scaled(v[j]);
+          }
+          codes[b * (kBlock / 8) + o] = e2m1_codes(v);
+        }
+      }
+      if (left > h && col < p.k)
+        *reinterpret_cast<uint4*>(p.q + (at + h) * p.pitch + col / 2) = make_uint4(codes[0], codes[1], codes[2], codes[3]);
+    }
+    __syncthreads();
+    // The tile's scales, an atom's four bytes of a row at a time.
+    for (int i = threadIdx.x; i < kTile * kWords; i += kThreads) {
+      const int row = i % kTile, word = i / kTile;
+      const int64_t r = row0 + row, atom = (int64_t)part * p.down + r / kAtomRows, across = (int64_t)segment * kWords + word;
+      if (across < p.across)
+        *reinterpret_cast<uint32_t*>(p.scales + (atom * p.across + across) * kAtomBytes + (r % 32) * 16 + r % kAtomRows / 32 * 4) =
+            *reinterpret_cast<const uint32_t*>(&bytes[row][word * 4]);
+    }
+    __syncthreads();      // before the next piece's bytes
   }
 }
 
@@ -322,67 +330,87 @@ struct DequantizeParams {
   const float* alpha;
   void* Y;
   int64_t rows, each, k, pitch;
-  int down, across, segments;
+  int down, across;
   int width;                   // elements of Y per access
-  int64_t items;
 };
+// Four codes (the low 16 bits) as bf16: their bytes out of tables of the eight magnitudes' upper and lower ones, and the signs.
+__device__ __forceinline__ void codes_to_bf16(uint32_t codes, uint32_t* lo, uint32_t* hi) {
+  const uint32_t pick = codes & 0x7777u;
+  const uint32_t upper = __byte_perm(0x3f3f3f00u, 0x40404040u, pick);      // of 0, 1/2, 1, 3/2 and 2, 3, 4, 6
+  const uint32_t lower = __byte_perm(0xc0800000u, 0xc0804000u, pick);
+  const uint32_t s = codes & 0x8888u;
+  *lo = __byte_perm(lower, upper, 0x5140) | (s & 0x8u) << 12 | (s & 0x80u) << 24;
+  *hi = __byte_perm(lower, upper, 0x7362) | (s & 0x800u) << 4 | (s & 0x8000u) << 16;
+}
+// a b, two bf16 at once, rounded to bf16 (e2m1 times a scale is exact).
+__device__ __forceinline__ uint32_t bf16_mul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 // A lane reads eight codes and their scale and writes eight values; a warp 256 columns of kRowsAtOnce rows.
 template <bool kNv, bool kF32>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const DequantizeParams p) {
   const int lane = threadIdx.x % 32;
-  const int64_t item = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  const int64_t col = (int64_t)blockIdx.x * 256 + lane * 8;
   pdl_wait();
   pdl_release();
-  if (item >= p.items) return;
-  const int64_t row0 = item / p.segments * kRowsAtOnce;
-  const int64_t col = (item % p.segments) * 256 + lane * 8;
   if (col >= p.k) return;
   const float alpha = p.alpha ? *p.alpha : 1.f;
-  const int block = (int)(col / (kNv ? 16 : 32));
-  uint32_t codes[kRowsAtOnce], byte[kRowsAtOnce];
+  for (int64_t row0 = ((int64_t)blockIdx.y * (kThreads / 32) + threadIdx.x / 32) * kRowsAtOnce; row0 < p.rows;
+       row0 += (int64_t)gridDim.y * (kThreads / 32) * kRowsAtOnce) {
+    const uint32_t part0 = p.each < p.rows ? (uint32_t)row0 / (uint32_t)p.each : 0u;
+    const int block = (int)(col / (kNv ? 16 : 32));
+    uint32_t codes[kRowsAtOnce], byte[kRowsAtOnce];
+    int64_t part = part0, r = row0 - part0 * p.each;
 #pragma unroll
-  for (int i = 0; i < kRowsAtOnce; ++i) {
-    const int64_t row = row0 + i;
-    codes[i] = byte[i] = 0u;
-    if (row < p.rows) {
-      codes[i] = *reinterpret_cast<const uint32_t*>(p.q + row * p.pitch + col / 2);
-      const int64_t part = row / p.each, r = row - part * p.each;
-      byte[i] = p.scales[((part * p.down + r / kAtomRows) * p.across + block / 4) * kAtomBytes + (r % 32) * 16 +
-                         r % kAtomRows / 32 * 4 + block % 4];
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kRowsAtOnce; ++i) {
-    const int64_t row = row0 + i;
-    if (row >= p.rows) return;
-    float s;
-    if constexpr (kNv) s = byte[i] == 0x7fu ? __uint_as_float(0x7fffffffu) : e4m3_value(byte[i]);
-    else s = byte[i] == 0xffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte[i] == 0u ? 0x400000u : byte[i] << 23);
-    uint32_t h[4];
-    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
-        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
-        : "r"(codes[i]));
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[2 * j] = f16_low(h[j]) * s * alpha;
-      v[2 * j + 1] = f16_high(h[j]) * s * alpha;
-    }
-    const int64_t at = row * p.k + col, left = p.k - col;
-    if constexpr (kF32) {
-      float* dst = static_cast<float*>(p.Y) + at;
-      if (left >= 8 && p.width >= 4) {
-        reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < left) dst[e] = v[e];
+    for (int i = 0; i < kRowsAtOnce; ++i) {
+      codes[i] = byte[i] = 0u;
+      if (row0 + i < p.rows) {
+        codes[i] = *reinterpret_cast<const uint32_t*>(p.q + (row0 + i) * p.pitch + col / 2);
+        byte[i] = p.scales[((part * p.down + r / kAtomRows) * p.across + block / 4) * kAtomBytes + (r % 32) * 16 +
+                           r % kAtomRows / 32 * 4 + block % 4];
       }
-    } else {
-      store8_raw(static_cast<uint16_t*>(p.Y) + at, p.width, left, pack8(v));
+      if (++r == p.each) {
+        r = 0;
+        ++part;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kRowsAtOnce; ++i) {
+      if (row0 + i >= p.rows) break;
+      float s;
+      if constexpr (kNv) s = byte[i] == 0x7fu ? __uint_as_float(0x7fffffffu) : e4m3_value(byte[i]);
+      else s = byte[i] == 0xffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte[i] == 0u ? 0x400000u : byte[i] << 23);
+      uint32_t w[4];
+      codes_to_bf16(codes[i], w, w + 1);
+      codes_to_bf16(codes[i] >> 16, w + 2, w + 3);
+      const uint32_t scale = bf16_pack(s, s);      // exact: at most 4 bits
+      const int64_t at = (row0 + i) * p.k + col, left = p.k - col;
+      if (!kF32 && !p.alpha) {
+        store8_raw(static_cast<uint16_t*>(p.Y) + at, p.width, left,
+                   make_uint4(bf16_mul2(w[0], scale), bf16_mul2(w[1], scale), bf16_mul2(w[2], scale), bf16_mul2(w[3], scale)));
+        continue;
+      }
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[2 * j] = bf16_low(w[j]) * s * alpha;
+        v[2 * j + 1] = bf16_high(w[j]) * s * alpha;
+      }
+      if constexpr (kF32) {
+        float* dst = static_cast<float*>(p.Y) + at;
+        if (left >= 8 && p.width >= 4) {
+          reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+          reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < left) dst[e] = v[e];
+        }
+      } else {
+        store8_raw(static_cast<uint16_t*>(p.Y) + at, p.width, left, pack8(v));
+      }
     }
   }
 }
@@ -390,6 +418,7 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const DequantizePa
 // --- host -----------------------------------------------------------------------------------
 
 constexpr int64_t kMaxExtent = (1ll << 31) - 1024;
+constexpr unsigned kMaxGridY = 65535;
 
 bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
@@ -412,10 +441,12 @@ int access_width_f32(int64_t cols, const void* p) {
 
 template <bool kNv, bool kF32, bool kMult>
 cudaError_t quantize_launch(const QuantizeParams& p, bool turned, cudaStream_t s) {
-  const int64_t blocks = turned ? p.parts * p.down * 2 * p.segments : (p.items + kThreads / 32 - 1) / (kThreads / 32);
-  if (blocks >= (1ll << 31)) return cudaErrorInvalidValue;
-  return turned ? launch_pdl(quantize_turned_kernel<kNv, kF32, kMult>, dim3((unsigned)blocks), dim3(kThreads), 0, s, 1, p)
-                : launch_pdl(quantize_kernel<kNv, kF32, kMult>, dim3((unsigned)blocks), dim3(kThreads), 0, s, 1, p);
+  const dim3 grid = turned ? dim3(p.bands, std::min((unsigned)p.segments, kMaxGridY)) : dim3((unsigned)p.segments, std::min(p.bands, kMaxGridY));
+  if (!turned) return launch_pdl(quantize_kernel<kNv, kF32, kMult>, grid, dim3(kThreads), 0, s, 1, p);
+  if constexpr (!kF32) {
+    if (p.width < 4) return launch_pdl(quantize_turned_kernel<kNv, false, kMult, false>, grid, dim3(kThreads), 0, s, 1, p);
+  }
+  return launch_pdl(quantize_turned_kernel<kNv, kF32, kMult, true>, grid, dim3(kThreads), 0, s, 1, p);
 }
 
 }  // namespace
@@ -459,11 +490,13 @@ int morello_fp4_quantize(int format, int x_type, int x_layout, int64_t rows, int
   p.pitch = fp4_pitch(k);
   p.down = (int)fp4_atoms_down(p.each);
   p.across = (int)fp4_atoms_across(nv, k);
+  const int64_t bands = parts * p.down * (turned ? (f32 ? 4 : 1) : 4);
+  if (bands >= (1ll << 31)) return MORELLO_ERR_INVALID_SHAPE;
   p.segments = (int)((k + 255) / 256);
-  // In the turned layout a lane's two rows are read together where every part begins on an even row.
-  const int64_t contiguous = turned ? (p.each % 2 == 0 ? rows : 1) : k;
+  p.bands = (unsigned)bands;
+  // In the turned layout a lane's rows are read together where every part begins at a multiple of them.
+  const int64_t contiguous = turned ? (p.each % 4 == 0 ? rows : 1) : k;
   p.width = f32 ? access_width_f32(contiguous, X) : access_width(contiguous, X);
-  p.items = parts * p.down * 32 * p.segments;
   cudaError_t e;
   switch (nv * 4 + f32 * 2 + (mult ? 1 : 0)) {
     case 0: e = quantize_launch<false, false, false>(p, turned, s); break;
@@ -502,12 +535,9 @@ int morello_fp4_dequantize(int format, int y_type, int64_t rows, int64_t parts, 
   p.pitch = fp4_pitch(k);
   p.down = (int)fp4_atoms_down(p.each);
   p.across = (int)fp4_atoms_across(nv, k);
-  p.segments = (int)((k + 255) / 256);
   p.width = f32 ? access_width_f32(k, Y) : access_width(k, Y);
-  p.items = (rows + kRowsAtOnce - 1) / kRowsAtOnce * p.segments;
-  const int64_t blocks = (p.items + kThreads / 32 - 1) / (kThreads / 32);
-  if (blocks >= (1ll << 31)) return MORELLO_ERR_INVALID_SHAPE;
-  const dim3 grid((unsigned)blocks), block(kThreads);
+  const int64_t each = kRowsAtOnce * (kThreads / 32);
+  const dim3 grid((unsigned)((k + 255) / 256), (unsigned)std::min<int64_t>((rows + each - 1) / each, kMaxGridY)), block(kThreads);
   cudaError_t e;
   if (nv) e = f32 ? launch_pdl(dequantize_kernel<true, true>, grid, block, 0, s, 1, p) : launch_pdl(dequantize_kernel<true, false>, grid, block, 0, s, 1, p);
   else e = f32 ? launch_pdl(dequantize_kernel<false, true>, grid, block, 0, s, 1, p) : launch_pdl(dequantize_kernel<false, false>, grid, block, 0, s, 1, p);
