@@ -436,6 +436,11 @@ cudaError_t launch_form(const DeviceInfo& dev, const Fp4Call& c, Fp4Params p, cu
   using S = Shape<kPair, kTileN, kNv>;
   static PerDeviceOnce once;
   cudaError_t e = once.run_current([] {
+    // A launch with fewer registers than its warpgroups end up with would wait for them for good.
+    cudaFuncAttributes attr{};
+    const cudaError_t got = cudaFuncGetAttributes(&attr, fp4_tile_kernel<kPair, kTileN, kGated, kNv>);
+    if (got != cudaSuccess) return got;
+    if (attr.numRegs * kThreads < 128 * kFewRegisters + 32 * kEpiWarps * kManyRegisters) return cudaErrorInvalidConfiguration;
     return cudaFuncSetAttribute(fp4_tile_kernel<kPair, kTileN, kGated, kNv>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 (int)S::kSmemBytes);
   });

@@ -242,7 +242,7 @@ __device__ __forceinline__ float join_parts(const Part* parts, float inv_n, floa
   }
   *base = m0;
   *off = shift;
-  return squares * inv_n;
+  return squares < 0.f ? 0.f : squares * inv_n;      // what rounding leaves of a row of one value
 }
 
 // d = x - mean of eight columns: their sum and their squares.
@@ -787,7 +787,8 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormParam
       squares = fmaf(d, d, squares);
     }
     if constexpr (!kRms) shift = block_sum(off, shared) * p.inv_n;
-    const float square = block_sum(squares, shared) * p.inv_n - shift * shift;
+    float square = block_sum(squares, shared) * p.inv_n - shift * shift;
+    if (square < 0.f) square = 0.f;
     const float rstd = rsqrtf(square + p.eps);
     if (threadIdx.x == 0) {
       if (!kRms && p.mean) p.mean[row] = base + shift;
