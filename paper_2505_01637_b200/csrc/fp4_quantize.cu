@@ -14,9 +14,11 @@
 // division.  amax / 6 is the f32 quotient to nearest (Markstein's correction of a product with the rounded reciprocal),
 // which never meets one of e4m3's midpoints (5 bits) from beside it, by the same argument.
 //
-// Bound by memory: one read of X, one write.  A lane takes eight elements of a row of the [rows][k] layout, a warp 256
-// columns of four rows 32 apart, which share the 16 contiguous bytes of an atom's scales.  The [k][rows] layout is
-// turned in registers: a lane takes two rows and 32 elements of each, a warp reads 64 columns' pairs side by side.
+// One read of X, one write: bound by memory once few enough instructions are spent on an element.  A lane takes 16 elements
+// of a row of the [rows][k] layout, a warp 512 columns of four rows 32 apart, which share the 16 contiguous bytes of an
+// atom's scales: a maximum and a scale a lane.  8192 x 4096 from bf16 16.8 us (nv) and 16.4 (mx), from f32 25.1; eight elements
+// a lane, 16 instructions an element, took 21.3.  The [k][rows] layout is turned in registers: a lane takes 32 elements of
+// four rows (f32: of one), a warp reads its lanes' rows side by side; 25 us, f32 40.  Reading back to bf16 takes 14.8 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -41,13 +43,13 @@ struct QuantizeParams {
   int64_t each, parts, k;      // rows of a part
   int64_t pitch;               // bytes of a row of q
   int down, across;            // atoms of a part
-  int segments;                // 256-column pieces of a row
+  int segments;                // turned: 256-element pieces of a row
   unsigned bands;              // groups of rows
   int width;                   // elements of X per access
 };
 // Blocks are numbered without long divisions (which took half of all instructions): grid.x along X's contiguous direction,
 // the pieces of a row or (turned) the rows, grid.y across it (in turns, if more than 65,535).  The other way round the
-// DRAM sees 512 bytes of every row, and 8192 x 4096 took 22.7 instead of 21.3 us.
+// DRAM sees 512 bytes of every row, and 8192 x 4096 took 1.4 us more.
 
 // Eight e2m1 codes, the first in the lowest four bits; beyond 6 is 6.
 __device__ __forceinline__ uint32_t e2m1_codes(const f32x2 (&v)[4]) {
@@ -69,6 +71,11 @@ __device__ __forceinline__ uint32_t e4m3_code(float v) {
 __device__ __forceinline__ float f16_low(uint32_t h) {
   float f;
   asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %1;\n\tcvt.f32.f16 %0, l;\n\t}" : "=f"(f) : "r"(h));
+  return f;
+}
+__device__ __forceinline__ float f16_high(uint32_t h) {
+  float f;
+  asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %1;\n\tcvt.f32.f16 %0, u;\n\t}" : "=f"(f) : "r"(h));
   return f;
 }
 __device__ __forceinline__ float e4m3_value(uint32_t code) {
@@ -110,48 +117,56 @@ struct Scaler {
   }
 };
 
-// Eight elements of X.
+// The larger of two pairs of 16-bit numbers.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Sixteen elements of X.
 template <bool kF32>
-struct Octet {
-  uint4 w[kF32 ? 2 : 1];
+struct Sixteen {
+  uint32_t w[kF32 ? 16 : 8];
   __device__ __forceinline__ void load(const void* X, int64_t at, int64_t cols, int width) {
+    auto put = [&](int i, const uint4& v) {
+      w[4 * i] = v.x;
+      w[4 * i + 1] = v.y;
+      w[4 * i + 2] = v.z;
+      w[4 * i + 3] = v.w;
+    };
     if constexpr (kF32) {
       const float* src = static_cast<const float*>(X) + at;
-      if (cols >= 8 && width >= 4) {
-        w[0] = reinterpret_cast<const uint4*>(src)[0];
-        w[1] = reinterpret_cast<const uint4*>(src)[1];
-      } else {
-        uint32_t v[8];
+      if (cols >= 16 && width >= 4) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = e < cols ? __float_as_uint(src[e]) : 0u;
-        w[0] = make_uint4(v[0], v[1], v[2], v[3]);
-        w[1] = make_uint4(v[4], v[5], v[6], v[7]);
+        for (int i = 0; i < 4; ++i) put(i, reinterpret_cast<const uint4*>(src)[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = e < cols ? __float_as_uint(src[e]) : 0u;
       }
     } else {
-      w[0] = cols > 0 ? load8_raw(static_cast<const uint16_t*>(X) + at, width, cols) : make_uint4(0u, 0u, 0u, 0u);
+      const uint16_t* src = static_cast<const uint16_t*>(X) + at;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) put(i, cols > 8 * i ? load8_raw(src + 8 * i, width, cols - 8 * i) : make_uint4(0u, 0u, 0u, 0u));
     }
   }
-  __device__ __forceinline__ void pairs(f32x2 (&v)[4]) const {
-    if constexpr (kF32) {
-      v[0] = pair_of(__uint_as_float(w[0].x), __uint_as_float(w[0].y));
-      v[1] = pair_of(__uint_as_float(w[0].z), __uint_as_float(w[0].w));
-      v[2] = pair_of(__uint_as_float(w[1].x), __uint_as_float(w[1].y));
-      v[3] = pair_of(__uint_as_float(w[1].z), __uint_as_float(w[1].w));
-    } else {
-      v[0] = pair_of(bf16_low(w[0].x), bf16_high(w[0].x));
-      v[1] = pair_of(bf16_low(w[0].y), bf16_high(w[0].y));
-      v[2] = pair_of(bf16_low(w[0].z), bf16_high(w[0].z));
-      v[3] = pair_of(bf16_low(w[0].w), bf16_high(w[0].w));
+  // Elements 8 i on.
+  __device__ __forceinline__ void pairs(int i, f32x2 (&v)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (kF32) v[j] = pair_of(__uint_as_float(w[8 * i + 2 * j]), __uint_as_float(w[8 * i + 2 * j + 1]));
+      else v[j] = pair_of(bf16_low(w[4 * i + j]), bf16_high(w[4 * i + j]));
     }
   }
   // Bits of the largest magnitude, as f32: NaN above infinity above the numbers.
   __device__ __forceinline__ uint32_t amax() const {
+    uint32_t a = 0;
     if constexpr (kF32) {
-      const uint32_t m = 0x7fffffffu;
-      return max(max(max(w[0].x & m, w[0].y & m), max(w[0].z & m, w[0].w & m)), max(max(w[1].x & m, w[1].y & m), max(w[1].z & m, w[1].w & m)));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a = max(a, w[i] & 0x7fffffffu);
+      return a;
     } else {
-      const uint32_t m = 0x7fff7fffu;
-      const uint32_t a = __vmaxu2(__vmaxu2(w[0].x & m, w[0].y & m), __vmaxu2(w[0].z & m, w[0].w & m));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a = max_u16x2(a, w[i] & 0x7fff7fffu);
       return max(a << 16, a & 0xffff0000u);
     }
   }
@@ -161,55 +176,65 @@ __device__ __forceinline__ uint32_t times(uint32_t amax, float mult) {
   return __float_as_uint(__uint_as_float(amax) * mult) & 0x7fffffffu;
 }
 
-constexpr int kRowsAtOnce = 4;      // 32 apart: an atom's rows of the same 16 bytes
+// Where a warp of the [rows][k] layout works: band 4 (part * down + atom) + eighth, 16 columns a lane, rows 32 apart.
+constexpr int kRowsAtOnce = 4;      // an atom's rows of the same 16 bytes
+constexpr int kWarpColumns = 512;   // of the quantisation
+constexpr int kReadColumns = 256;   // of reading back
+struct Band {
+  unsigned atom_row;
+  int r32;
+  int64_t part_row, row0;      // the part's first row, and the warp's first inside it
+  __device__ __forceinline__ Band(unsigned band, unsigned down, int64_t parts, int64_t each) {
+    r32 = (int)(band & 3u) * 8 + (int)threadIdx.x / 32;
+    atom_row = band >> 2;
+    const unsigned part = parts > 1 ? atom_row / down : 0u;
+    part_row = part * each;
+    row0 = (int64_t)(atom_row - part * down) * kAtomRows + r32;
+  }
+};
 
 template <bool kNv, bool kF32, bool kMult>
 __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeParams p) {
-  constexpr int kLanes = kNv ? 2 : 4;            // of a block
+  constexpr int kLanes = kNv ? 1 : 2, kBlock = 16 * kLanes;            // lanes of a block, its elements
   const int lane = threadIdx.x % 32;
   pdl_wait();
   pdl_release();
-  const int segment = (int)blockIdx.x;
-  const int64_t col = (int64_t)segment * 256 + lane * 8;
+  const int64_t col = (int64_t)blockIdx.x * kWarpColumns + lane * 16;
+  const int64_t across = (int64_t)blockIdx.x * (kWarpColumns / (4 * kBlock)) + lane / (4 * kLanes);
   const float mult = kMult ? *p.mult : 1.f;
   for (unsigned band = blockIdx.y; band < p.bands; band += gridDim.y) {
-    const int r32 = (int)(band & 3u) * 8 + (int)threadIdx.x / 32;
-    const unsigned atom_row = band >> 2;     // part * down + atom
-    const unsigned part = p.parts > 1 ? atom_row / (unsigned)p.down : 0u;
-    const int64_t row0 = (int64_t)(atom_row - part * (unsigned)p.down) * kAtomRows + r32;      // inside the part
-    Octet<kF32> x[kRowsAtOnce];
+    const Band at(band, (unsigned)p.down, p.parts, p.each);
+    Sixteen<kF32> x[kRowsAtOnce];
+    const int64_t first = at.part_row + at.row0;
 #pragma unroll
-    for (int i = 0; i < kRowsAtOnce; ++i) {
-      const int64_t row = row0 + 32 * i;
-      x[i].load(p.X, (part * p.each + row) * p.k + col, row < p.each ? p.k - col : 0, p.width);
-    }
+    for (int i = 0; i < kRowsAtOnce; ++i)
+      x[i].load(p.X, (first + 32 * i) * p.k + col, at.row0 + 32 * i < p.each ? p.k - col : 0, p.width);
     uint32_t words[kRowsAtOnce];
+    uint8_t* q = p.q + first * p.pitch + col / 2;
 #pragma unroll
     for (int i = 0; i < kRowsAtOnce; ++i) {
-      f32x2 v[4];
-      x[i].pairs(v);
       uint32_t amax = x[i].amax();
-#pragma unroll
-      for (int d = 1; d < kLanes; d <<= 1) amax = max(amax, __shfl_xor_sync(kFull, amax, d));
-      if constexpr (kMult) {
-        amax = times(amax, mult);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], pair_of(mult));
-      }
-      const bool there = row0 + 32 * i < p.each && col / (kNv ? 16 : 32) * (kNv ? 16 : 32) < p.k;
+      if constexpr (kLanes > 1) amax = max(amax, __shfl_xor_sync(kFull, amax, 1));
+      if constexpr (kMult) amax = times(amax, mult);
+      const bool row = at.row0 + 32 * i < p.each, there = row && col / kBlock * kBlock < p.k;
       const uint32_t byte = there ? scale_byte<kNv>(amax) : 0u;
       const Scaler<kNv, kF32 || kMult> scaled(byte);
+      uint32_t codes[2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = scaled(v[j]);
-      if (there || (row0 + 32 * i < p.each && col < 2 * p.pitch))
-        *reinterpret_cast<uint32_t*>(p.q + (part * p.each + row0 + 32 * i) * p.pitch + col / 2) = e2m1_codes(v);
+      for (int h = 0; h < 2; ++h) {
+        f32x2 v[4];
+        x[i].pairs(h, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = scaled(kMult ? mul2(v[j], pair_of(mult)) : v[j]);
+        codes[h] = e2m1_codes(v);
+      }
+      if (row && col < 2 * p.pitch) *reinterpret_cast<uint2*>(q + 32 * i * p.pitch) = make_uint2(codes[0], codes[1]);
       uint32_t word = byte << (8 * (lane / kLanes % 4));
       word |= __shfl_xor_sync(kFull, word, kLanes);
       words[i] = word | __shfl_xor_sync(kFull, word, 2 * kLanes);
     }
-    const int across = segment * (kNv ? 4 : 2) + lane / (4 * kLanes);
     if (lane % (4 * kLanes) == 0 && across < p.across)
-      *reinterpret_cast<uint4*>(p.scales + ((int64_t)atom_row * p.across + across) * kAtomBytes + r32 * 16) =
+      *reinterpret_cast<uint4*>(p.scales + ((int64_t)at.atom_row * p.across + across) * kAtomBytes + at.r32 * 16) =
           make_uint4(words[0], words[1], words[2], words[3]);
   }
 }
@@ -277,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, 2) quantize_turned_kernel(const Quan
 #pragma unroll
       for (int i = b * kBlock; i < (b + 1) * kBlock; ++i) {
         if constexpr (kF32) most[b].x = max(most[b].x, w[i].x & 0x7fffffffu);
-        else most[b] = make_uint2(__vmaxu2(most[b].x, w[i].x & 0x7fff7fffu), __vmaxu2(most[b].y, w[i].y & 0x7fff7fffu));
+        else most[b] = make_uint2(max_u16x2(most[b].x, w[i].x & 0x7fff7fffu), max_u16x2(most[b].y, w[i].y & 0x7fff7fffu));
       }
     }
 #pragma unroll
@@ -329,87 +354,73 @@ struct DequantizeParams {
   const uint8_t* scales;
   const float* alpha;
   void* Y;
-  int64_t rows, each, k, pitch;
+  int64_t each, parts, k, pitch;
   int down, across;
+  unsigned bands;
   int width;                   // elements of Y per access
 };
-// Four codes (the low 16 bits) as bf16: their bytes out of tables of the eight magnitudes' upper and lower ones, and the signs.
-__device__ __forceinline__ void codes_to_bf16(uint32_t codes, uint32_t* lo, uint32_t* hi) {
-  const uint32_t pick = codes & 0x7777u;
-  const uint32_t upper = __byte_perm(0x3f3f3f00u, 0x40404040u, pick);      // of 0, 1/2, 1, 3/2 and 2, 3, 4, 6
-  const uint32_t lower = __byte_perm(0xc0800000u, 0xc0804000u, pick);
-  const uint32_t s = codes & 0x8888u;
-  *lo = __byte_perm(lower, upper, 0x5140) | (s & 0x8u) << 12 | (s & 0x80u) << 24;
-  *hi = __byte_perm(lower, upper, 0x7362) | (s & 0x800u) << 4 | (s & 0x8000u) << 16;
+// Eight codes times a scale.
+__device__ __forceinline__ void codes_times(uint32_t codes, f32x2 scale, f32x2 (&v)[4]) {
+  uint32_t h[4];
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+      : "r"(codes));
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = mul2(pair_of(f16_low(h[j]), f16_high(h[j])), scale);
 }
-// a b, two bf16 at once, rounded to bf16 (e2m1 times a scale is exact).
-__device__ __forceinline__ uint32_t bf16_mul2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// A lane reads eight codes and their scale and writes eight values; a warp 256 columns of kRowsAtOnce rows.
+// A lane takes eight elements of each of its rows, so that a warp's stores are contiguous (sixteen a lane, as in the
+// quantisation, leave half of every line to a second store: 22.1 us for 8192 x 4096 where this takes 14.8).
 template <bool kNv, bool kF32>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const DequantizeParams p) {
+  constexpr int kBlock = kNv ? 16 : 32;
   const int lane = threadIdx.x % 32;
-  const int64_t col = (int64_t)blockIdx.x * 256 + lane * 8;
+  const int64_t col = (int64_t)blockIdx.x * kReadColumns + lane * 8, left = p.k - col;
   pdl_wait();
   pdl_release();
-  if (col >= p.k) return;
+  if (left <= 0) return;
   const float alpha = p.alpha ? *p.alpha : 1.f;
-  for (int64_t row0 = ((int64_t)blockIdx.y * (kThreads / 32) + threadIdx.x / 32) * kRowsAtOnce; row0 < p.rows;
-       row0 += (int64_t)gridDim.y * (kThreads / 32) * kRowsAtOnce) {
-    const uint32_t part0 = p.each < p.rows ? (uint32_t)row0 / (uint32_t)p.each : 0u;
-    const int block = (int)(col / (kNv ? 16 : 32));
-    uint32_t codes[kRowsAtOnce], byte[kRowsAtOnce];
-    int64_t part = part0, r = row0 - part0 * p.each;
+  const unsigned block = (unsigned)(col / kBlock);
+  for (unsigned band = blockIdx.y; band < p.bands; band += gridDim.y) {
+    const Band at(band, (unsigned)p.down, p.parts, p.each);
+    const int64_t first = at.part_row + at.row0, here = p.each - at.row0;
+    if (here <= 0) continue;
+    const uint4 scales = *reinterpret_cast<const uint4*>(p.scales + ((int64_t)at.atom_row * p.across + block / 4) * kAtomBytes + at.r32 * 16);
+    const uint32_t words[kRowsAtOnce] = {scales.x, scales.y, scales.z, scales.w};
+    const uint8_t* q = p.q + first * p.pitch + col / 2;
+    uint32_t codes[kRowsAtOnce];
+#pragma unroll
+    for (int i = 0; i < kRowsAtOnce; ++i) codes[i] = 32 * i < here ? *reinterpret_cast<const uint32_t*>(q + 32 * i * p.pitch) : 0u;
 #pragma unroll
     for (int i = 0; i < kRowsAtOnce; ++i) {
-      codes[i] = byte[i] = 0u;
-      if (row0 + i < p.rows) {
-        codes[i] = *reinterpret_cast<const uint32_t*>(p.q + (row0 + i) * p.pitch + col / 2);
-        byte[i] = p.scales[((part * p.down + r / kAtomRows) * p.across + block / 4) * kAtomBytes + (r % 32) * 16 +
-                           r % kAtomRows / 32 * 4 + block % 4];
-      }
-      if (++r == p.each) {
-        r = 0;
-        ++part;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kRowsAtOnce; ++i) {
-      if (row0 + i >= p.rows) break;
+      if (32 * i >= here) break;
+      const uint32_t byte = words[i] >> (8 * (block & 3)) & 0xffu;
       float s;
-      if constexpr (kNv) s = byte[i] == 0x7fu ? __uint_as_float(0x7fffffffu) : e4m3_value(byte[i]);
-      else s = byte[i] == 0xffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte[i] == 0u ? 0x400000u : byte[i] << 23);
-      uint32_t w[4];
-      codes_to_bf16(codes[i], w, w + 1);
-      codes_to_bf16(codes[i] >> 16, w + 2, w + 3);
-      const uint32_t scale = bf16_pack(s, s);      // exact: at most 4 bits
-      const int64_t at = (row0 + i) * p.k + col, left = p.k - col;
-      if (!kF32 && !p.alpha) {
-        store8_raw(static_cast<uint16_t*>(p.Y) + at, p.width, left,
-                   make_uint4(bf16_mul2(w[0], scale), bf16_mul2(w[1], scale), bf16_mul2(w[2], scale), bf16_mul2(w[3], scale)));
-        continue;
-      }
-      float v[8];
+      if constexpr (kNv) s = byte == 0x7fu ? __uint_as_float(0x7fffffffu) : e4m3_value(byte);
+      else s = byte == 0xffu ? __uint_as_float(0x7fffffffu) : __uint_as_float(byte == 0u ? 0x400000u : byte << 23);
+      f32x2 v[4];
+      codes_times(codes[i], pair_of(s), v);
+      if (p.alpha) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[2 * j] = bf16_low(w[j]) * s * alpha;
-        v[2 * j + 1] = bf16_high(w[j]) * s * alpha;
+        for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], pair_of(alpha));
       }
+      const float2 a = pair_values(v[0]), b = pair_values(v[1]), c = pair_values(v[2]), d = pair_values(v[3]);
+      const int64_t to = (first + 32 * i) * p.k + col;
       if constexpr (kF32) {
-        float* dst = static_cast<float*>(p.Y) + at;
+        float* dst = static_cast<float*>(p.Y) + to;
         if (left >= 8 && p.width >= 4) {
-          reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
-          reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+          reinterpret_cast<float4*>(dst)[0] = make_float4(a.x, a.y, b.x, b.y);
+          reinterpret_cast<float4*>(dst)[1] = make_float4(c.x, c.y, d.x, d.y);
         } else {
+          const float single[8] = {a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (e < left) dst[e] = v[e];
+            if (e < left) dst[e] = single[e];
         }
       } else {
-        store8_raw(static_cast<uint16_t*>(p.Y) + at, p.width, left, pack8(v));
+        store8_raw(static_cast<uint16_t*>(p.Y) + to, p.width, left,
+                   make_uint4(bf16_pack(a.x, a.y), bf16_pack(b.x, b.y), bf16_pack(c.x, c.y), bf16_pack(d.x, d.y)));
       }
     }
   }
@@ -441,7 +452,7 @@ int access_width_f32(int64_t cols, const void* p) {
 
 template <bool kNv, bool kF32, bool kMult>
 cudaError_t quantize_launch(const QuantizeParams& p, bool turned, cudaStream_t s) {
-  const dim3 grid = turned ? dim3(p.bands, std::min((unsigned)p.segments, kMaxGridY)) : dim3((unsigned)p.segments, std::min(p.bands, kMaxGridY));
+  const dim3 grid = turned ? dim3(p.bands, std::min((unsigned)p.segments, kMaxGridY)) : dim3((unsigned)((p.k + kWarpColumns - 1) / kWarpColumns), std::min(p.bands, kMaxGridY));
   if (!turned) return launch_pdl(quantize_kernel<kNv, kF32, kMult>, grid, dim3(kThreads), 0, s, 1, p);
   if constexpr (!kF32) {
     if (p.width < 4) return launch_pdl(quantize_turned_kernel<kNv, false, kMult, false>, grid, dim3(kThreads), 0, s, 1, p);
@@ -529,15 +540,17 @@ int morello_fp4_dequantize(int format, int y_type, int64_t rows, int64_t parts, 
   p.scales = static_cast<const uint8_t*>(scales);
   p.alpha = alpha;
   p.Y = Y;
-  p.rows = rows;
   p.each = rows / parts;
+  p.parts = parts;
   p.k = k;
   p.pitch = fp4_pitch(k);
   p.down = (int)fp4_atoms_down(p.each);
   p.across = (int)fp4_atoms_across(nv, k);
+  const int64_t bands = parts * p.down * 4;
+  if (bands >= (1ll << 31)) return MORELLO_ERR_INVALID_SHAPE;
+  p.bands = (unsigned)bands;
   p.width = f32 ? access_width_f32(k, Y) : access_width(k, Y);
-  const int64_t each = kRowsAtOnce * (kThreads / 32);
-  const dim3 grid((unsigned)((k + 255) / 256), (unsigned)std::min<int64_t>((rows + each - 1) / each, kMaxGridY)), block(kThreads);
+  const dim3 grid((unsigned)((k + kReadColumns - 1) / kReadColumns), std::min(p.bands, kMaxGridY)), block(kThreads);
   cudaError_t e;
   if (nv) e = f32 ? launch_pdl(dequantize_kernel<true, true>, grid, block, 0, s, 1, p) : launch_pdl(dequantize_kernel<true, false>, grid, block, 0, s, 1, p);
   else e = f32 ? launch_pdl(dequantize_kernel<false, true>, grid, block, 0, s, 1, p) : launch_pdl(dequantize_kernel<false, false>, grid, block, 0, s, 1, p);
