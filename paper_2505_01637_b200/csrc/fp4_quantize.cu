@@ -18,7 +18,7 @@
 // of a row of the [rows][k] layout, a warp 512 columns of four rows 32 apart, which share the 16 contiguous bytes of an
 // atom's scales: a maximum and a scale a lane.  8192 x 4096 from bf16 16.8 us (nv) and 16.4 (mx), from f32 25.1; eight elements
 // a lane, 16 instructions an element, took 21.3.  The [k][rows] layout is turned in registers: a lane takes 32 elements of
-// four rows (f32: of one), a warp reads its lanes' rows side by side; 25 us, f32 40.  Reading back to bf16 takes 14.8 us.
+// four rows (f32: of one), a warp reads its lanes' rows side by side; 19 us, f32 24.5.  Reading back to bf16 takes 14.8 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeParams
 // it reads together (one): 256 (128) bytes of memory a warp and element.
 // kTogether: rows and parts are multiples of a lane's rows, and X aligned to them; f32 always.
 template <bool kNv, bool kF32, bool kMult, bool kTogether>
-__global__ void __launch_bounds__(kThreads, 2) quantize_turned_kernel(const QuantizeParams p) {
+__global__ void __launch_bounds__(kThreads, kF32 ? 4 : 2) quantize_turned_kernel(const QuantizeParams p) {
   constexpr int kBlocks = kNv ? 2 : 1;           // blocks of 32 elements
   constexpr int kBlock = 32 / kBlocks;
   constexpr int kLaneRows = kF32 ? 1 : 4, kTile = 32 * kLaneRows, kWords = kNv ? 4 : 2;
@@ -272,6 +272,7 @@ __global__ void __launch_bounds__(kThreads, 2) quantize_turned_kernel(const Quan
           if constexpr (kF32) w[i].x = *src;
           else w[i] = *reinterpret_cast<const uint2*>(src);
         }
+        asm("" : "+l"(src));      // the next address from this one: all of them in registers at first took 25 us for 19
       }
     } else {
       static_assert(!kF32, "single rows");
