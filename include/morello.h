@@ -417,11 +417,12 @@ int morello_layer_norm(int rms, int x_type, int64_t m, int64_t n, float eps, con
  *     dX[i,j] = rstd_i * (g[i,j] - mean_j(g[i,:]) - h[i,j] * mean_j(g[i,:] * h[i,:])) + R[i,j]    (rms == 1: without mean(g))
  *     dgamma[j] = sum_i dY[i,j] * h[i,j],   dbeta[j] = sum_i dY[i,j]                               (f32)
  *
- * dX and R are of X's type; R, the gradient that reaches X past the norm, may be NULL, and may be dX itself.  dX, dgamma
- * and dbeta may each be NULL (not wanted); mean is not read when rms == 1.  accumulate == 1 adds to dgamma and dbeta
- * instead of setting them.  m == 0 sums are empty: zero, or nothing added.  Sums are f32, in an order that is fixed for a
- * shape, its types and whether all tensors are 16-byte aligned.  `workspace` (for dgamma and dbeta): morello_layer_norm_backward_workspace_bytes() bytes, 16-byte aligned, or
- * NULL and 0 for the library's own scratch (rules as in morello_matmul_accum).  Asynchronous on `stream`.
+ * dX and R are of X's type; R, the gradient that reaches X past the norm, may be NULL, and may be dX itself; no other
+ * overlap is allowed.  dX, dgamma and dbeta may each be NULL (not wanted); mean is not read when rms == 1.  accumulate == 1
+ * adds to dgamma and dbeta instead of setting them.  m == 0 sums are empty: zero, or nothing added.  Sums are f32, in an
+ * order that is fixed for a shape, its types and whether all tensors are 16-byte aligned.  `workspace` (for dgamma and
+ * dbeta): morello_layer_norm_backward_workspace_bytes() bytes, 16-byte aligned, or NULL and 0 for the library's own
+ * scratch (rules as in morello_matmul_accum).  Asynchronous on `stream`.
  */
 int morello_layer_norm_backward(int rms, int x_type, int accumulate, int64_t m, int64_t n, const void* X,
                                 const void* gamma, const float* mean, const float* rstd, const void* dY, const void* R,
@@ -442,6 +443,9 @@ enum { MORELLO_MXFP4 = 0, MORELLO_NVFP4 = 1 };
  *         zeros past k.  An element is e2m1: a sign bit and three bits for 0, 1/2, 1, 3/2, 2, 3, 4, 6.
  *     scales[parts][ceil(rows / parts / 128)][ceil(k / (4 block))][32][4][4] bytes: block j of row r of a part at
  *         [r / 128][j / 4][r % 32][(r % 128) / 32][j % 4], zeros where there is no such row or block.
+ *
+ * The zeros are part of the tensor: the products read them.  morello_fp4_quantize writes them; tensors from elsewhere bring
+ * their own.
  *
  * The rows are `parts` equal parts (rows % parts == 0), each with scales of its own from a multiple of 128 rows on:
  * 1, or 2 for the two halves of a gated layer's weights.  A weight matrix of k inputs and w outputs is a tensor of w

@@ -5,8 +5,9 @@
 //   backward   h = (x - mu) r, g = dy gamma:  dx = r (g - mean(g) - h mean(g h)) + R  (rms: without mean(g))
 //              dgamma = sum over rows of dy h, dbeta = sum over rows of dy
 //
-// Both passes are bound by memory: a row is read once, held in registers by a team of 32 to 512 threads, reduced and
-// written.  The variance is that of the differences from a mean (two sweeps over the registers), never a difference of
+// Both passes are bound by memory: a row is read once by a team of 8 to 512 threads, which hold it (backward: find it in
+// shared memory again) until it has been reduced, and written.  16384 x 4096 takes 49 us forward and 82 us backward, 5.5 and
+// 4.9 TB/s; 4096 x 2047 takes 16 and 27 us.  The variance is that of the differences from a mean (two sweeps over the registers), never a difference of
 // sums.  A warp takes its own mean and the squares about it, and one barrier later every thread joins the warps' three
 // numbers (Chan, Golub and LeVeque's formula for joining variances), so a row costs one barrier.
 //
@@ -347,7 +348,7 @@ norm_kernel(const NormParams p) {
 
 // --- rows through a ring in shared memory ------------------------------------------------------
 //
-// Whole batches: one or two persistent blocks of 16 warps to an SM.  A group is kTeams neighbouring rows, one to a team, and
+// The backward pass, and the forward pass of rows that are not whole octets: one persistent block of 16 warps to an SM.  A group is kTeams neighbouring rows, one to a team, and
 // contiguous in memory: one bulk copy per tensor.  The first thread keeps the ring full: behind every group it has worked
 // on it waits until the others are done with the one before, and has the next copied there.  The loads' latency, which a
 // team that loads its own rows waits out at every row, is behind the ring.  (A warp of its own for the copies takes 3 of
@@ -915,9 +916,10 @@ RingShape ring_shape(int64_t n, std::initializer_list<int> sizes, int64_t beside
   return r;
 }
 
-// Blocks at most that leave sums of their own.
+// Blocks at most that leave sums of their own.  Rows too long for the ring: a block's share is this many at least.
+constexpr int64_t kLongShare = 128;
 int64_t backward_parts(int64_t m, int64_t n) {
-  const int64_t rows = n > kRingColumns ? 1 : kRingThreads / team_of(n);      // long rows: of a block's share
+  const int64_t rows = n > kRingColumns ? kLongShare : kRingThreads / team_of(n);
   return std::min<int64_t>(kMaxParts, (m + rows - 1) / rows);
 }
 size_t backward_bytes(int64_t m, int64_t n) { return (size_t)backward_parts(m, n) * 2 * n * 4; }
@@ -1018,7 +1020,7 @@ cudaError_t backward_launch(const DeviceInfo& dev, const NormBackwardParams& p, 
                  : ring_launch<norm_backward_kernel<kT, 1, kIter, kF32, kRms>>(p, ring, kRingThreads / kT, parts, (size_t)beside, kJoined, s);
     });
   } else {
-    parts = (int)std::min<int64_t>(parts, (p.m + 127) / 128);
+    parts = (int)std::min<int64_t>(parts, (p.m + kLongShare - 1) / kLongShare);
     if (p.dX) {
       const int64_t blocks = std::min<int64_t>(p.m, (int64_t)dev.sms * 2);
       e = launch_pdl(norm_backward_long_kernel<kF32, kRms>, dim3((unsigned)blocks), dim3(kLongThreads), 0, s, 1, p);
