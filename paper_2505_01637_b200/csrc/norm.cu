@@ -522,7 +522,7 @@ __device__ __forceinline__ void block_barrier() { asm volatile("bar.sync 15, %0;
 // The forward pass of rows that are not whole octets.
 template <int kT, int kIter, bool kF32, bool kRms>
 __global__ void __launch_bounds__(kRingThreads, 1) norm_ring_kernel(const NormParams p, const RingShape ring) {
-  constexpr int kTeams = kRingThreads / kT, kWarps = kT / 32;
+  constexpr int kTeams = kRingThreads / kT, kLanes = kT < 32 ? kT : 32, kWarps = kT / kLanes;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ RingBars bars;
   __shared__ Part parts[2][kTeams][kWarps];
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_ring_kernel(const NormPa
   const Columns<kT, 1, kIter> c{(int)threadIdx.x % kT, p.n};
   uint16_t* copies = reinterpret_cast<uint16_t*>(smem + (size_t)ring.stages * ring.stage_bytes);
   const RingVector<kT, 1, kIter> gammas(p.gamma, 1.f, copies, c), betas(p.beta, 0.f, copies + p.n, c);
-  const float count = warp_sum(c.count()), inv_count = count > 0.f ? 1.f / count : 0.f;
+  const float count = warp_sum<kLanes>(c.count()), inv_count = count > 0.f ? 1.f / count : 0.f;
   __syncthreads();
   int turn = 0;
   bool ok = true;          // once a wait gave up the rows go by unread and unwritten: the team's barriers still meet
@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_ring_kernel(const NormPa
     }
     ring_release(&bars, at);
     Part mine{0.f, 0.f, 0.f, count};
-    if constexpr (!kRms) mine.mean = warp_sum(pair_sum(sums)) * inv_count;
+    if constexpr (!kRms) mine.mean = warp_sum<kLanes>(pair_sum(sums)) * inv_count;
     f32x2 off = 0, squares = 0;
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
@@ -569,9 +569,9 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_ring_kernel(const NormPa
       c.clear(i, d);
       spread<kRms>(d, 0, &off, &squares);
     }
-    if constexpr (!kRms) mine.off = warp_sum(pair_sum(off));
-    mine.squares = warp_sum(pair_sum(squares));
-    const ForwardFactors f = forward_factors<kT, 32, kTeams, kRms>(p, parts[turn], mine, team, warp, lane, row, live && c.t == 0);
+    if constexpr (!kRms) mine.off = warp_sum<kLanes>(pair_sum(off));
+    mine.squares = warp_sum<kLanes>(pair_sum(squares));
+    const ForwardFactors f = forward_factors<kT, kLanes, kTeams, kRms>(p, parts[turn], mine, team, warp, lane, row, live && c.t == 0);
 #pragma unroll
     for (int i = 0; i < kIter; ++i) {
       if (!live || !c.any(i)) continue;
@@ -627,7 +627,7 @@ __device__ __forceinline__ void add_four(f32x2 (&v)[4], const f32x2 (&r)[4]) {
 template <int kT, int kVec, int kIter, bool kF32, bool kRms>
 __global__ void __launch_bounds__(kRingThreads, 1)
 norm_backward_kernel(const NormBackwardParams p, const RingShape ring) {
-  constexpr int kTeams = kRingThreads / kT, kWarps = kT / 32;
+  constexpr int kTeams = kRingThreads / kT, kLanes = kT < 32 ? kT : 32, kWarps = kT / kLanes;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ RingBars bars;
   __shared__ float2 parts[2][kTeams][kWarps];
@@ -687,7 +687,7 @@ norm_backward_kernel(const NormBackwardParams p, const RingShape ring) {
       backward_sums<kRms>(d, g, dy, pair_of(rstd), &p1, &p2, sum_g[i], sum_b[i]);
     }
     if (p.dX) {
-      float s1 = kRms ? 0.f : warp_sum(pair_sum(p1)), s2 = warp_sum(pair_sum(p2));
+      float s1 = kRms ? 0.f : warp_sum<kLanes>(pair_sum(p1)), s2 = warp_sum<kLanes>(pair_sum(p2));
       if constexpr (kT > 32) {
         if (lane == 0) parts[turn][team][warp] = make_float2(s1, s2);
         team_barrier<kT, kRingThreads>(team);
@@ -899,8 +899,9 @@ constexpr int64_t kRingColumns = 16384;     // a team of 512 threads with 32 col
 
 bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
-// Teams of 16 columns to a thread (32 in the longest rows).
+// Teams of 16 columns to a thread (32 in the longest rows, 8 in the shortest).
 int team_of(int64_t n) {
+  if (n <= 128) return n <= 64 ? 8 : 16;
   int t = 32;
   while (t < 512 && n > t * 16) t *= 2;
   return t;
@@ -938,6 +939,8 @@ cudaError_t ring_launch(const Params& p, const RingShape& ring, int teams, int64
 template <typename Go>
 cudaError_t by_team(int64_t n, Go&& go) {
   using std::integral_constant;
+  if (n <= 64) return go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+  if (n <= 128) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
   if (n <= 256) return go(integral_constant<int, 32>{}, integral_constant<int, 1>{});
   if (n <= 512) return go(integral_constant<int, 32>{}, integral_constant<int, 2>{});
   if (n <= 1024) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});

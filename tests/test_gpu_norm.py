@@ -76,6 +76,15 @@ def test_batches(m, n, kind):
         test_backward(m, n, rms, kind)
 
 
+@pytest.mark.parametrize("n", [8, 9, 16, 57, 63, 64, 65, 72, 120, 121, 127, 128, 129, 136])
+def test_short_rows(n):
+    # the heads' rows: several to a warp, groups that end inside one
+    for m in (1, 3, 65, 9473):
+        for rms in (False, True):
+            test_forward(m, n, rms, BF)
+            test_backward(m, n, rms, BF)
+
+
 @pytest.mark.parametrize("kind", [BF, F32])
 @pytest.mark.parametrize("m,n", [(5, 256), (5, 2048), (5, 8192), (5, 16384), (5, 3), (17, 1), (40, 1), (100, 5), (1500, 7), (2000, 264),
                                  (700, 2048)])
