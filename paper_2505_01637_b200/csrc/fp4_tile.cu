@@ -295,6 +295,15 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         tma_load_3d(mine, &map_r, &bars->res_full[ew], col0 + 32 * s, (int)row0, 0);
       };
       if (res_tma && steps > 0) load_residual(0);
+      const int rows_here = (int)max((int64_t)0, min((int64_t)32, p.m - row0));
+      auto plain_block = [&](int s) {
+        const int col = col0 + 32 * s;
+        return PlainBlock{row0 * p.n + col + lane, p.n, lane < p.n - col ? rows_here : 0};
+      };
+      if (p.residual && !p.tma && steps > 0) {      // the same with loads: the next step's rows as far as L2
+        if (steps > 1 && lane < rows_here) prefetch_l2(p.residual + (row0 + lane) * p.n + col0 + 32);
+        block_in16<32>(block, lane, p.residual, plain_block(0));
+      }
       // The bias of a step's columns, one to a lane.
       float bias[kOutGroups], bias_up[kGated ? kOutGroups : 1];
 #pragma unroll
@@ -359,8 +368,8 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], u[i]);
         }
-        const int left = p.n - col, rows_here = (int)max((int64_t)0, min((int64_t)32, p.m - row0));
-        const PlainBlock plain{row0 * p.n + col + lane, p.n, lane < left ? rows_here : 0};
+        const int left = p.n - col;
+        const PlainBlock plain = plain_block(s);
         if (res_tma) {
           ok = mbar_wait(&bars->res_full[ew], res_phase, abort_flag, p.status, 55);
           ok = __all_sync(kFullMask, ok);
@@ -368,7 +377,7 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           if (!ok) return;
           add_pairs16(block, lane, v);
         } else if (p.residual) {
-          block_in16(block, lane, p.residual, plain);
+          if (s > 0) block_in16<16>(block, lane, p.residual, plain);
           __syncwarp();
           add_pairs16(block, lane, v);
         } else if (p.tma) {

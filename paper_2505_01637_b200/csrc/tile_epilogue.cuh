@@ -76,8 +76,9 @@ struct PlainBlock {
 __device__ __forceinline__ uint32_t place16(uint32_t block, int row, int lane) {
   return block + (uint32_t)row * 64u + ((((uint32_t)lane >> 3) ^ (((uint32_t)row >> 1) & 3u)) << 4) + ((uint32_t)lane & 7u) * 2u;
 }
+template <int kInFlight = 8>
 __device__ __forceinline__ void block_in16(uint32_t block, int lane, const uint16_t* src, const PlainBlock& g) {
-#pragma unroll 8
+#pragma unroll kInFlight
   for (int r = 0; r < 32; ++r) {
     const uint16_t v = r < g.rows ? src[g.at + r * g.pitch] : (uint16_t)0;
     asm volatile("st.shared.u16 [%0], %1;" ::"r"(place16(block, r, lane)), "h"(v) : "memory");
