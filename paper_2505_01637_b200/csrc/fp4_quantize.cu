@@ -371,31 +371,75 @@ __device__ __forceinline__ void codes_times(uint32_t codes, f32x2 scale, f32x2 (
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[j] = mul2(pair_of(f16_low(h[j]), f16_high(h[j])), scale);
 }
-// A lane takes eight elements of each of its rows, so that a warp's stores are contiguous (sixteen a lane, as in the
-// quantisation, leave half of every line to a second store: 22.1 us for 8192 x 4096 where this takes 14.8).
-template <bool kNv, bool kF32>
+// Where a warp's 256 elements of a row go through shared memory, so that its stores are contiguous.
+constexpr int kReadWarps = kThreads / 32;
+// bf16 rows off 16 bytes: words of two elements, 4 bytes aligned in memory.  `left` of the elements exist.
+__device__ __forceinline__ void store_words(uint16_t* dst, int64_t left, int lane, const uint4& mine, uint32_t* shared) {
+  *reinterpret_cast<uint4*>(shared + 4 * lane) = mine;
+  __syncwarp();
+  const int skew = (int)(reinterpret_cast<uintptr_t>(dst) >> 1) & 1;      // elements before the first whole word
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int word = 32 * j + lane, first = 2 * word + skew;
+    uint32_t v = shared[word];
+    if (skew) v = __funnelshift_r(v, shared[word + 1], 16);      // the word behind the last is not stored
+    if (first + 1 < min(left, (int64_t)kReadColumns)) *reinterpret_cast<uint32_t*>(dst + first) = v;
+    else if (first < min(left, (int64_t)kReadColumns)) dst[first] = (uint16_t)v;
+  }
+  if (skew && lane == 0) dst[0] = (uint16_t)shared[0];
+  __syncwarp();
+}
+// f32, four elements an access where rows are on 16 bytes, single ones where not.
+__device__ __forceinline__ void store_floats(float* dst, int64_t left, int lane, int width, const f32x2 (&v)[4], uint32_t* shared) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const float2 a = pair_values(v[2 * q]), b = pair_values(v[2 * q + 1]);
+    reinterpret_cast<float4*>(shared)[2 * lane + q] = make_float4(a.x, a.y, b.x, b.y);
+  }
+  __syncwarp();
+  if (width >= 4) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (4 * (32 * j + lane) < left) reinterpret_cast<uint4*>(dst)[32 * j + lane] = reinterpret_cast<const uint4*>(shared)[32 * j + lane];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (32 * j + lane < left) dst[32 * j + lane] = __uint_as_float(shared[32 * j + lane]);
+  }
+  __syncwarp();
+}
+// A lane takes eight elements of each of its rows: a warp's stores are contiguous (sixteen a lane, as in the quantisation,
+// leave half of every line to a second store: 22.1 us for 8192 x 4096 where this takes 14.8).
+// kShared: through shared memory: f32, and bf16 rows off 8 bytes (8192 x 4095 22.5 us instead of 92; 4100 columns take 16.3 by
+// two stores of a lane, 22.9 this way).
+template <bool kNv, bool kF32, bool kShared>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const DequantizeParams p) {
   constexpr int kBlock = kNv ? 16 : 32;
+  __shared__ __align__(16) uint32_t shared[kShared ? kReadWarps : 1][(kF32 ? kReadColumns : kReadColumns / 2) + 4];
   const int lane = threadIdx.x % 32;
-  const int64_t col = (int64_t)blockIdx.x * kReadColumns + lane * 8, left = p.k - col;
+  uint32_t* mine = shared[kShared ? threadIdx.x / 32 : 0];
+  const int64_t col0 = (int64_t)blockIdx.x * kReadColumns, col = col0 + lane * 8;
+  const bool any = col < p.k;
   pdl_wait();
   pdl_release();
-  if (left <= 0) return;
+  if (!kShared && !any) return;
   const float alpha = p.alpha ? *p.alpha : 1.f;
   const unsigned block = (unsigned)(col / kBlock);
   for (unsigned band = blockIdx.y; band < p.bands; band += gridDim.y) {
     const Band at(band, (unsigned)p.down, p.parts, p.each);
     const int64_t first = at.part_row + at.row0, here = p.each - at.row0;
     if (here <= 0) continue;
-    const uint4 scales = *reinterpret_cast<const uint4*>(p.scales + ((int64_t)at.atom_row * p.across + block / 4) * kAtomBytes + at.r32 * 16);
+    uint4 scales = make_uint4(0u, 0u, 0u, 0u);
+    if (any) scales = *reinterpret_cast<const uint4*>(p.scales + ((int64_t)at.atom_row * p.across + block / 4) * kAtomBytes + at.r32 * 16);
     const uint32_t words[kRowsAtOnce] = {scales.x, scales.y, scales.z, scales.w};
     const uint8_t* q = p.q + first * p.pitch + col / 2;
     uint32_t codes[kRowsAtOnce];
 #pragma unroll
-    for (int i = 0; i < kRowsAtOnce; ++i) codes[i] = 32 * i < here ? *reinterpret_cast<const uint32_t*>(q + 32 * i * p.pitch) : 0u;
+    for (int i = 0; i < kRowsAtOnce; ++i)
+      codes[i] = any && 32 * i < here ? *reinterpret_cast<const uint32_t*>(q + 32 * i * p.pitch) : 0u;
 #pragma unroll
     for (int i = 0; i < kRowsAtOnce; ++i) {
-      if (32 * i >= here) break;
+      if (32 * i >= here) break;      // of the whole warp
       const uint32_t byte = words[i] >> (8 * (block & 3)) & 0xffu;
       float s;
       if constexpr (kNv) s = byte == 0x7fu ? __uint_as_float(0x7fffffffu) : e4m3_value(byte);
@@ -406,22 +450,15 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const DequantizePa
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = mul2(v[j], pair_of(alpha));
       }
-      const float2 a = pair_values(v[0]), b = pair_values(v[1]), c = pair_values(v[2]), d = pair_values(v[3]);
-      const int64_t to = (first + 32 * i) * p.k + col;
+      const int64_t to = (first + 32 * i) * p.k + col0;
       if constexpr (kF32) {
-        float* dst = static_cast<float*>(p.Y) + to;
-        if (left >= 8 && p.width >= 4) {
-          reinterpret_cast<float4*>(dst)[0] = make_float4(a.x, a.y, b.x, b.y);
-          reinterpret_cast<float4*>(dst)[1] = make_float4(c.x, c.y, d.x, d.y);
-        } else {
-          const float single[8] = {a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < left) dst[e] = single[e];
-        }
+        store_floats(static_cast<float*>(p.Y) + to, p.k - col0, lane, p.width, v, mine);
       } else {
-        store8_raw(static_cast<uint16_t*>(p.Y) + to, p.width, left,
-                   make_uint4(bf16_pack(a.x, a.y), bf16_pack(b.x, b.y), bf16_pack(c.x, c.y), bf16_pack(d.x, d.y)));
+        const float2 a = pair_values(v[0]), b = pair_values(v[1]), c = pair_values(v[2]), d = pair_values(v[3]);
+        const uint4 packed = make_uint4(bf16_pack(a.x, a.y), bf16_pack(b.x, b.y), bf16_pack(c.x, c.y), bf16_pack(d.x, d.y));
+        uint16_t* dst = static_cast<uint16_t*>(p.Y) + to;
+        if constexpr (kShared) store_words(dst, p.k - col0, lane, packed, mine);
+        else store8_raw(dst + 8 * lane, p.width, p.k - col, packed);
       }
     }
   }
@@ -553,8 +590,10 @@ int morello_fp4_dequantize(int format, int y_type, int64_t rows, int64_t parts, 
   p.width = f32 ? access_width_f32(k, Y) : access_width(k, Y);
   const dim3 grid((unsigned)((k + kReadColumns - 1) / kReadColumns), std::min(p.bands, kMaxGridY)), block(kThreads);
   cudaError_t e;
-  if (nv) e = f32 ? launch_pdl(dequantize_kernel<true, true>, grid, block, 0, s, 1, p) : launch_pdl(dequantize_kernel<true, false>, grid, block, 0, s, 1, p);
-  else e = f32 ? launch_pdl(dequantize_kernel<false, true>, grid, block, 0, s, 1, p) : launch_pdl(dequantize_kernel<false, false>, grid, block, 0, s, 1, p);
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, block, 0, s, 1, p); };
+  if (f32) e = nv ? go(dequantize_kernel<true, true, true>) : go(dequantize_kernel<false, true, true>);
+  else if (p.width < 4) e = nv ? go(dequantize_kernel<true, false, true>) : go(dequantize_kernel<false, false, true>);
+  else e = nv ? go(dequantize_kernel<true, false, false>) : go(dequantize_kernel<false, false, false>);
   if (e != cudaSuccess) return record_cuda_error(e);
   count_launches(1);
   return MORELLO_OK;
