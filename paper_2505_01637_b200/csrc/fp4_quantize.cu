@@ -34,6 +34,7 @@ using namespace sm100;
 
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kThreads = 256;
+constexpr int kWarpColumns = 512;   // of the quantisation
 
 struct QuantizeParams {
   const void* X;
@@ -149,6 +150,30 @@ struct Sixteen {
       for (int i = 0; i < 2; ++i) put(i, cols > 8 * i ? load8_raw(src + 8 * i, width, cols - 8 * i) : make_uint4(0u, 0u, 0u, 0u));
     }
   }
+  // The same for f32 rows off 16 bytes: the warp's piece of the row (from `at`, `cols` of its 512 elements exist) by
+  // contiguous accesses, which spread() hands to the lanes that they are for.  (For bf16 rows, in words of two elements, that took
+  // 40 us for 8192 x 4095; a lane's own accesses take 30.)
+  __device__ __forceinline__ void load_piece(const void* X, int64_t at, int64_t cols, int lane) {
+    static_assert(kF32, "single elements");
+    const float* src = static_cast<const float*>(X) + at;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) w[j] = 32 * j + lane < cols ? __float_as_uint(src[32 * j + lane]) : 0u;
+  }
+  static constexpr int kStride = 16 + 4;      // of lanes: eight lanes' accesses in different banks
+  __device__ __forceinline__ void spread(uint32_t* shared, int lane) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) shared[(32 * j + lane) / 16 * kStride + lane % 16] = w[j];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 v = *reinterpret_cast<const uint4*>(shared + lane * kStride + 4 * i);
+      w[4 * i] = v.x;
+      w[4 * i + 1] = v.y;
+      w[4 * i + 2] = v.z;
+      w[4 * i + 3] = v.w;
+    }
+    __syncwarp();
+  }
   // Elements 8 i on.
   __device__ __forceinline__ void pairs(int i, f32x2 (&v)[4]) const {
 #pragma unroll
@@ -178,7 +203,6 @@ __device__ __forceinline__ uint32_t times(uint32_t amax, float mult) {
 
 // Where a warp of the [rows][k] layout works: band 4 (part * down + atom) + eighth, 16 columns a lane, rows 32 apart.
 constexpr int kRowsAtOnce = 4;      // an atom's rows of the same 16 bytes
-constexpr int kWarpColumns = 512;   // of the quantisation
 constexpr int kReadColumns = 256;   // of reading back
 struct Band {
   unsigned atom_row;
@@ -193,13 +217,15 @@ struct Band {
   }
 };
 
-template <bool kNv, bool kF32, bool kMult>
+// kShared: f32 rows off 16 bytes, through shared memory (8192 x 4095 32 us instead of 65).
+template <bool kNv, bool kF32, bool kMult, bool kShared>
 __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeParams p) {
   constexpr int kLanes = kNv ? 1 : 2, kBlock = 16 * kLanes;            // lanes of a block, its elements
   const int lane = threadIdx.x % 32;
+  __shared__ __align__(16) uint32_t shared[kShared ? kThreads / 32 : 1][kShared ? 32 * Sixteen<kF32>::kStride : 4];
   pdl_wait();
   pdl_release();
-  const int64_t col = (int64_t)blockIdx.x * kWarpColumns + lane * 16;
+  const int64_t col0 = (int64_t)blockIdx.x * kWarpColumns, col = col0 + lane * 16;
   const int64_t across = (int64_t)blockIdx.x * (kWarpColumns / (4 * kBlock)) + lane / (4 * kLanes);
   const float mult = kMult ? *p.mult : 1.f;
   for (unsigned band = blockIdx.y; band < p.bands; band += gridDim.y) {
@@ -207,12 +233,16 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantizeParams
     Sixteen<kF32> x[kRowsAtOnce];
     const int64_t first = at.part_row + at.row0;
 #pragma unroll
-    for (int i = 0; i < kRowsAtOnce; ++i)
-      x[i].load(p.X, (first + 32 * i) * p.k + col, at.row0 + 32 * i < p.each ? p.k - col : 0, p.width);
+    for (int i = 0; i < kRowsAtOnce; ++i) {
+      const bool row = at.row0 + 32 * i < p.each;
+      if constexpr (kShared) x[i].load_piece(p.X, (first + 32 * i) * p.k + col0, row ? p.k - col0 : 0, lane);
+      else x[i].load(p.X, (first + 32 * i) * p.k + col, row ? p.k - col : 0, p.width);
+    }
     uint32_t words[kRowsAtOnce];
     uint8_t* q = p.q + first * p.pitch + col / 2;
 #pragma unroll
     for (int i = 0; i < kRowsAtOnce; ++i) {
+      if constexpr (kShared) x[i].spread(shared[threadIdx.x / 32], lane);
       uint32_t amax = x[i].amax();
       if constexpr (kLanes > 1) amax = max(amax, __shfl_xor_sync(kFull, amax, 1));
       if constexpr (kMult) amax = times(amax, mult);
@@ -491,7 +521,10 @@ int access_width_f32(int64_t cols, const void* p) {
 template <bool kNv, bool kF32, bool kMult>
 cudaError_t quantize_launch(const QuantizeParams& p, bool turned, cudaStream_t s) {
   const dim3 grid = turned ? dim3(p.bands, std::min((unsigned)p.segments, kMaxGridY)) : dim3((unsigned)((p.k + kWarpColumns - 1) / kWarpColumns), std::min(p.bands, kMaxGridY));
-  if (!turned) return launch_pdl(quantize_kernel<kNv, kF32, kMult>, grid, dim3(kThreads), 0, s, 1, p);
+  if constexpr (kF32) {
+    if (!turned && p.width < 4) return launch_pdl(quantize_kernel<kNv, true, kMult, true>, grid, dim3(kThreads), 0, s, 1, p);
+  }
+  if (!turned) return launch_pdl(quantize_kernel<kNv, kF32, kMult, false>, grid, dim3(kThreads), 0, s, 1, p);
   if constexpr (!kF32) {
     if (p.width < 4) return launch_pdl(quantize_turned_kernel<kNv, false, kMult, false>, grid, dim3(kThreads), 0, s, 1, p);
   }
