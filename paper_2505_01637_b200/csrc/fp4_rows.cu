@@ -1,5 +1,6 @@
 // Products of 4-bit tensors on few rows (at most 16): a decoding step.  The call streams the weights once and is bound by
-// memory, and on small layers by the chain of a launch.  (With 32 and 64 rows, one thread to a column of Y, finishing them
+// memory, and on small layers by the chain of a launch: 1 x 2048 x 16384 takes 6.4 us, gated 2 x 8192 7.2, 16 rows with bias,
+// GELU and residual 8.3, of which the 17 MB are 2.6.  (With 32 and 64 rows, one thread to a column of Y, finishing them
 // takes longer than the stream: 64 rows of 2048 x 16384 12.1 us here, 8.8 by the tile kernel; 4096 x 4096 8.5 and 9.4.)
 //
 // The operands trade places: a block owns 128 rows of W (columns of Y; gated: of either half), which become the M side of

@@ -4,13 +4,16 @@
 //
 // The block-scaled MMA multiplies 64 elements of e2m1 a step and applies both operands' scales, which it reads from tensor
 // memory.  Persistent blocks (or CTA pairs) walk output tiles, warps specialised into a TMA producer, an MMA issuer and
-// eight epilogue warps.  A stage is 256 elements of the contraction: 128 bytes of every row in the 128-byte swizzle, and
+// sixteen epilogue warps.  A stage is 256 elements of the contraction: 128 bytes of every row in the 128-byte swizzle, and
 // the scales of those rows, whole 512-byte atoms that the issuer copies to tensor memory ahead of the stage's four MMA
 // steps, to one of two places in turn.
 //
 // A 256-column accumulator and the scales leave no room for a second one in the 512 columns of tensor memory: the epilogue
 // warps take all of a tile's sums into registers, hand the accumulator back, and finish the tile under the next one's main
 // loop.  Gated tiles hold 128 columns of either half of W.
+//
+// 4096 x 4096 x 4096 takes 31 us (4.4 PFLOP/s), 8192 x 8192 x 8192 185 to 200 (5.5 to 5.9), bound by the hand-over of the one
+// accumulator, the copies of the scales and the board's power.
 #include <algorithm>
 #include <type_traits>
 
@@ -35,7 +38,7 @@ constexpr int kScaleColumns = 64;                    // of tensor memory, per st
 constexpr int kTmemColumns = 512;
 constexpr int kEpiWarps = 16;                        // four per quarter of the rows
 constexpr int kParts = kEpiWarps / 4;
-constexpr int kThreads = 128 + 32 * kEpiWarps;       // a warpgroup for the producer and the issuer, two for the epilogue
+constexpr int kThreads = 128 + 32 * kEpiWarps;       // a warpgroup for the producer and the issuer, four for the epilogue
 // 640 threads are launched with 96 registers each; the epilogue's hold up to 64 sums besides.  (Eight epilogue warps with twice
 // the sums each leave the schedulers short of warps: 4096 x 4096 x 4096 with GELU, bias and residual 46 us.)
 constexpr int kFewRegisters = 32, kManyRegisters = 112;

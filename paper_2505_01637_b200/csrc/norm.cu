@@ -6,8 +6,8 @@
 //              dgamma = sum over rows of dy h, dbeta = sum over rows of dy
 //
 // Both passes are bound by memory: a row is read once by a team of 8 to 512 threads, which hold it (backward: find it in
-// shared memory again) until it has been reduced, and written.  16384 x 4096 takes 49 us forward and 82 us backward, 5.5 and
-// 4.9 TB/s; 4096 x 2047 takes 16 and 27 us.  The variance is that of the differences from a mean (two sweeps over the registers), never a difference of
+// shared memory again) until it has been reduced, and written.  16384 x 4096 takes 49 us forward and 83 us backward, 5.4 and
+// 4.9 TB/s; 4096 x 2047 takes 16 and 30 us.  The variance is that of the differences from a mean (two sweeps over the registers), never a difference of
 // sums.  A warp takes its own mean and the squares about it, and one barrier later every thread joins the warps' three
 // numbers (Chan, Golub and LeVeque's formula for joining variances), so a row costs one barrier.
 //
