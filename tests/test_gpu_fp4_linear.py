@@ -192,3 +192,17 @@ def test_stream_and_graph(m):
     graph.replay()
     torch.cuda.synchronize()
     check(x2)
+
+
+@pytest.mark.parametrize("n", [4096, 4001])
+def test_elements_past_two_to_the_31(n):
+    m, k = 540000, 32
+    g = gen(n)
+    xq, xs, x = tensor(g, m, k, MX)
+    wq, ws, w = tensor(g, n, k, MX)
+    y = torch.full((m, n), 77.0, dtype=BF, device="cuda")
+    mb.morello_fp4_linear(MX, 0, 0, 0, m, k, n, xq, xs, wq, ws, None, None, None, y)
+    device_ok()
+    for at in (slice(0, 300), slice(m - 300, m)):
+        want, bound = linear64(x[at], w, None, None, None, "none", False, k, False)
+        assert_close(y[at], want, bound, "y")

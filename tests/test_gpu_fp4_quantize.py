@@ -170,3 +170,46 @@ def test_empty_stream_and_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(y.double(), values_of(*quantized64(x, NV), NV))
+
+
+@pytest.mark.parametrize("off", [0, 1, 2, 4])
+@pytest.mark.parametrize("rows,k", [(1, 1), (2, 255), (33, 256), (130, 257), (40, 258), (3, 511), (129, 513), (64, 1028), (5, 2047)])
+def test_nothing_beside_the_tensors(rows, k, off):
+    # Y, Q and the scales lie in larger buffers whose other bytes stay as they are.
+    x = torch.randn(rows, k, generator=gen(k), device="cuda").to(BF)
+    nq, ns = mb.morello_fp4_bytes(rows, k), mb.morello_fp4_scale_bytes(NV, rows, 1, k)
+    guarded = torch.full((32 + nq + 32 + ns + 32,), 0x5A, dtype=torch.uint8, device="cuda")
+    ns0 = 32 + nq + (-nq) % 16
+    q, s = guarded[32:32 + nq], guarded[ns0:ns0 + ns]
+    mb.morello_fp4_quantize(NV, 0, 1, rows, 1, k, x, None, q, s)
+    beside = torch.ones_like(guarded, dtype=torch.bool)
+    beside[32:32 + nq] = False
+    beside[ns0:ns0 + ns] = False
+    assert torch.all(guarded[beside] == 0x5A)
+    want = values_of(*quantized64(x, NV), NV)
+    for out in (BF, F32):
+        whole = torch.full((16 + rows * k + 16,), 9.0, dtype=out, device="cuda")
+        y = whole[8 + off:8 + off + rows * k].view(rows, k)
+        mb.morello_fp4_dequantize(NV, int(out == F32), rows, 1, k, q, s, None, y)
+        assert torch.equal(y.double(), want)
+        assert torch.all(whole[:8 + off] == 9.0) and torch.all(whole[8 + off + rows * k:] == 9.0)
+
+
+@pytest.mark.parametrize("rowmajor,rows,k", [(False, 2100000, 16), (False, 530000, 4100), (True, 3, 16800000), (True, 2200000, 1000)])
+def test_long_tensors(rowmajor, rows, k):
+    # More groups of rows, or pieces of a row, than a grid has, and elements past 2^31: the last ones as by themselves.
+    x = torch.empty(k if rowmajor else rows, rows if rowmajor else k, dtype=BF, device="cuda")
+    x.normal_(generator=gen(3))
+    q, s = buffers(MX, rows, 1, k)
+    mb.morello_fp4_quantize(MX, 0, int(not rowmajor), rows, 1, k, x, None, q, s)
+    last = min(rows, 200 + rows % 128)              # from an atom's first row on, or all of them
+    few = 64 * 128 if rows < 200 else k
+    part = (x[-few:, -last:].t() if rowmajor else x[-last:]).contiguous()
+    q2, s2 = quantize(part, MX)
+    pitch, pitch2 = (k + 31) // 32 * 16, (few + 31) // 32 * 16
+    assert torch.equal(q[:rows * pitch].view(rows, pitch)[-last:, -pitch2:], q2[:last * pitch2].view(last, pitch2))
+    y = torch.empty(rows, k, dtype=BF, device="cuda")
+    mb.morello_fp4_dequantize(MX, 0, rows, 1, k, q, s, None, y)
+    y2 = torch.empty(last, few, dtype=BF, device="cuda")
+    mb.morello_fp4_dequantize(MX, 0, last, 1, few, q2, s2, None, y2)
+    assert torch.equal(y[-last:, -few:], y2)

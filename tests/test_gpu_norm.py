@@ -215,3 +215,19 @@ def test_workspace_stream_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         check()
+
+
+@pytest.mark.parametrize("n", [16384, 16383])
+def test_elements_past_two_to_the_31(n):
+    m = 140000
+    g = gen(n)
+    x = torch.empty(m, n, device="cuda", dtype=BF).normal_(generator=g)
+    gamma = (1 + 0.3 * torch.randn(n, generator=g, device="cuda")).to(BF)
+    y, mean, rstd = forward(x, gamma, None, 1e-5, False)
+    for at in (slice(0, 3), slice(m - 3, m)):
+        check_forward(x[at], gamma, None, 1e-5, False, y[at], mean[at], rstd[at])
+    dy = y.normal_(generator=g)
+    dx = torch.full_like(x, float("nan"))
+    mb.morello_layer_norm_backward(0, 0, 0, m, n, x, gamma, mean, rstd, dy, None, dx, None, None)
+    for at in (slice(0, 3), slice(m - 3, m)):
+        check_backward(x[at], gamma, mean[at], rstd[at], dy[at], None, False, dx[at], None, None)
