@@ -231,3 +231,19 @@ def test_elements_past_two_to_the_31(n):
     mb.morello_layer_norm_backward(0, 0, 0, m, n, x, gamma, mean, rstd, dy, None, dx, None, None)
     for at in (slice(0, 3), slice(m - 3, m)):
         check_backward(x[at], gamma, mean[at], rstd[at], dy[at], None, False, dx[at], None, None)
+
+
+@pytest.mark.parametrize("kind", [BF, F32])
+@pytest.mark.parametrize("m,n", [(300, 20001), (1, 20000), (129, 16392), (300, 16384), (700, 64), (77, 63), (9, 8191), (1100, 16383), (149, 4096)])
+def test_workspace_of_the_reported_size(m, n, kind):
+    x, gamma, _, dy, r = make(m, n, kind, m)
+    mean, rstd, _, _ = norm64(x, None, None, 1e-5, False)
+    mean, rstd = mean[:, 0].float(), rstd[:, 0].float()
+    need = mb.morello_layer_norm_backward_workspace_bytes(m, n)
+    ws = torch.full((need + 64,), 0xAB, device="cuda", dtype=torch.uint8)
+    dx = torch.full_like(x, float("nan"))
+    dg, db = torch.full((n,), float("nan"), device="cuda"), torch.full((n,), float("nan"), device="cuda")
+    for move in (lambda t: t, misaligned):
+        mb.morello_layer_norm_backward(0, int(kind == F32), 0, m, n, move(x), gamma, mean, rstd, move(dy), r, dx, dg, db, ws, need)
+        check_backward(x, gamma, mean, rstd, dy, r, False, dx, dg, db)
+        assert torch.all(ws[need:] == 0xAB)
