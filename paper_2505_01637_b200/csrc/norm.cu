@@ -60,6 +60,7 @@ struct NormBackwardParams {
   float* partial;        // [blocks][2][n]: the blocks' sums for dgamma and dbeta
   bool beta;             // dbeta is wanted
   uint32_t* status;
+  bool ring_r;           // longest rows: R comes through the ring; else, where that leaves no room for two stages, straight from memory
 };
 
 // Sum over kLanes neighbouring lanes, in every one of them.
@@ -640,7 +641,7 @@ norm_backward_kernel(const NormBackwardParams p, const RingShape ring) {
   pdl_release();
   const uint32_t row16 = (uint32_t)p.n * 2, row_x = kF32 ? 2 * row16 : row16;
   const uint32_t area_x = ring_area(kTeams, row_x), area16 = ring_area(kTeams, row16);
-  const RingTensor tensors[3] = {{p.X, row_x, area_x}, {p.dY, row16, area16}, {p.dX ? p.R : nullptr, row_x, area_x}};
+  const RingTensor tensors[3] = {{p.X, row_x, area_x}, {p.dY, row16, area16}, {(kIter == 4 ? p.ring_r : p.dX != nullptr) ? p.R : nullptr, row_x, area_x}};
   RingPlace at;
   ring_start<kTeams, kVec == 8>(&bars, smem, ring, &at, p.m, tensors);
   const int team = (int)threadIdx.x / kT, warp = (int)threadIdx.x % kT / 32, lane = (int)threadIdx.x % 32;
@@ -674,6 +675,10 @@ norm_backward_kernel(const NormBackwardParams p, const RingShape ring) {
     const uint8_t* x_row = ring_row<kVec == 8>(area, tensors[0], row0, team);
     const uint8_t* dy_row = ring_row<kVec == 8>(area + area_x, tensors[1], row0, team);
     const uint8_t* r_row = ring_row<kVec == 8>(area + area_x + area16, tensors[2], row0, team);
+    // Only the longest rows leave R no room (asked for at any length, this cost the others 5 %).
+    if constexpr (kIter == 4) {
+      if (!p.ring_r) r_row = static_cast<const uint8_t*>(p.R) + row * row_x;
+    }
     auto terms = [&](int i, f32x2 (&d)[4], f32x2 (&g)[4], f32x2 (&dy)[4]) {
       f32x2 x[4], gamma[4];
       gammas.get(c, i, gamma);
@@ -1008,7 +1013,7 @@ cudaError_t forward_launch(const DeviceInfo& dev, const NormParams& p, bool vec,
 }
 
 template <bool kF32, bool kRms>
-cudaError_t backward_launch(const DeviceInfo& dev, const NormBackwardParams& p, float* dgamma, float* dbeta,
+cudaError_t backward_launch(const DeviceInfo& dev, NormBackwardParams p, float* dgamma, float* dbeta,
                             bool accumulate, bool vec, cudaStream_t s, uint64_t* launches) {
   cudaError_t e = cudaSuccess;
   const bool sums = dgamma || dbeta;
@@ -1016,8 +1021,11 @@ cudaError_t backward_launch(const DeviceInfo& dev, const NormBackwardParams& p, 
   constexpr int kSize = kF32 ? 4 : 2;
   const int64_t beside = vec || p.n > kRingColumns ? 0 : 2 * p.n;       // gamma
   // With R or without: what a call asks for besides does not change the order of its sums.
-  if (ring_shape(p.n, {kSize, 2, kSize}, beside).stages >= 2) {
-    const RingShape ring = ring_shape(p.n, {kSize, 2, p.R && p.dX ? kSize : 0}, beside);
+  RingShape ring = ring_shape(p.n, {kSize, 2}, beside);
+  if (ring.stages >= 2) {
+    const RingShape with_r = ring_shape(p.n, {kSize, 2, kSize}, beside);
+    p.ring_r = p.R && p.dX && with_r.stages >= 2;
+    if (p.ring_r) ring = with_r;
     const int64_t teams = kRingThreads / team_of(p.n);
     parts = (int)std::min<int64_t>(std::min(parts, dev.sms), (p.m + teams - 1) / teams);
     e = by_team(p.n, [&](auto team, auto eights) {
@@ -1113,7 +1121,7 @@ int morello_layer_norm_backward(int rms, int x_type, int accumulate, int64_t m, 
   }
   if (!dX && !sums) return MORELLO_OK;
   const NormBackwardParams p{m, (int)n, 1.f / (float)n, X, static_cast<const uint16_t*>(gamma), rms ? nullptr : mean, rstd,
-                             static_cast<const uint16_t*>(dY), R, dX, static_cast<float*>(ws), dbeta != nullptr, dev.status};
+                             static_cast<const uint16_t*>(dY), R, dX, static_cast<float*>(ws), dbeta != nullptr, dev.status, false};
   const bool vec = n % 8 == 0 && aligned(X, 16) && aligned(gamma, 16) && aligned(dY, 16) && aligned(R, 16) && aligned(dX, 16) &&
                    aligned(ws, 16);
   uint64_t launches = 0;
