@@ -206,7 +206,8 @@ fp4_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         mma_commit(&bars->empty[stage]);
         if (++stage == S::kStages) { stage = 0; phase ^= 1; }
       }
-      if (ok) mma_commit(&bars->acc_full);
+      // Of an empty sum nobody waits for a part, and an arrival must not come when the block has gone.
+      if (ok && kb1 > kb0) mma_commit(&bars->acc_full);
     }
     __syncwarp();
   } else {

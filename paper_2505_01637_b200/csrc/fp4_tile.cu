@@ -204,7 +204,9 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       int stage = 0, buf = 0;
       uint32_t phase = 0, acc_phase = 0, turn = 0;
       bool ok = true;
-      for (int t = unit; t < p.tiles && ok; t += units) {
+      // Of an empty sum the epilogue awaits no accumulator, and an arrival must not come when the block has gone.
+      const int tiles = p.k_blocks > 0 ? p.tiles : 0;
+      for (int t = unit; t < tiles && ok; t += units) {
         uint32_t d_tmem = 0;
         int in_chunk = 0;
         for (int kb = 0; kb < p.k_blocks; ++kb) {
