@@ -761,8 +761,8 @@ norm_backward_kernel(const NormBackwardParams p, const RingShape ring) {
   }
 }
 
-// Rows longer than a team's registers: a block of 1024 threads sweeps the row three times (the second and third time from
-// L2, where it fits).
+// Rows longer than a team's registers: a block of 1024 threads, two blocks to an SM, sweeps the row three times (the second and
+// third time from L2, where it fits).  1024 x 32768 takes 75 us (f32 77), its backward pass 166.
 constexpr int kLongThreads = 1024;
 __device__ __forceinline__ float block_sum(float v, float* shared) {
   v = warp_sum(v);
@@ -776,28 +776,54 @@ __device__ __forceinline__ float element(const void* p, int64_t i) {
   if constexpr (kF32) return static_cast<const float*>(p)[i];
   else return bf16_value(static_cast<const uint16_t*>(p)[i]);
 }
+// A thread's sums over its columns of a row, begun anew every kLongPart columns and joined in 64 bits: as one chain of f32
+// additions a row of 2^24 equal values was off by more than 2^-16 of its sum.  add(j, part) adds column j's terms.
+constexpr int kLongPart = 32;
+template <int kSums, typename Add>
+__device__ __forceinline__ void long_sums(int64_t n, float (&sums)[kSums], Add&& add) {
+  double total[kSums];
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) total[i] = 0.0;
+  for (int64_t first = threadIdx.x; first < n; first += kLongPart * kLongThreads) {
+    float part[kSums];
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) part[i] = 0.f;
+    if (first + (kLongPart - 1) * kLongThreads < n) {
+#pragma unroll
+      for (int e = 0; e < kLongPart; ++e) add(first + e * kLongThreads, part);
+    } else {
+#pragma unroll 4
+      for (int64_t j = first; j < n; j += kLongThreads) add(j, part);
+    }
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) total[i] += part[i];
+  }
+#pragma unroll
+  for (int i = 0; i < kSums; ++i) sums[i] = (float)total[i];
+}
 
 template <bool kF32, bool kRms>
-__global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kLongThreads, 2) norm_long_kernel(const NormParams p) {
   __shared__ float shared[kLongThreads / 32];
   pdl_wait();
   pdl_release();
   for (int64_t row = blockIdx.x; row < p.m; row += gridDim.x) {
     const int64_t at = row * p.n;
+    const void* x = static_cast<const char*>(p.X) + at * (kF32 ? 4 : 2);
     float base = 0.f, shift = 0.f;
     if constexpr (!kRms) {
-      float s = 0.f;
-      for (int64_t j = threadIdx.x; j < p.n; j += kLongThreads) s += element<kF32>(p.X, at + j);
-      base = block_sum(s, shared) * p.inv_n;
+      float s[1];
+      long_sums(p.n, s, [&](int64_t j, float (&part)[1]) { part[0] += element<kF32>(x, j); });
+      base = block_sum(s[0], shared) * p.inv_n;
     }
-    float off = 0.f, squares = 0.f;
-    for (int64_t j = threadIdx.x; j < p.n; j += kLongThreads) {
-      const float d = element<kF32>(p.X, at + j) - base;
-      off += d;
-      squares = fmaf(d, d, squares);
-    }
-    if constexpr (!kRms) shift = block_sum(off, shared) * p.inv_n;
-    float square = block_sum(squares, shared) * p.inv_n - shift * shift;
+    float s[2];      // differences and squares
+    long_sums(p.n, s, [&](int64_t j, float (&part)[2]) {
+      const float d = element<kF32>(x, j) - base;
+      part[0] += d;
+      part[1] = fmaf(d, d, part[1]);
+    });
+    if constexpr (!kRms) shift = block_sum(s[0], shared) * p.inv_n;
+    float square = block_sum(s[1], shared) * p.inv_n - shift * shift;
     if (square < 0.f) square = 0.f;
     const float rstd = rsqrtf(square + p.eps);
     if (threadIdx.x == 0) {
@@ -805,7 +831,7 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormParam
       if (p.rstd) p.rstd[row] = rstd;
     }
     for (int64_t j = threadIdx.x; j < p.n; j += kLongThreads) {
-      const float d = (element<kF32>(p.X, at + j) - base) - shift;
+      const float d = (element<kF32>(x, j) - base) - shift;
       const float g = p.gamma ? bf16_value(p.gamma[j]) : 1.f, b = p.beta ? bf16_value(p.beta[j]) : 0.f;
       p.Y[at + j] = bf16_round(fmaf(d * rstd, g, b));
     }
@@ -815,25 +841,26 @@ __global__ void __launch_bounds__(kLongThreads) norm_long_kernel(const NormParam
 // Rows longer than that: dx by a block of 1024 threads that sweeps the row twice, and the sums over rows by a launch of
 // their own, 32 columns x 32 rows of threads to a block, that reads x and dy again.
 template <bool kF32, bool kRms>
-__global__ void __launch_bounds__(kLongThreads) norm_backward_long_kernel(const NormBackwardParams p) {
+__global__ void __launch_bounds__(kLongThreads, 2) norm_backward_long_kernel(const NormBackwardParams p) {
   __shared__ float shared[kLongThreads / 32];
   pdl_wait();
   pdl_release();
   for (int64_t row = blockIdx.x; row < p.m; row += gridDim.x) {
     const int64_t at = row * p.n;
     const float mean = kRms ? 0.f : p.mean[row], rstd = p.rstd[row];
-    float s1 = 0.f, s2 = 0.f;
-    for (int64_t j = threadIdx.x; j < p.n; j += kLongThreads) {
-      const float g = bf16_value(p.dY[at + j]) * (p.gamma ? bf16_value(p.gamma[j]) : 1.f);
-      s1 += g;
-      s2 = fmaf(g, element<kF32>(p.X, at + j) - mean, s2);
-    }
-    s1 = kRms ? 0.f : block_sum(s1, shared);
-    s2 = block_sum(s2, shared);
+    float s[2];      // g, and g (x - mean)
+    const void* x = static_cast<const char*>(p.X) + at * (kF32 ? 4 : 2);
+    const uint16_t* dy = p.dY + at;
+    long_sums(p.n, s, [&](int64_t j, float (&part)[2]) {
+      const float g = bf16_value(dy[j]) * (p.gamma ? bf16_value(p.gamma[j]) : 1.f);
+      part[0] += g;
+      part[1] = fmaf(g, element<kF32>(x, j) - mean, part[1]);
+    });
+    const float s1 = kRms ? 0.f : block_sum(s[0], shared), s2 = block_sum(s[1], shared);
     const float mean_g = s1 * p.inv_n, slope = s2 * rstd * p.inv_n * rstd;
     for (int64_t j = threadIdx.x; j < p.n; j += kLongThreads) {
-      const float g = bf16_value(p.dY[at + j]) * (p.gamma ? bf16_value(p.gamma[j]) : 1.f);
-      float v = rstd * fmaf(-slope, element<kF32>(p.X, at + j) - mean, g - mean_g);
+      const float g = bf16_value(dy[j]) * (p.gamma ? bf16_value(p.gamma[j]) : 1.f);
+      float v = rstd * fmaf(-slope, element<kF32>(x, j) - mean, g - mean_g);
       if (p.R) v += element<kF32>(p.R, at + j);
       if constexpr (kF32) static_cast<float*>(p.dX)[at + j] = v;
       else static_cast<uint16_t*>(p.dX)[at + j] = bf16_round(v);
