@@ -31,7 +31,9 @@ using namespace sm100;
 
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kBlockThreads = 256;
-constexpr int kMaxParts = 296;          // blocks that leave sums of their own: two to an SM of 148
+// Blocks that leave sums of their own, at most.  The ring's kernel is one block to an SM: it leaves 148, and a thread of it adds
+// up ceil(ceil(m / teams) / 148) rows; only rows past the ring are cut into more parts.
+constexpr int kMaxParts = 296;
 
 struct NormParams {
   int64_t m;
