@@ -15,6 +15,11 @@ as they come:
     n, h -> 4 bits                              morello_fp4_quantize
     both products                               morello_fp4_linear
 
+Blocks of 16 have scales in e4m3, which loses bits below 2^-6: the weights of a wide layer, 1 / sqrt(f), would be there.  So
+each tensor gets a factor that puts its largest scale near the top of e4m3's range, the weights' from the weights, the
+activations' from sample rows; the inverse of both goes into the product's alpha.  (Blocks of 32 have powers of two and
+need none.)
+
 The forward result is compared with a plain computation in 64 bits, the gradients with central differences of the loss
 along random directions, also in 64 bits, and the 4-bit result with the bf16 one."""
 import argparse
@@ -31,6 +36,11 @@ BF, F32, U8 = torch.bfloat16, torch.float32, torch.uint8
 EPS = 1e-5
 
 
+def kept(there, value):
+    """value, in the memory that an earlier one had: captured passes read it there."""
+    return value if there is None else there.copy_(value)
+
+
 class Fp4:
     """A 4-bit tensor of the library: its two buffers, and what is needed to fill them."""
 
@@ -38,10 +48,23 @@ class Fp4:
         self.rows, self.k, self.fmt, self.parts = rows, k, fmt, parts
         self.q = torch.empty(mb.morello_fp4_bytes(rows, k), dtype=U8, device="cuda")
         self.scales = torch.empty(mb.morello_fp4_scale_bytes(fmt, rows, parts, k), dtype=U8, device="cuda")
+        self.mult = None        # the tensor's factor, one f32 on the device
+
+    def fit(self, x, room=1.0):
+        """A factor for tensors whose largest magnitude is up to `room` times that of x."""
+        if self.fmt == mb.MORELLO_NVFP4:
+            self.mult = kept(self.mult, (448 * 6 / (room * x.float().abs().amax().clamp(min=1e-30))).reshape(1))
+        return self
 
     def quantize(self, x, layout=mb.MORELLO_W_COLMAJOR):
-        mb.morello_fp4_quantize(self.fmt, int(x.dtype == F32), layout, self.rows, self.parts, self.k, x, None, self.q, self.scales)
+        mb.morello_fp4_quantize(self.fmt, int(x.dtype == F32), layout, self.rows, self.parts, self.k, x, self.mult, self.q,
+                                self.scales)
         return self
+
+
+def alpha_of(there, x, w):
+    """What takes two tensors' factors out of their product again."""
+    return None if x.mult is None or w.mult is None else kept(there, 1 / (x.mult * w.mult))
 
 
 class NormBlock:
@@ -71,6 +94,7 @@ class NormBlock:
         # 4 bits
         self.n4, self.h4 = Fp4(tokens, d, fmt), Fp4(tokens, f, fmt)
         self.w1_4, self.w2_4 = Fp4(2 * f, d, fmt, parts=2), Fp4(d, f, fmt)
+        self.alpha1 = self.alpha2 = None
 
     def norm(self, x):
         mb.morello_layer_norm(0, mb.MORELLO_BF16, self.t, self.d, EPS, x, self.gamma, self.beta, self.n, self.mean, self.rstd)
@@ -93,7 +117,17 @@ class NormBlock:
                                        self.dgamma, self.dbeta)
         return self.dx, self.dgamma, self.dbeta, self.dw1, self.dw2
 
-    def quantize_weights(self):
+    def quantize_weights(self, sample=None):
+        """The weights to 4 bits.  sample: rows of x, from whose bf16 pass the activations' factors are taken (with room for
+        four times as much: beyond that, magnitudes are cut off); None: every tensor without a factor."""
+        if sample is not None:
+            self.forward(sample)
+            self.n4.fit(self.n, 4.0)
+            self.h4.fit(self.h, 4.0)
+            self.w1_4.fit(self.w1)
+            self.w2_4.fit(self.w2)
+            self.alpha1 = alpha_of(self.alpha1, self.n4, self.w1_4)
+            self.alpha2 = alpha_of(self.alpha2, self.h4, self.w2_4)
         self.w1_4.quantize(self.w1, mb.MORELLO_W_ROWMAJOR)
         self.w2_4.quantize(self.w2, mb.MORELLO_W_ROWMAJOR)
 
@@ -103,10 +137,10 @@ class NormBlock:
         self.norm(x)
         n, h = self.n4.quantize(self.n), self.h4
         mb.morello_fp4_linear(self.fmt, mb.MORELLO_ACT_SILU, 1, mb.MORELLO_BF16, t, d, f, n.q, n.scales, self.w1_4.q, self.w1_4.scales,
-                              None, None, None, self.h)
+                              self.alpha1, None, None, self.h)
         h.quantize(self.h)
         mb.morello_fp4_linear(self.fmt, mb.MORELLO_ACT_NONE, 0, mb.MORELLO_BF16, t, f, d, h.q, h.scales, self.w2_4.q, self.w2_4.scales,
-                              None, None, x, self.out)
+                              self.alpha2, None, x, self.out)
         return self.out
 
 
@@ -150,7 +184,7 @@ def main():
     x, dout = (torch.randn(args.tokens, args.d, generator=g, device="cuda").to(BF) for _ in range(2))
     forward, worst = check(block, x, dout)
     full = block.forward(x).clone()
-    block.quantize_weights()
+    block.quantize_weights(x)
     low = block.serve(x)
     change = (full.double() - x.double()).norm()
     print("forward error %.2e, worst gradient error %.2e, 4 bits against bf16 %.2e (of the block's own part)" %
