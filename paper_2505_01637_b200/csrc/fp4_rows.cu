@@ -34,6 +34,9 @@ constexpr int kMaxStages = 8;
 constexpr int kRing = 108 * 1024;            // two blocks to an SM
 constexpr int kPrefetch = 8;                 // stages asked into L2 before the wait
 constexpr int kScaleColumns = 32;            // of tensor memory, per stage in turn
+// Of tensor memory: accumulators of either half, the totals of their parts, and the scales of two stages.  Two blocks to an SM
+// take half of it, so that blocks of different clusters never wait for one another's.
+constexpr int kTmemColumns = 128;
 
 template <int kRows, bool kNv>
 struct Shape {
@@ -46,13 +49,13 @@ struct Shape {
   static constexpr size_t kSmemBytes = (size_t)kStages * kStageBytes + 1024 + 256;
   static constexpr int kBatch = kRows == 8 ? 4 : 8;      // rows a thread finishes at a time
   static_assert(2 * kRows * kStrip * 4 <= kStages * kStageBytes, "the parked sums reuse the stages");
+  static_assert(4 * kRows + 2 * kScaleColumns <= kTmemColumns, "tensor memory");
 };
 
 struct Fp4RowsParams {
   int m, n;
   int k_blocks, per_slice, split, chunk;      // blocks of the contraction, of a slice, slices; blocks of a part of the sums
   int up_rows, up_atoms;
-  int tmem_columns;
   uint8_t gated, act, out_f32;
   const float* alpha;
   const uint16_t* bias;
@@ -118,7 +121,7 @@ fp4_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     }
   }
   if (warp == 1) {
-    tmem_alloc(&bars->tmem_base, (uint32_t)p.tmem_columns);
+    tmem_alloc(&bars->tmem_base, (uint32_t)kTmemColumns);
     tmem_relinquish();
   }
   tc_fence_before_sync();
@@ -188,7 +191,7 @@ fp4_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         const uint32_t sw = smem_u32(stages + (size_t)stage * S::kStageBytes);
         const uint32_t sx = sw + kStripBytes, scales = sx + S::kRowsBytes;
         const uint32_t d_tmem = tmem_base + (uint32_t)(half * kRows);
-        const uint32_t ta = tmem_base + (uint32_t)(p.tmem_columns - 2 * kScaleColumns) + turn * kScaleColumns, tb = ta + S::kAtomsK * 4;
+        const uint32_t ta = tmem_base + (uint32_t)(kTmemColumns - 2 * kScaleColumns) + turn * kScaleColumns, tb = ta + S::kAtomsK * 4;
         turn ^= 1u;
 #pragma unroll
         for (int j = 0; j < S::kAtomsK; ++j) {
@@ -315,7 +318,7 @@ fp4_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   tc_fence_after_sync();
   if (warp == 1) {
     __syncwarp();
-    tmem_dealloc(tmem_base, (uint32_t)p.tmem_columns);
+    tmem_dealloc(tmem_base, (uint32_t)kTmemColumns);
   }
 }
 
@@ -351,12 +354,6 @@ cudaError_t launch(const DeviceInfo& dev, const Fp4Call& c, cudaStream_t stream)
   p.split = split;
   p.per_slice = std::max(1, (p.k_blocks + split - 1) / split);
   p.chunk = c.epi.out_f32 ? std::min(p.per_slice, kPreciseChunk) : p.per_slice;
-  // Accumulators of either half, the totals of parts behind them, and the scales of two stages.  At most half of an SM's, so
-  // that two blocks of different clusters never wait for one another's.
-  const int columns = (p.chunk < p.per_slice ? (p.gated ? 4 : 3) : p.gated ? 2 : 1) * kRows + 2 * kScaleColumns;
-  p.tmem_columns = 128;
-  while (p.tmem_columns < columns) p.tmem_columns *= 2;
-  if (p.tmem_columns > 256 || strips * split >= (1ll << 31)) return cudaErrorInvalidValue;
   CUtensorMap x{}, w{}, sx{}, sw{};
   if (c.k > 0) {
     const int64_t pitch = fp4_pitch(c.k), across = fp4_atoms_across(kNv, c.k), parts = p.gated ? 2 : 1;
