@@ -211,6 +211,7 @@ fp4_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       }
       // Of an empty sum nobody waits for a part, and an arrival must not come when the block has gone.
       if (ok && kb1 > kb0) mma_commit(&bars->acc_full);
+      if (!ok) let_copies_land();
     }
     __syncwarp();
   } else {

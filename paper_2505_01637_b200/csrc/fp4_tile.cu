@@ -253,6 +253,7 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         else mma_commit(&bars->acc_full[buf]);
         if (++buf == S::kBuffers) { buf = 0; acc_phase ^= 1; }
       }
+      if (!ok) let_copies_land();
     }
     }
   } else {
@@ -426,6 +427,7 @@ fp4_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     // Shared memory must outlive the engine's reads, and the stores must have been performed before the
     // kernel counts as complete.
     if (lane == 0) bulk_wait_group<0>();
+    if (!ok) let_copies_land();      // the residual's
   }
 
   __syncwarp();

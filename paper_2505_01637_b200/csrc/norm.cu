@@ -590,6 +590,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) norm_ring_kernel(const NormPa
     }
     ok = ring_next<kTeams, false>(&bars, smem, ring, &at, p.m, tensors, p.status) && ok;
   }
+  if (!ok) let_copies_land();
 }
 
 // A row's x - mean, g = dy gamma and dy, eight columns of them.
@@ -727,6 +728,7 @@ norm_backward_kernel(const NormBackwardParams p, const RingShape ring) {
     ring_release(&bars, at);
     ok = ring_next<kTeams, kVec == 8>(&bars, smem, ring, &at, p.m, tensors, p.status) && ok;
   }
+  if (!ok) let_copies_land();
   if (!p.partial) return;
   // The teams' sums meet in the ring's memory, whose last copies every team has read.
   constexpr int kWide = kT * kIter * 8;

@@ -129,6 +129,14 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
   }
 }
 
+// A block that gave up a wait may have copies on their way to its shared memory, which is the next block's once it leaves: it
+// stays for a hundredth of a second more.  (Such a copy takes microseconds; awaiting each one's own phase kept registers
+// for it through the loops and cost 1 to 3 % of every call.)
+__device__ __forceinline__ void let_copies_land() {
+  const uint64_t t0 = globaltimer_ns();
+  while (globaltimer_ns() - t0 < 10000000ull) {}
+}
+
 // ---- thread-block clusters (pairs of CTAs for cta_group::2) ---------------------
 __device__ __forceinline__ uint32_t cluster_ctarank() {
   uint32_t r;
