@@ -463,7 +463,8 @@ int64_t morello_fp4_scale_bytes(int format, int64_t rows, int64_t parts, int64_t
  *     s = 2^(floor(log2 amax) - 2), exponent at least -127;    or s = amax / 6 rounded to e4m3, at most 448
  *     Q = x / s rounded to e2m1, at most 6; 0 where s is 0
  *
- * All roundings are to nearest, ties to even, of the exact quotient.  A block that holds a NaN or an infinity has a NaN
+ * All roundings are to nearest, ties to even, of the exact quotient; a zero that Q is rounded to may have either sign.
+ * A block that holds a NaN or an infinity has a NaN
  * scale.  `mult` keeps e4m3 scales in range for the tensor as a whole (448 * 6 / the tensor's amax, say); its
  * inverse goes into the product's alpha.  rows == 0 or k == 0 does nothing.  Any extent up to 2^31 - 1024 and alignment
  * of X.  Needs no workspace.  Deterministic, asynchronous on `stream`.
@@ -472,7 +473,8 @@ int morello_fp4_quantize(int format, int x_type, int x_layout, int64_t rows, int
                          const float* mult, void* Q, void* scales, void* stream);
 
 /* Y[rows][k] (bf16 or f32, y_type) = the tensor's values times the one f32 at `alpha` (device memory, NULL: 1); without
- * alpha exact in either type.  What a NaN scale serves is NaN. */
+ * alpha exact in either type.  What a NaN scale serves is NaN; values past f32's largest (with scales of 2^126 and 2^127, which
+ * morello_fp4_quantize does not write) are infinite, before alpha. */
 int morello_fp4_dequantize(int format, int y_type, int64_t rows, int64_t parts, int64_t k, const void* Q,
                            const void* scales, const float* alpha, void* Y, void* stream);
 

@@ -14,10 +14,13 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmorello.so")
 SOURCES = ["api.cu", "skinny.cu", "gemv_stream.cu", "gemm_tcgen05.cu", "f32_split.cu", "pad.cu", "selftest.cu", "tensormap.cu", "noalloc.cu",
-           "linear_api.cu", "linear_tile.cu", "linear_rows.cu", "linear_aux.cu", "route.cu", "norm.cu", "fp4_quantize.cu", "fp4_tile.cu", "fp4_rows.cu", "fp4_api.cu"]
+           "linear_api.cu", "linear_tile.cu", "linear_rows.cu", "linear_aux.cu", "route.cu",
+           "norm.cu", "fp4_quantize.cu", "fp4_tile.cu", "fp4_rows.cu", "fp4_api.cu"]
 HEADERS = [os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "sm100.cuh"),
            os.path.join(CSRC, "tensormap.h"), os.path.join(CSRC, "linear.h"), os.path.join(CSRC, "route.h"),
-           os.path.join(CSRC, "activation.cuh"), os.path.join(CSRC, "column_sums.cuh"), os.path.join(CSRC, "octets.cuh"), os.path.join(CSRC, "activation_pairs.cuh"), os.path.join(CSRC, "tile_epilogue.cuh"), os.path.join(CSRC, "fp4.h"),
+           os.path.join(CSRC, "activation.cuh"), os.path.join(CSRC, "column_sums.cuh"),
+           os.path.join(CSRC, "octets.cuh"), os.path.join(CSRC, "activation_pairs.cuh"),
+           os.path.join(CSRC, "tile_epilogue.cuh"), os.path.join(CSRC, "fp4.h"),
            os.path.join(os.path.dirname(HERE), "include", "morello.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",

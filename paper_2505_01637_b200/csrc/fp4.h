@@ -29,7 +29,7 @@ struct Fp4Call {
   LinearEpilogue epi;
   int64_t wide() const { return epi.gated ? 2 * n : n; }
 };
-// At most kFp4FewRows rows: W streamed once.
+// At most kFp4FewRows rows: W streamed once, the contraction cut over clusters (both sides' times at the head of fp4_rows.cu).
 constexpr int kFp4FewRows = 16;
 cudaError_t fp4_rows_launch(const DeviceInfo& dev, const Fp4Call& call, cudaStream_t stream, uint64_t* launches);
 cudaError_t fp4_tile_launch(const DeviceInfo& dev, const Fp4Call& call, cudaStream_t stream, uint64_t* launches);

@@ -1,7 +1,12 @@
 // Products of 4-bit tensors on few rows (at most 16): a decoding step.  The call streams the weights once and is bound by
 // memory, and on small layers by the chain of a launch: 1 x 2048 x 16384 takes 6.4 us, gated 2 x 8192 7.2, 16 rows with bias,
-// GELU and residual 8.3, of which the 17 MB are 2.6.  (With 32 and 64 rows, one thread to a column of Y, finishing them
-// takes longer than the stream: 64 rows of 2048 x 16384 12.1 us here, 8.8 by the tile kernel; 4096 x 4096 8.5 and 9.4.)
+// GELU and residual 8.3, of which the 17 MB are 2.6.
+//
+// Here and by the tile kernel, in us (contraction x columns): one row, 16384 x 2048 8.0 and 20.5, 4096 x 4096 5.7 and 8.2, 2048 x 16384 6.6 and 8.2; 16
+// rows 9.6 and 20.5, 7.5 and 8.3, 7.8 and 8.2.  Where the contraction is a block or two and finishing the rows, one thread to
+// a column of Y, is most of the work, the tile kernel is ahead at 16 rows (512 x 512 4.3 and 3.5, 256 x 65536 11.9 and 8.4) and
+// even at 8 (256 x 65536 8.6 and 8.3).  With 32 and 64 rows that holds for wide layers too: 64 rows of 2048 x 16384 12.1 and
+// 8.8, but 4096 x 4096 8.5 and 9.4; a form for so many rows is not kept.
 //
 // The operands trade places: a block owns 128 rows of W (columns of Y; gated: of either half), which become the M side of
 // the MMA, and the rows of X, rounded up to 8 or 16, are its N side.  A contraction is cut over the blocks of

@@ -8,12 +8,13 @@
 // the scales of those rows, whole 512-byte atoms that the issuer copies to tensor memory ahead of the stage's four MMA
 // steps, to one of two places in turn.
 //
-// A 256-column accumulator and the scales leave no room for a second one in the 512 columns of tensor memory: the epilogue
-// warps take all of a tile's sums into registers, hand the accumulator back, and finish the tile under the next one's main
-// loop.  Gated tiles hold 128 columns of either half of W.
+// A 256-column accumulator and two stages' scales (24 or 48 columns each) leave no room for a second one as wide in the 512
+// columns of tensor memory (two of 192 columns would fit; not tried): the epilogue warps take all of a tile's sums into
+// registers, hand the accumulator back, and finish the tile under the next one's main loop.  Gated tiles hold 128 columns
+// of either half of W.
 //
-// 4096 x 4096 x 4096 takes 31 us (4.4 PFLOP/s), 8192 x 8192 x 8192 185 to 200 (5.5 to 5.9), bound by the hand-over of the one
-// accumulator, the copies of the scales and the board's power.
+// 4096 x 4096 x 4096 takes 31 us (4.4 PFLOP/s), 8192 x 8192 x 8192 185 to 200 (5.5 to 5.9), gated 4096 x 4096 x (2 x 4096) with
+// SiLU 53 (5.2), bound by the hand-over of the one accumulator, the copies of the scales and the board's power.
 #include <algorithm>
 #include <type_traits>
 

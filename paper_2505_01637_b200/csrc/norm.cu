@@ -5,11 +5,15 @@
 //   backward   h = (x - mu) r, g = dy gamma:  dx = r (g - mean(g) - h mean(g h)) + R  (rms: without mean(g))
 //              dgamma = sum over rows of dy h, dbeta = sum over rows of dy
 //
-// Both passes are bound by memory: a row is read once by a team of 8 to 512 threads, which hold it (backward: find it in
-// shared memory again) until it has been reduced, and written.  16384 x 4096 takes 49 us forward and 83 us backward, 5.4 and
-// 4.9 TB/s; 4096 x 2047 takes 16 and 30 us.  The variance is that of the differences from a mean (two sweeps over the registers), never a difference of
-// sums.  A warp takes its own mean and the squares about it, and one barrier later every thread joins the warps' three
-// numbers (Chan, Golub and LeVeque's formula for joining variances), so a row costs one barrier.
+// A row is read once by a team of 8 to 512 threads, which hold it (backward: find it in shared memory again) until it has been
+// reduced, and written.  In a row of calls 16384 x 4096 takes 49.5 us forward and 83.6 backward, 5.4 and 4.8 TB/s: bound by
+// memory.  Short rows are not: 65536 x 128 takes 9.1 and 19.7 us with 65 and 53 % of the issue slots in use, and a warp's
+// joins waited for in between.  Nor are rows off 16 bytes: 4096 x 2047 takes 16.5 and 30.6 us, at 17.8 and 28.0 M
+// instructions for 8192 x 2047 (every element is an access of its own to shared memory, and a store), 57 and 58 % of the slots.
+//
+// The variance is that of the differences from a mean (two sweeps over the registers), never a difference of sums.  A warp
+// takes its own mean and the squares about it, and one barrier later every thread joins the warps' three numbers (Chan,
+// Golub and LeVeque's formula for joining variances), so a row costs one barrier.
 //
 // The backward pass's threads keep the columns they own through all the rows of a block, so dgamma and dbeta add up in
 // registers; the blocks' sums are joined by a second launch in the order of the blocks.  No atomics: the same sums in the
@@ -1017,8 +1021,8 @@ cudaError_t forward_launch(const DeviceInfo& dev, const NormParams& p, bool vec,
                       dim3(kLongThreads), 0, s, 1, p);
   if (vec) {
     // 16 columns to a thread; 32 of long rows where there are many: half the teams' joins, and 16 bytes more of every thread
-    // in flight (2048 x 8192: 15.5 instead of 19.0 us, f32 4096 x 4096 18.2 instead of 20.8; 16384 x 4096 53.0 and 53.9,
-    // 4096 x 2048 9.6 and 8.7; 128 x 4096 3.5 and 2.6).
+    // in flight (in a row of calls, 32 and 16 columns: 2048 x 8192 15.6 and 18.5 us, 16384 x 4096 49.5 and 53.0, 4096 x 4096 16.4
+    // and 15.6, rms 13.8 and 14.6, f32 18.4 and 18.5; 128 x 4096 3.5 and 2.6; 4096 x 2048, where it is 16, 9.6 and 8.7).
     const bool many = p.m >= 4 * (int64_t)dev.sms;
     if (n <= 64) MORELLO_NORM(8, 1);
     if (n <= 128) MORELLO_NORM(16, 1);
