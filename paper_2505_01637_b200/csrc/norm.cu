@@ -35,8 +35,7 @@ using namespace sm100;
 
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr int kBlockThreads = 256;
-// Blocks that leave sums of their own, at most.  The ring's kernel is one block to an SM: it leaves 148, and a thread of it adds
-// up ceil(ceil(m / teams) / 148) rows; only rows past the ring are cut into more parts.
+// Blocks that leave sums of their own, at most, but for very many rows: see ring_blocks().
 constexpr int kMaxParts = 296;
 
 struct NormParams {
@@ -961,11 +960,19 @@ RingShape ring_shape(int64_t n, std::initializer_list<int> sizes, int64_t beside
   return r;
 }
 
+// Blocks of the backward pass through the ring on so many SMs: one to each, but a block, whose threads add up a row of every
+// group, takes kChain groups at most: of more rows there are two blocks to an SM, or three, one after the other (2^31 rows of one
+// column were 226,719 additions in a row, and dgamma off by 1e-4).
+constexpr int64_t kChain = 2048;
+int64_t ring_blocks(int64_t groups, int64_t sms) {
+  return std::min(groups, std::max<int64_t>(1, (groups + kChain * sms - 1) / (kChain * sms)) * sms);
+}
 // Blocks at most that leave sums of their own.  Rows too long for the ring: a block's share is this many at least.
 constexpr int64_t kLongShare = 128;
 int64_t backward_parts(int64_t m, int64_t n) {
-  const int64_t rows = n > kRingColumns ? kLongShare : kRingThreads / team_of(n);
-  return std::min<int64_t>(kMaxParts, (m + rows - 1) / rows);
+  const int64_t rows = n > kRingColumns ? kLongShare : kRingThreads / team_of(n), shares = (m + rows - 1) / rows;
+  const int64_t parts = std::min<int64_t>(kMaxParts, shares);
+  return n > kRingColumns ? parts : std::max(parts, ring_blocks(shares, kMaxParts / 2));
 }
 size_t backward_bytes(int64_t m, int64_t n) { return (size_t)backward_parts(m, n) * 2 * n * 4; }
 
@@ -1062,7 +1069,7 @@ cudaError_t backward_launch(const DeviceInfo& dev, NormBackwardParams p, float* 
     p.ring_r = p.R && p.dX && with_r.stages >= 2;
     if (p.ring_r) ring = with_r;
     const int64_t teams = kRingThreads / team_of(p.n);
-    parts = (int)std::min<int64_t>(std::min(parts, dev.sms), (p.m + teams - 1) / teams);
+    parts = (int)std::min<int64_t>(parts, ring_blocks((p.m + teams - 1) / teams, dev.sms));
     e = by_team(p.n, [&](auto team, auto eights) {
       constexpr int kT = team.value, kIter = eights.value;
       constexpr size_t kJoined = (size_t)kRingThreads * kIter * 64;      // the teams' sums

@@ -46,3 +46,24 @@ def test_many_rows(m, n, equal, kind):
     bound = (rows + teams(n) + (-(-sms // 8)) + 8 + 3) * 2.0 ** -24
     assert torch.all((dgamma.double() - sums[0]).abs() <= bound * sums[1])
     assert torch.all((dbeta.double() - sums[2]).abs() <= bound * sums[3])
+
+
+@pytest.mark.parametrize("value", [1.1, 0.7])
+@pytest.mark.parametrize("m,n", [(1 << 29, 1), (1 << 27, 8)])
+def test_no_chain_grows_with_the_rows(m, n, value):
+    # A block takes 2048 groups of rows at most; equal terms, so that every addition of a chain rounds the same way.
+    x = torch.full((m, n), value, device="cuda")
+    dy = torch.full((m, n), 0.3, dtype=BF, device="cuda")
+    mean, rstd = torch.full((m,), 0.1, device="cuda"), torch.full((m,), 1.3, device="cuda")
+    dgamma, dbeta = torch.full((n,), float("nan"), device="cuda"), torch.full((n,), float("nan"), device="cuda")
+    need = mb.morello_layer_norm_backward_workspace_bytes(m, n)
+    ws = torch.full((need + 64,), 0xAB, dtype=torch.uint8, device="cuda")
+    mb.morello_layer_norm_backward(0, 1, 0, m, n, x, None, mean, rstd, dy, None, None, dgamma, dbeta, ws, need)
+    assert torch.all(ws[need:] == 0xAB)
+    d = float(dy[0, 0])
+    t = (float(x[0, 0]) - float(mean[0])) * float(rstd[0]) * d
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    parts = -(-(-(-m // teams(n))) // (2048 * sms)) * sms
+    bound = (2048 + -(-parts // 8) + teams(n) + 8 + 3) * 2.0 ** -24
+    assert torch.all((dgamma.double() - m * t).abs() <= bound * m * abs(t)), float(dgamma[0]) / (m * t) - 1
+    assert torch.all((dbeta.double() - m * d).abs() <= bound * m * d), float(dbeta[0]) / (m * d) - 1
